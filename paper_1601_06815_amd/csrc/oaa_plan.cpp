@@ -14,10 +14,10 @@
 #include <cstring>
 #include <mutex>
 #include <new>
-#include <string>
 #include <vector>
 
 #include "oaa_internal.hpp"
+#include "oaa_status.hpp"
 
 // Block tiles (the input with overlap-add, the gradient with overlap-save)
 // go through the window transform (window side = pitch = b) where its
@@ -103,21 +103,33 @@ bool blocks_as_windows(const oaa_plan_s* p) {
 
 namespace {
 
-thread_local std::string g_detail;
+thread_local char g_detail[512];
 
-oaa_status_t fail(oaa_status_t st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+}  // namespace
+
+namespace oaa {
 
 oaa_status_t fail(oaa_status_t st, const char* fmt, ...) {
-  char buf[512];
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
+  vsnprintf(g_detail, sizeof g_detail, fmt, ap);
   va_end(ap);
-  g_detail = buf;
   return st;
 }
 
-constexpr size_t kAlign = 256;
+oaa_status_t hip_status(hipError_t e, const char* what) {
+  if (e == hipSuccess) return OAA_OK;
+  return fail(OAA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+}  // namespace oaa
+
+namespace {
+
+using oaa::fail;
+using oaa::hip_status;
+
+constexpr size_t kAlign = oaa::kWorkspaceAlign;
 constexpr unsigned long long kMaxElems = 1ull << 60;
 constexpr int kMaxSide = 128;   // largest transform side
 constexpr int kMaxKernel = 64;  // largest kernel side (2n - 1 <= kMaxSide)
@@ -136,11 +148,6 @@ oaa_status_t check_plan(oaa_plan_t plan, bool need_ws) {
   if (need_ws && !plan->ws)
     return fail(OAA_ERR_NO_WORKSPACE, "no workspace bound (need %zu bytes)", plan->ws_bytes);
   return OAA_OK;
-}
-
-oaa_status_t hip_status(hipError_t e, const char* what) {
-  if (e == hipSuccess) return OAA_OK;
-  return fail(OAA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
 // What one pass runs against: the plan, the device memory its spectra live in
@@ -840,7 +847,7 @@ const char* oaa_status_string(oaa_status_t status) {
   return "OAA_ERR_UNKNOWN";
 }
 
-const char* oaa_last_error_detail(void) { return g_detail.c_str(); }
+const char* oaa_last_error_detail(void) { return g_detail; }
 
 oaa_status_t oaa_plan_create(oaa_plan_t* out, int B, int C, int K, int N, int n) {
   if (n >= 1 && n <= kMaxKernel) return oaa_plan_create_tiled(out, B, C, K, N, n, pow2_at_least(2 * n - 1), n);
