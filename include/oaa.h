@@ -292,6 +292,107 @@ oaa_status_t oaa_plan_set_kernel_chain(oaa_plan_t plan, const float* w1, int J, 
 oaa_status_t oaa_conv_forward_noalloc(oaa_plan_t plan, const float* x, const float* w, float* y,
                                       void* hip_stream);
 
+/* ---- Between the layers: group normalisation with an activation ------------
+ *
+ * x holds B images of C channels at S positions each (S = M M after a layer
+ * above), its channels in G groups of D = C / G neighbours. Over the n = D S
+ * values of one group of one image:
+ *
+ *   mean = sum x / n     var = sum (x - mean)^2 / n     rstd = 1 / sqrt(var + eps)
+ *   xh = (x - mean) rstd     z = weight[c] xh + bias[c]     y = act(z)
+ *
+ * and, for the upstream gradient dy of y, with dz = dy act'(z), t = weight[c] dz:
+ *
+ *   dbias[c] = sum_{b,s} dz     dweight[c] = sum_{b,s} dz xh
+ *   dx = rstd (t - sum t / n - xh sum (t xh) / n)       (sums over the group)
+ *
+ * Statistics and sums are held in 32 bits or more whatever the types; every
+ * output is rounded once. A value that is not finite makes its own group of
+ * its own image NaN and, backward, dweight and dbias of that group's channels.
+ * The derivative of the ReLU at 0 is 0. */
+typedef enum {
+  OAA_LAYOUT_PLANES = 0,       /* element (b, c, s) at b image + c S + s             */
+  OAA_LAYOUT_CHANNELS_LAST = 1 /* element (b, c, s) at b image + s row + c           */
+} oaa_layout_t;
+
+typedef enum { OAA_FLOAT32 = 0, OAA_BFLOAT16 = 1, OAA_FLOAT16 = 2 } oaa_dtype_t;
+
+typedef enum {
+  OAA_ACT_NONE = 0, /* z                                          */
+  OAA_ACT_RELU = 1, /* max(z, 0)                                  */
+  OAA_ACT_SILU = 2, /* z / (1 + exp(-z))                          */
+  OAA_ACT_GELU = 3  /* z Phi(z), Phi the normal distribution      */
+} oaa_activation_t;
+
+/* Element strides of one tensor: between images, and (channels last) between
+ * positions. Both 0: dense. In planes row must be 0 or S. A tensor that is
+ * written must not overlap itself; one that is read may (image = 0 repeats
+ * one image). */
+typedef struct {
+  long long image, row;
+} oaa_strides_t;
+
+typedef struct {
+  int B, C, G;      /* images, channels, groups: B >= 0, C >= 1, G divides C  */
+  long long S;      /* positions per image, >= 0                              */
+  int layout;       /* oaa_layout_t of x, y, dy and dx                        */
+  int dtype;        /* oaa_dtype_t of x, y, dy and dx                         */
+  int param_dtype;  /* of weight, bias and their gradients: OAA_FLOAT32 or dtype */
+  int activation;   /* oaa_activation_t                                       */
+  float eps;        /* >= 0                                                   */
+  oaa_strides_t x, y, dy, dx;
+} oaa_group_norm_t;
+
+/* Device workspace a call needs, in bytes (a multiple of 256, 0 if none): of
+ * the forward pass, or with backward != 0 of the backward pass. 0 also for an
+ * invalid description, which the calls refuse. */
+size_t oaa_group_norm_workspace_bytes(const oaa_group_norm_t* d, int backward);
+
+/* y from x. weight or bias NULL: 1 or 0. mean and rstd ([B][G] float32, for
+ * the backward pass) may be NULL, each. The workspace (256-byte aligned; NULL
+ * if none is needed) holds nothing between calls and is free again once the
+ * call's work on `stream` is done. Only enqueues work on the stream; validates
+ * first. An empty x (B or S = 0) is no work. */
+oaa_status_t oaa_group_norm_forward(const oaa_group_norm_t* d, const void* x, const void* weight, const void* bias,
+                                    void* y, float* mean, float* rstd, void* workspace, size_t workspace_bytes,
+                                    void* hip_stream);
+
+/* dx, dweight and dbias from dy, the forward pass's x, weight and bias and its
+ * mean and rstd. Each of the three outputs may be NULL (at least one is not).
+ * An empty x gives zeros in dweight and dbias. */
+oaa_status_t oaa_group_norm_backward(const oaa_group_norm_t* d, const void* dy, const void* x, const void* weight,
+                                     const void* bias, const float* mean, const float* rstd, void* dx, void* dweight,
+                                     void* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- After the backward passes: the norm of all gradients, and clipping ------
+ *
+ * Over every value of `count` dense tensors of any sizes and types,
+ *
+ *   norm = (sum |g|^p)^(1/p)  for p = 1, 2, or  max |g|;
+ *   clip: out = g k  with  k = min(1, max_norm / (norm + 1e-6)).
+ *
+ * Sums are held in 64 bits and added in a fixed order: equal calls give equal
+ * bits. A NaN anywhere gives norm NaN and k NaN; an infinity gives norm
+ * infinity and k 0. norm (one float32) stays on the device: nothing waits for
+ * it. No tensors, or only empty ones, have norm 0. */
+typedef enum { OAA_NORM_SUM = 1, OAA_NORM_EUCLIDEAN = 2, OAA_NORM_MAX = 3 } oaa_norm_t;
+
+/* Device workspace of either call for `count` tensors, in bytes. */
+size_t oaa_grad_workspace_bytes(int count);
+
+/* grads[i]: device pointer to sizes[i] >= 0 values of oaa_dtype_t dtypes[i]
+ * (NULL allowed if sizes[i] is 0). The three host arrays are read before the
+ * call returns. The workspace is as for oaa_group_norm_forward. */
+oaa_status_t oaa_grad_norm(int count, const void* const* grads, const long long* sizes, const int* dtypes,
+                           oaa_norm_t type, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The same norm, then out[i] = grads[i] k, each rounded once to the type of
+ * grads[i]. out[i] is grads[i] (in place: with k = 1 nothing is written) or
+ * memory that overlaps no gradient and no other output. max_norm >= 0. */
+oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out, const long long* sizes,
+                           const int* dtypes, oaa_norm_t type, float max_norm, float* norm, void* workspace,
+                           size_t workspace_bytes, void* hip_stream);
+
 /* Static text for a status code. */
 const char* oaa_status_string(oaa_status_t status);
 

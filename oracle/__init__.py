@@ -29,8 +29,12 @@ oas
     The output-tiled alternative: overlap-and-save forward over L x L windows
     of x at hop L - n + 1, the error propagation as overlap-and-add over
     blocks of g, and the weight gradient from the same windows and blocks.
+norm
+    Group normalisation with an activation, forward and backward, and the norm
+    and clipping of gradients: what stands between such layers and at the end
+    of a training step. Not from the paper; written from the formulas.
 
-Every function states the passage it follows. Pins (tests/test_oracle.py)
+Every function of the layer states the passage it follows. Pins (tests/test_oracle.py)
 tie each function to library routines, closed forms and invariants that are
 independent of this code.
 """
@@ -40,3 +44,4 @@ from .direct import (conv_forward, conv_backward_data, conv_backward_filter,  # 
 from .dft import dft_conv_forward  # noqa: F401
 from . import oaa  # noqa: F401
 from . import oas  # noqa: F401
+from . import norm  # noqa: F401

@@ -1,4 +1,5 @@
-"""torch.autograd binding of the OaA convolution layer.
+"""torch.autograd binding of the OaA convolution layer, of group normalisation
+with an activation, and the clipping of a network's gradients.
 
 Training needs the forward convolution and the two backward convolutions
 (arXiv:1601.06815, Section 3.2); ``OaAConv2dFunction`` connects them to
@@ -14,6 +15,10 @@ reuses the kernel and input spectra of its own forward pass when the plan has
 run nothing since (its ``generation`` counter, which every pass of the plan
 advances, is unchanged), and recomputes them from the saved tensors
 otherwise.
+
+``group_norm`` (``GroupNorm`` as a layer) takes the convolution's output in
+planes, or tensors in torch's channels_last layout; ``clip_grad_norm_`` clips
+the gradients that the backward passes left in a network's parameters.
 """
 
 import math
@@ -78,3 +83,78 @@ class OaAConv2d(torch.nn.Module):
         if C != self.C or N != N2:
             raise ValueError(f"expected x[B,{self.C},N,N], got {tuple(x.shape)}")
         return OaAConv2dFunction.apply(x, self.weight, self.plan_for(B, N))
+
+
+def _laid_out(t, layout=None):
+    """t if the library takes its strides (in `layout`, if one is given), or a
+    dense copy of it."""
+    try:
+        binding._norm_layout(t, "x", layout)
+    except ValueError:
+        if layout == binding.LAYOUT_CHANNELS_LAST:
+            return t.movedim(1, -1).contiguous().movedim(-1, 1)
+        return t.contiguous()
+    return t
+
+
+class GroupNormFunction(torch.autograd.Function):
+    """y = act(group_norm(x) weight + bias)."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, num_groups, eps, activation):
+        y, mean, rstd = binding.group_norm_forward(x, num_groups, weight, bias, eps, activation)
+        ctx.num_groups, ctx.activation = num_groups, activation
+        ctx.save_for_backward(x, weight, bias, mean, rstd)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, mean, rstd = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dy = _laid_out(dy, binding._norm_layout(x, "x")[0])
+        dx, dweight, dbias = binding.group_norm_backward(dy, x, ctx.num_groups, weight, bias, mean, rstd,
+                                                         ctx.activation, need[0], need[1], need[2])
+        return dx, dweight, dbias, None, None, None
+
+
+def group_norm(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none"):
+    """Group normalisation of x[B, C, ...] over num_groups groups of neighbouring
+    channels, with weight[C] and bias[C], then the activation ("none", "relu",
+    "silu", "gelu"). x is float32, bfloat16 or float16 in planes or channels
+    last, and y like it; parameters are float32 or of x's type."""
+    x = _laid_out(x)
+    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
+                                    (bias is not None and bias.requires_grad)):
+        return GroupNormFunction.apply(x, weight, bias, num_groups, eps, activation)
+    return binding.group_norm_forward(x, num_groups, weight, bias, eps, activation, stats=False)[0]
+
+
+class GroupNorm(torch.nn.Module):
+    """Group normalisation layer over num_channels channels in num_groups groups,
+    with its activation; ``affine`` gives it a weight and a bias."""
+
+    def __init__(self, num_groups, num_channels, eps=1e-5, affine=True, activation="none", device="cuda",
+                 dtype=torch.float32):
+        super().__init__()
+        if num_groups < 1 or num_channels % num_groups:
+            raise ValueError(f"{num_channels} channels do not divide into {num_groups} groups")
+        if activation not in binding.ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(binding.ACTIVATIONS)}, got {activation!r}")
+        self.G, self.C, self.eps, self.activation = num_groups, num_channels, eps, activation
+        for name, value in (("weight", 1.0), ("bias", 0.0)):
+            self.register_parameter(name, torch.nn.Parameter(torch.full((num_channels,), value, device=device,
+                                                                        dtype=dtype)) if affine else None)
+
+    def forward(self, x):
+        if x.dim() < 2 or x.shape[1] != self.C:
+            raise ValueError(f"expected x[B,{self.C},...], got {tuple(x.shape)}")
+        return group_norm(x, self.G, self.weight, self.bias, self.eps, self.activation)
+
+
+@torch.no_grad()
+def clip_grad_norm_(parameters, max_norm, norm_type=2.0):
+    """Scale the gradients of the parameters in place so that their norm is at
+    most max_norm; returns the norm before, a scalar on the device (nothing
+    waits for it). Parameters without a gradient are left out."""
+    return binding.grad_clip([p.grad for p in parameters if p.grad is not None], max_norm, norm_type)

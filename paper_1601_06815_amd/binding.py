@@ -1,13 +1,17 @@
 """ctypes binding of liboaa.so (include/oaa.h). Argument marshalling only.
 
 Functions carry the C names and take plain integers for device pointers and
-streams. ``Plan`` wraps them for torch tensors: torch supplies device memory
-(the workspace is a uint8 tensor) and the current stream; every step of every
-pass runs in the library's HIP kernels. There is no fallback: if the library
+streams. ``Plan``, ``group_norm_*`` and ``grad_*`` wrap them for torch tensors:
+torch supplies device memory (workspaces are uint8 tensors) and the current
+stream; every step of every pass runs in the library's HIP kernels. There is no fallback: if the library
 is missing, ``load()`` raises.
 """
 
+import array
+import contextlib
 import ctypes
+import functools
+import math
 import os
 
 from .build import LIB_PATH
@@ -21,6 +25,11 @@ METHOD_OVERLAP_ADD, METHOD_OVERLAP_SAVE = 0, 1
 STAGES = ["w_spectrum", "x_spectrum", "g_spectrum", "fwd_product", "fwd_inverse",
           "bwd_data_product", "bwd_data_inverse", "bwd_filter_product", "bwd_filter_inverse"]
 
+LAYOUT_PLANES, LAYOUT_CHANNELS_LAST = 0, 1
+FLOAT32, BFLOAT16, FLOAT16 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+NORM_SUM, NORM_EUCLIDEAN, NORM_MAX = 1, 2, 3
+
 # every symbol include/oaa.h declares, with its ctypes signature
 _c_int, _c_size, _vp = ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p
 
@@ -28,6 +37,18 @@ _c_int, _c_size, _vp = ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p
 class Geometry(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int) for k in ("B", "C", "K", "N", "n", "M", "T", "P", "L", "F", "split", "b",
                                             "method", "fused")]
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("image", ctypes.c_longlong), ("row", ctypes.c_longlong)]
+
+
+class GroupNormDesc(ctypes.Structure):
+    """oaa_group_norm_t."""
+    _fields_ = [("B", ctypes.c_int), ("C", ctypes.c_int), ("G", ctypes.c_int), ("S", ctypes.c_longlong),
+                ("layout", ctypes.c_int), ("dtype", ctypes.c_int), ("param_dtype", ctypes.c_int),
+                ("activation", ctypes.c_int), ("eps", ctypes.c_float),
+                ("x", Strides), ("y", Strides), ("dy", Strides), ("dx", Strides)]
 
 
 SIGNATURES = {
@@ -49,6 +70,12 @@ SIGNATURES = {
     "oaa_conv_forward_noalloc": (_c_int, [_vp, _vp, _vp, _vp, _vp]),
     "oaa_plan_chain_scratch_bytes": (_c_size, [_vp, _c_int]),
     "oaa_plan_set_kernel_chain": (_c_int, [_vp, _vp, _c_int, _c_int, _vp, _c_int, _vp, _c_size, _vp]),
+    "oaa_group_norm_workspace_bytes": (_c_size, [_vp, _c_int]),
+    "oaa_group_norm_forward": (_c_int, [_vp] * 8 + [_c_size, _vp]),
+    "oaa_group_norm_backward": (_c_int, [_vp] * 11 + [_c_size, _vp]),
+    "oaa_grad_workspace_bytes": (_c_size, [_c_int]),
+    "oaa_grad_norm": (_c_int, [_c_int, _vp, _vp, _vp, _c_int, _vp, _vp, _c_size, _vp]),
+    "oaa_grad_clip": (_c_int, [_c_int, _vp, _vp, _vp, _vp, _c_int, ctypes.c_float, _vp, _vp, _c_size, _vp]),
     "oaa_status_string": (ctypes.c_char_p, [_c_int]),
     "oaa_last_error_detail": (ctypes.c_char_p, []),
 }
@@ -182,6 +209,41 @@ def oaa_plan_chain_scratch_bytes(plan, J):
 
 def oaa_plan_set_kernel_chain(plan, w1, J, n1, w2, n2, scratch, scratch_bytes, stream):
     return _check(load().oaa_plan_set_kernel_chain(plan, w1, J, n1, w2, n2, scratch, scratch_bytes, stream))
+
+
+def oaa_group_norm_workspace_bytes(desc, backward):
+    """desc: a GroupNormDesc or its address."""
+    return load().oaa_group_norm_workspace_bytes(_address(desc), 1 if backward else 0)
+
+
+def oaa_group_norm_forward(desc, x, weight, bias, y, mean, rstd, workspace, workspace_bytes, stream):
+    return _check(load().oaa_group_norm_forward(_address(desc), x, weight, bias, y, mean, rstd, workspace,
+                                                workspace_bytes, stream))
+
+
+def oaa_group_norm_backward(desc, dy, x, weight, bias, mean, rstd, dx, dweight, dbias, workspace, workspace_bytes,
+                            stream):
+    return _check(load().oaa_group_norm_backward(_address(desc), dy, x, weight, bias, mean, rstd, dx, dweight, dbias,
+                                                 workspace, workspace_bytes, stream))
+
+
+def oaa_grad_workspace_bytes(count):
+    return load().oaa_grad_workspace_bytes(count)
+
+
+def oaa_grad_norm(count, grads, sizes, dtypes, norm_type, norm, workspace, workspace_bytes, stream):
+    """grads, sizes, dtypes: addresses of host arrays."""
+    return _check(load().oaa_grad_norm(count, grads, sizes, dtypes, norm_type, norm, workspace, workspace_bytes,
+                                       stream))
+
+
+def oaa_grad_clip(count, grads, out, sizes, dtypes, norm_type, max_norm, norm, workspace, workspace_bytes, stream):
+    return _check(load().oaa_grad_clip(count, grads, out, sizes, dtypes, norm_type, max_norm, norm, workspace,
+                                       workspace_bytes, stream))
+
+
+def _address(desc):
+    return desc if isinstance(desc, int) or desc is None else ctypes.addressof(desc)
 
 
 def oaa_status_string(status):
@@ -337,3 +399,236 @@ class Plan:
         import torch
         off, size = oaa_plan_region(self.handle, which)
         return self.workspace[off:off + size].view(torch.complex64)
+
+
+# ---- group normalisation and gradients of torch tensors ------------------------
+
+def _dtype_codes():
+    import torch
+    return {torch.float32: FLOAT32, torch.bfloat16: BFLOAT16, torch.float16: FLOAT16}
+
+
+_dtype_codes = functools.lru_cache(maxsize=None)(_dtype_codes)
+
+
+def _on_device(index):
+    """The raw current stream of device `index`, and a context in which that
+    device is current (kernels are launched on the current device)."""
+    import torch
+    guard = _NO_GUARD if torch.cuda.current_device() == index else torch.cuda.device(index)
+    return torch._C._cuda_getCurrentRawStream(index), guard
+
+
+_NO_GUARD = contextlib.nullcontext()
+
+
+def _norm_layout(t, name, want=None):
+    """(layout, S, image stride, row stride) of t[B, C, ...], in planes or channels
+    last with any strides between positions and images; `want`: only this
+    layout will do (one position or one channel is both)."""
+    shape = t.shape
+    if len(shape) < 2:
+        raise ValueError(f"{name} must have shape [B, C, ...], got {tuple(shape)}")
+    C = shape[1]
+    S = math.prod(shape[2:])
+    if want != LAYOUT_CHANNELS_LAST and t.is_contiguous():
+        return LAYOUT_PLANES, S, C * S, S
+    strides = t.stride()
+    # the positions' dimensions as one: row-major with one step between neighbours
+    step = expect = None
+    for k, st in zip(reversed(shape[2:]), reversed(strides[2:])):
+        if k == 1:
+            continue
+        if step is None:
+            step = expect = st
+        if st != expect:
+            raise ValueError(f"{name}: positions of {tuple(shape)} with strides {strides} are not evenly spaced")
+        expect *= k
+    image = strides[0] if shape[0] > 1 else C * S
+    if want != LAYOUT_CHANNELS_LAST and step in (None, 1) and (C == 1 or strides[1] == S):
+        return LAYOUT_PLANES, S, image, S
+    if want != LAYOUT_PLANES and (C == 1 or strides[1] == 1):
+        return LAYOUT_CHANNELS_LAST, S, image, C if step is None else step
+    kind = {None: "planes or channels last", LAYOUT_PLANES: "planes", LAYOUT_CHANNELS_LAST: "channels last"}[want]
+    raise ValueError(f"{name}: strides {strides} of {tuple(shape)} are not {kind}")
+
+
+@functools.lru_cache(maxsize=1024)
+def _group_norm_desc(B, C, G, S, layout, dtype, param_dtype, activation, eps, x, y, dy, dx):
+    """A description for these sizes (its address and what keeps it), and the
+    workspace bytes of the two passes."""
+    d = GroupNormDesc(B, C, G, S, layout, dtype, param_dtype, activation, eps, Strides(*x), Strides(*y), Strides(*dy),
+                      Strides(*dx))
+    return (ctypes.addressof(d), d, oaa_group_norm_workspace_bytes(d, False),
+            oaa_group_norm_workspace_bytes(d, True))
+
+
+def _group_norm_args(x, num_groups, weight, bias, activation):
+    codes = _dtype_codes()
+    if not x.is_cuda or x.dtype not in codes:
+        raise ValueError(f"x must be a float32, bfloat16 or float16 tensor on the GPU, got {x.dtype} on {x.device}")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
+    param = x.dtype if weight is None and bias is None else (weight if weight is not None else bias).dtype
+    C = x.shape[1] if x.dim() > 1 else 0
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is None:
+            continue
+        if t.dtype != param or t.dtype not in codes or t.device != x.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous, on {x.device}, and of the other parameter's type")
+        if t.dim() != 1 or t.shape[0] != C:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({C},)")
+    return codes[x.dtype], codes[param]
+
+
+def _like(x, layout):
+    """A dense tensor of x's shape in the layout."""
+    import torch
+    if layout == LAYOUT_PLANES:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if x.dim() == 4:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device, memory_format=torch.channels_last)
+    return torch.empty((x.shape[0], *x.shape[2:], x.shape[1]), dtype=x.dtype, device=x.device).movedim(-1, 1)
+
+
+def _matching(t, x, layout, name):
+    """Image and row strides of t, which has x's shape, type, device and layout."""
+    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+        raise ValueError(f"{name} must be a {x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
+    return _norm_layout(t, name, layout)[2:]
+
+
+def group_norm_forward(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none", y=None, stats=True):
+    """oaa_group_norm_forward on torch's current stream of x's device: (y, mean,
+    rstd), the last two [B, G] float32 (None without ``stats``). x[B, C, ...]
+    is laid out in planes or channels last, and so is y."""
+    import torch
+    dtype, param = _group_norm_args(x, num_groups, weight, bias, activation)
+    layout, S, image, row = _norm_layout(x, "x")
+    B, C = x.shape[0], x.shape[1]
+    if y is None:
+        y, out = _like(x, layout), (0, 0)
+    else:
+        out = _matching(y, x, layout, "y")
+    desc, _, need, _ = _group_norm_desc(B, C, num_groups, S, layout, dtype, param, ACTIVATIONS[activation], eps,
+                                        (image, row), out, (0, 0), (0, 0))
+    device = x.device
+    mean = rstd = mean_p = rstd_p = None
+    if stats:
+        mean, rstd = torch.empty((2, B, num_groups), dtype=torch.float32, device=device).unbind(0)
+        mean_p, rstd_p = mean.data_ptr(), rstd.data_ptr()
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    stream, guard = _on_device(device.index)
+    with guard:
+        oaa_group_norm_forward(desc, x.data_ptr(), None if weight is None else weight.data_ptr(),
+                               None if bias is None else bias.data_ptr(), y.data_ptr(), mean_p, rstd_p,
+                               None if ws is None else ws.data_ptr(), need, stream)
+    return y, mean, rstd
+
+
+def group_norm_backward(dy, x, num_groups, weight, bias, mean, rstd, activation="none", need_x=True, need_weight=True,
+                        need_bias=True):
+    """oaa_group_norm_backward on torch's current stream of x's device: (dx,
+    dweight, dbias), None for each that is not needed or whose parameter is
+    None. mean and rstd are the forward pass's."""
+    import torch
+    dtype, param = _group_norm_args(x, num_groups, weight, bias, activation)
+    layout, S, image, row = _norm_layout(x, "x")
+    B, C = x.shape[0], x.shape[1]
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.shape != (B, num_groups) or t.dtype != torch.float32 or t.device != x.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {(B, num_groups)} on {x.device}")
+    desc, _, _, need = _group_norm_desc(B, C, num_groups, S, layout, dtype, param, ACTIVATIONS[activation], 0.0,
+                                        (image, row), (0, 0), _matching(dy, x, layout, "dy"), (0, 0))
+    device = x.device
+    dx = _like(x, layout) if need_x else None
+    dweight = torch.empty_like(weight) if need_weight and weight is not None else None
+    dbias = torch.empty_like(bias) if need_bias and bias is not None else None
+    if dx is None and dweight is None and dbias is None:
+        return None, None, None
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    stream, guard = _on_device(device.index)
+    with guard:
+        oaa_group_norm_backward(desc, dy.data_ptr(), x.data_ptr(), None if weight is None else weight.data_ptr(),
+                                None if bias is None else bias.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr(),
+                                None if dbias is None else dbias.data_ptr(), None if ws is None else ws.data_ptr(),
+                                need, stream)
+    return dx, dweight, dbias
+
+
+NORM_TYPES = {1.0: NORM_SUM, 2.0: NORM_EUCLIDEAN, float("inf"): NORM_MAX}
+
+
+def _dense(t):
+    """Whether t's values fill their memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    expect = 1
+    for st, k in sorted((st, k) for st, k in zip(t.stride(), t.shape) if k != 1):
+        if st != expect:
+            return False
+        expect *= k
+    return True
+
+
+def _grad_lists(grads, device):
+    """Host arrays of the tensors' addresses, sizes and types."""
+    codes = _dtype_codes()
+    kinds = []
+    for i, t in enumerate(grads):
+        if t.dtype not in codes or t.device != device:
+            raise ValueError(f"gradient {i} must be a float32, bfloat16 or float16 tensor on {device}")
+        if not _dense(t):
+            raise ValueError(f"gradient {i} of shape {tuple(t.shape)} has gaps or overlaps (strides {t.stride()})")
+        kinds.append(codes[t.dtype])
+    return (array.array("Q", [t.data_ptr() for t in grads]), array.array("q", [t.numel() for t in grads]),
+            array.array("i", kinds))
+
+
+def _grad_call(grads, norm_type, device):
+    import torch
+    if norm_type not in NORM_TYPES:
+        raise ValueError(f"norm_type must be one of {sorted(NORM_TYPES)}, got {norm_type!r}")
+    if device is None:
+        device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+    if device.type != "cuda":
+        raise ValueError(f"gradients must be on the GPU, not on {device}")
+    need = oaa_grad_workspace_bytes(len(grads))
+    return (device, _grad_lists(grads, device), torch.empty((), dtype=torch.float32, device=device),
+            torch.empty(need, dtype=torch.uint8, device=device))
+
+
+def grad_norm(grads, norm_type=2.0):
+    """oaa_grad_norm on torch's current stream: the norm over all values of the
+    tensors, a float32 scalar on their device. norm_type: 1, 2 or infinity."""
+    grads = list(grads)
+    device, (src, sizes, kinds), norm, ws = _grad_call(grads, norm_type, None)
+    stream, guard = _on_device(device.index)
+    with guard:
+        oaa_grad_norm(len(grads), src.buffer_info()[0], sizes.buffer_info()[0], kinds.buffer_info()[0],
+                      NORM_TYPES[norm_type], norm.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    return norm
+
+
+def grad_clip(grads, max_norm, norm_type=2.0, out=None):
+    """oaa_grad_clip on torch's current stream: the tensors scaled by min(1,
+    max_norm / (norm + 1e-6)), in place or into ``out`` (tensors of the same
+    shapes, types and strides). Returns the norm before clipping."""
+    grads = list(grads)
+    device, (src, sizes, kinds), norm, ws = _grad_call(grads, norm_type, None)
+    dst = src
+    if out is not None:
+        out = list(out)
+        if len(out) != len(grads):
+            raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
+        for i, (g, o) in enumerate(zip(grads, out)):
+            if o.dtype != g.dtype or o.device != device or o.shape != g.shape or o.stride() != g.stride():
+                raise ValueError(f"output {i} differs from its gradient in shape, strides, type or device")
+        dst = array.array("Q", [t.data_ptr() for t in out])
+    stream, guard = _on_device(device.index)
+    with guard:
+        oaa_grad_clip(len(grads), src.buffer_info()[0], dst.buffer_info()[0], sizes.buffer_info()[0],
+                      kinds.buffer_info()[0], NORM_TYPES[norm_type], max_norm, norm.data_ptr(), ws.data_ptr(),
+                      ws.numel(), stream)
+    return norm

@@ -1,0 +1,64 @@
+// The element types of the normalisation and gradient operators: values are
+// computed in float32 and rounded to the nearest (ties to even) where they are
+// stored in 16 bits.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "oaa.h"
+
+namespace oaa {
+
+using bf16 = __bf16;
+using f16 = _Float16;
+
+inline size_t dtype_size(int dtype) { return dtype == OAA_FLOAT32 ? 4 : 2; }
+
+// V neighbouring elements, aligned to one element only: rows of any length
+// start anywhere, and gfx950 loads and stores 16 bytes at any address.
+template <typename T, int V>
+struct VecOf {
+  typedef T raw __attribute__((ext_vector_type(V)));
+  typedef raw type __attribute__((aligned(sizeof(T))));
+};
+template <typename T>
+struct VecOf<T, 1> {
+  typedef T type;
+};
+template <typename T, int V>
+using Vec = typename VecOf<T, V>::type;
+
+template <typename T, int V>
+__device__ __forceinline__ float element(const Vec<T, V>& v, int i) {
+  if constexpr (V == 1)
+    return float(v);
+  else
+    return float(v[i]);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void set_element(Vec<T, V>& v, int i, float f) {
+  if constexpr (V == 1)
+    v = T(f);
+  else
+    v[i] = T(f);
+}
+
+// One element of a parameter (weight, bias) whose type is known at run time.
+__device__ __forceinline__ float load_param(const void* p, int dtype, long i, float absent) {
+  if (!p) return absent;
+  if (dtype == OAA_FLOAT32) return static_cast<const float*>(p)[i];
+  if (dtype == OAA_BFLOAT16) return float(static_cast<const bf16*>(p)[i]);
+  return float(static_cast<const f16*>(p)[i]);
+}
+
+__device__ __forceinline__ void store_param(void* p, int dtype, long i, float f) {
+  if (dtype == OAA_FLOAT32)
+    static_cast<float*>(p)[i] = f;
+  else if (dtype == OAA_BFLOAT16)
+    static_cast<bf16*>(p)[i] = bf16(f);
+  else
+    static_cast<f16*>(p)[i] = f16(f);
+}
+
+}  // namespace oaa

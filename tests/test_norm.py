@@ -1,0 +1,523 @@
+"""Group normalisation with an activation, through the public calls, against
+the fp64 oracle.
+
+Bars, set by the arithmetic: a float32 result passes about ten roundings of
+2^-24 at the magnitude of its largest terms, and sums of up to 10^6 float32
+terms are held in 64 bits or summed pairwise, so 2e-5 of the largest magnitude
+(the convolution's bar) leaves a wide margin; a 16-bit result adds half a step
+of its own type. The input gradient is a difference of terms of size
+rstd |t|, so that is its magnitude.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import norm as oracle
+from paper_1601_06815_amd import autograd, binding
+
+DEV = "cuda:0"
+TOL = 2e-5
+STEP = {torch.float32: 0.0, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+LEAST = {torch.float32: 0.0, torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}
+ACTS = sorted(binding.ACTIVATIONS)
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def wide(t):
+    return t.detach().cpu().double().numpy()
+
+
+def close(got, ref, dtype, scale=None, tol=TOL, what=""):
+    got = wide(got)
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    scale = np.max(np.abs(ref), initial=0.0) if scale is None else scale
+    bound = tol * scale + STEP[dtype] * (np.abs(ref) + tol * scale) + LEAST[dtype]
+    off = np.abs(got - ref)
+    worst = float(np.max(off - bound, initial=-1.0))
+    assert worst <= 0 and not np.isnan(got).any(), (what, worst, float(np.max(off, initial=0.0)), scale)
+
+
+def lay(t, layout):
+    """The same values in planes or channels last, dense."""
+    return t.contiguous() if layout == "planes" else t.movedim(1, -1).contiguous().movedim(-1, 1)
+
+
+def make(shape, G, layout="planes", dtype=torch.float32, params=torch.float32, seed=0, offset=0.5):
+    rng = np.random.default_rng(seed)
+    C = shape[1]
+    side = (1, C) + (1,) * (len(shape) - 2)
+    x = rng.standard_normal(shape) * (0.5 + np.abs(rng.standard_normal(side))) + offset * rng.standard_normal(side)
+    x, dy = (lay(torch.from_numpy(a).to(DEV, dtype), layout) for a in (x, rng.standard_normal(shape) * 0.1))
+    w, b = (torch.from_numpy(a).to(DEV, params) for a in (1 + 0.2 * rng.standard_normal(C), 0.2 * rng.standard_normal(C)))
+    return x, dy, w, b
+
+
+def away_from_zero(x, dy, G, w, b, eps):
+    """dy, zero where the pre-activation is so near 0 that rounding decides
+    which side of the ReLU's corner it lies on."""
+    z = oracle.group_norm_preactivation(wide(x), G, None if w is None else wide(w), None if b is None else wide(b), eps)
+    return dy.clone().masked_fill_(torch.from_numpy(np.abs(z) < 1e-3).to(dy.device), 0.0)
+
+
+def check(x, dy, G, w, b, act, eps=1e-5, stats_tol=1e-6, tol=TOL):
+    """Forward and backward against the oracle."""
+    dtype = x.dtype
+    if act == "relu":
+        dy = away_from_zero(x, dy, G, w, b, eps)
+    y, mean, rstd = binding.group_norm_forward(x, G, w, b, eps, act)
+    dx, dw, db = binding.group_norm_backward(dy, x, G, w, b, mean, rstd, act)
+    torch.cuda.synchronize()
+    X, DY = wide(x), wide(dy)
+    W, Bv = (None if t is None else wide(t) for t in (w, b))
+    ry, rmean, rrstd = oracle.group_norm_forward(X, G, W, Bv, eps, act)
+    rdx, rdw, rdb = oracle.group_norm_backward(DY, X, G, W, Bv, eps, act)
+    spread = np.abs(X).max()
+    close(mean, rmean, torch.float32, scale=spread, tol=stats_tol, what="mean")
+    close(rstd / torch.from_numpy(rrstd).to(DEV), np.ones_like(rrstd), torch.float32, tol=stats_tol, what="rstd")
+    close(y, ry, dtype, scale=max(1.0, np.abs(ry).max()), tol=tol, what="y")
+    t = DY * (1 if W is None else np.abs(W).reshape((1, -1) + (1,) * (X.ndim - 2))) * 1.2
+    close(dx, rdx, dtype, scale=float(rrstd.max() * np.abs(t).max()), tol=tol, what="dx")
+    n = X.shape[0] * int(np.prod(X.shape[2:]))
+    for name, got, ref in (("dweight", dw, rdw), ("dbias", db, rdb)):
+        if got is not None:
+            # the sum of n terms of either sign: errors of its terms add up like their square root
+            close(got, ref, got.dtype, scale=float(np.sqrt(n) * np.abs(DY).max() * 4), tol=tol, what=name)
+    return y, dx, dw, db
+
+
+SHAPES = [  # (B, C, G, spatial sizes): odd and ragged, one value, one position, one group, one channel a group
+    ((1, 4, 28, 28), 2), ((1, 1, 1, 1), 1), ((2, 6, 1, 1), 3), ((3, 5, 7, 3), 5), ((2, 27, 13, 11), 3),
+    ((4, 12, 5, 5), 1), ((1, 100, 63, 63), 4), ((2, 96, 20, 20), 32), ((3, 8, 33, 1), 8), ((1, 500, 9, 9), 20),
+    ((2, 33, 113, 113), 11), ((130, 64, 2, 2), 8), ((1, 7, 1, 2), 7), ((5, 257, 3, 3), 1), ((1, 1030, 2, 2), 2),
+    ((2, 2100, 1, 3), 3), ((7, 40, 16, 16), 5), ((128, 256, 1, 1), 32), ((2, 16, 252, 251), 2), ((3, 64, 31, 33), 16),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,G", SHAPES, ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else f"g{v}")
+def test_both_passes(gpu_lib, shape, G, layout):
+    i = [s for s, _ in SHAPES].index(shape)
+    dtype, act = TYPES[i % 3], ACTS[(i // 3 + (layout == "last")) % 4]
+    params = [torch.float32, dtype][i % 2]
+    print(shape, G, layout, dtype, params, act, flush=True)
+    x, dy, w, b = make(shape, G, layout, dtype, params, seed=i)
+    y, dx, _, _ = check(x, dy, G, w, b, act)
+    if shape[1] > 1 and np.prod(shape[2:]) > 1:
+        assert y.stride() == x.stride() and dx.stride() == x.stride()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_types_and_activations(gpu_lib, layout, dtype, act):
+    for shape, G, params in (((2, 24, 17, 19), 4, torch.float32), ((40, 16, 9, 9), 4, dtype)):
+        x, dy, w, b = make(shape, G, layout, dtype, params, seed=3)
+        check(x, dy, G, w, b, act)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape", [(2, 10), (3, 8, 37), (2, 6, 3, 5, 7)], ids=str)
+def test_other_ranks_and_absent_parameters(gpu_lib, shape, layout):
+    x, dy, w, b = make(shape, 2, layout, seed=5)
+    for weight, bias in ((None, None), (w, None), (None, b)):
+        check(x, dy, 2, weight, bias, "silu")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("view", ["channels", "channels last", "rows last", "images", "one image many times",
+                                  "one image many times, last", "odd address"])
+def test_strided_inputs(gpu_lib, view, dtype):
+    """Slices of larger tensors are read in place, and written in place through y."""
+    base, other, _, _ = make((4, 12, 9, 7), 1, "last" if "last" in view else "planes", dtype, seed=7)
+    cut = {"channels": lambda t: t[:, 3:9], "channels last": lambda t: t[:, 3:9], "rows last": lambda t: t[:, :6, 2:6],
+           "images": lambda t: t[::2, :6], "one image many times": lambda t: t[:1, :6].expand(3, 6, 9, 7),
+           "one image many times, last": lambda t: t[:1, 1:7].expand(3, 6, 9, 7),
+           "odd address": lambda t: t.flatten()[1:1 + 2 * 6 * 63].view(2, 6, 9, 7)}[view]
+    x, dy = cut(base), cut(other)
+    w, b = make((1, 6, 1, 1), 1, seed=8)[2:]
+    check(x, dy, 3, w, b, "gelu")
+    # a slice as the output: what lies around it stays
+    room = torch.full((4, 20, 11, 7), 7.0, device=DEV, dtype=dtype)
+    room = room.to(memory_format=torch.channels_last) if "last" in view else room
+    y = (room[:x.shape[0], 5:11, 1:10] if "last" in view else room.flatten(2)[:x.shape[0], 5:11, :63].unflatten(2, (9, 7)))
+    if "last" not in view:
+        room = torch.full((4, 20, 63), 7.0, device=DEV, dtype=dtype)
+        y = room[:x.shape[0], 5:11].unflatten(2, (9, 7))
+    y = y[:, :, :x.shape[2]]
+    got = binding.group_norm_forward(x, 3, w, b, 1e-5, "gelu", y=y)[0]
+    assert got is y
+    close(y, oracle.group_norm_forward(wide(x), 3, wide(w), wide(b), 1e-5, "gelu")[0], dtype)
+    assert int((room != 7.0).sum()) <= y.numel()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,G", [((2, 8, 20, 20), 2), ((1, 8, 200, 200), 2), ((40, 32, 24, 24), 4)], ids=str)
+def test_large_offsets(gpu_lib, shape, G, layout):
+    """Means of 1000 and 10^6 deviations: the variance keeps its digits; x - mean
+    has the spacing of float32 at the mean, which is the bound's second term."""
+    for offset in (1e3, 1e6):
+        x, dy, w, b = make(shape, G, layout, seed=11, offset=0.0)
+        x = lay(torch.round(x * 16) / 16 + offset, layout)
+        rstd = oracle.group_norm_forward(wide(x), G)[2].max()
+        check(x, dy, G, w, b, "none", stats_tol=1e-6 + 2.0 ** -23, tol=TOL + 4 * offset * 2.0 ** -24 * float(rstd))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("size", [1e30, 3e38, 1e-30])
+def test_range_of_float32(gpu_lib, size, layout):
+    """Squares beyond float32's range, and variances far below eps."""
+    x, dy, w, b = make((2, 6, 15, 15), 3, layout, seed=13, offset=0.0)
+    x = (x / x.abs().max()) * size
+    y, mean, rstd = binding.group_norm_forward(x, 3, w, b, 1e-5, "silu")
+    ry, _, rrstd = oracle.group_norm_forward(wide(x), 3, wide(w), wide(b), 1e-5, "silu")
+    close(y, ry, torch.float32, scale=max(1.0, np.abs(ry).max()))
+    assert np.abs(wide(rstd) / rrstd - 1).max() < (1e-6 if size < 1e38 else 1e-5)  # 1e-38 is next to the subnormals
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,G", [((3, 8, 20, 21), 4), ((2, 8, 150, 151), 4), ((64, 32, 30, 30), 8)], ids=str)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_values_that_are_not_finite(gpu_lib, value, shape, G, layout):
+    """One bad value makes its own group of its own image NaN, and nothing else
+    but that group's parameter gradients."""
+    x, dy, w, b = make(shape, G, layout, seed=17)
+    D = shape[1] // G
+    bad = x.clone()
+    bad[1, D + 1, -1, -1] = value
+    y, mean, rstd = binding.group_norm_forward(bad, G, w, b, 1e-5, "silu")
+    dx, dw, db = binding.group_norm_backward(dy, bad, G, w, b, mean, rstd, "silu")
+    clean = binding.group_norm_forward(x, G, w, b, 1e-5, "silu")
+    cdx, cdw, cdb = binding.group_norm_backward(dy, x, G, w, b, clean[1], clean[2], "silu")
+    for got, ref in ((y, clean[0]), (dx, cdx)):
+        inside = torch.zeros_like(got, dtype=torch.bool)
+        inside[1, D:2 * D] = True
+        assert bool(torch.isnan(got[inside]).all())
+        assert bool((got[~inside] == ref[~inside]).all())
+    channels = torch.zeros(shape[1], dtype=torch.bool, device=DEV)
+    channels[D:2 * D] = True
+    for got, ref in ((dw, cdw), (db, cdb)):
+        assert bool(torch.isnan(got[channels]).all()) and bool((got[~channels] == ref[~channels]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_equal_values(gpu_lib, layout):
+    """A group without variance is act(bias), and its input gradient is finite."""
+    x = lay(torch.full((2, 6, 30, 30), 1000.1, device=DEV), layout)
+    _, dy, w, b = make((2, 6, 30, 30), 3, layout, seed=19)
+    y, mean, rstd = binding.group_norm_forward(x, 3, w, b, 1e-5, "none")
+    assert bool((y == b.reshape(1, 6, 1, 1)).all())
+    dx, dw, _ = binding.group_norm_backward(dy, x, 3, w, b, mean, rstd, "none")
+    assert bool((dw == 0).all()) and bool(torch.isfinite(dx).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape", [(0, 6, 4, 4), (3, 6, 0, 4)], ids=str)
+def test_empty(gpu_lib, shape, layout):
+    x = torch.empty(shape, device=DEV)
+    x = x.to(memory_format=torch.channels_last) if layout == "last" else x
+    w, b = torch.ones(6, device=DEV), torch.ones(6, device=DEV)
+    y, mean, rstd = binding.group_norm_forward(x, 3, w, b)
+    assert y.shape == x.shape
+    dx, dw, db = binding.group_norm_backward(torch.empty_like(x), x, 3, w, b, mean, rstd)
+    assert dx.shape == x.shape and bool((dw == 0).all()) and bool((db == 0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_only_what_is_needed(gpu_lib, layout):
+    x, dy, w, b = make((3, 8, 19, 19), 4, layout, seed=23)
+    _, mean, rstd = binding.group_norm_forward(x, 4, w, b, activation="silu")
+    whole = binding.group_norm_backward(dy, x, 4, w, b, mean, rstd, "silu")
+    for need in ((True, False, False), (False, True, False), (False, False, True), (True, False, True),
+                 (False, False, False)):
+        part = binding.group_norm_backward(dy, x, 4, w, b, mean, rstd, "silu", *need)
+        for want, got, ref in zip(need, part, whole):
+            assert (got is not None) == want
+            assert not want or torch.equal(got, ref)
+    assert torch.equal(binding.group_norm_forward(x, 4, w, b, activation="silu", stats=False)[0],
+                       binding.group_norm_forward(x, 4, w, b, activation="silu")[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+def test_gradients_against_differences(gpu_lib, act, layout):
+    """<dy, (y(p + h v) - y(p - h v)) / 2h> = <gradient, v> for x, weight and
+    bias. y carries 1e-7 of itself, so the quotient is off by about 1e-7 / h per
+    value, added like a square root, and by h^2 times a third derivative of
+    order 1: with h = 1e-2 both are under 1e-3 of the largest term."""
+    x, dy, w, b = make((2, 6, 8, 9), 3, layout, seed=29)
+    _, mean, rstd = binding.group_norm_forward(x, 3, w, b, activation=act)
+    grads = binding.group_norm_backward(dy, x, 3, w, b, mean, rstd, act)
+    rng = np.random.default_rng(31)
+    h = 1e-2
+    for i, p in enumerate((x, w, b)):
+        v = lay(torch.from_numpy(rng.choice([-1.0, 1.0], size=tuple(p.shape))).to(DEV, torch.float32), layout) \
+            if p.dim() > 1 else torch.from_numpy(rng.choice([-1.0, 1.0], size=tuple(p.shape))).to(DEV, torch.float32)
+        args = [x, w, b]
+        ends = []
+        for sign in (1, -1):
+            args[i] = p + sign * h * v
+            ends.append(wide(binding.group_norm_forward(args[0], 3, args[1], args[2], activation=act)[0]))
+        quotient = float(((ends[0] - ends[1]) / (2 * h) * wide(dy)).sum())
+        got = float((wide(grads[i]) * wide(v)).sum())
+        scale = float(np.sqrt(dy.numel()) * np.abs(wide(dy)).max() * max(1.0, float(rstd.max())))
+        assert abs(quotient - got) < 1e-3 * scale, (i, quotient, got, scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_autograd(gpu_lib, layout):
+    """The layer against its own direct calls, broadcast upstream gradients,
+    inputs that need a copy, and no gradient of a gradient."""
+    x, dy, w, b = make((3, 12, 11, 10), 4, layout, seed=37)
+    layer = autograd.GroupNorm(4, 12, activation="gelu", device=DEV)
+    with torch.no_grad():
+        layer.weight.copy_(w)
+        layer.bias.copy_(b)
+    x.requires_grad_()
+    y = layer(x)
+    got = torch.autograd.grad(y, (x, layer.weight, layer.bias), dy)
+    y0, mean, rstd = binding.group_norm_forward(x.detach(), 4, w, b, activation="gelu")
+    ref = binding.group_norm_backward(dy, x.detach(), 4, w, b, mean, rstd, "gelu")
+    assert torch.equal(y, y0) and all(torch.equal(a, r) for a, r in zip(got, ref))
+    # y.sum(): the upstream gradient is one value with strides of zero
+    (gx,) = torch.autograd.grad(layer(x).sum(), x)
+    rx = binding.group_norm_backward(torch.ones_like(x), x.detach(), 4, w, b, mean, rstd, "gelu")[0]
+    assert torch.equal(gx, rx)
+    # the other layout upstream
+    flipped = lay(dy, "last" if layout == "planes" else "planes")
+    assert torch.equal(torch.autograd.grad(layer(x), x, flipped)[0], got[0])
+    # every second row of a larger tensor: evenly spaced in neither layout
+    big = torch.zeros((3, 12, 22, 10), device=DEV)
+    big[:, :, ::2] = x.detach()
+    assert torch.equal(layer(big[:, :, ::2].requires_grad_()).contiguous(), y.contiguous())
+    with torch.no_grad():
+        assert torch.equal(layer(x), y)
+    twice = torch.autograd.grad(layer(x).sum(), x, create_graph=True)[0]
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(twice.sum(), x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,G", [((1, 4, 28, 28), 2), ((2, 16, 130, 129), 4), ((300, 32, 9, 9), 8)], ids=str)
+def test_equal_calls_give_equal_bits(gpu_lib, shape, G, layout):
+    x, dy, w, b = make(shape, G, layout, seed=41)
+    runs = []
+    for _ in range(3):
+        y, mean, rstd = binding.group_norm_forward(x, G, w, b, activation="silu")
+        runs.append((y, mean, rstd) + binding.group_norm_backward(dy, x, G, w, b, mean, rstd, "silu"))
+    for r in runs[1:]:
+        assert all(torch.equal(a, c) for a, c in zip(runs[0], r))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,G", [((1, 4, 28, 28), 2), ((2, 16, 130, 129), 4)], ids=str)
+def test_other_stream_and_graph(gpu_lib, shape, G, layout):
+    x, dy, w, b = make(shape, G, layout, seed=43)
+
+    def both():
+        y, mean, rstd = binding.group_norm_forward(x, G, w, b, activation="silu")
+        return (y,) + binding.group_norm_backward(dy, x, G, w, b, mean, rstd, "silu")
+
+    ref = both()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = both()
+    side.synchronize()
+    assert all(torch.equal(a, r) for a, r in zip(got, ref))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both()
+    for k in range(4):
+        x.mul_(-1) if k % 2 else x.add_(0.25)
+        eager = [t.clone() for t in both()]
+        for t in out:
+            t.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, r) for a, r in zip(out, eager)), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_past_32_bit_offsets(gpu_lib, layout):
+    """2.2 * 10^9 values in two groups: the second lies beyond 2^31 elements in
+    planes, and both do channels last."""
+    side = 16600
+    x = torch.empty((1, 8, side, side), dtype=torch.bfloat16, device=DEV,
+                    memory_format=torch.channels_last if layout == "last" else torch.contiguous_format)
+    x.normal_().mul_(0.5)
+    x[0, 4:] += 1.0
+    w, b = torch.linspace(0.5, 1.5, 8, device=DEV), torch.linspace(-1, 1, 8, device=DEV)
+    y, mean, rstd = binding.group_norm_forward(x, 2, w, b, activation="silu")
+    n = 4.0 * side * side
+    m, q = [], []
+    for g in range(2):
+        part = x[0, 4 * g:4 * g + 4]
+        s = sum(part[:, r:r + 1000].double().sum() for r in range(0, side, 1000))
+        m.append(float(s) / n)
+        q.append(float(sum((part[:, r:r + 1000].double() - m[g]).square().sum() for r in range(0, side, 1000))) / n)
+    close(mean, np.array([m]), torch.float32)
+    close(rstd, np.array([1 / np.sqrt(np.array(q) + 1e-5)]), torch.float32)
+    for rows in (slice(0, 3), slice(side // 2, side // 2 + 3), slice(side - 3, side)):
+        part = x[0, :, rows].double().cpu().numpy()
+        mu, var = np.repeat(m, 4).reshape(8, 1, 1), np.repeat(q, 4).reshape(8, 1, 1)
+        z = (part - mu) / np.sqrt(var + 1e-5) * wide(w).reshape(8, 1, 1) + wide(b).reshape(8, 1, 1)
+        close(y[0, :, rows], z / (1 + np.exp(-z)), torch.bfloat16)
+    del y
+    dy = torch.zeros_like(x)
+    dy[0, :, -1, -1] = 1.0
+    dx, dw, db = binding.group_norm_backward(dy, x, 2, w, b, mean, rstd, "none")
+    xh = (x[0, :, -1, -1].double().cpu().numpy() - np.repeat(m, 4)) / np.sqrt(np.repeat(q, 4) + 1e-5)
+    close(db, np.ones(8), torch.float32)
+    close(dw, xh, torch.float32)
+    close(dx[0, :, -1, -1], wide(w) / np.sqrt(np.repeat(q, 4) + 1e-5), torch.bfloat16)
+    assert float(dx[0, :, 0, 0].abs().max()) < 1e-6
+
+
+# ---- no GPU ---------------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def lib():
+    import os
+
+    from paper_1601_06815_amd import build
+    if not os.path.exists(build.LIB_PATH):
+        build.build()
+    return binding.load()
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("shape,G", [((2, 6, 5, 4), 3), ((1, 4, 7), 1), ((3, 4), 2)], ids=str)
+def test_oracle_matches_float64_autograd(act, shape, G):
+    rng = np.random.default_rng(47)
+    x, dy = rng.standard_normal(shape) + 0.3, rng.standard_normal(shape)
+    w, b = 1 + 0.1 * rng.standard_normal(shape[1]), 0.1 * rng.standard_normal(shape[1])
+    tx, tw, tb = (torch.from_numpy(a).requires_grad_() for a in (x, w, b))
+    z = torch.nn.functional.group_norm(tx, G, tw, tb, 1e-5)
+    y = {"none": z, "relu": z.relu(), "silu": torch.nn.functional.silu(z), "gelu": torch.nn.functional.gelu(z)}[act]
+    refs = torch.autograd.grad(y, (tx, tw, tb), torch.from_numpy(dy))
+    assert np.allclose(oracle.group_norm_forward(x, G, w, b, 1e-5, act)[0], y.detach().numpy(), rtol=1e-11, atol=1e-12)
+    for got, ref in zip(oracle.group_norm_backward(dy, x, G, w, b, 1e-5, act), refs):
+        assert np.allclose(got, ref.numpy(), rtol=1e-9, atol=1e-11)
+
+
+def desc(B=2, C=6, G=3, S=10, layout=0, dtype=0, param_dtype=0, activation=0, eps=1e-5, **strides):
+    return binding.GroupNormDesc(B, C, G, S, layout, dtype, param_dtype, activation, eps,
+                                 *(binding.Strides(*strides.get(k, (0, 0))) for k in ("x", "y", "dy", "dx")))
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(B=-1), 1), (dict(C=0), 1), (dict(G=0), 1), (dict(G=4), 1), (dict(S=-1), 1), (dict(layout=2), 1),
+    (dict(dtype=3), 1), (dict(param_dtype=1), 1), (dict(dtype=1, param_dtype=2), 1), (dict(activation=4), 1),
+    (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1), (dict(S=1 << 60), 2), (dict(B=1 << 30, C=1 << 10, G=1), 2),
+    (dict(x=(60, 11)), 2), (dict(x=(-1, 0)), 1), (dict(y=(59, 10)), 1), (dict(layout=1, y=(60, 5)), 1),
+    (dict(layout=1, y=(59, 6)), 1), (dict(layout=1, dx=(60, 5)), 1), (dict(layout=1, x=(1 << 60, 6)), 2),
+    (dict(layout=1, x=(0, 1)), 3), (dict(layout=1, y=(60, 6)), 3), (dict(layout=1, y=(100, 8)), 3), (dict(), 3),
+])
+def test_refused_descriptions(lib, change, status):
+    """Refused before any launch; 3: the description is fine, the missing workspace is not."""
+    d = desc(**change)
+    with pytest.raises(binding.OaaError) as e:
+        binding.oaa_group_norm_backward(d, 256, 256, None, None, 256, 256, 256, None, None, None, 0, None)
+    assert e.value.status == status and e.value.detail
+    assert (binding.oaa_group_norm_workspace_bytes(d, True) > 0) == (status == 3)
+
+
+@pytest.mark.parametrize("args,status", [
+    ((None, 256), 1), ((256, None), 1), ((255, 256), 1), ((256, 258), 1),
+])
+def test_refused_pointers(lib, args, status):
+    with pytest.raises(binding.OaaError) as e:
+        binding.oaa_group_norm_forward(desc(), args[0], None, None, args[1], 256, 256, 512, 1 << 20, None)
+    assert e.value.status == status
+    for bad in (dict(dx=None), dict(dy=None), dict(x=None), dict(mean=None), dict(rstd=None), dict(dw=254), dict(ws=8)):
+        k = dict(dy=256, x=256, mean=256, rstd=256, dx=256, dw=None, ws=256, **{})
+        k.update(bad)
+        with pytest.raises(binding.OaaError) as e:
+            binding.oaa_group_norm_backward(desc(), k["dy"], k["x"], None, None, k["mean"], k["rstd"], k["dx"], k["dw"],
+                                            None, k["ws"], 1 << 20, None)
+        assert e.value.status == 1, bad
+    with pytest.raises(binding.OaaError) as e:
+        binding.oaa_group_norm_forward(None, 256, None, None, 256, None, None, 256, 1 << 20, None)
+    assert e.value.status == 1
+
+
+def test_empty_is_no_work(lib):
+    for d in (desc(B=0), desc(S=0)):
+        assert binding.oaa_group_norm_workspace_bytes(d, False) == 0
+        binding.oaa_group_norm_forward(d, None, None, None, None, None, None, None, 0, None)
+        binding.oaa_group_norm_backward(d, None, None, None, None, None, None, 256, None, None, None, 0, None)
+
+
+@pytest.mark.parametrize("shape,strides,want,found", [
+    ((2, 3, 4, 5), (60, 20, 5, 1), None, (0, 20, 60, 20)), ((2, 3, 4, 5), (60, 1, 15, 3), None, (1, 20, 60, 3)),
+    ((2, 3, 4, 5), (200, 1, 50, 10), None, (1, 20, 200, 10)), ((2, 3, 4, 5), (0, 20, 5, 1), None, (0, 20, 0, 20)),
+    ((2, 3, 1, 1), (3, 1, 1, 1), None, (0, 1, 3, 1)), ((2, 3, 1, 1), (3, 1, 1, 1), 1, (1, 1, 3, 3)),
+    ((2, 1, 4, 5), (20, 1, 5, 1), 1, (1, 20, 20, 1)), ((1, 3, 4, 5), (7, 20, 5, 1), None, (0, 20, 60, 20)),
+    ((2, 3, 4, 5), (60, 20, 5, 1), 1, None), ((2, 3, 4, 5), (60, 1, 15, 3), 0, None),
+    ((2, 3, 4, 5), (120, 40, 10, 1), None, None), ((2, 3, 4, 5), (120, 40, 10, 2), None, None),
+    ((2, 3, 4, 5), (60, 1, 3, 12), None, None), ((2, 3), (3, 1), None, (0, 1, 3, 1)), ((6,), (1,), None, None),
+])
+def test_layouts_recognised(shape, strides, want, found):
+    t = torch.empty(400).as_strided(shape, strides)
+    if found is None:
+        with pytest.raises(ValueError):
+            binding._norm_layout(t, "x", want)
+    else:
+        assert binding._norm_layout(t, "x", want) == found
+
+
+def test_binding_refuses_with_reasons():
+    x = torch.zeros(2, 6, 4, 4)
+    with pytest.raises(ValueError, match="on the GPU"):
+        binding.group_norm_forward(x, 3)
+    with pytest.raises(ValueError, match="divide"):
+        autograd.GroupNorm(4, 6, device="cpu")
+    with pytest.raises(ValueError, match="activation"):
+        autograd.GroupNorm(3, 6, activation="tanh", device="cpu")
+    with pytest.raises(ValueError, match="expected"):
+        autograd.GroupNorm(3, 6, device="cpu")(torch.zeros(2, 5, 4, 4))
+
+
+@pytest.mark.gpu
+def test_binding_refuses_on_the_gpu(gpu_lib):
+    x, dy, w, b = make((2, 6, 4, 4), 3)
+    _, mean, rstd = binding.group_norm_forward(x, 3, w, b)
+    with pytest.raises(ValueError, match="activation"):
+        binding.group_norm_forward(x, 3, w, b, activation="tanh")
+    for bad in (w[:5], w.double(), w.cpu(), w.reshape(6, 1)):
+        with pytest.raises(ValueError, match="weight"):
+            binding.group_norm_forward(x, 3, bad, b)
+    with pytest.raises(ValueError, match="bias"):
+        binding.group_norm_forward(x, 3, w, b.bfloat16())
+    with pytest.raises(ValueError, match="x must be"):
+        binding.group_norm_forward(x.double(), 3)
+    with pytest.raises(binding.OaaError, match="divide"):
+        binding.group_norm_forward(x, 4, w, b)
+    with pytest.raises(ValueError, match="y must be"):
+        binding.group_norm_forward(x, 3, w, b, y=torch.empty((2, 6, 4, 5), device=DEV))
+    with pytest.raises(ValueError, match="planes"):
+        binding.group_norm_forward(x, 3, w, b, y=lay(x, "last"))
+    with pytest.raises(binding.OaaError, match="overlaps"):
+        binding.group_norm_forward(x, 3, w, b, y=x[:1].expand(2, 6, 4, 4))
+    with pytest.raises(ValueError, match="dy"):
+        binding.group_norm_backward(dy[:1], x, 3, w, b, mean, rstd)
+    with pytest.raises(ValueError, match="mean"):
+        binding.group_norm_backward(dy, x, 3, w, b, mean[:1], rstd)
+    with pytest.raises(ValueError, match="rstd"):
+        binding.group_norm_backward(dy, x, 3, w, b, mean, rstd.double())
