@@ -24,6 +24,28 @@ struct GroupNormParams {
   char* ws;
 };
 
+// How a pass is cut over the device. split: groups go to several workgroups, in
+// `count` slices of `slice` each (of a group, a row or an image, by layout and
+// pass); otherwise each group to one (channels last, in `count` slabs an image).
+struct NormCut {
+  bool split;
+  long slice, count;
+};
+
+// Where the backward pass leaves each channel's sums of dz and dz xh, in
+// `count` parts: part k of channel c of image b is sums[b image + c channel + k
+// slot]. means[B][G], the groups' means of t and t xh, are needed only where
+// groups are split: launch_norm_join makes them before dx.
+struct NormSums {
+  float2* sums;
+  float2* means;
+  long count, image, channel, slot;
+};
+
+// One launch handles at most this many channels of images, so that its grid
+// has fewer than 2^32 threads.
+constexpr long kMostChannels = 1 << 21;
+
 // Workspace bytes of a pass (a multiple of kWorkspaceAlign).
 size_t group_norm_forward_ws(const GroupNormParams& p);
 size_t group_norm_backward_ws(const GroupNormParams& p);
@@ -31,5 +53,24 @@ hipError_t launch_group_norm_forward(const GroupNormParams& p, hipStream_t s);
 hipError_t launch_group_norm_backward(const GroupNormParams& p, hipStream_t s);
 // dweight and dbias of no images: zeros.
 hipError_t launch_group_norm_no_images(const GroupNormParams& p, hipStream_t s);
+
+// Per layout, for at most kMostChannels / C images. A cut serves the images it
+// was made for and any fewer.
+NormCut planes_forward_cut(const GroupNormParams& p);
+size_t planes_forward_ws(const GroupNormParams& p, const NormCut& cut);
+hipError_t launch_planes_forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s);
+NormCut planes_backward_cut(const GroupNormParams& p);
+NormSums planes_sums(const GroupNormParams& p, const NormCut& cut);  // its layout, no pointers
+hipError_t launch_planes_backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s);
+NormCut last_forward_cut(const GroupNormParams& p);
+size_t last_forward_ws(const GroupNormParams& p, const NormCut& cut);
+hipError_t launch_last_forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s);
+NormCut last_backward_cut(const GroupNormParams& p);
+NormSums last_sums(const GroupNormParams& p, const NormCut& cut);
+hipError_t launch_last_backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s);
+
+// means of p's groups (where at.means is set), and dweight and dbias over p's
+// images (where p has them).
+hipError_t launch_norm_join(const GroupNormParams& p, const NormSums& at, hipStream_t s);
 
 }  // namespace oaa

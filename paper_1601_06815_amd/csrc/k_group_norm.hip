@@ -1,250 +1,160 @@
-// Group normalisation with an activation, forward and backward.
-//
-//   mean, var over the n = D S values of a group of an image;
-//   xh = (x - mean) rstd, z = w xh + b, y = act(z);
-//   dz = dy act'(z), t = w dz, dx = rstd (t - sum t / n - xh sum (t xh) / n).
-//
-// One workgroup per group sums, one element per lane is applied. Sums are in
-// float64 of d = x - x0, x0 the group's first value: the variance is E[d^2] -
-// E[d]^2, which loses nothing however far the mean is from 0.
-#include "group_norm.hpp"
-#include "oaa_status.hpp"
-#include "scalar_types.hpp"
+// Group normalisation: the order of launches, and what both layouts share: the
+// join of the backward pass's sums. The passes over the values are in
+// k_norm_planes.hip and k_norm_last.hip.
+#include <algorithm>
+
+#include "norm_common.hpp"
 
 namespace oaa {
 namespace {
 
 constexpr int kThreads = 256;
+// dweight and dbias: a workgroup takes kColumns channels, 64 bytes of the sums'
+// rows where those run along the channels, on kThreads / kColumns lanes each.
+constexpr int kColumns = 8, kLanes = kThreads / kColumns;
 
-size_t align_up(size_t v) { return (v + kWorkspaceAlign - 1) / kWorkspaceAlign * kWorkspaceAlign; }
-
-__device__ __forceinline__ float sigmoid(float z) { return 1.0f / (1.0f + expf(-z)); }
-
-template <int ACT>
-__device__ __forceinline__ float act(float z) {
-  if constexpr (ACT == OAA_ACT_RELU) return z < 0.0f ? 0.0f : z;  // NaN stays NaN
-  if constexpr (ACT == OAA_ACT_SILU) return z * sigmoid(z);
-  if constexpr (ACT == OAA_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-  return z;
-}
-
-template <int ACT>
-__device__ __forceinline__ float act_slope(float z) {
-  if constexpr (ACT == OAA_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
-  if constexpr (ACT == OAA_ACT_SILU) {
-    const float s = sigmoid(z);
-    return s * (1.0f + z * (1.0f - s));
-  }
-  if constexpr (ACT == OAA_ACT_GELU)
-    return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
-  return 1.0f;
-}
-
-// Sum of (a, b) over the workgroup, in every lane; the order is fixed.
-__device__ __forceinline__ void block_sum(double& a, double& b) {
-  __shared__ double part[2][kThreads / 64];
-  for (int m = 32; m; m >>= 1) {
-    a += __shfl_xor(a, m);
-    b += __shfl_xor(b, m);
-  }
-  const int wave = threadIdx.x / 64;
-  if (threadIdx.x % 64 == 0) {
-    part[0][wave] = a;
-    part[1][wave] = b;
-  }
-  __syncthreads();
-  a = b = 0.0;
-  for (int i = 0; i < kThreads / 64; ++i) {
-    a += part[0][i];
-    b += part[1][i];
-  }
-}
-
-__device__ __forceinline__ long offset(const GroupNormParams& p, long image, long row, long b, long c, long s) {
-  return b * image + (p.last ? s * row + c : c * p.S + s);
-}
-
-// Channel and position of the i-th value of a group, in the order of the layout.
-__device__ __forceinline__ void place(const GroupNormParams& p, long i, long& c, long& s) {
-  if (p.last) {
-    s = i / p.D;
-    c = i % p.D;
-  } else {
-    c = i / p.S;
-    s = i % p.S;
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gn_stats_kernel(GroupNormParams p) {
-  const long bg = blockIdx.x, b = bg / p.G, g = bg % p.G, n = p.D * p.S;
-  const T* x = static_cast<const T*>(p.x);
-  const double x0 = float(x[offset(p, p.x_image, p.x_row, b, g * p.D, 0)]);
-  double sum = 0.0, sq = 0.0;
-  for (long i = threadIdx.x; i < n; i += kThreads) {
-    long c, s;
-    place(p, i, c, s);
-    const double v = float(x[offset(p, p.x_image, p.x_row, b, g * p.D + c, s)]) - x0;
-    sum += v;
-    sq += v * v;
-  }
-  block_sum(sum, sq);
-  if (threadIdx.x == 0) {
-    const double mean = sum / n, var = sq / n - mean * mean;
-    p.mean[bg] = float(x0 + mean);
-    p.rstd[bg] = float(1.0 / sqrt((var < 0.0 ? 0.0 : var) + p.eps));
-  }
-}
-
-template <typename T, int ACT>
-__global__ __launch_bounds__(kThreads) void gn_apply_kernel(GroupNormParams p) {
-  const long n = p.D * p.S, total = n * p.B * p.G;
-  for (long e = blockIdx.x * long(kThreads) + threadIdx.x; e < total; e += gridDim.x * long(kThreads)) {
-    const long bg = e / n, b = bg / p.G, g = bg % p.G;
-    long c, s;
-    place(p, e % n, c, s);
-    c += g * p.D;
-    const float v = float(static_cast<const T*>(p.x)[offset(p, p.x_image, p.x_row, b, c, s)]);
-    const float z = (v - p.mean[bg]) * p.rstd[bg] * load_param(p.weight, p.param_dtype, c, 1.0f) +
-                    load_param(p.bias, p.param_dtype, c, 0.0f);
-    static_cast<T*>(p.y)[offset(p, p.y_image, p.y_row, b, c, s)] = T(act<ACT>(z));
-  }
-}
-
-// sums[b][c] = (sum dz, sum dz xh) over the positions of a channel of an image.
-template <typename T, int ACT>
-__global__ __launch_bounds__(kThreads) void gn_channel_sums_kernel(GroupNormParams p, double2* sums) {
-  const long bc = blockIdx.x, b = bc / p.C, c = bc % p.C, bg = b * p.G + c / p.D;
-  const float mean = p.mean[bg], rstd = p.rstd[bg];
-  const float w = load_param(p.weight, p.param_dtype, c, 1.0f), bias = load_param(p.bias, p.param_dtype, c, 0.0f);
-  double sa = 0.0, sb = 0.0;
-  for (long s = threadIdx.x; s < p.S; s += kThreads) {
-    const float xh = (float(static_cast<const T*>(p.x)[offset(p, p.x_image, p.x_row, b, c, s)]) - mean) * rstd;
-    const float dy = float(static_cast<const T*>(p.dy)[offset(p, p.dy_image, p.dy_row, b, c, s)]);
-    const float dz = dy * act_slope<ACT>(xh * w + bias);
-    sa += dz;
-    sb += double(dz) * xh;
-  }
-  block_sum(sa, sb);
-  if (threadIdx.x == 0) sums[bc] = {sa, sb};
-}
-
-// Group means of t and t xh, one lane a group; after them dweight and dbias,
-// one lane a channel.
-__global__ __launch_bounds__(kThreads) void gn_join_kernel(GroupNormParams p, const double2* sums, float2* means) {
-  const long i = blockIdx.x * long(kThreads) + threadIdx.x, groups = long(p.B) * p.G;
-  if (i < groups) {
-    const long b = i / p.G, g = i % p.G;
-    double m1 = 0.0, m2 = 0.0;
-    for (long c = g * p.D; c < (g + 1) * p.D; ++c) {
-      const double w = load_param(p.weight, p.param_dtype, c, 1.0f);
-      m1 += w * sums[b * p.C + c].x;
-      m2 += w * sums[b * p.C + c].y;
+// Workgroups [0, groups): the means of t and t xh of a group each. The others:
+// dweight and dbias.
+__global__ __launch_bounds__(kThreads) void norm_join_kernel(GroupNormParams p, NormSums at, int groups) {
+  if (int(blockIdx.x) < groups) {
+    __shared__ double part[2 * kThreads / 64];
+    const long bg = blockIdx.x, b = bg / p.G, c0 = (bg - b * p.G) * p.D;
+    const float2* sums = at.sums + b * at.image + c0 * at.channel;
+    double a = 0.0, d = 0.0;
+    for (long i = threadIdx.x; i < p.D * at.count; i += kThreads) {
+      const long k = i / p.D, c = i - k * p.D;
+      const float2 v = sums[c * at.channel + k * at.slot];
+      const double w = load_param(p.weight, p.param_dtype, c0 + c, 1.0f);
+      a = fma(w, double(v.x), a);
+      d = fma(w, double(v.y), d);
     }
+    thread_sum<kThreads>(a, d, part);
     const double n = double(p.D) * p.S;
-    means[i] = {float(m1 / n), float(m2 / n)};
-  } else if (i < groups + p.C) {
-    const long c = i - groups;
-    double sa = 0.0, sb = 0.0;
-    for (long b = 0; b < p.B; ++b) {
-      sa += sums[b * p.C + c].x;
-      sb += sums[b * p.C + c].y;
+    if (threadIdx.x == 0) at.means[bg] = {float(a / n), float(d / n)};
+    return;
+  }
+  __shared__ double2 lanes[kLanes][kColumns];
+  const int col = threadIdx.x % kColumns, lane = threadIdx.x / kColumns;
+  const long c = long(blockIdx.x - groups) * kColumns + col;
+  double a = 0.0, d = 0.0;
+  if (c < p.C) {
+    const float2* sums = at.sums + c * at.channel;
+    const long entries = p.B * at.count;
+#pragma unroll 8
+    for (long i = lane; i < entries; i += kLanes) {
+      const long b = i / at.count, k = i - b * at.count;
+      const float2 v = sums[b * at.image + k * at.slot];
+      a += v.x;
+      d += v.y;
     }
-    if (p.dbias) store_param(p.dbias, p.param_dtype, c, float(sa));
-    if (p.dweight) store_param(p.dweight, p.param_dtype, c, float(sb));
   }
+  lanes[lane][col] = {a, d};
+  __syncthreads();
+  if (lane || c >= p.C) return;
+  for (int i = 1; i < kLanes; ++i) {
+    a += lanes[i][col].x;
+    d += lanes[i][col].y;
+  }
+  if (p.dbias) store_param(p.dbias, p.param_dtype, c, float(a));
+  if (p.dweight) store_param(p.dweight, p.param_dtype, c, float(d));
 }
 
-template <typename T, int ACT>
-__global__ __launch_bounds__(kThreads) void gn_dx_kernel(GroupNormParams p, const float2* means) {
-  const long n = p.D * p.S, total = n * p.B * p.G;
-  for (long e = blockIdx.x * long(kThreads) + threadIdx.x; e < total; e += gridDim.x * long(kThreads)) {
-    const long bg = e / n, b = bg / p.G, g = bg % p.G;
-    long c, s;
-    place(p, e % n, c, s);
-    c += g * p.D;
-    const float rstd = p.rstd[bg];
-    const float xh = (float(static_cast<const T*>(p.x)[offset(p, p.x_image, p.x_row, b, c, s)]) - p.mean[bg]) * rstd;
-    const float w = load_param(p.weight, p.param_dtype, c, 1.0f), bias = load_param(p.bias, p.param_dtype, c, 0.0f);
-    const float dy = float(static_cast<const T*>(p.dy)[offset(p, p.dy_image, p.dy_row, b, c, s)]);
-    const float t = w * (dy * act_slope<ACT>(xh * w + bias));
-    static_cast<T*>(p.dx)[offset(p, p.dx_image, p.dx_row, b, c, s)] = T(rstd * (t - means[bg].x - xh * means[bg].y));
-  }
-}
-
-__global__ __launch_bounds__(kThreads) void gn_zero_params_kernel(void* dweight, void* dbias, int dtype, int C) {
+__global__ __launch_bounds__(kThreads) void norm_zero_params_kernel(void* dweight, void* dbias, int dtype, int C) {
   const int c = blockIdx.x * kThreads + threadIdx.x;
   if (c >= C) return;
   if (dweight) store_param(dweight, dtype, c, 0.0f);
   if (dbias) store_param(dbias, dtype, c, 0.0f);
 }
 
-template <typename Fn>
-hipError_t for_type(int dtype, Fn&& f) {
-  if (dtype == OAA_FLOAT32) return f(float{});
-  if (dtype == OAA_BFLOAT16) return f(bf16{});
-  return f(f16{});
+// The description of images [first, first + count).
+GroupNormParams images(const GroupNormParams& p, long first, long count) {
+  const long size = long(dtype_size(p.dtype)), stats = first * p.G;
+  GroupNormParams q = p;
+  q.B = int(count);
+  auto shift = [&](const void* ptr, long image) {
+    return ptr ? const_cast<char*>(static_cast<const char*>(ptr)) + first * image * size : nullptr;
+  };
+  q.x = shift(p.x, p.x_image);
+  q.dy = shift(p.dy, p.dy_image);
+  q.y = shift(p.y, p.y_image);
+  q.dx = shift(p.dx, p.dx_image);
+  q.mean = p.mean ? p.mean + stats : nullptr;
+  q.rstd = p.rstd ? p.rstd + stats : nullptr;
+  return q;
 }
 
-template <int A>
-struct Act {
-  static constexpr int value = A;
-};
+// Images of one launch.
+long batch(const GroupNormParams& p) { return std::min<long>(p.B, std::max<long>(1, kMostChannels / p.C)); }
 
-template <typename Fn>
-hipError_t for_act(int act, Fn&& f) {
-  if (act == OAA_ACT_NONE) return f(Act<OAA_ACT_NONE>{});
-  if (act == OAA_ACT_RELU) return f(Act<OAA_ACT_RELU>{});
-  if (act == OAA_ACT_SILU) return f(Act<OAA_ACT_SILU>{});
-  return f(Act<OAA_ACT_GELU>{});
+NormCut forward_cut(const GroupNormParams& p) {
+  const GroupNormParams q = images(p, 0, batch(p));
+  return p.last ? last_forward_cut(q) : planes_forward_cut(q);
 }
 
-unsigned elementwise_grid(const GroupNormParams& p) {
-  const long blocks = (long(p.B) * p.C * p.S + kThreads - 1) / kThreads;
-  return unsigned(blocks < 65536 ? blocks : 65536);
+NormCut backward_cut(const GroupNormParams& p) {
+  const GroupNormParams q = images(p, 0, batch(p));
+  return p.last ? last_backward_cut(q) : planes_backward_cut(q);
+}
+
+NormSums sums_layout(const GroupNormParams& p, const NormCut& cut) {
+  return p.last ? last_sums(p, cut) : planes_sums(p, cut);
+}
+
+size_t sums_bytes(const GroupNormParams& p, const NormSums& at) {
+  return align_workspace(sizeof(float2) * p.B * p.C * at.count);
 }
 
 }  // namespace
 
-size_t group_norm_forward_ws(const GroupNormParams& p) { return align_up(2 * sizeof(float) * p.B * p.G); }
-
-size_t group_norm_backward_ws(const GroupNormParams& p) {
-  return align_up(sizeof(double2) * p.B * p.C) + align_up(sizeof(float2) * p.B * p.G);
+hipError_t launch_norm_join(const GroupNormParams& p, const NormSums& at, hipStream_t s) {
+  const int groups = at.means ? p.B * p.G : 0;
+  const int columns = p.dweight || p.dbias ? (p.C + kColumns - 1) / kColumns : 0;
+  if (groups + columns == 0) return hipSuccess;
+  norm_join_kernel<<<groups + columns, kThreads, 0, s>>>(p, at, groups);
+  return hipGetLastError();
 }
 
-hipError_t launch_group_norm_forward(const GroupNormParams& in, hipStream_t s) {
-  GroupNormParams p = in;
-  if (!p.mean) p.mean = reinterpret_cast<float*>(p.ws);
-  if (!p.rstd) p.rstd = reinterpret_cast<float*>(p.ws) + long(p.B) * p.G;
-  return for_type(p.dtype, [&](auto t) {
-    using T = decltype(t);
-    gn_stats_kernel<T><<<p.B * p.G, kThreads, 0, s>>>(p);
-    return for_act(p.act, [&](auto a) {
-      gn_apply_kernel<T, decltype(a)::value><<<elementwise_grid(p), kThreads, 0, s>>>(p);
-      return hipGetLastError();
-    });
-  });
+size_t group_norm_forward_ws(const GroupNormParams& p) {
+  const GroupNormParams q = images(p, 0, batch(p));
+  return p.last ? last_forward_ws(q, forward_cut(p)) : planes_forward_ws(q, forward_cut(p));
+}
+
+size_t group_norm_backward_ws(const GroupNormParams& p) {
+  const NormCut cut = backward_cut(p);
+  return sums_bytes(p, sums_layout(p, cut)) + (cut.split ? align_workspace(sizeof(float2) * p.B * p.G) : 0);
+}
+
+hipError_t launch_group_norm_forward(const GroupNormParams& p, hipStream_t s) {
+  const NormCut cut = forward_cut(p);
+  for (long b = 0; b < p.B; b += batch(p)) {
+    const GroupNormParams q = images(p, b, std::min(batch(p), p.B - b));
+    if (hipError_t e = p.last ? launch_last_forward(q, cut, s) : launch_planes_forward(q, cut, s)) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_group_norm_backward(const GroupNormParams& p, hipStream_t s) {
+  const NormCut cut = backward_cut(p);
+  NormSums all = sums_layout(p, cut);
+  all.sums = reinterpret_cast<float2*>(p.ws);
+  float2* means = cut.split ? reinterpret_cast<float2*>(p.ws + sums_bytes(p, all)) : nullptr;
+  // dweight and dbias come with the groups' means where all images do
+  const bool one = batch(p) == p.B;
+  for (long b = 0; b < p.B; b += batch(p)) {
+    GroupNormParams q = images(p, b, std::min(batch(p), p.B - b));
+    if (!one) q.dweight = q.dbias = nullptr;
+    NormSums at = all;
+    at.sums += b * at.image;
+    at.means = means ? means + b * p.G : nullptr;
+    if (hipError_t e = p.last ? launch_last_backward(q, cut, at, s) : launch_planes_backward(q, cut, at, s)) return e;
+  }
+  return one && cut.split ? hipSuccess : launch_norm_join(p, all, s);
 }
 
 hipError_t launch_group_norm_no_images(const GroupNormParams& p, hipStream_t s) {
   if (!p.dweight && !p.dbias) return hipSuccess;
-  gn_zero_params_kernel<<<(p.C + kThreads - 1) / kThreads, kThreads, 0, s>>>(p.dweight, p.dbias, p.param_dtype, p.C);
+  norm_zero_params_kernel<<<(p.C + kThreads - 1) / kThreads, kThreads, 0, s>>>(p.dweight, p.dbias, p.param_dtype, p.C);
   return hipGetLastError();
-}
-
-hipError_t launch_group_norm_backward(const GroupNormParams& p, hipStream_t s) {
-  double2* sums = reinterpret_cast<double2*>(p.ws);
-  float2* means = reinterpret_cast<float2*>(p.ws + align_up(sizeof(double2) * p.B * p.C));
-  return for_type(p.dtype, [&](auto t) {
-    using T = decltype(t);
-    return for_act(p.act, [&](auto a) {
-      constexpr int A = decltype(a)::value;
-      gn_channel_sums_kernel<T, A><<<p.B * p.C, kThreads, 0, s>>>(p, sums);
-      gn_join_kernel<<<unsigned((long(p.B) * p.G + p.C + kThreads - 1) / kThreads), kThreads, 0, s>>>(p, sums, means);
-      if (p.dx) gn_dx_kernel<T, A><<<elementwise_grid(p), kThreads, 0, s>>>(p, means);
-      return hipGetLastError();
-    });
-  });
 }
 
 }  // namespace oaa

@@ -1,0 +1,661 @@
+// Group normalisation with an activation, channels last: an image is S rows (its
+// positions) of C neighbouring channels, and a group is D of the columns.
+//
+//   mean, rstd over the n = D S values; xh = (x - mean) rstd, z = w xh + b, y = act(z);
+//   dz = dy act'(z), t = w dz, dx = rstd (t - sum t / n - xh sum (t xh) / n).
+//
+// A workgroup takes a slab of neighbouring columns. Each of its threads has one
+// access of V columns, the same in every row it visits, so parameters and sums
+// of its columns stay in its registers; the last access of a slab whose width
+// is no multiple of V is moved back to end with the slab, and its first `dup`
+// columns, which the access before it has too, count once.
+//
+// Every pass is bound by memory. Where a slab's rows fit the registers of one
+// workgroup, they are read once. Otherwise the rows are sliced over the device,
+// in three launches each way: sums, their join, the result.
+//
+// Statistics are summed in float64 about the group's first value x0: the
+// variance is E[d^2] - E[d]^2 of d = x - x0, which keeps its digits however far
+// the mean is from 0.
+#include <algorithm>
+
+#include "norm_common.hpp"
+
+namespace oaa {
+namespace {
+
+// A thread's place in a slab of `width` columns: access `p` of row lane `lane`,
+// of `lanes` rows at a time; its columns start at `col`, and the first `dup` of
+// them are another thread's. Threads beyond the last whole row have no rows.
+template <int V, int THREADS>
+struct Place {
+  int lanes, lane, p, col, dup;
+  __device__ __forceinline__ Place(int tid, int width) {
+    const int accesses = (width + V - 1) / V;
+    lanes = THREADS / accesses;
+    lane = tid / accesses;
+    p = tid - lane * accesses;
+    const int s = p * V;
+    col = s + V > width ? width - V : s;
+    dup = s - col;
+  }
+  __device__ __forceinline__ bool active() const { return lane < lanes; }
+};
+
+// Group (from the slab's first) of each of a thread's columns: `first` is the
+// slab's first channel's place in its group.
+template <int V>
+__device__ __forceinline__ void groups_of(int col, int first, int D, int (&g)[V]) {
+  const int c = col + first;
+  int group = c / D, left = D - (c - group * D);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    g[i] = group;
+    if (--left == 0) {
+      ++group;
+      left = D;
+    }
+  }
+}
+
+// Sums over a slab's entries of each of its groups: entry (lane, column) lies at
+// entries[lane * pitch + column]. Lanes of a wave share a group. done(g, a, b)
+// is called once per group by one lane.
+template <int THREADS, typename E, typename Fn>
+__device__ __forceinline__ void group_sums(int tid, int lanes, int pitch, int width, int first, int D, E&& entry,
+                                           Fn&& done) {
+  const int groups = (first + width + D - 1) / D;
+  int share = 64;  // lanes of a group
+  while (share > 1 && share * groups > THREADS) share /= 2;
+  for (int base = 0; base < groups; base += THREADS / share) {
+    const int g = base + tid / share;
+    const int begin = max(g * D - first, 0), end = min((g + 1) * D - first, width), own = end - begin;
+    double a = 0.0, b = 0.0;
+    if (g < groups)
+      for (int i = tid % share; i < own * lanes; i += share) {
+        const int lane = i / own;
+        entry(lane * pitch + begin + i - lane * own, begin + i - lane * own, a, b);
+      }
+    for (int m = share / 2; m; m >>= 1) {
+      a += __shfl_xor(a, m);
+      b += __shfl_xor(b, m);
+    }
+    if (g < groups && tid % share == 0) done(g, a, b);
+  }
+}
+
+// A thread's accumulated moments of its V columns.
+template <typename T, int V>
+struct Moments {
+  double sum[V], sq[V], x0[V];
+  __device__ __forceinline__ Moments(const T* row0, const int (&g)[V], int first, int D) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      sum[i] = sq[i] = 0.0;
+      x0[i] = float(row0[g[i] * D - first]);
+    }
+  }
+  __device__ __forceinline__ void add(const Vec<T, V>& v) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const double d = double(element<T, V>(v, i)) - x0[i];
+      sum[i] += d;
+      sq[i] = fma(d, d, sq[i]);
+    }
+  }
+};
+
+constexpr int kAhead = 4;
+
+// Most groups of a slab that one workgroup keeps.
+constexpr int kMostGroups = 128;
+
+// ---- forward, one slab per THREADS threads -----------------------------------
+
+// Slab j of `slabs`: whole groups [j G / slabs, (j + 1) G / slabs).
+template <typename T, int ACT, int V, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_forward_kernel(GroupNormParams p, int slabs) {
+  constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kSlabs = kBlock / THREADS;
+  __shared__ double2 entries[kSlabs][THREADS * V];
+  __shared__ float2 stats[kSlabs][kMostGroups];
+  const int sub = threadIdx.x / THREADS, tid = threadIdx.x % THREADS;
+  const long slab = long(blockIdx.x) * kSlabs + sub;
+  const bool active = slab < long(p.B) * slabs;
+  const long b = active ? slab / slabs : 0;
+  const int j = active ? int(slab - b * slabs) : 0;
+  const int g0 = int(long(j) * p.G / slabs), groups = int(long(j + 1) * p.G / slabs) - g0;
+  const int D = p.D, width = groups * D, S = active ? int(p.S) : 0;
+  const long c0 = long(g0) * D;
+  const Place<V, THREADS> at(tid, width);
+  const bool works = at.active();
+  const T* x = static_cast<const T*>(p.x) + b * p.x_image + c0;
+  const T* xt = x + at.col;
+  int g[V];
+  groups_of<V>(at.col, 0, D, g);
+
+  Vec<T, V> held[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int s = at.lane + k * at.lanes;
+    if (works && s < S) held[k] = load<T, V>(xt + s * p.x_row);
+  }
+  float w[V], bias[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    w[i] = works ? load_param(p.weight, p.param_dtype, c0 + at.col + i, 1.0f) : 0.0f;
+    bias[i] = works ? load_param(p.bias, p.param_dtype, c0 + at.col + i, 0.0f) : 0.0f;
+  }
+  {
+    if (!works) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) g[i] = 0;
+    }
+    Moments<T, V> m(x, g, 0, D);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (works && at.lane + k * at.lanes < S) m.add(held[k]);
+    if (works) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i >= at.dup) entries[sub][at.lane * width + at.col + i] = {m.sum[i], m.sq[i]};
+    }
+  }
+  __syncthreads();
+  group_sums<THREADS>(
+      tid, at.lanes, width, width, 0, D,
+      [&](int e, int, double& a, double& q) {
+        a += entries[sub][e].x;
+        q += entries[sub][e].y;
+      },
+      [&](int gi, double a, double q) {
+        float mean, rstd;
+        statistics(a, q, double(float(x[gi * D])), double(D) * p.S, p.eps, mean, rstd);
+        stats[sub][gi] = {mean, rstd};
+        if (active) {
+          if (p.mean) p.mean[b * p.G + g0 + gi] = mean;
+          if (p.rstd) p.rstd[b * p.G + g0 + gi] = rstd;
+        }
+      });
+  __syncthreads();
+  if (!works) return;
+  float mean[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float2 st = stats[sub][g[i]];
+    mean[i] = st.x;
+    w[i] *= st.y;
+  }
+  T* y = static_cast<T*>(p.y) + b * p.y_image + c0 + at.col;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int s = at.lane + k * at.lanes;
+    if (s >= S) continue;
+    Vec<T, V> out;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      set_element<T, V>(out, i, act<ACT>(fmaf(element<T, V>(held[k], i) - mean[i], w[i], bias[i])));
+    store<T, V>(y + s * p.y_row, out);
+  }
+}
+
+// ---- forward, rows sliced over the device ------------------------------------------
+
+constexpr int kSplitThreads = 256;
+
+// Slabs of at most kSplitThreads accesses, where rows are sliced: slab j is
+// columns [j C / slabs, (j + 1) C / slabs), which may cut a group.
+template <int V>
+__host__ __device__ inline int split_slabs(int C) {
+  return (C + kSplitThreads * V - 1) / (kSplitThreads * V);
+}
+
+// A workgroup's place: image b, slice k of its rows, slab j.
+template <int V>
+struct SplitPlace {
+  long b, k;
+  int j, slabs, c0, width;
+  long begin, end;
+  __device__ __forceinline__ SplitPlace(const GroupNormParams& p, long slice, int count) {
+    slabs = split_slabs<V>(p.C);
+    const long i = blockIdx.x / slabs;
+    j = int(blockIdx.x - i * slabs);
+    b = i / count;
+    k = i - b * count;
+    c0 = int(long(j) * p.C / slabs);
+    width = int(long(j + 1) * p.C / slabs) - c0;
+    begin = k * slice;
+    end = begin + slice < p.S ? begin + slice : p.S;
+  }
+};
+
+// sums[b][k slabs + j][g] = moments of the part of group g in slab j and slice k.
+template <typename T, int V>
+__global__ __launch_bounds__(kSplitThreads) void last_moments_kernel(GroupNormParams p, long slice, int count,
+                                                                     double2* sums) {
+  __shared__ double2 entries[kSplitThreads * V];
+  const SplitPlace<V> in(p, slice, count);
+  const Place<V, kSplitThreads> at(threadIdx.x, in.width);
+  const int D = p.D, g0 = in.c0 / D, own = in.c0 - g0 * D;
+  const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c0;
+  if (at.active()) {
+    int g[V];
+    groups_of<V>(at.col, own, D, g);
+    Moments<T, V> m(x, g, own, D);
+    const T* xt = x + at.col;
+    for (long s = in.begin + at.lane; s < in.end; s += kAhead * at.lanes) {
+      Vec<T, V> v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (s + u * at.lanes < in.end) v[u] = load<T, V>(xt + (s + u * at.lanes) * p.x_row);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (s + u * at.lanes < in.end) m.add(v[u]);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i >= at.dup) entries[at.lane * in.width + at.col + i] = {m.sum[i], m.sq[i]};
+  }
+  __syncthreads();
+  double2* out = sums + ((in.b * count + in.k) * in.slabs + in.j) * p.G;
+  const int groups = (own + in.width + D - 1) / D;
+  for (int i = threadIdx.x; i < p.G; i += kSplitThreads)
+    if (i < g0 || i >= g0 + groups) out[i] = {0.0, 0.0};
+  group_sums<kSplitThreads>(
+      threadIdx.x, at.lanes, in.width, in.width, own, D,
+      [&](int e, int, double& a, double& q) {
+        a += entries[e].x;
+        q += entries[e].y;
+      },
+      [&](int gi, double a, double q) { out[g0 + gi] = {a, q}; });
+}
+
+// mean and rstd of a group from the moments of its `count` parts.
+template <typename T>
+__global__ __launch_bounds__(kSplitThreads) void last_statistics_kernel(GroupNormParams p, int count,
+                                                                        const double2* sums) {
+  __shared__ double part[2 * kSplitThreads / 64];
+  const long bg = blockIdx.x, b = bg / p.G, g = bg - b * p.G;
+  double a = 0.0, q = 0.0;
+  for (int i = threadIdx.x; i < count; i += kSplitThreads) {
+    const double2 v = sums[(b * count + i) * p.G + g];
+    a += v.x;
+    q += v.y;
+  }
+  thread_sum<kSplitThreads>(a, q, part);
+  if (threadIdx.x == 0) {
+    const T* x = static_cast<const T*>(p.x) + b * p.x_image + g * p.D;
+    statistics(a, q, double(float(x[0])), double(p.D) * p.S, p.eps, p.mean[bg], p.rstd[bg]);
+  }
+}
+
+// A thread's statistics and parameters of its V columns.
+template <int V>
+struct Columns {
+  float mean[V], rstd[V], w[V], bias[V];
+  __device__ __forceinline__ Columns(const GroupNormParams& p, long b, int c0) {
+    int g[V];
+    groups_of<V>(c0, 0, p.D, g);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      mean[i] = p.mean[b * p.G + g[i]];
+      rstd[i] = p.rstd[b * p.G + g[i]];
+      w[i] = load_param(p.weight, p.param_dtype, c0 + i, 1.0f);
+      bias[i] = load_param(p.bias, p.param_dtype, c0 + i, 0.0f);
+    }
+  }
+};
+
+template <typename T, int ACT, int V>
+__global__ __launch_bounds__(kSplitThreads) void last_apply_kernel(GroupNormParams p, long slice, int count) {
+  const SplitPlace<V> in(p, slice, count);
+  const Place<V, kSplitThreads> at(threadIdx.x, in.width);
+  if (!at.active()) return;
+  Columns<V> col(p, in.b, in.c0 + at.col);
+#pragma unroll
+  for (int i = 0; i < V; ++i) col.w[i] *= col.rstd[i];
+  const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c0 + at.col;
+  T* y = static_cast<T*>(p.y) + in.b * p.y_image + in.c0 + at.col;
+  for (long s = in.begin + at.lane; s < in.end; s += kAhead * at.lanes) {
+    Vec<T, V> v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (s + u * at.lanes < in.end) v[u] = load<T, V>(x + (s + u * at.lanes) * p.x_row);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (s + u * at.lanes >= in.end) continue;
+      Vec<T, V> out;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        set_element<T, V>(out, i, act<ACT>(fmaf(element<T, V>(v[u], i) - col.mean[i], col.w[i], col.bias[i])));
+      store<T, V>(y + (s + u * at.lanes) * p.y_row, out);
+    }
+  }
+}
+
+// ---- backward ---------------------------------------------------------------------
+
+// Adds a row's dz and dz xh to a thread's sums of its columns.
+template <typename T, int ACT, int V>
+__device__ __forceinline__ void add_gradient(const Vec<T, V>& x, const Vec<T, V>& dy, const Columns<V>& col,
+                                             float (&sa)[V], float (&sb)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    float dz, xh;
+    gradient<ACT>(element<T, V>(x, i), element<T, V>(dy, i), col.mean[i], col.rstd[i], col.w[i], col.bias[i], dz, xh);
+    sa[i] += dz;
+    sb[i] = fmaf(dz, xh, sb[i]);
+  }
+}
+
+template <typename T, int ACT, int V>
+__device__ __forceinline__ Vec<T, V> input_gradient(const Vec<T, V>& x, const Vec<T, V>& dy, const Columns<V>& col,
+                                                    const float (&m1)[V], const float (&m2)[V]) {
+  Vec<T, V> out;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    float dz, xh;
+    gradient<ACT>(element<T, V>(x, i), element<T, V>(dy, i), col.mean[i], col.rstd[i], col.w[i], col.bias[i], dz, xh);
+    set_element<T, V>(out, i, col.rstd[i] * (fmaf(col.w[i], dz, -m1[i]) - xh * m2[i]));
+  }
+  return out;
+}
+
+// sums[b][c] = (sum dz, sum dz xh) of a channel of an image, and dx.
+template <typename T, int ACT, int V, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_backward_kernel(GroupNormParams p, int slabs,
+                                                                                      float2* sums) {
+  constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kSlabs = kBlock / THREADS;
+  __shared__ float2 entries[kSlabs][THREADS * V];
+  __shared__ float2 columns[kSlabs][THREADS * V];
+  __shared__ float2 means[kSlabs][kMostGroups];
+  const int sub = threadIdx.x / THREADS, tid = threadIdx.x % THREADS;
+  const long slab = long(blockIdx.x) * kSlabs + sub;
+  const bool active = slab < long(p.B) * slabs;
+  const long b = active ? slab / slabs : 0;
+  const int j = active ? int(slab - b * slabs) : 0;
+  const int g0 = int(long(j) * p.G / slabs), groups = int(long(j + 1) * p.G / slabs) - g0;
+  const int D = p.D, width = groups * D, S = active ? int(p.S) : 0;
+  const long c0 = long(g0) * D;
+  const Place<V, THREADS> at(tid, width);
+  const bool works = at.active();
+  const T* x = static_cast<const T*>(p.x) + b * p.x_image + c0 + at.col;
+  const T* dy = static_cast<const T*>(p.dy) + b * p.dy_image + c0 + at.col;
+
+  Vec<T, V> hx[NV], hdy[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int s = at.lane + k * at.lanes;
+    if (works && s < S) {
+      hx[k] = load<T, V>(x + s * p.x_row);
+      hdy[k] = load<T, V>(dy + s * p.dy_row);
+    }
+  }
+  const Columns<V> col(p, b, int(c0) + (works ? at.col : 0));
+  float sa[V], sb[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sa[i] = sb[i] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (works && at.lane + k * at.lanes < S) add_gradient<T, ACT, V>(hx[k], hdy[k], col, sa, sb);
+  if (works) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i >= at.dup) entries[sub][at.lane * width + at.col + i] = {sa[i], sb[i]};
+  }
+  __syncthreads();
+  group_sums<THREADS>(
+      tid, at.lanes, width, width, 0, 1,
+      [&](int e, int, double& a, double& d) {
+        a += entries[sub][e].x;
+        d += entries[sub][e].y;
+      },
+      [&](int c, double a, double d) {
+        columns[sub][c] = {float(a), float(d)};
+        if (sums && active) sums[b * p.C + c0 + c] = {float(a), float(d)};
+      });
+  if (!p.dx) return;
+  __syncthreads();
+  const double n = double(D) * p.S;
+  group_sums<THREADS>(
+      tid, 1, width, width, 0, D,
+      [&](int e, int c, double& a, double& d) {
+        const double w = load_param(p.weight, p.param_dtype, c0 + c, 1.0f);
+        a = fma(w, double(columns[sub][e].x), a);
+        d = fma(w, double(columns[sub][e].y), d);
+      },
+      [&](int gi, double a, double d) { means[sub][gi] = {float(a / n), float(d / n)}; });
+  __syncthreads();
+  if (!works) return;
+  int g[V];
+  groups_of<V>(at.col, 0, D, g);
+  float m1[V], m2[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    m1[i] = means[sub][g[i]].x;
+    m2[i] = means[sub][g[i]].y;
+  }
+  T* dx = static_cast<T*>(p.dx) + b * p.dx_image + c0 + at.col;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int s = at.lane + k * at.lanes;
+    if (s < S) store<T, V>(dx + s * p.dx_row, input_gradient<T, ACT, V>(hx[k], hdy[k], col, m1, m2));
+  }
+}
+
+// sums[b][k][c] = (sum dz, sum dz xh) of channel c over slice k of image b's rows.
+template <typename T, int ACT, int V>
+__global__ __launch_bounds__(kSplitThreads) void last_column_sums_kernel(GroupNormParams p, long slice, int count,
+                                                                         float2* sums) {
+  __shared__ float2 entries[kSplitThreads * V];
+  const SplitPlace<V> in(p, slice, count);
+  const Place<V, kSplitThreads> at(threadIdx.x, in.width);
+  if (at.active()) {
+    const Columns<V> col(p, in.b, in.c0 + at.col);
+    const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c0 + at.col;
+    const T* dy = static_cast<const T*>(p.dy) + in.b * p.dy_image + in.c0 + at.col;
+    float sa[V], sb[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sa[i] = sb[i] = 0.0f;
+    for (long s = in.begin + at.lane; s < in.end; s += kAhead * at.lanes) {
+      Vec<T, V> vx[kAhead], vdy[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (s + u * at.lanes < in.end) {
+          vx[u] = load<T, V>(x + (s + u * at.lanes) * p.x_row);
+          vdy[u] = load<T, V>(dy + (s + u * at.lanes) * p.dy_row);
+        }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (s + u * at.lanes < in.end) add_gradient<T, ACT, V>(vx[u], vdy[u], col, sa, sb);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i >= at.dup) entries[at.lane * in.width + at.col + i] = {sa[i], sb[i]};
+  }
+  __syncthreads();
+  float2* out = sums + (in.b * count + in.k) * p.C + in.c0;
+  group_sums<kSplitThreads>(
+      threadIdx.x, at.lanes, in.width, in.width, 0, 1,
+      [&](int e, int, double& a, double& d) {
+        a += entries[e].x;
+        d += entries[e].y;
+      },
+      [&](int c, double a, double d) { out[c] = {float(a), float(d)}; });
+}
+
+template <typename T, int ACT, int V>
+__global__ __launch_bounds__(kSplitThreads) void last_input_gradient_kernel(GroupNormParams p, long slice, int count,
+                                                                            const float2* means) {
+  const SplitPlace<V> in(p, slice, count);
+  const Place<V, kSplitThreads> at(threadIdx.x, in.width);
+  if (!at.active()) return;
+  const Columns<V> col(p, in.b, in.c0 + at.col);
+  int g[V];
+  groups_of<V>(in.c0 + at.col, 0, p.D, g);
+  float m1[V], m2[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    m1[i] = means[in.b * p.G + g[i]].x;
+    m2[i] = means[in.b * p.G + g[i]].y;
+  }
+  const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c0 + at.col;
+  const T* dy = static_cast<const T*>(p.dy) + in.b * p.dy_image + in.c0 + at.col;
+  T* dx = static_cast<T*>(p.dx) + in.b * p.dx_image + in.c0 + at.col;
+  for (long s = in.begin + at.lane; s < in.end; s += kAhead * at.lanes) {
+    Vec<T, V> vx[kAhead], vdy[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (s + u * at.lanes < in.end) {
+        vx[u] = load<T, V>(x + (s + u * at.lanes) * p.x_row);
+        vdy[u] = load<T, V>(dy + (s + u * at.lanes) * p.dy_row);
+      }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (s + u * at.lanes < in.end)
+        store<T, V>(dx + (s + u * at.lanes) * p.dx_row, input_gradient<T, ACT, V>(vx[u], vdy[u], col, m1, m2));
+  }
+}
+
+// ---- choice -----------------------------------------------------------------------
+
+// Workgroups that the sliced kernels aim for.
+constexpr long kSlices = 2048;
+
+int vector_of(const GroupNormParams& p) {
+  const int V = p.dtype == OAA_FLOAT32 ? 4 : 8;
+  return p.C >= V ? V : 1;
+}
+
+// Slabs of an image where a slab goes to one workgroup: whole groups, 128 bytes
+// of a row (a line) or more, fewer where workgroups would be few.
+int whole_slabs(const GroupNormParams& p) {
+  const long row = long(p.D) * long(dtype_size(p.dtype)), total = long(p.B) * p.G;
+  long q = (128 + row - 1) / row;
+  if (total < 256 * q) q = std::max(std::max<long>(1, total / 256), (long(vector_of(p)) + p.D - 1) / p.D);
+  return int(std::max<long>(1, p.G / q));
+}
+
+// Whether a workgroup of so many threads, with so many rows a lane, holds a slab.
+bool holds(const GroupNormParams& p, int slabs, int threads, int rows) {
+  const long groups = (p.G + slabs - 1) / slabs, V = vector_of(p), accesses = (groups * p.D + V - 1) / V;
+  return groups <= kMostGroups && accesses <= threads && p.S <= threads / accesses * rows;
+}
+
+constexpr int kForwardThreads = 512, kForwardRows = 32, kBackwardThreads = 512, kBackwardRows = 16;
+
+// Whether a slab goes to one workgroup. The alternative reads everything twice
+// and takes two launches more.
+NormCut cut_rows(const GroupNormParams& p, int threads, int rows) {
+  const int slabs = whole_slabs(p);
+  if (holds(p, slabs, threads, rows) && (long(p.B) * slabs >= 128 || p.S <= 1024)) return {false, 0, slabs};
+  const int V = vector_of(p), cuts = V == 1 ? split_slabs<1>(p.C) : V == 4 ? split_slabs<4>(p.C) : split_slabs<8>(p.C);
+  const long lanes = std::max<long>(1, kSplitThreads / std::max<long>(1, ((p.C + cuts - 1) / cuts + V - 1) / V));
+  const long images = long(p.B) * cuts;
+  long slice = (p.S * images + kSlices - 1) / kSlices;
+  slice = (slice + lanes * kAhead - 1) / (lanes * kAhead) * (lanes * kAhead);
+  return {true, slice, (p.S + slice - 1) / slice};
+}
+
+template <int V>
+long parts(const GroupNormParams& p, const NormCut& cut) {
+  return cut.count * split_slabs<V>(p.C);
+}
+
+long parts_of(const GroupNormParams& p, const NormCut& cut) {
+  const int V = vector_of(p);
+  return V == 1 ? parts<1>(p, cut) : V == 4 ? parts<4>(p, cut) : parts<8>(p, cut);
+}
+
+template <typename T, int ACT, int V, int THREADS, int NV>
+hipError_t forward_slabs(const GroupNormParams& p, int slabs, hipStream_t s) {
+  constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kSlabs = kBlock / THREADS;
+  const long total = long(p.B) * slabs;
+  last_forward_kernel<T, ACT, V, THREADS, NV><<<unsigned((total + kSlabs - 1) / kSlabs), kBlock, 0, s>>>(p, slabs);
+  return hipGetLastError();
+}
+
+template <typename T, int ACT, int V>
+hipError_t forward(const GroupNormParams& in, const NormCut& cut, hipStream_t s) {
+  if (!cut.split) {
+    const int slabs = int(cut.count);
+    if (holds(in, slabs, 64, 4)) return forward_slabs<T, ACT, V, 64, 4>(in, slabs, s);
+    if (holds(in, slabs, 256, 4)) return forward_slabs<T, ACT, V, 256, 4>(in, slabs, s);
+    if (holds(in, slabs, 256, 16)) return forward_slabs<T, ACT, V, 256, 16>(in, slabs, s);
+    return forward_slabs<T, ACT, V, kForwardThreads, kForwardRows>(in, slabs, s);
+  }
+  GroupNormParams p = in;
+  double2* sums = reinterpret_cast<double2*>(p.ws);
+  float* stats = reinterpret_cast<float*>(p.ws + align_workspace(sizeof(double2) * p.B * p.G * parts<V>(p, cut)));
+  if (!p.mean) p.mean = stats;
+  if (!p.rstd) p.rstd = stats + long(p.B) * p.G;
+  const unsigned blocks = unsigned(p.B * parts<V>(p, cut));
+  last_moments_kernel<T, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), sums);
+  last_statistics_kernel<T><<<p.B * p.G, kSplitThreads, 0, s>>>(p, int(parts<V>(p, cut)), sums);
+  last_apply_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count));
+  return hipGetLastError();
+}
+
+template <typename T, int ACT, int V, int THREADS, int NV>
+hipError_t backward_slabs(const GroupNormParams& p, int slabs, const NormSums& at, hipStream_t s) {
+  constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kSlabs = kBlock / THREADS;
+  const long total = long(p.B) * slabs;
+  last_backward_kernel<T, ACT, V, THREADS, NV>
+      <<<unsigned((total + kSlabs - 1) / kSlabs), kBlock, 0, s>>>(p, slabs, at.sums);
+  return hipGetLastError();
+}
+
+template <typename T, int ACT, int V>
+hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s) {
+  if (!cut.split) {
+    const int slabs = int(cut.count);
+    if (holds(p, slabs, 64, 4)) return backward_slabs<T, ACT, V, 64, 4>(p, slabs, at, s);
+    if (holds(p, slabs, 256, 4)) return backward_slabs<T, ACT, V, 256, 4>(p, slabs, at, s);
+    if (holds(p, slabs, 256, 8)) return backward_slabs<T, ACT, V, 256, 8>(p, slabs, at, s);
+    return backward_slabs<T, ACT, V, kBackwardThreads, kBackwardRows>(p, slabs, at, s);
+  }
+  const unsigned blocks = unsigned(p.B * parts<V>(p, cut));
+  last_column_sums_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at.sums);
+  if (hipError_t e = launch_norm_join(p, at, s)) return e;
+  if (p.dx)
+    last_input_gradient_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at.means);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+NormCut last_forward_cut(const GroupNormParams& p) { return cut_rows(p, kForwardThreads, kForwardRows); }
+
+size_t last_forward_ws(const GroupNormParams& p, const NormCut& cut) {
+  if (!cut.split) return 0;
+  return align_workspace(sizeof(double2) * p.B * p.G * parts_of(p, cut)) +
+         align_workspace(2 * sizeof(float) * p.B * p.G);
+}
+
+NormCut last_backward_cut(const GroupNormParams& p) { return cut_rows(p, kBackwardThreads, kBackwardRows); }
+
+NormSums last_sums(const GroupNormParams& p, const NormCut& cut) {
+  const long count = cut.split ? cut.count : 1;
+  return {nullptr, nullptr, count, p.C * count, 1, p.C};
+}
+
+hipError_t launch_last_forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s) {
+  return for_type(p.dtype, [&](auto t) {
+    using T = typename decltype(t)::type;
+    return for_act(p.act, [&](auto a) {
+      constexpr int A = decltype(a)::value;
+      return vector_of(p) > 1 ? forward<T, A, kVec<T>>(p, cut, s) : forward<T, A, 1>(p, cut, s);
+    });
+  });
+}
+
+hipError_t launch_last_backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s) {
+  return for_type(p.dtype, [&](auto t) {
+    using T = typename decltype(t)::type;
+    return for_act(p.act, [&](auto a) {
+      constexpr int A = decltype(a)::value;
+      return vector_of(p) > 1 ? backward<T, A, kVec<T>>(p, cut, at, s) : backward<T, A, 1>(p, cut, at, s);
+    });
+  });
+}
+
+}  // namespace oaa

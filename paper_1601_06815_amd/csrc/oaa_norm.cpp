@@ -57,6 +57,7 @@ oaa_status_t describe(const oaa_group_norm_t* d, oaa::GroupNormParams* p) {
   if (d->activation < OAA_ACT_NONE || d->activation > OAA_ACT_GELU)
     return fail(OAA_ERR_INVALID_ARG, "unknown activation %d", d->activation);
   if (!(d->eps >= 0.0f)) return fail(OAA_ERR_INVALID_ARG, "eps must not be negative");
+  if (d->C > oaa::kMostChannels) return fail(OAA_ERR_UNSUPPORTED, "more than %ld channels", oaa::kMostChannels);
   if (d->S > kMaxElems || (long long)d->B * d->C > kMaxInt ||
       (d->S > 0 && (long long)d->B * d->C > kMaxElems / d->S))
     return fail(OAA_ERR_UNSUPPORTED, "too large (B=%d C=%d S=%lld)", d->B, d->C, d->S);
@@ -66,7 +67,8 @@ oaa_status_t describe(const oaa_group_norm_t* d, oaa::GroupNormParams* p) {
   p->G = d->G;
   p->D = d->C / d->G;
   p->S = long(d->S);
-  p->last = d->layout == OAA_LAYOUT_CHANNELS_LAST;
+  // one position is both layouts: the channels-last kernels take whole images
+  p->last = d->layout == OAA_LAYOUT_CHANNELS_LAST || d->S == 1;
   p->dtype = d->dtype;
   p->param_dtype = d->param_dtype;
   p->act = d->activation;
