@@ -17,7 +17,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "liboaa.so")
 SOURCES = ["oaa_plan.cpp", "k_tile_fft.hip", "k_fold_fft.hip", "k_big_fft.hip", "k_wide_fft.hip", "k_fused.hip", "k_cgemm.hip", "k_narrow.hip",
-           "oaa_norm.cpp", "k_group_norm.hip", "k_norm_planes.hip", "k_norm_last.hip", "oaa_grad.cpp", "k_grad.hip"]
+           "oaa_norm.cpp", "k_norm_planes_f32.hip", "k_norm_planes_bf16.hip", "k_norm_planes_f16.hip", "k_norm_last_f32.hip",
+           "k_norm_last_bf16.hip", "k_norm_last_f16.hip", "k_group_norm.hip", "oaa_grad.cpp", "k_grad.hip"]
 
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 FLAGS = [

@@ -16,6 +16,7 @@ struct GroupNormParams {
   bool last;       // channels last
   int dtype, param_dtype, act;
   float eps;
+  bool once;  // the output is too large for a cache
   // element strides between images and (channels last) positions
   long x_image, x_row, y_image, y_row, dy_image, dy_row, dx_image, dx_row;
   const void *x, *dy, *weight, *bias;
@@ -54,19 +55,15 @@ hipError_t launch_group_norm_backward(const GroupNormParams& p, hipStream_t s);
 // dweight and dbias of no images: zeros.
 hipError_t launch_group_norm_no_images(const GroupNormParams& p, hipStream_t s);
 
-// Per layout, for at most kMostChannels / C images. A cut serves the images it
-// was made for and any fewer.
-NormCut planes_forward_cut(const GroupNormParams& p);
-size_t planes_forward_ws(const GroupNormParams& p, const NormCut& cut);
+// The passes of a layout over at most kMostChannels / C images of type T. A cut
+// serves the images it was made for and any fewer.
+template <typename T>
 hipError_t launch_planes_forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s);
-NormCut planes_backward_cut(const GroupNormParams& p);
-NormSums planes_sums(const GroupNormParams& p, const NormCut& cut);  // its layout, no pointers
+template <typename T>
 hipError_t launch_planes_backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s);
-NormCut last_forward_cut(const GroupNormParams& p);
-size_t last_forward_ws(const GroupNormParams& p, const NormCut& cut);
+template <typename T>
 hipError_t launch_last_forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s);
-NormCut last_backward_cut(const GroupNormParams& p);
-NormSums last_sums(const GroupNormParams& p, const NormCut& cut);
+template <typename T>
 hipError_t launch_last_backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s);
 
 // means of p's groups (where at.means is set), and dweight and dbias over p's

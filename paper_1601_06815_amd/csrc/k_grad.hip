@@ -67,10 +67,27 @@ __device__ __forceinline__ int tensor_of(const GradBatch& t, unsigned chunk) {
   return lo;
 }
 
+// Accesses of 16 bytes loaded before the first of them is used.
+constexpr int kAhead = 8;
+
 template <int TYPE, typename T>
-__device__ __forceinline__ void chunk_norm(const void* src, long n, double& sum, unsigned& top) {
-  const T* g = static_cast<const T*>(src);
-  for (long i = threadIdx.x; i < n; i += kThreads) take<TYPE>(sum, top, float(g[i]));
+__device__ __forceinline__ void chunk_norm(const T* g, int n, double& sum, unsigned& top) {
+  constexpr int V = 16 / int(sizeof(T));
+  const int whole = n / V;
+  for (int i = threadIdx.x; i < whole; i += kAhead * kThreads) {
+    Vec<T, V> v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i + k * kThreads < whole) v[k] = *reinterpret_cast<const Vec<T, V>*>(g + (i + k * kThreads) * V);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i + k * kThreads >= whole) break;
+#pragma unroll
+      for (int e = 0; e < V; ++e) take<TYPE>(sum, top, element<T, V>(v[k], e));
+    }
+  }
+  const int i = whole * V + threadIdx.x;
+  if (i < n) take<TYPE>(sum, top, float(g[i]));
 }
 
 template <int TYPE>
@@ -80,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void grad_partials_kernel(GradBatch t, do
   for (unsigned chunk = blockIdx.x; chunk < t.chunks; chunk += gridDim.x) {
     const int i = tensor_of(t, chunk);
     const long at = long(chunk - t.first[i]) * kGradChunk;
-    const long n = t.size[i] - at < kGradChunk ? t.size[i] - at : kGradChunk;
+    const int n = t.size[i] - at < kGradChunk ? int(t.size[i] - at) : kGradChunk;
     if (t.dtype[i] == OAA_FLOAT32)
       chunk_norm<TYPE, float>(static_cast<const float*>(t.src[i]) + at, n, sum, top);
     else if (t.dtype[i] == OAA_BFLOAT16)
@@ -117,10 +134,24 @@ __global__ __launch_bounds__(kThreads) void grad_join_kernel(const double* part,
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const void* src, void* dst, long at, long n, float k) {
-  const T* g = static_cast<const T*>(src) + at;
-  T* o = static_cast<T*>(dst) + at;
-  for (long i = threadIdx.x; i < n; i += kThreads) o[i] = T(float(g[i]) * k);
+__device__ __forceinline__ void chunk_scale(const T* g, T* o, int n, float k) {
+  constexpr int V = 16 / int(sizeof(T));
+  const int whole = n / V;
+  for (int i = threadIdx.x; i < whole; i += kAhead * kThreads) {
+    Vec<T, V> v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i + u * kThreads < whole) v[u] = *reinterpret_cast<const Vec<T, V>*>(g + (i + u * kThreads) * V);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (i + u * kThreads >= whole) break;
+#pragma unroll
+      for (int e = 0; e < V; ++e) set_element<T, V>(v[u], e, element<T, V>(v[u], e) * k);
+      *reinterpret_cast<Vec<T, V>*>(o + (i + u * kThreads) * V) = v[u];
+    }
+  }
+  const int i = whole * V + threadIdx.x;
+  if (i < n) o[i] = T(float(g[i]) * k);
 }
 
 template <int TYPE>
@@ -134,13 +165,13 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradBatch t, const 
     const int i = tensor_of(t, chunk);
     if (k == 1.0f && t.src[i] == t.dst[i]) continue;
     const long at = long(chunk - t.first[i]) * kGradChunk;
-    const long n = t.size[i] - at < kGradChunk ? t.size[i] - at : kGradChunk;
+    const int n = t.size[i] - at < kGradChunk ? int(t.size[i] - at) : kGradChunk;
     if (t.dtype[i] == OAA_FLOAT32)
-      chunk_scale<float>(t.src[i], t.dst[i], at, n, k);
+      chunk_scale(static_cast<const float*>(t.src[i]) + at, static_cast<float*>(t.dst[i]) + at, n, k);
     else if (t.dtype[i] == OAA_BFLOAT16)
-      chunk_scale<bf16>(t.src[i], t.dst[i], at, n, k);
+      chunk_scale(static_cast<const bf16*>(t.src[i]) + at, static_cast<bf16*>(t.dst[i]) + at, n, k);
     else
-      chunk_scale<f16>(t.src[i], t.dst[i], at, n, k);
+      chunk_scale(static_cast<const f16*>(t.src[i]) + at, static_cast<f16*>(t.dst[i]) + at, n, k);
   }
 }
 

@@ -1,6 +1,6 @@
 // Group normalisation: the order of launches, and what both layouts share: the
 // join of the backward pass's sums. The passes over the values are in
-// k_norm_planes.hip and k_norm_last.hip.
+// norm_planes.hpp and norm_last.hpp.
 #include <algorithm>
 
 #include "norm_common.hpp"
@@ -10,50 +10,78 @@ namespace {
 
 constexpr int kThreads = 256;
 // dweight and dbias: a workgroup takes kColumns channels, 64 bytes of the sums'
-// rows where those run along the channels, on kThreads / kColumns lanes each.
-constexpr int kColumns = 8, kLanes = kThreads / kColumns;
+// rows where those run along the channels.
+constexpr int kColumns = 8;
 
 // Workgroups [0, groups): the means of t and t xh of a group each. The others:
 // dweight and dbias.
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void norm_join_kernel(GroupNormParams p, NormSums at, int groups) {
   if (int(blockIdx.x) < groups) {
     __shared__ double part[2 * kThreads / 64];
     const long bg = blockIdx.x, b = bg / p.G, c0 = (bg - b * p.G) * p.D;
     const float2* sums = at.sums + b * at.image + c0 * at.channel;
     double a = 0.0, d = 0.0;
-    for (long i = threadIdx.x; i < p.D * at.count; i += kThreads) {
-      const long k = i / p.D, c = i - k * p.D;
+    // entry (part k, channel c of the group) = k D + c
+    long step = kThreads / p.D, k = threadIdx.x / p.D;
+    int rest = kThreads % p.D, c = threadIdx.x % p.D;
+    while (k < at.count) {
       const float2 v = sums[c * at.channel + k * at.slot];
       const double w = load_param(p.weight, p.param_dtype, c0 + c, 1.0f);
       a = fma(w, double(v.x), a);
       d = fma(w, double(v.y), d);
+      k += step;
+      c += rest;
+      if (c >= p.D) {
+        c -= p.D;
+        ++k;
+      }
     }
     thread_sum<kThreads>(a, d, part);
     const double n = double(p.D) * p.S;
     if (threadIdx.x == 0) at.means[bg] = {float(a / n), float(d / n)};
     return;
   }
-  __shared__ double2 lanes[kLanes][kColumns];
+  constexpr int kLanes = kThreads / kColumns;
+  __shared__ double2 waves[kThreads / 64][kColumns];
   const int col = threadIdx.x % kColumns, lane = threadIdx.x / kColumns;
   const long c = long(blockIdx.x - groups) * kColumns + col;
   double a = 0.0, d = 0.0;
   if (c < p.C) {
     const float2* sums = at.sums + c * at.channel;
-    const long entries = p.B * at.count;
-#pragma unroll 8
-    for (long i = lane; i < entries; i += kLanes) {
-      const long b = i / at.count, k = i - b * at.count;
-      const float2 v = sums[b * at.image + k * at.slot];
-      a += v.x;
-      d += v.y;
+    // entry (image b, part k) = b count + k
+    const long step = kLanes / at.count, rest = kLanes % at.count;
+    long b = lane / at.count, k = lane % at.count;
+    while (b < p.B) {
+      float2 v[8];  // loaded together: the sums lie in another die's cache or in memory
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        v[u] = b < p.B ? sums[b * at.image + k * at.slot] : float2{0.0f, 0.0f};
+        b += step;
+        k += rest;
+        if (k >= at.count) {
+          k -= at.count;
+          ++b;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        a += v[u].x;
+        d += v[u].y;
+      }
     }
   }
-  lanes[lane][col] = {a, d};
+#pragma unroll
+  for (int m = 32; m >= kColumns; m >>= 1) {
+    a += __shfl_xor(a, m);
+    d += __shfl_xor(d, m);
+  }
+  if (threadIdx.x % 64 < kColumns) waves[threadIdx.x / 64][col] = {a, d};
   __syncthreads();
   if (lane || c >= p.C) return;
-  for (int i = 1; i < kLanes; ++i) {
-    a += lanes[i][col].x;
-    d += lanes[i][col].y;
+  for (int i = 1; i < kThreads / 64; ++i) {
+    a += waves[i][col].x;
+    d += waves[i][col].y;
   }
   if (p.dbias) store_param(p.dbias, p.param_dtype, c, float(a));
   if (p.dweight) store_param(p.dweight, p.param_dtype, c, float(d));
@@ -86,6 +114,12 @@ GroupNormParams images(const GroupNormParams& p, long first, long count) {
 // Images of one launch.
 long batch(const GroupNormParams& p) { return std::min<long>(p.B, std::max<long>(1, kMostChannels / p.C)); }
 
+// Whether the output does not stay in the last cache (256 MB) beside what else a
+// program touches before it is read.
+bool beyond_caches(const GroupNormParams& p) {
+  return double(p.B) * p.C * p.S * dtype_size(p.dtype) >= 64.0 * (1 << 20);
+}
+
 NormCut forward_cut(const GroupNormParams& p) {
   const GroupNormParams q = images(p, 0, batch(p));
   return p.last ? last_forward_cut(q) : planes_forward_cut(q);
@@ -110,7 +144,10 @@ hipError_t launch_norm_join(const GroupNormParams& p, const NormSums& at, hipStr
   const int groups = at.means ? p.B * p.G : 0;
   const int columns = p.dweight || p.dbias ? (p.C + kColumns - 1) / kColumns : 0;
   if (groups + columns == 0) return hipSuccess;
-  norm_join_kernel<<<groups + columns, kThreads, 0, s>>>(p, at, groups);
+  if (p.B * at.count <= 512)
+    norm_join_kernel<256><<<groups + columns, 256, 0, s>>>(p, at, groups);
+  else
+    norm_join_kernel<1024><<<groups + columns, 1024, 0, s>>>(p, at, groups);
   return hipGetLastError();
 }
 
@@ -124,16 +161,24 @@ size_t group_norm_backward_ws(const GroupNormParams& p) {
   return sums_bytes(p, sums_layout(p, cut)) + (cut.split ? align_workspace(sizeof(float2) * p.B * p.G) : 0);
 }
 
-hipError_t launch_group_norm_forward(const GroupNormParams& p, hipStream_t s) {
+hipError_t launch_group_norm_forward(const GroupNormParams& in, hipStream_t s) {
+  GroupNormParams p = in;
+  p.once = beyond_caches(p);
   const NormCut cut = forward_cut(p);
   for (long b = 0; b < p.B; b += batch(p)) {
     const GroupNormParams q = images(p, b, std::min(batch(p), p.B - b));
-    if (hipError_t e = p.last ? launch_last_forward(q, cut, s) : launch_planes_forward(q, cut, s)) return e;
+    const hipError_t e = for_type(p.dtype, [&](auto t) {
+      using T = typename decltype(t)::type;
+      return p.last ? launch_last_forward<T>(q, cut, s) : launch_planes_forward<T>(q, cut, s);
+    });
+    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-hipError_t launch_group_norm_backward(const GroupNormParams& p, hipStream_t s) {
+hipError_t launch_group_norm_backward(const GroupNormParams& in, hipStream_t s) {
+  GroupNormParams p = in;
+  p.once = beyond_caches(p);
   const NormCut cut = backward_cut(p);
   NormSums all = sums_layout(p, cut);
   all.sums = reinterpret_cast<float2*>(p.ws);
@@ -146,7 +191,11 @@ hipError_t launch_group_norm_backward(const GroupNormParams& p, hipStream_t s) {
     NormSums at = all;
     at.sums += b * at.image;
     at.means = means ? means + b * p.G : nullptr;
-    if (hipError_t e = p.last ? launch_last_backward(q, cut, at, s) : launch_planes_backward(q, cut, at, s)) return e;
+    const hipError_t e = for_type(p.dtype, [&](auto t) {
+      using T = typename decltype(t)::type;
+      return p.last ? launch_last_backward<T>(q, cut, at, s) : launch_planes_backward<T>(q, cut, at, s);
+    });
+    if (e != hipSuccess) return e;
   }
   return one && cut.split ? hipSuccess : launch_norm_join(p, all, s);
 }

@@ -1,0 +1,9 @@
+// The kernels of norm_last.hpp for float32.
+#include "norm_last.hpp"
+
+namespace oaa {
+
+template hipError_t launch_last_forward<float>(const GroupNormParams&, const NormCut&, hipStream_t);
+template hipError_t launch_last_backward<float>(const GroupNormParams&, const NormCut&, const NormSums&, hipStream_t);
+
+}  // namespace oaa

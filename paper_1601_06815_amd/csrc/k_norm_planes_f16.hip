@@ -1,0 +1,9 @@
+// The kernels of norm_planes.hpp for float16.
+#include "norm_planes.hpp"
+
+namespace oaa {
+
+template hipError_t launch_planes_forward<f16>(const GroupNormParams&, const NormCut&, hipStream_t);
+template hipError_t launch_planes_backward<f16>(const GroupNormParams&, const NormCut&, const NormSums&, hipStream_t);
+
+}  // namespace oaa

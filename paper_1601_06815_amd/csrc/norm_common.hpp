@@ -4,25 +4,46 @@
 
 #include <hip/hip_runtime.h>
 
-#include "group_norm.hpp"
-#include "oaa_status.hpp"
+#include "norm_choice.hpp"
 #include "scalar_types.hpp"
 
 namespace oaa {
-
-inline size_t align_workspace(size_t v) { return (v + kWorkspaceAlign - 1) / kWorkspaceAlign * kWorkspaceAlign; }
 
 // Elements of one 16-byte access.
 template <typename T>
 constexpr int kVec = 16 / int(sizeof(T));
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.0f / (1.0f + expf(-z)); }
+// e^x through the hardware's 2^x. Rounding x log2(e) costs |x| 2^-24 of the
+// result, which the uses below multiply by something that falls faster.
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+__device__ __forceinline__ float fast_reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }  // within one step
+
+__device__ __forceinline__ float sigmoid(float z) { return fast_reciprocal(1.0f + fast_exp(-z)); }
+
+// The normal distribution Phi(z), and e = exp(-z^2 / 2): erfc(u) = (a1 t + .. +
+// a5 t^5) exp(-u^2), t = 1 / (1 + 0.3275911 u), u = |z| / sqrt(2) (Abramowitz and
+// Stegun, 7.1.26), within 1.5e-7, so Phi is within one and a quarter steps of a
+// float32 at 1. The library's erf takes three times the instructions, and the
+// passes over 16-bit values would be bound by it.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float u = fabsf(z) * 0.70710678f, t = fast_reciprocal(fmaf(0.3275911f, u, 1.0f));
+  e = fast_exp(-u * u);
+  float q = fmaf(1.061405429f, t, -1.453152027f);
+  q = fmaf(q, t, 1.421413741f);
+  q = fmaf(q, t, -0.284496736f);
+  q = fmaf(q, t, 0.254829592f);
+  const float half = 0.5f * q * t * e;
+  return z < 0.0f ? half : 1.0f - half;
+}
 
 template <int ACT>
 __device__ __forceinline__ float act(float z) {
   if constexpr (ACT == OAA_ACT_RELU) return z < 0.0f ? 0.0f : z;  // NaN stays NaN
   if constexpr (ACT == OAA_ACT_SILU) return z * sigmoid(z);
-  if constexpr (ACT == OAA_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+  if constexpr (ACT == OAA_ACT_GELU) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   return z;
 }
 
@@ -31,10 +52,13 @@ __device__ __forceinline__ float act_slope(float z) {
   if constexpr (ACT == OAA_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
   if constexpr (ACT == OAA_ACT_SILU) {
     const float s = sigmoid(z);
-    return s * (1.0f + z * (1.0f - s));
+    return fmaf(z * s, 1.0f - s, s);
   }
-  if constexpr (ACT == OAA_ACT_GELU)
-    return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+  if constexpr (ACT == OAA_ACT_GELU) {
+    float e;
+    const float cdf = normal_cdf(z, e);
+    return fmaf(z * 0.39894228f, e, cdf);
+  }
   return 1.0f;
 }
 
@@ -85,9 +109,18 @@ __device__ __forceinline__ Vec<T, V> load(const T* p) {
   return *reinterpret_cast<const Vec<T, V>*>(p);
 }
 
+// A store; `once`: of memory too large to be found in a cache when it is read
+// next. Such a store leaves the caches to what the pass reads.
 template <typename T, int V>
-__device__ __forceinline__ void store(T* p, const Vec<T, V>& v) {
-  *reinterpret_cast<Vec<T, V>*>(p) = v;
+__device__ __forceinline__ void store(T* p, const Vec<T, V>& v, bool once) {
+  if (once) {
+    // the empty statements keep the compiler from making one plain store of both
+    asm volatile("");
+    __builtin_nontemporal_store(v, reinterpret_cast<Vec<T, V>*>(p));
+    asm volatile("");
+  } else {
+    *reinterpret_cast<Vec<T, V>*>(p) = v;
+  }
 }
 
 // dz and xh of one value.
@@ -97,6 +130,15 @@ __device__ __forceinline__ void gradient(float x, float dy, float mean, float rs
   xh = (x - mean) * rstd;
   dz = dy * act_slope<ACT>(fmaf(xh, w, b));
 }
+
+// What the input gradient takes of a channel: dx = rstd (w dz - m1 - xh m2).
+struct InputGradient {
+  float w, m1, m2;
+  __device__ __forceinline__ InputGradient() {}
+  __device__ __forceinline__ InputGradient(float rstd, float w_, float m1_, float m2_)
+      : w(rstd * w_), m1(rstd * m1_), m2(rstd * m2_) {}
+  __device__ __forceinline__ float operator()(float dz, float xh) const { return fmaf(w, dz, -fmaf(xh, m2, m1)); }
+};
 
 template <typename T>
 struct Type {

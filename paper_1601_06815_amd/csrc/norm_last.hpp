@@ -17,6 +17,8 @@
 // Statistics are summed in float64 about the group's first value x0: the
 // variance is E[d^2] - E[d]^2 of d = x - x0, which keeps its digits however far
 // the mean is from 0.
+#pragma once
+
 #include <algorithm>
 
 #include "norm_common.hpp"
@@ -105,11 +107,6 @@ struct Moments {
   }
 };
 
-constexpr int kAhead = 4;
-
-// Most groups of a slab that one workgroup keeps.
-constexpr int kMostGroups = 128;
-
 // ---- forward, one slab per THREADS threads -----------------------------------
 
 // Slab j of `slabs`: whole groups [j G / slabs, (j + 1) G / slabs).
@@ -194,20 +191,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_forward_ke
 #pragma unroll
     for (int i = 0; i < V; ++i)
       set_element<T, V>(out, i, act<ACT>(fmaf(element<T, V>(held[k], i) - mean[i], w[i], bias[i])));
-    store<T, V>(y + s * p.y_row, out);
+    store<T, V>(y + s * p.y_row, out, p.once);
   }
 }
 
 // ---- forward, rows sliced over the device ------------------------------------------
-
-constexpr int kSplitThreads = 256;
-
-// Slabs of at most kSplitThreads accesses, where rows are sliced: slab j is
-// columns [j C / slabs, (j + 1) C / slabs), which may cut a group.
-template <int V>
-__host__ __device__ inline int split_slabs(int C) {
-  return (C + kSplitThreads * V - 1) / (kSplitThreads * V);
-}
 
 // A workgroup's place: image b, slice k of its rows, slab j.
 template <int V>
@@ -215,10 +203,10 @@ struct SplitPlace {
   long b, k;
   int j, slabs, c0, width;
   long begin, end;
-  __device__ __forceinline__ SplitPlace(const GroupNormParams& p, long slice, int count) {
-    slabs = split_slabs<V>(p.C);
-    const long i = blockIdx.x / slabs;
-    j = int(blockIdx.x - i * slabs);
+  __device__ __forceinline__ SplitPlace(const GroupNormParams& p, long slice, int count, unsigned block) {
+    slabs = split_slabs(p.C, V);
+    const long i = block / slabs;
+    j = int(block - i * slabs);
     b = i / count;
     k = i - b * count;
     c0 = int(long(j) * p.C / slabs);
@@ -233,7 +221,7 @@ template <typename T, int V>
 __global__ __launch_bounds__(kSplitThreads) void last_moments_kernel(GroupNormParams p, long slice, int count,
                                                                      double2* sums) {
   __shared__ double2 entries[kSplitThreads * V];
-  const SplitPlace<V> in(p, slice, count);
+  const SplitPlace<V> in(p, slice, count, blockIdx.x);
   const Place<V, kSplitThreads> at(threadIdx.x, in.width);
   const int D = p.D, g0 = in.c0 / D, own = in.c0 - g0 * D;
   const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c0;
@@ -307,7 +295,7 @@ struct Columns {
 
 template <typename T, int ACT, int V>
 __global__ __launch_bounds__(kSplitThreads) void last_apply_kernel(GroupNormParams p, long slice, int count) {
-  const SplitPlace<V> in(p, slice, count);
+  const SplitPlace<V> in(p, slice, count, gridDim.x - 1 - blockIdx.x);
   const Place<V, kSplitThreads> at(threadIdx.x, in.width);
   if (!at.active()) return;
   Columns<V> col(p, in.b, in.c0 + at.col);
@@ -327,21 +315,30 @@ __global__ __launch_bounds__(kSplitThreads) void last_apply_kernel(GroupNormPara
 #pragma unroll
       for (int i = 0; i < V; ++i)
         set_element<T, V>(out, i, act<ACT>(fmaf(element<T, V>(v[u], i) - col.mean[i], col.w[i], col.bias[i])));
-      store<T, V>(y + (s + u * at.lanes) * p.y_row, out);
+      store<T, V>(y + (s + u * at.lanes) * p.y_row, out, p.once);
     }
   }
 }
 
 // ---- backward ---------------------------------------------------------------------
 
+// Whether xh and dz of a row take the place of its x and dy: in float32 nothing
+// is lost, and the second half of the pass does not compute them again.
+template <typename T>
+constexpr bool kInPlace = sizeof(T) == 4;
+
 // Adds a row's dz and dz xh to a thread's sums of its columns.
 template <typename T, int ACT, int V>
-__device__ __forceinline__ void add_gradient(const Vec<T, V>& x, const Vec<T, V>& dy, const Columns<V>& col,
-                                             float (&sa)[V], float (&sb)[V]) {
+__device__ __forceinline__ void add_gradient(Vec<T, V>& x, Vec<T, V>& dy, const Columns<V>& col, float (&sa)[V],
+                                             float (&sb)[V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     float dz, xh;
     gradient<ACT>(element<T, V>(x, i), element<T, V>(dy, i), col.mean[i], col.rstd[i], col.w[i], col.bias[i], dz, xh);
+    if constexpr (kInPlace<T>) {
+      set_element<T, V>(x, i, xh);
+      set_element<T, V>(dy, i, dz);
+    }
     sa[i] += dz;
     sb[i] = fmaf(dz, xh, sb[i]);
   }
@@ -349,14 +346,25 @@ __device__ __forceinline__ void add_gradient(const Vec<T, V>& x, const Vec<T, V>
 
 template <typename T, int ACT, int V>
 __device__ __forceinline__ Vec<T, V> input_gradient(const Vec<T, V>& x, const Vec<T, V>& dy, const Columns<V>& col,
-                                                    const float (&m1)[V], const float (&m2)[V]) {
+                                                    const InputGradient (&of)[V]) {
   Vec<T, V> out;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     float dz, xh;
     gradient<ACT>(element<T, V>(x, i), element<T, V>(dy, i), col.mean[i], col.rstd[i], col.w[i], col.bias[i], dz, xh);
-    set_element<T, V>(out, i, col.rstd[i] * (fmaf(col.w[i], dz, -m1[i]) - xh * m2[i]));
+    set_element<T, V>(out, i, of[i](dz, xh));
   }
+  return out;
+}
+
+// The same after add_gradient has seen the row.
+template <typename T, int ACT, int V>
+__device__ __forceinline__ Vec<T, V> held_input_gradient(const Vec<T, V>& x, const Vec<T, V>& dy,
+                                                         const Columns<V>& col, const InputGradient (&of)[V]) {
+  if constexpr (!kInPlace<T>) return input_gradient<T, ACT, V>(x, dy, col, of);
+  Vec<T, V> out;
+#pragma unroll
+  for (int i = 0; i < V; ++i) set_element<T, V>(out, i, of[i](element<T, V>(dy, i), element<T, V>(x, i)));
   return out;
 }
 
@@ -428,17 +436,17 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_backward_k
   if (!works) return;
   int g[V];
   groups_of<V>(at.col, 0, D, g);
-  float m1[V], m2[V];
+  InputGradient of[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    m1[i] = means[sub][g[i]].x;
-    m2[i] = means[sub][g[i]].y;
+    const float2 m = means[sub][g[i]];
+    of[i] = InputGradient(col.rstd[i], col.w[i], m.x, m.y);
   }
   T* dx = static_cast<T*>(p.dx) + b * p.dx_image + c0 + at.col;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int s = at.lane + k * at.lanes;
-    if (s < S) store<T, V>(dx + s * p.dx_row, input_gradient<T, ACT, V>(hx[k], hdy[k], col, m1, m2));
+    if (s < S) store<T, V>(dx + s * p.dx_row, held_input_gradient<T, ACT, V>(hx[k], hdy[k], col, of), p.once);
   }
 }
 
@@ -447,7 +455,7 @@ template <typename T, int ACT, int V>
 __global__ __launch_bounds__(kSplitThreads) void last_column_sums_kernel(GroupNormParams p, long slice, int count,
                                                                          float2* sums) {
   __shared__ float2 entries[kSplitThreads * V];
-  const SplitPlace<V> in(p, slice, count);
+  const SplitPlace<V> in(p, slice, count, blockIdx.x);
   const Place<V, kSplitThreads> at(threadIdx.x, in.width);
   if (at.active()) {
     const Columns<V> col(p, in.b, in.c0 + at.col);
@@ -486,17 +494,17 @@ __global__ __launch_bounds__(kSplitThreads) void last_column_sums_kernel(GroupNo
 template <typename T, int ACT, int V>
 __global__ __launch_bounds__(kSplitThreads) void last_input_gradient_kernel(GroupNormParams p, long slice, int count,
                                                                             const float2* means) {
-  const SplitPlace<V> in(p, slice, count);
+  const SplitPlace<V> in(p, slice, count, gridDim.x - 1 - blockIdx.x);
   const Place<V, kSplitThreads> at(threadIdx.x, in.width);
   if (!at.active()) return;
   const Columns<V> col(p, in.b, in.c0 + at.col);
   int g[V];
   groups_of<V>(in.c0 + at.col, 0, p.D, g);
-  float m1[V], m2[V];
+  InputGradient of[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    m1[i] = means[in.b * p.G + g[i]].x;
-    m2[i] = means[in.b * p.G + g[i]].y;
+    const float2 m = means[in.b * p.G + g[i]];
+    of[i] = InputGradient(col.rstd[i], col.w[i], m.x, m.y);
   }
   const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c0 + at.col;
   const T* dy = static_cast<const T*>(p.dy) + in.b * p.dy_image + in.c0 + at.col;
@@ -512,59 +520,11 @@ __global__ __launch_bounds__(kSplitThreads) void last_input_gradient_kernel(Grou
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
       if (s + u * at.lanes < in.end)
-        store<T, V>(dx + (s + u * at.lanes) * p.dx_row, input_gradient<T, ACT, V>(vx[u], vdy[u], col, m1, m2));
+        store<T, V>(dx + (s + u * at.lanes) * p.dx_row, input_gradient<T, ACT, V>(vx[u], vdy[u], col, of), p.once);
   }
 }
 
 // ---- choice -----------------------------------------------------------------------
-
-// Workgroups that the sliced kernels aim for.
-constexpr long kSlices = 2048;
-
-int vector_of(const GroupNormParams& p) {
-  const int V = p.dtype == OAA_FLOAT32 ? 4 : 8;
-  return p.C >= V ? V : 1;
-}
-
-// Slabs of an image where a slab goes to one workgroup: whole groups, 128 bytes
-// of a row (a line) or more, fewer where workgroups would be few.
-int whole_slabs(const GroupNormParams& p) {
-  const long row = long(p.D) * long(dtype_size(p.dtype)), total = long(p.B) * p.G;
-  long q = (128 + row - 1) / row;
-  if (total < 256 * q) q = std::max(std::max<long>(1, total / 256), (long(vector_of(p)) + p.D - 1) / p.D);
-  return int(std::max<long>(1, p.G / q));
-}
-
-// Whether a workgroup of so many threads, with so many rows a lane, holds a slab.
-bool holds(const GroupNormParams& p, int slabs, int threads, int rows) {
-  const long groups = (p.G + slabs - 1) / slabs, V = vector_of(p), accesses = (groups * p.D + V - 1) / V;
-  return groups <= kMostGroups && accesses <= threads && p.S <= threads / accesses * rows;
-}
-
-constexpr int kForwardThreads = 512, kForwardRows = 32, kBackwardThreads = 512, kBackwardRows = 16;
-
-// Whether a slab goes to one workgroup. The alternative reads everything twice
-// and takes two launches more.
-NormCut cut_rows(const GroupNormParams& p, int threads, int rows) {
-  const int slabs = whole_slabs(p);
-  if (holds(p, slabs, threads, rows) && (long(p.B) * slabs >= 128 || p.S <= 1024)) return {false, 0, slabs};
-  const int V = vector_of(p), cuts = V == 1 ? split_slabs<1>(p.C) : V == 4 ? split_slabs<4>(p.C) : split_slabs<8>(p.C);
-  const long lanes = std::max<long>(1, kSplitThreads / std::max<long>(1, ((p.C + cuts - 1) / cuts + V - 1) / V));
-  const long images = long(p.B) * cuts;
-  long slice = (p.S * images + kSlices - 1) / kSlices;
-  slice = (slice + lanes * kAhead - 1) / (lanes * kAhead) * (lanes * kAhead);
-  return {true, slice, (p.S + slice - 1) / slice};
-}
-
-template <int V>
-long parts(const GroupNormParams& p, const NormCut& cut) {
-  return cut.count * split_slabs<V>(p.C);
-}
-
-long parts_of(const GroupNormParams& p, const NormCut& cut) {
-  const int V = vector_of(p);
-  return V == 1 ? parts<1>(p, cut) : V == 4 ? parts<4>(p, cut) : parts<8>(p, cut);
-}
 
 template <typename T, int ACT, int V, int THREADS, int NV>
 hipError_t forward_slabs(const GroupNormParams& p, int slabs, hipStream_t s) {
@@ -585,13 +545,15 @@ hipError_t forward(const GroupNormParams& in, const NormCut& cut, hipStream_t s)
   }
   GroupNormParams p = in;
   double2* sums = reinterpret_cast<double2*>(p.ws);
-  float* stats = reinterpret_cast<float*>(p.ws + align_workspace(sizeof(double2) * p.B * p.G * parts<V>(p, cut)));
+  float* stats = reinterpret_cast<float*>(p.ws + align_workspace(sizeof(double2) * p.B * p.G * parts(p, cut)));
   if (!p.mean) p.mean = stats;
   if (!p.rstd) p.rstd = stats + long(p.B) * p.G;
-  const unsigned blocks = unsigned(p.B * parts<V>(p, cut));
+  const unsigned blocks = unsigned(p.B * parts(p, cut));
   last_moments_kernel<T, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), sums);
-  last_statistics_kernel<T><<<p.B * p.G, kSplitThreads, 0, s>>>(p, int(parts<V>(p, cut)), sums);
-  last_apply_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count));
+  last_statistics_kernel<T><<<p.B * p.G, kSplitThreads, 0, s>>>(p, int(parts(p, cut)), sums);
+  const long slice = row_slice(p, kResultSlices), count = (p.S + slice - 1) / slice;
+  last_apply_kernel<T, ACT, V>
+      <<<unsigned(p.B * count * split_slabs(p.C, V)), kSplitThreads, 0, s>>>(p, slice, int(count));
   return hipGetLastError();
 }
 
@@ -613,48 +575,32 @@ hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums
     if (holds(p, slabs, 256, 8)) return backward_slabs<T, ACT, V, 256, 8>(p, slabs, at, s);
     return backward_slabs<T, ACT, V, kBackwardThreads, kBackwardRows>(p, slabs, at, s);
   }
-  const unsigned blocks = unsigned(p.B * parts<V>(p, cut));
+  const unsigned blocks = unsigned(p.B * parts(p, cut));
   last_column_sums_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at.sums);
   if (hipError_t e = launch_norm_join(p, at, s)) return e;
-  if (p.dx)
-    last_input_gradient_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at.means);
+  if (p.dx) {
+    const long slice = row_slice(p, kResultSlices), count = (p.S + slice - 1) / slice;
+    last_input_gradient_kernel<T, ACT, V>
+        <<<unsigned(p.B * count * split_slabs(p.C, V)), kSplitThreads, 0, s>>>(p, slice, int(count), at.means);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
-NormCut last_forward_cut(const GroupNormParams& p) { return cut_rows(p, kForwardThreads, kForwardRows); }
-
-size_t last_forward_ws(const GroupNormParams& p, const NormCut& cut) {
-  if (!cut.split) return 0;
-  return align_workspace(sizeof(double2) * p.B * p.G * parts_of(p, cut)) +
-         align_workspace(2 * sizeof(float) * p.B * p.G);
-}
-
-NormCut last_backward_cut(const GroupNormParams& p) { return cut_rows(p, kBackwardThreads, kBackwardRows); }
-
-NormSums last_sums(const GroupNormParams& p, const NormCut& cut) {
-  const long count = cut.split ? cut.count : 1;
-  return {nullptr, nullptr, count, p.C * count, 1, p.C};
-}
-
+template <typename T>
 hipError_t launch_last_forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s) {
-  return for_type(p.dtype, [&](auto t) {
-    using T = typename decltype(t)::type;
-    return for_act(p.act, [&](auto a) {
-      constexpr int A = decltype(a)::value;
-      return vector_of(p) > 1 ? forward<T, A, kVec<T>>(p, cut, s) : forward<T, A, 1>(p, cut, s);
-    });
+  return for_act(p.act, [&](auto a) {
+    constexpr int A = decltype(a)::value;
+    return vector_of(p) > 1 ? forward<T, A, kVec<T>>(p, cut, s) : forward<T, A, 1>(p, cut, s);
   });
 }
 
+template <typename T>
 hipError_t launch_last_backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s) {
-  return for_type(p.dtype, [&](auto t) {
-    using T = typename decltype(t)::type;
-    return for_act(p.act, [&](auto a) {
-      constexpr int A = decltype(a)::value;
-      return vector_of(p) > 1 ? backward<T, A, kVec<T>>(p, cut, at, s) : backward<T, A, 1>(p, cut, at, s);
-    });
+  return for_act(p.act, [&](auto a) {
+    constexpr int A = decltype(a)::value;
+    return vector_of(p) > 1 ? backward<T, A, kVec<T>>(p, cut, at, s) : backward<T, A, 1>(p, cut, at, s);
   });
 }
 

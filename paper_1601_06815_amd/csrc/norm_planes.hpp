@@ -18,6 +18,10 @@
 // Statistics are summed in float64 about the group's first value x0: the
 // variance is E[d^2] - E[d]^2 of d = x - x0, which keeps its digits however far
 // the mean is from 0.
+#pragma once
+
+#include <algorithm>
+
 #include "norm_common.hpp"
 
 namespace oaa {
@@ -80,10 +84,16 @@ struct Cursor {
       ++r;
     }
   }
+  __device__ __forceinline__ void back() {
+    u -= STEP;
+    r -= dr;
+    v -= dv;
+    if (v < 0) {
+      v += nv;
+      --r;
+    }
+  }
 };
-
-// Units loaded before the first of them is used, where a group's values stream.
-constexpr int kAhead = 4;
 
 // Moments of units [at.u, end), STEP apart.
 template <typename T, int V, int STEP, typename I>
@@ -104,30 +114,33 @@ __device__ __forceinline__ void stream_moments(const T* x, Cursor<STEP, I> at, I
   }
 }
 
-// y of units [at.u, end), STEP apart; param(r, w, b) gives a row's parameters.
+// y of units u, u + STEP, ... of [u, end), the last first: what was read last is
+// still in a cache. param(r, w, b) gives a row's parameters.
 template <typename T, int ACT, int V, int STEP, typename I, typename Param>
-__device__ __forceinline__ void stream_normalised(const T* x, T* y, Cursor<STEP, I> at, I end, I S, float mean,
-                                                  float rstd, Param&& param) {
-  while (at.u < end) {
+__device__ __forceinline__ void stream_normalised(const T* x, T* y, I u, I end, I nv, I S, float mean, float rstd,
+                                                  bool once, Param&& param) {
+  if (u >= end) return;
+  Cursor<STEP, I> at(u + (end - 1 - u) / STEP * STEP, nv);
+  while (at.u >= u) {
     Vec<T, V> v[kAhead];
     I o[kAhead], r[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       int dup;
       r[k] = -1;
-      if (at.u < end) {
+      if (at.u >= u) {
         r[k] = at.r;
         o[k] = unit_at<V, I>(at.r, at.v, S, dup);
         v[k] = load<T, V>(x + o[k]);
       }
-      at.next();
+      at.back();
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (r[k] < 0) continue;
       float w, b;
       param(r[k], w, b);
-      store<T, V>(y + o[k], normalised<T, ACT, V>(v[k], mean, rstd * w, b));
+      store<T, V>(y + o[k], normalised<T, ACT, V>(v[k], mean, rstd * w, b), once);
     }
   }
 }
@@ -183,7 +196,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void planes_forward_
     if (p.mean) p.mean[bg] = mean;
     if (p.rstd) p.rstd[bg] = rstd;
   }
-  stream_normalised<T, ACT, V>(x, y, far, units, S, mean, rstd, [&](int r, float& wr, float& br) {
+  stream_normalised<T, ACT, V, THREADS>(x, y, far.u, units, nv, S, mean, rstd, p.once, [&](int r, float& wr, float& br) {
     wr = w[r];
     br = w[D + r];
   });
@@ -193,15 +206,13 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void planes_forward_
     int dup;
     if (at.u < units) {
       const int o = unit_at<V>(at.r, at.v, S, dup);
-      store<T, V>(y + o, normalised<T, ACT, V>(held[k], mean, rstd * w[at.r], w[D + at.r]));
+      store<T, V>(y + o, normalised<T, ACT, V>(held[k], mean, rstd * w[at.r], w[D + at.r]), p.once);
     }
     at.next();
   }
 }
 
 // ---- forward, few large groups: `count` slices of each ----------------------------
-
-constexpr int kSplitThreads = 256;
 
 template <typename T, int V>
 __global__ __launch_bounds__(kSplitThreads) void planes_moments_kernel(GroupNormParams p, long slice, int count,
@@ -239,23 +250,32 @@ __global__ __launch_bounds__(kSplitThreads) void planes_apply_kernel(GroupNormPa
     if (p.rstd) p.rstd[bg] = rstd;
   }
   const long begin = slot * slice, end = begin + slice < units ? begin + slice : units;
-  stream_normalised<T, ACT, V>(x, y, Cursor<kSplitThreads, long>(begin + threadIdx.x, nv), end, S, mean, rstd,
-                               [&](long r, float& wr, float& br) {
-                                 wr = load_param(p.weight, p.param_dtype, c0 + r, 1.0f);
-                                 br = load_param(p.bias, p.param_dtype, c0 + r, 0.0f);
-                               });
+  stream_normalised<T, ACT, V, kSplitThreads>(x, y, begin + threadIdx.x, end, nv, S, mean, rstd, p.once,
+                                              [&](long r, float& wr, float& br) {
+                                                wr = load_param(p.weight, p.param_dtype, c0 + r, 1.0f);
+                                                br = load_param(p.bias, p.param_dtype, c0 + r, 0.0f);
+                                              });
 }
 
 // ---- backward ---------------------------------------------------------------------
 
+// Whether a unit's xh and dz take the place of its x and dy: in float32 nothing
+// is lost, and the second half of the pass does not compute them again.
+template <typename T>
+constexpr bool kInPlace = sizeof(T) == 4;
+
 // Sums of dz and dz xh over a unit, its first `dup` values left out.
 template <typename T, int ACT, int V>
-__device__ __forceinline__ void add_gradient(const Vec<T, V>& x, const Vec<T, V>& dy, int dup, float mean, float rstd,
-                                             float w, float b, float& sa, float& sb) {
+__device__ __forceinline__ void add_gradient(Vec<T, V>& x, Vec<T, V>& dy, int dup, float mean, float rstd, float w,
+                                             float b, float& sa, float& sb) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     float dz, xh;
     gradient<ACT>(element<T, V>(x, i), element<T, V>(dy, i), mean, rstd, w, b, dz, xh);
+    if constexpr (kInPlace<T>) {
+      set_element<T, V>(x, i, xh);
+      set_element<T, V>(dy, i, dz);
+    }
     dz = i < dup ? 0.0f : dz;
     sa += dz;
     sb = fmaf(dz, xh, sb);
@@ -265,33 +285,55 @@ __device__ __forceinline__ void add_gradient(const Vec<T, V>& x, const Vec<T, V>
 template <typename T, int ACT, int V>
 __device__ __forceinline__ Vec<T, V> input_gradient(const Vec<T, V>& x, const Vec<T, V>& dy, float mean, float rstd,
                                                     float w, float b, float m1, float m2) {
+  const InputGradient of(rstd, w, m1, m2);
   Vec<T, V> out;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     float dz, xh;
     gradient<ACT>(element<T, V>(x, i), element<T, V>(dy, i), mean, rstd, w, b, dz, xh);
-    set_element<T, V>(out, i, rstd * (fmaf(w, dz, -m1) - xh * m2));
+    set_element<T, V>(out, i, of(dz, xh));
   }
   return out;
 }
 
-// Row and access of a thread's k-th unit, rows going to 2^lpr lanes each.
-struct RowCursor {
-  int r, v;
-  int lane, step_r, step_v, nv;
-  __device__ __forceinline__ RowCursor(int tid, int threads, int lpr, int nv_) : nv(nv_) {
+// The same after add_gradient has seen the unit.
+template <typename T, int ACT, int V>
+__device__ __forceinline__ Vec<T, V> held_input_gradient(const Vec<T, V>& x, const Vec<T, V>& dy, float mean,
+                                                         float rstd, float w, float b, float m1, float m2) {
+  if constexpr (!kInPlace<T>) return input_gradient<T, ACT, V>(x, dy, mean, rstd, w, b, m1, m2);
+  const InputGradient of(rstd, w, m1, m2);
+  Vec<T, V> out;
+#pragma unroll
+  for (int i = 0; i < V; ++i) set_element<T, V>(out, i, of(element<T, V>(dy, i), element<T, V>(x, i)));
+  return out;
+}
+
+// A thread's units, rows going to 2^lpr lanes each: step k is access lane + vi
+// 2^lpr of row r0 + ri step_r, with vi and ri counted alike in all lanes.
+struct RowSteps {
+  int r0, lane, step_r, step_v, accesses;
+  int ri = 0, vi = 0;
+  __device__ __forceinline__ RowSteps(int tid, int threads, int lpr, int nv) {
     step_v = 1 << lpr;
-    lane = tid & (step_v - 1);
     step_r = threads >> lpr;
-    r = tid >> lpr;
-    v = lane;
+    lane = tid & (step_v - 1);
+    r0 = tid >> lpr;
+    accesses = (nv + step_v - 1) >> lpr;
   }
-  // Whether the row ends here, for all of its lanes.
-  __device__ __forceinline__ bool last() const { return v - lane + step_v >= nv; }
+  __device__ __forceinline__ int r() const { return r0 + ri * step_r; }
+  __device__ __forceinline__ int v() const { return lane + vi * step_v; }
+  __device__ __forceinline__ bool last() const { return vi == accesses - 1; }  // of the row
   __device__ __forceinline__ void next() {
-    const bool end = last();
-    r = end ? r + step_r : r;
-    v = end ? lane : v + step_v;
+    if (++vi == accesses) {
+      vi = 0;
+      ++ri;
+    }
+  }
+  __device__ __forceinline__ void back() {
+    if (--vi < 0) {
+      vi = accesses - 1;
+      --ri;
+    }
   }
 };
 
@@ -317,12 +359,14 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void planes_backward
   const float mean = active ? p.mean[bg] : 0.0f, rstd = active ? p.rstd[bg] : 0.0f;
 
   Vec<T, V> hx[NV], hdy[NV];
-  RowCursor at(tid, THREADS, lpr, nv);
+  const RowSteps first(tid, THREADS, lpr, nv);
+  auto at = first;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     int dup;
-    if (at.r < rows && at.v < nv) {
-      const int o = unit_at<V>(at.r, at.v, S, dup);
+    const int r = at.r(), v = at.v();
+    if (r < rows && v < nv) {
+      const int o = unit_at<V>(r, v, S, dup);
       hx[k] = load<T, V>(x + o);
       hdy[k] = load<T, V>(dy + o);
     }
@@ -344,24 +388,40 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void planes_backward
     if (r < rows && (tid & 63 & ((1 << lpr) - 1)) == 0) row_sums[r * wpr + (lpr > 6 ? tid / 64 % wpr : 0)] = {sa, sb};
     sa = sb = 0.0f;
   };
-  at = RowCursor(tid, THREADS, lpr, nv);
+  at = first;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     int dup;
-    unit_at<V>(at.r, at.v, S, dup);
-    if (at.r < rows && at.v < nv)
-      add_gradient<T, ACT, V>(hx[k], hdy[k], dup, mean, rstd, w[at.r], w[D + at.r], sa, sb);
-    if (at.last()) row_end(at.r);
+    const int r = at.r(), v = at.v();
+    unit_at<V>(r, v, S, dup);
+    if (r < rows && v < nv) add_gradient<T, ACT, V>(hx[k], hdy[k], dup, mean, rstd, w[r], w[D + r], sa, sb);
+    if (at.last()) row_end(r);
     at.next();
   }
   const auto far = at;
-  for (auto f = far; f.r - (tid >> lpr) < rows; f.next()) {
-    if (f.r < rows && f.v < nv) {
+  while (at.ri * at.step_r < rows) {
+    Vec<T, V> vx[kAhead], vdy[kAhead];
+    auto ahead = at;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
       int dup;
-      const int o = unit_at<V>(f.r, f.v, S, dup);
-      add_gradient<T, ACT, V>(load<T, V>(x + o), load<T, V>(dy + o), dup, mean, rstd, w[f.r], w[D + f.r], sa, sb);
+      const int r = ahead.r(), v = ahead.v();
+      if (r < rows && v < nv) {
+        const int o = unit_at<V>(r, v, S, dup);
+        vx[k] = load<T, V>(x + o);
+        vdy[k] = load<T, V>(dy + o);
+      }
+      ahead.next();
     }
-    if (f.last()) row_end(f.r);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      int dup;
+      const int r = at.r(), v = at.v();
+      unit_at<V>(r, v, S, dup);
+      if (r < rows && v < nv) add_gradient<T, ACT, V>(vx[k], vdy[k], dup, mean, rstd, w[r], w[D + r], sa, sb);
+      if (at.last()) row_end(r);
+      at.next();
+    }
   }
   __syncthreads();
   double ta = 0.0, tb = 0.0;
@@ -380,23 +440,44 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void planes_backward
   const double n = double(D) * S;
   const float m1 = float(ta / n), m2 = float(tb / n);
   T* dx = static_cast<T*>(p.dx) + b * p.dx_image + long(c0) * S;
-  for (auto f = far; f.r < rows; f.next()) {
-    if (f.v < nv) {
-      int dup;
-      const int o = unit_at<V>(f.r, f.v, S, dup);
-      store<T, V>(dx + o, input_gradient<T, ACT, V>(load<T, V>(x + o), load<T, V>(dy + o), mean, rstd, w[f.r],
-                                                    w[D + f.r], m1, m2));
+  // what was read last is still in a cache
+  const int begun = far.ri * far.accesses + far.vi, all = (rows + far.step_r - 1) / far.step_r * far.accesses;
+  if (begun < all) {
+    at.ri = (rows + far.step_r - 1) / far.step_r - 1;
+    at.vi = far.accesses - 1;
+    for (int left = all - begun; left > 0; left -= kAhead) {
+      Vec<T, V> vx[kAhead], vdy[kAhead];
+      auto ahead = at;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        int dup;
+        const int r = ahead.r(), v = ahead.v();
+        if (k < left && r < rows && v < nv) {
+          const int o = unit_at<V>(r, v, S, dup);
+          vx[k] = load<T, V>(x + o);
+          vdy[k] = load<T, V>(dy + o);
+        }
+        ahead.back();
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        int dup;
+        const int r = at.r(), v = at.v();
+        if (k < left && r < rows && v < nv)
+          store<T, V>(dx + unit_at<V>(r, v, S, dup),
+                      input_gradient<T, ACT, V>(vx[k], vdy[k], mean, rstd, w[r], w[D + r], m1, m2), p.once);
+        at.back();
+      }
     }
   }
-  at = RowCursor(tid, THREADS, lpr, nv);
+  at = first;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     int dup;
-    if (at.r < rows && at.v < nv) {
-      const int o = unit_at<V>(at.r, at.v, S, dup);
-      store<T, V>(dx + o,
-                  input_gradient<T, ACT, V>(hx[k], hdy[k], mean, rstd, w[at.r], w[D + at.r], m1, m2));
-    }
+    const int r = at.r(), v = at.v();
+    if (r < rows && v < nv)
+      store<T, V>(dx + unit_at<V>(r, v, S, dup),
+                  held_input_gradient<T, ACT, V>(hx[k], hdy[k], mean, rstd, w[r], w[D + r], m1, m2), p.once);
     at.next();
   }
 }
@@ -414,10 +495,21 @@ __global__ __launch_bounds__(kSplitThreads) void planes_row_sums_kernel(GroupNor
   const float w = load_param(p.weight, p.param_dtype, c, 1.0f), bias = load_param(p.bias, p.param_dtype, c, 0.0f);
   const long begin = k * slice, end = begin + slice < nv ? begin + slice : nv;
   float sa = 0.0f, sb = 0.0f;
-  for (long v = begin + threadIdx.x; v < end; v += kSplitThreads) {
-    int dup;
-    const long o = unit_at<V>(0l, v, S, dup);
-    add_gradient<T, ACT, V>(load<T, V>(x + o), load<T, V>(dy + o), dup, mean, rstd, w, bias, sa, sb);
+  for (long v = begin + threadIdx.x; v < end; v += kAhead * kSplitThreads) {
+    Vec<T, V> vx[kAhead], vdy[kAhead];
+    int dup[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const long u = v + k * kSplitThreads, o = unit_at<V>(0l, u, S, dup[k]);
+      if (u < end) {
+        vx[k] = load<T, V>(x + o);
+        vdy[k] = load<T, V>(dy + o);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (v + k * kSplitThreads < end)
+        add_gradient<T, ACT, V>(vx[k], vdy[k], dup[k], mean, rstd, w, bias, sa, sb);
   }
   double a = sa, d = sb;
   thread_sum<kSplitThreads>(a, d, part);
@@ -436,46 +528,27 @@ __global__ __launch_bounds__(kSplitThreads) void planes_input_gradient_kernel(Gr
   const float w = load_param(p.weight, p.param_dtype, c, 1.0f), bias = load_param(p.bias, p.param_dtype, c, 0.0f);
   const float2 m = means[bg];
   const long begin = k * slice, end = begin + slice < nv ? begin + slice : nv;
-  for (long v = begin + threadIdx.x; v < end; v += kSplitThreads) {
-    int dup;
-    const long o = unit_at<V>(0l, v, S, dup);
-    store<T, V>(dx + o,
-                input_gradient<T, ACT, V>(load<T, V>(x + o), load<T, V>(dy + o), mean, rstd, w, bias, m.x, m.y));
+  for (long v = begin + threadIdx.x; v < end; v += kAhead * kSplitThreads) {
+    Vec<T, V> vx[kAhead], vdy[kAhead];
+    long o[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      int dup;
+      const long u = v + k * kSplitThreads;
+      o[k] = unit_at<V>(0l, u, S, dup);
+      if (u < end) {
+        vx[k] = load<T, V>(x + o[k]);
+        vdy[k] = load<T, V>(dy + o[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (v + k * kSplitThreads < end)
+        store<T, V>(dx + o[k], input_gradient<T, ACT, V>(vx[k], vdy[k], mean, rstd, w, bias, m.x, m.y), p.once);
   }
 }
 
 // ---- choice -----------------------------------------------------------------------
-
-// Whether rows are taken V values at a time; shorter ones go value by value.
-template <typename T>
-bool whole_accesses(const GroupNormParams& p) {
-  return p.S >= kVec<T>;
-}
-
-long accesses(const GroupNormParams& p) {
-  const long V = p.dtype == OAA_FLOAT32 ? 4 : 8;
-  return p.S >= V ? (p.S + V - 1) / V : p.S;
-}
-
-// Workgroups that the sliced kernels aim for.
-constexpr long kSlices = 2048;
-// Most channels of a group whose parameters a workgroup keeps.
-constexpr int kMostRows = 2048;
-
-// Whether a group goes to one workgroup. The alternative is to slice groups
-// over the device, which reads everything twice and takes one launch more.
-bool group_per_workgroup(const GroupNormParams& p) {
-  const long units = p.D * accesses(p), groups = long(p.B) * p.G;
-  if (p.D > kMostRows || double(p.D) * p.S > double(1 << 30)) return false;
-  return units <= 16384 || groups >= 192;
-}
-
-// `rows` of `units` each in about kSlices slices of 1024 units or more.
-NormCut sliced(long rows, long units) {
-  long slice = (units * rows + kSlices - 1) / kSlices;
-  slice = (slice + 1023) / 1024 * 1024;
-  return {true, slice, (units + slice - 1) / slice};
-}
 
 template <typename T, int ACT, int V, int THREADS, int NV>
 hipError_t forward_groups(const GroupNormParams& p, hipStream_t s) {
@@ -492,32 +565,14 @@ hipError_t forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s) 
   if (!cut.split) {
     if (units <= 64 * 4) return forward_groups<T, ACT, V, 64, 4>(p, s);
     if (units <= 256 * 4) return forward_groups<T, ACT, V, 256, 4>(p, s);
-    if (units <= 256 * 16) return forward_groups<T, ACT, V, 256, 16>(p, s);
-    return forward_groups<T, ACT, V, 1024, 16>(p, s);
+    if (units <= 512 * 8) return forward_groups<T, ACT, V, 512, 8>(p, s);
+    return forward_groups<T, ACT, V, 1024, 12>(p, s);
   }
   double2* sums = reinterpret_cast<double2*>(p.ws);
   const unsigned blocks = unsigned(cut.count * groups);
   planes_moments_kernel<T, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), sums);
   planes_apply_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), sums);
   return hipGetLastError();
-}
-
-// Lanes of a row (log2): the fewest steps for all rows, and of those the
-// longest runs.
-int row_lanes(const GroupNormParams& p, int threads, long nv) {
-  int best = 0;
-  long least = -1;
-  for (int lpr = 0; (1 << lpr) <= threads; ++lpr) {
-    const int rows = threads >> lpr;
-    const long wpr = lpr > 6 ? 1 << (lpr - 6) : 1;
-    if ((2 + 2 * wpr) * p.D * 4 > 49152) continue;
-    const long steps = ((p.D + rows - 1) / rows) * ((nv + (1 << lpr) - 1) >> lpr);
-    if (least < 0 || steps <= least) {
-      least = steps;
-      best = lpr;
-    }
-  }
-  return best;
 }
 
 template <typename T, int ACT, int V, int THREADS, int NV>
@@ -537,8 +592,8 @@ hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums
   if (!cut.split) {
     if (units <= 64 * 4) return backward_groups<T, ACT, V, 64, 4>(p, at.sums, s);
     if (units <= 256 * 4) return backward_groups<T, ACT, V, 256, 4>(p, at.sums, s);
-    if (units <= 256 * 8) return backward_groups<T, ACT, V, 256, 8>(p, at.sums, s);
-    return backward_groups<T, ACT, V, 1024, 8>(p, at.sums, s);
+    if (units <= 256 * 12) return backward_groups<T, ACT, V, 256, 12>(p, at.sums, s);
+    return backward_groups<T, ACT, V, 1024, 6>(p, at.sums, s);
   }
   const unsigned blocks = unsigned(cut.count * p.B * p.C);
   planes_row_sums_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at.sums);
@@ -550,41 +605,19 @@ hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums
 
 }  // namespace
 
-NormCut planes_forward_cut(const GroupNormParams& p) {
-  if (group_per_workgroup(p)) return {false, 0, 1};
-  return sliced(long(p.B) * p.G, p.D * accesses(p));
-}
-
-size_t planes_forward_ws(const GroupNormParams& p, const NormCut& cut) {
-  return cut.split ? align_workspace(sizeof(double2) * p.B * p.G * cut.count) : 0;
-}
-
-NormCut planes_backward_cut(const GroupNormParams& p) {
-  if (group_per_workgroup(p)) return {false, 0, 1};
-  return sliced(long(p.B) * p.C, accesses(p));
-}
-
-NormSums planes_sums(const GroupNormParams& p, const NormCut& cut) {
-  return {nullptr, nullptr, cut.count, p.C * cut.count, cut.count, 1};
-}
-
+template <typename T>
 hipError_t launch_planes_forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s) {
-  return for_type(p.dtype, [&](auto t) {
-    using T = typename decltype(t)::type;
-    return for_act(p.act, [&](auto a) {
-      constexpr int A = decltype(a)::value;
-      return whole_accesses<T>(p) ? forward<T, A, kVec<T>>(p, cut, s) : forward<T, A, 1>(p, cut, s);
-    });
+  return for_act(p.act, [&](auto a) {
+    constexpr int A = decltype(a)::value;
+    return whole_accesses(p) ? forward<T, A, kVec<T>>(p, cut, s) : forward<T, A, 1>(p, cut, s);
   });
 }
 
+template <typename T>
 hipError_t launch_planes_backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s) {
-  return for_type(p.dtype, [&](auto t) {
-    using T = typename decltype(t)::type;
-    return for_act(p.act, [&](auto a) {
-      constexpr int A = decltype(a)::value;
-      return whole_accesses<T>(p) ? backward<T, A, kVec<T>>(p, cut, at, s) : backward<T, A, 1>(p, cut, at, s);
-    });
+  return for_act(p.act, [&](auto a) {
+    constexpr int A = decltype(a)::value;
+    return whole_accesses(p) ? backward<T, A, kVec<T>>(p, cut, at, s) : backward<T, A, 1>(p, cut, at, s);
   });
 }
 
