@@ -111,11 +111,10 @@ class GroupNormFunction(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x, weight, bias, mean, rstd = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        dy = _laid_out(dy, binding._norm_layout(x, "x")[0])
-        dx, dweight, dbias = binding.group_norm_backward(dy, x, ctx.num_groups, weight, bias, mean, rstd,
-                                                         ctx.activation, need[0], need[1], need[2])
-        return dx, dweight, dbias, None, None, None
+        if dy.stride() != x.stride():
+            dy = _laid_out(dy, binding._norm_layout(x, "x")[0])
+        return (*binding.group_norm_backward(dy, x, ctx.num_groups, weight, bias, mean, rstd, ctx.activation,
+                                             *ctx.needs_input_grad[:3]), None, None, None)
 
 
 def group_norm(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none"):
@@ -123,7 +122,8 @@ def group_norm(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none
     channels, with weight[C] and bias[C], then the activation ("none", "relu",
     "silu", "gelu"). x is float32, bfloat16 or float16 in planes or channels
     last, and y like it; parameters are float32 or of x's type."""
-    x = _laid_out(x)
+    if not x.is_contiguous():
+        x = _laid_out(x)
     if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
                                     (bias is not None and bias.requires_grad)):
         return GroupNormFunction.apply(x, weight, bias, num_groups, eps, activation)

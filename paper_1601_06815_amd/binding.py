@@ -8,7 +8,6 @@ is missing, ``load()`` raises.
 """
 
 import array
-import contextlib
 import ctypes
 import functools
 import math
@@ -403,37 +402,52 @@ class Plan:
 
 # ---- group normalisation and gradients of torch tensors ------------------------
 
+@functools.lru_cache(maxsize=None)
 def _dtype_codes():
     import torch
     return {torch.float32: FLOAT32, torch.bfloat16: BFLOAT16, torch.float16: FLOAT16}
 
 
-_dtype_codes = functools.lru_cache(maxsize=None)(_dtype_codes)
-
-
-def _on_device(index):
-    """The raw current stream of device `index`, and a context in which that
-    device is current (kernels are launched on the current device)."""
+@functools.lru_cache(maxsize=None)
+def _torch():
+    """torch, and its calls for the current device and its raw stream."""
     import torch
-    guard = _NO_GUARD if torch.cuda.current_device() == index else torch.cuda.device(index)
-    return torch._C._cuda_getCurrentRawStream(index), guard
+    return torch, torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
 
 
-_NO_GUARD = contextlib.nullcontext()
+def _launch(fn, index, *args):
+    """fn(*args, stream) on the current stream of device `index`, with that
+    device current: kernels are launched there."""
+    torch, current_device, raw_stream = _torch()
+    if current_device() == index:
+        status = fn(*args, raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, raw_stream(index))
+    if status != OAA_OK:
+        _check(status)
 
 
-def _norm_layout(t, name, want=None):
-    """(layout, S, image stride, row stride) of t[B, C, ...], in planes or channels
-    last with any strides between positions and images; `want`: only this
-    layout will do (one position or one channel is both)."""
-    shape = t.shape
+def _is_dense(shape, strides):
+    expect = 1
+    for k, st in zip(reversed(shape), reversed(strides)):
+        if k != 1:
+            if st != expect:
+                return math.prod(shape) == 0
+            expect *= k
+    return True
+
+
+def _layout_of(shape, strides, name, want=None):
+    """(layout, S, image stride, row stride) of a tensor [B, C, ...], in planes or
+    channels last with any strides between positions and images; `want`: only
+    this layout will do (one position or one channel is both)."""
     if len(shape) < 2:
         raise ValueError(f"{name} must have shape [B, C, ...], got {tuple(shape)}")
     C = shape[1]
     S = math.prod(shape[2:])
-    if want != LAYOUT_CHANNELS_LAST and t.is_contiguous():
+    if want != LAYOUT_CHANNELS_LAST and _is_dense(shape, strides):
         return LAYOUT_PLANES, S, C * S, S
-    strides = t.stride()
     # the positions' dimensions as one: row-major with one step between neighbours
     step = expect = None
     for k, st in zip(reversed(shape[2:]), reversed(strides[2:])):
@@ -453,76 +467,88 @@ def _norm_layout(t, name, want=None):
     raise ValueError(f"{name}: strides {strides} of {tuple(shape)} are not {kind}")
 
 
-@functools.lru_cache(maxsize=1024)
-def _group_norm_desc(B, C, G, S, layout, dtype, param_dtype, activation, eps, x, y, dy, dx):
-    """A description for these sizes (its address and what keeps it), and the
-    workspace bytes of the two passes."""
-    d = GroupNormDesc(B, C, G, S, layout, dtype, param_dtype, activation, eps, Strides(*x), Strides(*y), Strides(*dy),
-                      Strides(*dx))
-    return (ctypes.addressof(d), d, oaa_group_norm_workspace_bytes(d, False),
-            oaa_group_norm_workspace_bytes(d, True))
+def _norm_layout(t, name, want=None):
+    return _layout_of(t.shape, t.stride(), name, want)
 
 
-def _group_norm_args(x, num_groups, weight, bias, activation):
-    codes = _dtype_codes()
-    if not x.is_cuda or x.dtype not in codes:
+class _NormCall:
+    """What a call works out from shapes, strides and types alone: the checks of
+    them, the description and the workspaces' sizes."""
+
+    def __init__(self, shape, strides, y_strides, dy_strides, dtype, weight, bias, G, eps, activation):
+        codes = _dtype_codes()
+        if dtype not in codes:
+            raise ValueError(f"x must be a float32, bfloat16 or float16 tensor on the GPU, got {dtype}")
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
+        self.layout, S, image, row = _layout_of(shape, strides, "x")
+        param = dtype if weight is None and bias is None else (weight or bias)[0]
+        for name, p in (("weight", weight), ("bias", bias)):
+            if p is None:
+                continue
+            if p[0] != param or p[0] not in codes:
+                raise ValueError(f"{name} must be of the other parameter's type, got {p[0]}")
+            if tuple(p[1]) != (shape[1],):
+                raise ValueError(f"{name} has shape {tuple(p[1])}, expected ({shape[1]},)")
+        # a dense tensor like x is what torch.empty_like makes, unless x has gaps
+        self.gaps = (image, row) != (shape[1] * S, S if self.layout == LAYOUT_PLANES else shape[1])
+        out, dy = ((0, 0) if st is None else _layout_of(shape, st, name, self.layout)[2:]
+                   for name, st in (("y", y_strides), ("dy", dy_strides)))
+        self.desc = GroupNormDesc(shape[0], shape[1], G, S, self.layout, codes[dtype], codes[param],
+                                  ACTIVATIONS[activation], eps, Strides(image, row), Strides(*out), Strides(*dy),
+                                  Strides(0, 0))
+        self.address = ctypes.addressof(self.desc)
+        self.forward_bytes = oaa_group_norm_workspace_bytes(self.desc, False)
+        self.backward_bytes = oaa_group_norm_workspace_bytes(self.desc, True)
+
+
+_norm_call = functools.lru_cache(maxsize=4096)(_NormCall)
+
+
+def _device_of(x, weight, bias):
+    """The index of the one device that all are on."""
+    index = x.get_device()
+    if index < 0:
         raise ValueError(f"x must be a float32, bfloat16 or float16 tensor on the GPU, got {x.dtype} on {x.device}")
-    if activation not in ACTIVATIONS:
-        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
-    param = x.dtype if weight is None and bias is None else (weight if weight is not None else bias).dtype
-    C = x.shape[1] if x.dim() > 1 else 0
     for name, t in (("weight", weight), ("bias", bias)):
-        if t is None:
-            continue
-        if t.dtype != param or t.dtype not in codes or t.device != x.device or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous, on {x.device}, and of the other parameter's type")
-        if t.dim() != 1 or t.shape[0] != C:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({C},)")
-    return codes[x.dtype], codes[param]
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous and on {x.device}")
+    return index
 
 
-def _like(x, layout):
-    """A dense tensor of x's shape in the layout."""
-    import torch
-    if layout == LAYOUT_PLANES:
+def _like(x, call):
+    """A dense tensor of x's shape in its layout."""
+    torch = _torch()[0]
+    if not call.gaps:
+        return torch.empty_like(x)
+    if call.layout == LAYOUT_PLANES:
         return torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if x.dim() == 4:
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device, memory_format=torch.channels_last)
     return torch.empty((x.shape[0], *x.shape[2:], x.shape[1]), dtype=x.dtype, device=x.device).movedim(-1, 1)
-
-
-def _matching(t, x, layout, name):
-    """Image and row strides of t, which has x's shape, type, device and layout."""
-    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
-        raise ValueError(f"{name} must be a {x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
-    return _norm_layout(t, name, layout)[2:]
 
 
 def group_norm_forward(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none", y=None, stats=True):
     """oaa_group_norm_forward on torch's current stream of x's device: (y, mean,
     rstd), the last two [B, G] float32 (None without ``stats``). x[B, C, ...]
     is laid out in planes or channels last, and so is y."""
-    import torch
-    dtype, param = _group_norm_args(x, num_groups, weight, bias, activation)
-    layout, S, image, row = _norm_layout(x, "x")
-    B, C = x.shape[0], x.shape[1]
+    torch = _torch()[0]
+    index = _device_of(x, weight, bias)
+    if y is not None and (y.shape != x.shape or y.dtype != x.dtype or y.get_device() != index):
+        raise ValueError(f"y must be a {x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
+    call = _norm_call(x.shape, x.stride(), None if y is None else y.stride(), None, x.dtype,
+                      None if weight is None else (weight.dtype, weight.shape),
+                      None if bias is None else (bias.dtype, bias.shape), num_groups, eps, activation)
     if y is None:
-        y, out = _like(x, layout), (0, 0)
-    else:
-        out = _matching(y, x, layout, "y")
-    desc, _, need, _ = _group_norm_desc(B, C, num_groups, S, layout, dtype, param, ACTIVATIONS[activation], eps,
-                                        (image, row), out, (0, 0), (0, 0))
-    device = x.device
-    mean = rstd = mean_p = rstd_p = None
+        y = _like(x, call)
+    mean = rstd = ws = None
     if stats:
-        mean, rstd = torch.empty((2, B, num_groups), dtype=torch.float32, device=device).unbind(0)
-        mean_p, rstd_p = mean.data_ptr(), rstd.data_ptr()
-    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    stream, guard = _on_device(device.index)
-    with guard:
-        oaa_group_norm_forward(desc, x.data_ptr(), None if weight is None else weight.data_ptr(),
-                               None if bias is None else bias.data_ptr(), y.data_ptr(), mean_p, rstd_p,
-                               None if ws is None else ws.data_ptr(), need, stream)
+        mean = torch.empty((x.shape[0], num_groups), dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+    if call.forward_bytes:
+        ws = torch.empty(call.forward_bytes, dtype=torch.uint8, device=x.device)
+    _launch(load().oaa_group_norm_forward, index, call.address, x.data_ptr(), weight if weight is None else
+            weight.data_ptr(), bias if bias is None else bias.data_ptr(), y.data_ptr(), mean if mean is None else
+            mean.data_ptr(), rstd if rstd is None else rstd.data_ptr(), ws if ws is None else ws.data_ptr(),
+            call.forward_bytes)
     return y, mean, rstd
 
 
@@ -531,29 +557,27 @@ def group_norm_backward(dy, x, num_groups, weight, bias, mean, rstd, activation=
     """oaa_group_norm_backward on torch's current stream of x's device: (dx,
     dweight, dbias), None for each that is not needed or whose parameter is
     None. mean and rstd are the forward pass's."""
-    import torch
-    dtype, param = _group_norm_args(x, num_groups, weight, bias, activation)
-    layout, S, image, row = _norm_layout(x, "x")
-    B, C = x.shape[0], x.shape[1]
+    torch = _torch()[0]
+    index = _device_of(x, weight, bias)
+    if dy.shape != x.shape or dy.dtype != x.dtype or dy.get_device() != index:
+        raise ValueError(f"dy must be a {x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
+    call = _norm_call(x.shape, x.stride(), None, dy.stride(), x.dtype,
+                      None if weight is None else (weight.dtype, weight.shape),
+                      None if bias is None else (bias.dtype, bias.shape), num_groups, 0.0, activation)
+    groups = (x.shape[0], num_groups)
     for name, t in (("mean", mean), ("rstd", rstd)):
-        if t.shape != (B, num_groups) or t.dtype != torch.float32 or t.device != x.device or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {(B, num_groups)} on {x.device}")
-    desc, _, _, need = _group_norm_desc(B, C, num_groups, S, layout, dtype, param, ACTIVATIONS[activation], 0.0,
-                                        (image, row), (0, 0), _matching(dy, x, layout, "dy"), (0, 0))
-    device = x.device
-    dx = _like(x, layout) if need_x else None
+        if t.shape != groups or t.dtype != torch.float32 or t.get_device() != index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {groups} on {x.device}")
+    dx = _like(x, call) if need_x else None
     dweight = torch.empty_like(weight) if need_weight and weight is not None else None
     dbias = torch.empty_like(bias) if need_bias and bias is not None else None
     if dx is None and dweight is None and dbias is None:
         return None, None, None
-    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    stream, guard = _on_device(device.index)
-    with guard:
-        oaa_group_norm_backward(desc, dy.data_ptr(), x.data_ptr(), None if weight is None else weight.data_ptr(),
-                                None if bias is None else bias.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr(),
-                                None if dbias is None else dbias.data_ptr(), None if ws is None else ws.data_ptr(),
-                                need, stream)
+    ws = torch.empty(call.backward_bytes, dtype=torch.uint8, device=x.device) if call.backward_bytes else None
+    _launch(load().oaa_group_norm_backward, index, call.address, dy.data_ptr(), x.data_ptr(), weight if weight is None
+            else weight.data_ptr(), bias if bias is None else bias.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+            dx if dx is None else dx.data_ptr(), dweight if dweight is None else dweight.data_ptr(),
+            dbias if dbias is None else dbias.data_ptr(), ws if ws is None else ws.data_ptr(), call.backward_bytes)
     return dx, dweight, dbias
 
 
@@ -572,42 +596,41 @@ def _dense(t):
     return True
 
 
-def _grad_lists(grads, device):
+def _grad_lists(grads, index):
     """Host arrays of the tensors' addresses, sizes and types."""
     codes = _dtype_codes()
-    kinds = []
+    kinds = [codes.get(t.dtype) for t in grads]
+    if None in kinds or not all(t.get_device() == index for t in grads):
+        i = next(i for i, (t, k) in enumerate(zip(grads, kinds)) if k is None or t.get_device() != index)
+        raise ValueError(f"gradient {i} must be a float32, bfloat16 or float16 tensor on cuda:{index}")
     for i, t in enumerate(grads):
-        if t.dtype not in codes or t.device != device:
-            raise ValueError(f"gradient {i} must be a float32, bfloat16 or float16 tensor on {device}")
-        if not _dense(t):
+        if not t.is_contiguous() and not _dense(t):
             raise ValueError(f"gradient {i} of shape {tuple(t.shape)} has gaps or overlaps (strides {t.stride()})")
-        kinds.append(codes[t.dtype])
     return (array.array("Q", [t.data_ptr() for t in grads]), array.array("q", [t.numel() for t in grads]),
             array.array("i", kinds))
 
 
-def _grad_call(grads, norm_type, device):
-    import torch
+def _grad_call(grads, norm_type):
+    """The device's index, the host arrays, the norm and the workspace of a call."""
+    torch, current_device, _ = _torch()
     if norm_type not in NORM_TYPES:
         raise ValueError(f"norm_type must be one of {sorted(NORM_TYPES)}, got {norm_type!r}")
-    if device is None:
-        device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
-    if device.type != "cuda":
-        raise ValueError(f"gradients must be on the GPU, not on {device}")
-    need = oaa_grad_workspace_bytes(len(grads))
-    return (device, _grad_lists(grads, device), torch.empty((), dtype=torch.float32, device=device),
-            torch.empty(need, dtype=torch.uint8, device=device))
+    index = grads[0].get_device() if grads else current_device()
+    if index < 0:
+        raise ValueError(f"gradients must be on the GPU, not on {grads[0].device}")
+    lists = _grad_lists(grads, index)
+    device = torch.device("cuda", index)
+    return (index, lists, torch.empty((), dtype=torch.float32, device=device),
+            torch.empty(oaa_grad_workspace_bytes(len(grads)), dtype=torch.uint8, device=device))
 
 
 def grad_norm(grads, norm_type=2.0):
     """oaa_grad_norm on torch's current stream: the norm over all values of the
     tensors, a float32 scalar on their device. norm_type: 1, 2 or infinity."""
     grads = list(grads)
-    device, (src, sizes, kinds), norm, ws = _grad_call(grads, norm_type, None)
-    stream, guard = _on_device(device.index)
-    with guard:
-        oaa_grad_norm(len(grads), src.buffer_info()[0], sizes.buffer_info()[0], kinds.buffer_info()[0],
-                      NORM_TYPES[norm_type], norm.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    index, (src, sizes, kinds), norm, ws = _grad_call(grads, norm_type)
+    _launch(load().oaa_grad_norm, index, len(grads), src.buffer_info()[0], sizes.buffer_info()[0],
+            kinds.buffer_info()[0], NORM_TYPES[norm_type], norm.data_ptr(), ws.data_ptr(), ws.numel())
     return norm
 
 
@@ -616,19 +639,17 @@ def grad_clip(grads, max_norm, norm_type=2.0, out=None):
     max_norm / (norm + 1e-6)), in place or into ``out`` (tensors of the same
     shapes, types and strides). Returns the norm before clipping."""
     grads = list(grads)
-    device, (src, sizes, kinds), norm, ws = _grad_call(grads, norm_type, None)
+    index, (src, sizes, kinds), norm, ws = _grad_call(grads, norm_type)
     dst = src
     if out is not None:
         out = list(out)
         if len(out) != len(grads):
             raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
         for i, (g, o) in enumerate(zip(grads, out)):
-            if o.dtype != g.dtype or o.device != device or o.shape != g.shape or o.stride() != g.stride():
+            if o.dtype != g.dtype or o.get_device() != index or o.shape != g.shape or o.stride() != g.stride():
                 raise ValueError(f"output {i} differs from its gradient in shape, strides, type or device")
         dst = array.array("Q", [t.data_ptr() for t in out])
-    stream, guard = _on_device(device.index)
-    with guard:
-        oaa_grad_clip(len(grads), src.buffer_info()[0], dst.buffer_info()[0], sizes.buffer_info()[0],
-                      kinds.buffer_info()[0], NORM_TYPES[norm_type], max_norm, norm.data_ptr(), ws.data_ptr(),
-                      ws.numel(), stream)
+    _launch(load().oaa_grad_clip, index, len(grads), src.buffer_info()[0], dst.buffer_info()[0],
+            sizes.buffer_info()[0], kinds.buffer_info()[0], NORM_TYPES[norm_type], max_norm, norm.data_ptr(),
+            ws.data_ptr(), ws.numel())
     return norm
