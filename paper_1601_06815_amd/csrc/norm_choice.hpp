@@ -34,18 +34,35 @@ inline long accesses(const GroupNormParams& p) {
 // Most channels of a group whose parameters a workgroup keeps.
 constexpr int kMostRows = 2048;
 
-// Whether a group goes to one workgroup. The alternative is to slice groups
-// over the device, which reads everything twice and takes one launch more.
-inline bool group_per_workgroup(const GroupNormParams& p) {
-  const long units = p.D * accesses(p), groups = long(p.B) * p.G;
-  if (p.D > kMostRows || double(p.D) * p.S > double(1 << 30)) return false;
-  return units <= 16384 || groups >= 192;
+// Whether a workgroup can hold a group's parameters and address its values with
+// 32 bits.
+inline bool one_workgroup_can(const GroupNormParams& p) {
+  return p.D <= kMostRows && double(p.D) * p.S <= double(1 << 30);
 }
 
-// `rows` of `units` each in about kSlices slices of 1024 units or more.
-inline NormCut sliced(long rows, long units) {
-  long slice = (units * rows + kSlices - 1) / kSlices;
-  slice = (slice + 1023) / 1024 * 1024;
+// Whether a group goes to one workgroup, forward. The alternative, slices of
+// groups over the device, reads everything twice in two launches. Measured, us,
+// one workgroup first (float32, D = 8, SiLU): 4 groups of 64 KB 5.6 / 8.4, of 128
+// KB 8.8 / 8.4, of 256 KB 14.0 / 8.6; 128 groups of 128 KB 10.8 / 14.4, of 256 KB
+// 18.7 / 21.8; 1024 groups of 399 KB 195 / 260.
+inline bool forward_one_workgroup(const GroupNormParams& p) {
+  return one_workgroup_can(p) && (p.D * accesses(p) <= 6144 || long(p.B) * p.G >= 128);
+}
+
+// Backward. The alternative takes one launch more, but its lanes are not bound
+// by one compute unit's arithmetic; it loses where x and dy, read twice, leave
+// the caches. Measured (the same): 4 groups of 8 KB 8.8 / 8.3, of 32 KB 14.6 /
+// 9.5, of 256 KB 28 / 9.5; 256 groups of 8 KB 9.2 / 9.5, of 64 KB 18.6 / 17.7, of
+// 128 KB 29.8 / 33.3, of 256 KB 47 / 57; 1024 groups of 399 KB 305 / 400.
+inline bool backward_one_workgroup(const GroupNormParams& p) {
+  const long units = p.D * accesses(p), groups = long(p.B) * p.G;
+  return one_workgroup_can(p) && (units <= 512 || (groups >= 192 && units * groups > 5 << 18));
+}
+
+// `rows` of `units` each in about `most` slices, each a multiple of `least` units.
+inline NormCut sliced(long rows, long units, long most, long least) {
+  long slice = (units * rows + most - 1) / most;
+  slice = (slice + least - 1) / least * least;
   return {true, slice, (units + slice - 1) / slice};
 }
 
@@ -68,8 +85,8 @@ inline int row_lanes(const GroupNormParams& p, int threads, long nv) {
 }
 
 inline NormCut planes_forward_cut(const GroupNormParams& p) {
-  if (group_per_workgroup(p)) return {false, 0, 1};
-  return sliced(long(p.B) * p.G, p.D * accesses(p));
+  if (forward_one_workgroup(p)) return {false, 0, 1};
+  return sliced(long(p.B) * p.G, p.D * accesses(p), kSlices, kSplitThreads * kAhead);
 }
 
 inline size_t planes_forward_ws(const GroupNormParams& p, const NormCut& cut) {
@@ -77,8 +94,8 @@ inline size_t planes_forward_ws(const GroupNormParams& p, const NormCut& cut) {
 }
 
 inline NormCut planes_backward_cut(const GroupNormParams& p) {
-  if (group_per_workgroup(p)) return {false, 0, 1};
-  return sliced(long(p.B) * p.C, accesses(p));
+  if (backward_one_workgroup(p)) return {false, 0, 1};
+  return sliced(long(p.B) * p.C, accesses(p), kSlices * (kSplitThreads / 64), 64 * kAhead);
 }
 
 inline NormSums planes_sums(const GroupNormParams& p, const NormCut& cut) {
@@ -99,10 +116,10 @@ inline int vector_of(const GroupNormParams& p) {
   return p.C >= V ? V : 1;
 }
 
-// Slabs of an image where a slab goes to one workgroup: whole groups, 128 bytes
-// of a row (a line) or more, fewer where workgroups would be few.
+// Slabs of an image where a slab goes to one workgroup: whole groups, a line of
+// a row or more, less where workgroups would be fewer than 256.
 inline int whole_slabs(const GroupNormParams& p) {
-  const long row = long(p.D) * long(dtype_size(p.dtype)), total = long(p.B) * p.G;
+  const long total = long(p.B) * p.G, row = long(p.D) * long(dtype_size(p.dtype));
   long q = (128 + row - 1) / row;
   if (total < 256 * q) q = std::max(std::max<long>(1, total / 256), (long(vector_of(p)) + p.D - 1) / p.D);
   return int(std::max<long>(1, p.G / q));
@@ -124,11 +141,24 @@ inline long row_slice(const GroupNormParams& p, long slices) {
   return (slice + lanes * kAhead - 1) / (lanes * kAhead) * (lanes * kAhead);
 }
 
-// Whether a slab goes to one workgroup. The alternative reads everything twice
-// and takes two launches more.
-inline NormCut cut_rows(const GroupNormParams& p, int threads, int rows) {
-  const int slabs = whole_slabs(p);
-  if (holds(p, slabs, threads, rows) && (long(p.B) * slabs >= 128 || p.S <= 1024)) return {false, 0, slabs};
+// Whether a slab goes to one workgroup. The alternative, slices of rows, reads
+// everything twice in two launches more. Measured, us, one workgroup first
+// (SiLU, D = 8 and S up to 8192 positions, slabs of one group up to 256 groups),
+// forward in float32: 16 groups of 64 KB 8.8 / 10.6, of 128 KB 12.4 / 10.7; 128
+// groups of 128 KB 16.4 / 18.1; 256 groups of 256 KB 74 / 40; 4096 groups of 24
+// KB 44 / 58. Backward in bfloat16: 16 groups of 32 KB 15.5 / 15.2, of 64 KB 20.5
+// / 15.2; 128 groups of 64 KB 22.6 / 22.7, of 128 KB 39 / 31; 256 groups of 128
+// KB 45 / 50; 4096 groups of 12 KB 56 / 90.
+inline NormCut cut_rows(const GroupNormParams& p, bool backward) {
+  const int slabs = whole_slabs(p), step = backward ? 1 : 2;
+  const long total = long(p.B) * p.G, width = (p.G + slabs - 1) / slabs * p.D;
+  const long most = total < 128    ? 32768 * step
+                    : total < 256  ? 65536 * step
+                    : total < 1024 ? 131072
+                                   : 1l << 30;
+  const bool fits = backward ? holds(p, slabs, kBackwardThreads, kBackwardRows)
+                             : holds(p, slabs, kForwardThreads, kForwardRows);
+  if (fits && p.S * width * long(dtype_size(p.dtype)) <= most) return {false, 0, slabs};
   const long slice = row_slice(p, kSlices);
   return {true, slice, (p.S + slice - 1) / slice};
 }
@@ -136,7 +166,7 @@ inline NormCut cut_rows(const GroupNormParams& p, int threads, int rows) {
 // Parts of a group's moments.
 inline long parts(const GroupNormParams& p, const NormCut& cut) { return cut.count * split_slabs(p.C, vector_of(p)); }
 
-inline NormCut last_forward_cut(const GroupNormParams& p) { return cut_rows(p, kForwardThreads, kForwardRows); }
+inline NormCut last_forward_cut(const GroupNormParams& p) { return cut_rows(p, false); }
 
 inline size_t last_forward_ws(const GroupNormParams& p, const NormCut& cut) {
   if (!cut.split) return 0;
@@ -144,7 +174,7 @@ inline size_t last_forward_ws(const GroupNormParams& p, const NormCut& cut) {
          align_workspace(2 * sizeof(float) * p.B * p.G);
 }
 
-inline NormCut last_backward_cut(const GroupNormParams& p) { return cut_rows(p, kBackwardThreads, kBackwardRows); }
+inline NormCut last_backward_cut(const GroupNormParams& p) { return cut_rows(p, true); }
 
 inline NormSums last_sums(const GroupNormParams& p, const NormCut& cut) {
   const long count = cut.split ? cut.count : 1;

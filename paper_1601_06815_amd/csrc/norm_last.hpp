@@ -22,6 +22,7 @@
 #include <algorithm>
 
 #include "norm_common.hpp"
+#include "tile_common.hpp"
 
 namespace oaa {
 namespace {
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_forward_ke
   __shared__ double2 entries[kSlabs][THREADS * V];
   __shared__ float2 stats[kSlabs][kMostGroups];
   const int sub = threadIdx.x / THREADS, tid = threadIdx.x % THREADS;
-  const long slab = long(blockIdx.x) * kSlabs + sub;
+  const long slab = long(tile::xcd_local_order(blockIdx.x, gridDim.x)) * kSlabs + sub;
   const bool active = slab < long(p.B) * slabs;
   const long b = active ? slab / slabs : 0;
   const int j = active ? int(slab - b * slabs) : 0;
@@ -377,7 +378,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_backward_k
   __shared__ float2 columns[kSlabs][THREADS * V];
   __shared__ float2 means[kSlabs][kMostGroups];
   const int sub = threadIdx.x / THREADS, tid = threadIdx.x % THREADS;
-  const long slab = long(blockIdx.x) * kSlabs + sub;
+  const long slab = long(tile::xcd_local_order(blockIdx.x, gridDim.x)) * kSlabs + sub;
   const bool active = slab < long(p.B) * slabs;
   const long b = active ? slab / slabs : 0;
   const int j = active ? int(slab - b * slabs) : 0;

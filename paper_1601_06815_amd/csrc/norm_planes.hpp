@@ -482,68 +482,81 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void planes_backward
   }
 }
 
-// Few large groups: `count` slices of each row (channel c of image b).
+// Few large groups: `count` slices of each row (channel c of image b), one wave
+// a slice.
+struct RowSlice {
+  long bc, b, c, bg, begin, end;
+  bool active;
+  __device__ __forceinline__ RowSlice(const GroupNormParams& p, long nv, long slice, int count) {
+    const long i = long(blockIdx.x) * (kSplitThreads / 64) + threadIdx.x / 64;
+    bc = i / count;
+    active = bc < long(p.B) * p.C;
+    if (!active) bc = 0;
+    b = bc / p.C;
+    c = bc - b * p.C;
+    bg = b * p.G + c / p.D;
+    begin = (i - i / count * count) * slice;
+    end = !active ? 0 : begin + slice < nv ? begin + slice : nv;
+  }
+};
+
 template <typename T, int ACT, int V>
 __global__ __launch_bounds__(kSplitThreads) void planes_row_sums_kernel(GroupNormParams p, long slice, int count,
                                                                         float2* sums) {
-  __shared__ double part[2 * kSplitThreads / 64];
   const long S = p.S, nv = (S + V - 1) / V;
-  const long bc = blockIdx.x / count, k = blockIdx.x - bc * count, b = bc / p.C, c = bc - b * p.C, bg = b * p.G + c / p.D;
-  const T* x = static_cast<const T*>(p.x) + b * p.x_image + c * S;
-  const T* dy = static_cast<const T*>(p.dy) + b * p.dy_image + c * S;
-  const float mean = p.mean[bg], rstd = p.rstd[bg];
-  const float w = load_param(p.weight, p.param_dtype, c, 1.0f), bias = load_param(p.bias, p.param_dtype, c, 0.0f);
-  const long begin = k * slice, end = begin + slice < nv ? begin + slice : nv;
+  const RowSlice in(p, nv, slice, count);
+  const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c * S;
+  const T* dy = static_cast<const T*>(p.dy) + in.b * p.dy_image + in.c * S;
+  const float mean = p.mean[in.bg], rstd = p.rstd[in.bg];
+  const float w = load_param(p.weight, p.param_dtype, in.c, 1.0f), bias = load_param(p.bias, p.param_dtype, in.c, 0.0f);
   float sa = 0.0f, sb = 0.0f;
-  for (long v = begin + threadIdx.x; v < end; v += kAhead * kSplitThreads) {
+  for (long v = in.begin + threadIdx.x % 64; v < in.end; v += kAhead * 64) {
     Vec<T, V> vx[kAhead], vdy[kAhead];
     int dup[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const long u = v + k * kSplitThreads, o = unit_at<V>(0l, u, S, dup[k]);
-      if (u < end) {
+      const long u = v + k * 64, o = unit_at<V>(0l, u, S, dup[k]);
+      if (u < in.end) {
         vx[k] = load<T, V>(x + o);
         vdy[k] = load<T, V>(dy + o);
       }
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-      if (v + k * kSplitThreads < end)
-        add_gradient<T, ACT, V>(vx[k], vdy[k], dup[k], mean, rstd, w, bias, sa, sb);
+      if (v + k * 64 < in.end) add_gradient<T, ACT, V>(vx[k], vdy[k], dup[k], mean, rstd, w, bias, sa, sb);
   }
   double a = sa, d = sb;
-  thread_sum<kSplitThreads>(a, d, part);
-  if (threadIdx.x == 0) sums[blockIdx.x] = {float(a), float(d)};
+  lane_sum<64>(a, d);
+  if (in.active && threadIdx.x % 64 == 0) sums[in.bc * count + in.begin / slice] = {float(a), float(d)};
 }
 
 template <typename T, int ACT, int V>
 __global__ __launch_bounds__(kSplitThreads) void planes_input_gradient_kernel(GroupNormParams p, long slice, int count,
                                                                               const float2* means) {
   const long S = p.S, nv = (S + V - 1) / V;
-  const long bc = blockIdx.x / count, k = blockIdx.x - bc * count, b = bc / p.C, c = bc - b * p.C, bg = b * p.G + c / p.D;
-  const T* x = static_cast<const T*>(p.x) + b * p.x_image + c * S;
-  const T* dy = static_cast<const T*>(p.dy) + b * p.dy_image + c * S;
-  T* dx = static_cast<T*>(p.dx) + b * p.dx_image + c * S;
-  const float mean = p.mean[bg], rstd = p.rstd[bg];
-  const float w = load_param(p.weight, p.param_dtype, c, 1.0f), bias = load_param(p.bias, p.param_dtype, c, 0.0f);
-  const float2 m = means[bg];
-  const long begin = k * slice, end = begin + slice < nv ? begin + slice : nv;
-  for (long v = begin + threadIdx.x; v < end; v += kAhead * kSplitThreads) {
+  const RowSlice in(p, nv, slice, count);
+  const T* x = static_cast<const T*>(p.x) + in.b * p.x_image + in.c * S;
+  const T* dy = static_cast<const T*>(p.dy) + in.b * p.dy_image + in.c * S;
+  T* dx = static_cast<T*>(p.dx) + in.b * p.dx_image + in.c * S;
+  const float mean = p.mean[in.bg], rstd = p.rstd[in.bg];
+  const float w = load_param(p.weight, p.param_dtype, in.c, 1.0f), bias = load_param(p.bias, p.param_dtype, in.c, 0.0f);
+  const float2 m = means[in.bg];
+  for (long v = in.begin + threadIdx.x % 64; v < in.end; v += kAhead * 64) {
     Vec<T, V> vx[kAhead], vdy[kAhead];
     long o[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       int dup;
-      const long u = v + k * kSplitThreads;
+      const long u = v + k * 64;
       o[k] = unit_at<V>(0l, u, S, dup);
-      if (u < end) {
+      if (u < in.end) {
         vx[k] = load<T, V>(x + o[k]);
         vdy[k] = load<T, V>(dy + o[k]);
       }
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-      if (v + k * kSplitThreads < end)
+      if (v + k * 64 < in.end)
         store<T, V>(dx + o[k], input_gradient<T, ACT, V>(vx[k], vdy[k], mean, rstd, w, bias, m.x, m.y), p.once);
   }
 }
@@ -595,7 +608,8 @@ hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums
     if (units <= 256 * 12) return backward_groups<T, ACT, V, 256, 12>(p, at.sums, s);
     return backward_groups<T, ACT, V, 1024, 6>(p, at.sums, s);
   }
-  const unsigned blocks = unsigned(cut.count * p.B * p.C);
+  constexpr int kWaves = kSplitThreads / 64;
+  const unsigned blocks = unsigned((cut.count * p.B * p.C + kWaves - 1) / kWaves);
   planes_row_sums_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at.sums);
   if (hipError_t e = launch_norm_join(p, at, s)) return e;
   if (p.dx)
