@@ -114,10 +114,8 @@ GroupNormParams images(const GroupNormParams& p, long first, long count) {
 // Images of one launch.
 long batch(const GroupNormParams& p) { return std::min<long>(p.B, std::max<long>(1, kMostChannels / p.C)); }
 
-// Whether the output does not stay in the last cache (256 MB) beside what else a
-// program touches before it is read.
 bool beyond_caches(const GroupNormParams& p) {
-  return double(p.B) * p.C * p.S * dtype_size(p.dtype) >= 64.0 * (1 << 20);
+  return double(p.B) * p.C * p.S * dtype_size(p.dtype) >= kBeyondCaches;
 }
 
 NormCut forward_cut(const GroupNormParams& p) {

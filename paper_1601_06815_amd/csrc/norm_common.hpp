@@ -104,25 +104,6 @@ __device__ __forceinline__ void statistics(double sum, double sq, double x0, dou
   rstd = float(1.0 / sqrt((var < 0.0 ? 0.0 : var) + double(eps)));  // a NaN is no smaller than 0
 }
 
-template <typename T, int V>
-__device__ __forceinline__ Vec<T, V> load(const T* p) {
-  return *reinterpret_cast<const Vec<T, V>*>(p);
-}
-
-// A store; `once`: of memory too large to be found in a cache when it is read
-// next. Such a store leaves the caches to what the pass reads.
-template <typename T, int V>
-__device__ __forceinline__ void store(T* p, const Vec<T, V>& v, bool once) {
-  if (once) {
-    // the empty statements keep the compiler from making one plain store of both
-    asm volatile("");
-    __builtin_nontemporal_store(v, reinterpret_cast<Vec<T, V>*>(p));
-    asm volatile("");
-  } else {
-    *reinterpret_cast<Vec<T, V>*>(p) = v;
-  }
-}
-
 // dz and xh of one value.
 template <int ACT>
 __device__ __forceinline__ void gradient(float x, float dy, float mean, float rstd, float w, float b, float& dz,

@@ -57,13 +57,15 @@ oaa_status_t check(const Lists& l, oaa_norm_t type, const float* norm, void* ws,
   return OAA_OK;
 }
 
-long long chunks_of(long long size) { return (size + oaa::kGradChunk - 1) / oaa::kGradChunk; }
+long long chunks_of(long long size, int chunk) { return (size + chunk - 1) / chunk; }
 
 // The next batch of tensors from `*next` on that have values. False if there
 // is none.
-bool next_batch(const Lists& l, int* next, GradBatch* t) {
+bool next_batch(const Lists& l, int chunk, bool once, int* next, GradBatch* t) {
   t->count = 0;
+  t->chunk = chunk;
   t->chunks = 0;
+  t->once = once;
   while (*next < l.count && t->count < oaa::kGradBatch) {
     const int i = *next;
     ++*next;
@@ -74,25 +76,39 @@ bool next_batch(const Lists& l, int* next, GradBatch* t) {
     t->size[k] = long(l.sizes[i]);
     t->dtype[k] = (unsigned char)l.dtypes[i];
     t->first[k] = t->chunks;
-    t->chunks += unsigned(chunks_of(l.sizes[i]));
+    t->chunks += unsigned(chunks_of(l.sizes[i], chunk));
   }
   return t->count > 0;
 }
 
-// All partial results of the norm; their number in *parts.
-oaa_status_t partials(const Lists& l, oaa_norm_t type, double* part, int* parts, hipStream_t s) {
-  long long all = 0;
-  for (int i = 0; i < l.count; ++i) all += chunks_of(l.sizes[i]);
-  GradBatch t;
-  *parts = 0;
-  for (int next = 0; next_batch(l, &next, &t);) {
-    // each batch gets its share of the partial results, by its chunks
-    const long long share = all <= oaa::kGradPartials ? t.chunks : (long long)(double(oaa::kGradPartials) * t.chunks / all);
-    const int blocks = int(std::max(1ll, share));
-    if (oaa_status_t st = hip_status(oaa::launch_grad_partials(t, type, part + *parts, blocks, s), "gradient norm"))
-      return st;
-    *parts += blocks;
+// Norm and clipping (where l has outputs).
+oaa_status_t run(const Lists& l, oaa_norm_t type, float max_norm, float* norm, void* ws, hipStream_t s) {
+  long* part = static_cast<long*>(ws);
+  long long few = 0, chunks = 0;
+  double bytes = 0.0;
+  for (int i = 0; i < l.count; ++i) {
+    few += chunks_of(l.sizes[i], oaa::kGradFewChunk);
+    chunks += chunks_of(l.sizes[i], oaa::kGradChunk);
+    bytes += double(l.sizes[i]) * oaa::dtype_size(l.dtypes[i]);
   }
+  GradBatch t;
+  int next = 0;
+  if (few <= oaa::kGradFewChunks && next_batch(l, oaa::kGradFewChunk, false, &next, &t))
+    return hip_status(oaa::launch_grad_few(t, type, l.dst != nullptr, max_norm, norm, s), "gradient norm");
+  int parts = 0;
+  for (next = 0; next_batch(l, oaa::kGradChunk, false, &next, &t);) {
+    // each batch gets its share of the partial results, by its chunks
+    const long long share =
+        chunks <= oaa::kGradPartials ? t.chunks : (long long)(double(oaa::kGradPartials) * t.chunks / chunks);
+    const int blocks = int(std::max(1ll, share));
+    if (oaa_status_t st = hip_status(oaa::launch_grad_partials(t, type, part + parts, blocks, s), "gradient norm"))
+      return st;
+    parts += blocks;
+  }
+  if (!l.dst || parts == 0) return hip_status(oaa::launch_grad_join(part, parts, type, norm, s), "gradient norm");
+  for (next = 0; next_batch(l, oaa::kGradChunk, bytes >= oaa::kBeyondCaches, &next, &t);)
+    if (oaa_status_t st = hip_status(oaa::launch_grad_clip(t, part, parts, type, max_norm, norm, s), "clipping"))
+      return st;
   return OAA_OK;
 }
 
@@ -112,11 +128,7 @@ oaa_status_t oaa_grad_norm(int count, const void* const* grads, const long long*
   const Lists l{count, grads, nullptr, sizes, dtypes};
   if (oaa_status_t st = check(l, type, norm, ws, ws_bytes)) return st;
   (void)hipGetLastError();
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  double* part = static_cast<double*>(ws);
-  int parts = 0;
-  if (oaa_status_t st = partials(l, type, part, &parts, s)) return st;
-  return hip_status(oaa::launch_grad_join(part, parts, type, norm, s), "gradient norm");
+  return run(l, type, 0.0f, norm, ws, static_cast<hipStream_t>(stream));
 }
 
 oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out, const long long* sizes,
@@ -127,16 +139,7 @@ oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out
   if (!(max_norm >= 0.0f)) return fail(OAA_ERR_INVALID_ARG, "max_norm must not be negative");
   if (oaa_status_t st = check(l, type, norm, ws, ws_bytes)) return st;
   (void)hipGetLastError();
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  double* part = static_cast<double*>(ws);
-  int parts = 0;
-  if (oaa_status_t st = partials(l, type, part, &parts, s)) return st;
-  if (parts == 0) return hip_status(oaa::launch_grad_join(part, 0, type, norm, s), "gradient norm");
-  GradBatch t;
-  for (int next = 0; next_batch(l, &next, &t);)
-    if (oaa_status_t st = hip_status(oaa::launch_grad_clip(t, part, parts, type, max_norm, norm, s), "clipping"))
-      return st;
-  return OAA_OK;
+  return run(l, type, max_norm, norm, ws, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

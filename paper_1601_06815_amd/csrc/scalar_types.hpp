@@ -44,6 +44,30 @@ __device__ __forceinline__ void set_element(Vec<T, V>& v, int i, float f) {
     v[i] = T(f);
 }
 
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> load(const T* p) {
+  return *reinterpret_cast<const Vec<T, V>*>(p);
+}
+
+// A store; `once`: of memory too large to be found in a cache when it is read
+// next. Such a store leaves the caches to what the pass reads.
+template <typename T, int V>
+__device__ __forceinline__ void store(T* p, const Vec<T, V>& v, bool once) {
+  if (once) {
+    // the empty statements keep the compiler from making one plain store of both
+    asm volatile("");
+    __builtin_nontemporal_store(v, reinterpret_cast<Vec<T, V>*>(p));
+    asm volatile("");
+  } else {
+    *reinterpret_cast<Vec<T, V>*>(p) = v;
+  }
+}
+
+// Bytes of outputs from which they do not stay in the last cache (256 MB) beside
+// what else a program touches before it reads them. Stored past the caches, large
+// outputs took the next pass's reads from 4.0 to 5.3 TB/s.
+constexpr double kBeyondCaches = 64.0 * (1 << 20);
+
 // One element of a parameter (weight, bias) whose type is known at run time.
 __device__ __forceinline__ float load_param(const void* p, int dtype, long i, float absent) {
   if (!p) return absent;
