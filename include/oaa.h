@@ -348,7 +348,7 @@ typedef struct {
  * invalid description, which the calls refuse. */
 size_t oaa_group_norm_workspace_bytes(const oaa_group_norm_t* d, int backward);
 
-/* y from x. weight or bias NULL: 1 or 0. mean and rstd ([B][G] float32, for
+/* y from x, into memory that does not overlap it. weight or bias NULL: 1 or 0. mean and rstd ([B][G] float32, for
  * the backward pass) may be NULL, each. The workspace (256-byte aligned; NULL
  * if none is needed) holds nothing between calls and is free again once the
  * call's work on `stream` is done. Only enqueues work on the stream; validates
@@ -358,7 +358,7 @@ oaa_status_t oaa_group_norm_forward(const oaa_group_norm_t* d, const void* x, co
                                     void* hip_stream);
 
 /* dx, dweight and dbias from dy, the forward pass's x, weight and bias and its
- * mean and rstd. Each of the three outputs may be NULL (at least one is not).
+ * mean and rstd; no output overlaps an input. Each of the three outputs may be NULL (at least one is not).
  * An empty x gives zeros in dweight and dbias. */
 oaa_status_t oaa_group_norm_backward(const oaa_group_norm_t* d, const void* dy, const void* x, const void* weight,
                                      const void* bias, const float* mean, const float* rstd, void* dx, void* dweight,

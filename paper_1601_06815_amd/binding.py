@@ -477,6 +477,8 @@ class _NormCall:
 
     def __init__(self, shape, strides, y_strides, dy_strides, dtype, weight, bias, G, eps, activation):
         codes = _dtype_codes()
+        if max(shape[:2], default=0) >= 1 << 31:
+            raise ValueError(f"x has shape {tuple(shape)}: images and channels are counted in 32 bits")
         if dtype not in codes:
             raise ValueError(f"x must be a float32, bfloat16 or float16 tensor on the GPU, got {dtype}")
         if activation not in ACTIVATIONS:

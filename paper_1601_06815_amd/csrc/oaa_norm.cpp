@@ -121,6 +121,7 @@ oaa_status_t oaa_group_norm_forward(const oaa_group_norm_t* d, const void* x, co
   if (oaa_status_t st = aligned(mean, OAA_FLOAT32, "mean")) return st;
   if (oaa_status_t st = aligned(rstd, OAA_FLOAT32, "rstd")) return st;
   if (oaa_status_t st = workspace(&p, oaa::group_norm_forward_ws(p), ws, ws_bytes)) return st;
+  if (y == x) return fail(OAA_ERR_INVALID_ARG, "y is x: the input is read again after the first results are written");
   p.x = x;
   p.weight = weight;
   p.bias = bias;
@@ -154,6 +155,8 @@ oaa_status_t oaa_group_norm_backward(const oaa_group_norm_t* d, const void* dy, 
   if (oaa_status_t st = aligned(mean, OAA_FLOAT32, "mean")) return st;
   if (oaa_status_t st = aligned(rstd, OAA_FLOAT32, "rstd")) return st;
   if (oaa_status_t st = workspace(&p, oaa::group_norm_backward_ws(p), ws, ws_bytes)) return st;
+  if (dx && (dx == x || dx == dy))
+    return fail(OAA_ERR_INVALID_ARG, "dx is x or dy: both are read again after the first results are written");
   p.x = x;
   p.dy = dy;
   p.weight = weight;

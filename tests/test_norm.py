@@ -108,6 +108,37 @@ def test_both_passes(gpu_lib, shape, G, layout):
         assert y.stride() == x.stride() and dx.stride() == x.stride()
 
 
+# Sizes at which each kernel takes over: groups of 1 to 4096 and more accesses in
+# one workgroup and in slices, slabs of few and of many rows, groups wider than a
+# slab, more channels of images than a launch takes.
+REACH = [
+    ("planes", (2, 16, 40, 41), 4, torch.float32), ("planes", (3, 8, 97, 97), 2, torch.float32),
+    ("planes", (1, 6, 200, 201), 2, torch.bfloat16), ("planes", (64, 8, 97, 97), 4, torch.float32),
+    ("planes", (100, 8, 61, 61), 4, torch.float32), ("planes", (64, 16, 54, 54), 4, torch.float32),
+    ("planes", (128, 16, 54, 54), 4, torch.float32), ("planes", (200, 16, 72, 73), 4, torch.bfloat16),
+    ("planes", (50, 12, 137, 131), 4, torch.bfloat16), ("planes", (60, 12, 97, 199), 4, torch.float16),
+    ("planes", (1, 4200, 1, 9), 2, torch.float32), ("planes", (40000, 64, 1, 2), 8, torch.float32),
+    ("planes", (3, 20, 1, 5), 5, torch.float16), ("planes", (60, 40, 9, 9), 10, torch.bfloat16),
+    ("planes", (70, 30, 3, 700), 2, torch.float16), ("planes", (200, 6, 5, 7), 2, torch.float32),
+    ("last", (2, 8, 5, 5), 2, torch.float32), ("last", (2, 32, 24, 25), 4, torch.float32),
+    ("last", (300, 32, 28, 28), 4, torch.float32), ("last", (300, 32, 28, 27), 4, torch.bfloat16),
+    ("last", (150, 64, 40, 41), 8, torch.float32), ("last", (150, 64, 50, 51), 8, torch.bfloat16),
+    ("last", (64, 24, 60, 61), 8, torch.float16), ("last", (40, 34, 45, 45), 2, torch.float32),
+    ("last", (2, 5000, 3, 3), 2, torch.float32), ("last", (1, 9000, 2, 3), 1, torch.bfloat16),
+    ("last", (40000, 64, 1, 2), 8, torch.bfloat16), ("last", (2, 3, 70, 71), 1, torch.float32),
+    ("last", (2, 6, 31, 33), 2, torch.float16), ("last", (700, 20, 1, 1), 5, torch.float32),
+    ("last", (4, 200, 90, 91), 200, torch.float16), ("last", (1200, 17, 12, 13), 1, torch.float32),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout,shape,G,dtype", REACH, ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else str(v))
+def test_kernel_choices(gpu_lib, layout, shape, G, dtype):
+    print(layout, shape, G, dtype, flush=True)
+    x, dy, w, b = make(shape, G, layout, dtype, seed=G)
+    check(x, dy, G, w, b, "silu")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
@@ -452,6 +483,13 @@ def test_refused_pointers(lib, args, status):
             binding.oaa_group_norm_backward(desc(), k["dy"], k["x"], None, None, k["mean"], k["rstd"], k["dx"], k["dw"],
                                             None, k["ws"], 1 << 20, None)
         assert e.value.status == 1, bad
+    for alias in (dict(dx=256), dict(dx=512)):
+        with pytest.raises(binding.OaaError, match="dx is") as e:
+            binding.oaa_group_norm_backward(desc(), 256, 512, None, None, 1024, 1024, alias["dx"], None, None, 2048,
+                                            1 << 20, None)
+        assert e.value.status == 1
+    with pytest.raises(binding.OaaError, match="y is x") as e:
+        binding.oaa_group_norm_forward(desc(), 256, None, None, 256, None, None, 2048, 1 << 20, None)
     with pytest.raises(binding.OaaError) as e:
         binding.oaa_group_norm_forward(None, 256, None, None, 256, None, None, 256, 1 << 20, None)
     assert e.value.status == 1
