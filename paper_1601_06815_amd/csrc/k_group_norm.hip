@@ -132,6 +132,10 @@ NormSums sums_layout(const GroupNormParams& p, const NormCut& cut) {
   return p.last ? last_sums(p, cut) : planes_sums(p, cut);
 }
 
+// Whether the kernel that sums writes dweight and dbias: one image, and no other
+// workgroup has a part of a channel. Measured: a launch of 4 us less.
+bool sums_are_final(const GroupNormParams& p, const NormCut& cut) { return p.B == 1 && !cut.split; }
+
 size_t sums_bytes(const GroupNormParams& p, const NormSums& at) {
   return align_workspace(sizeof(float2) * p.B * p.C * at.count);
 }
@@ -156,6 +160,7 @@ size_t group_norm_forward_ws(const GroupNormParams& p) {
 
 size_t group_norm_backward_ws(const GroupNormParams& p) {
   const NormCut cut = backward_cut(p);
+  if (sums_are_final(p, cut)) return 0;
   return sums_bytes(p, sums_layout(p, cut)) + (cut.split ? align_workspace(sizeof(float2) * p.B * p.G) : 0);
 }
 
@@ -179,7 +184,8 @@ hipError_t launch_group_norm_backward(const GroupNormParams& in, hipStream_t s) 
   p.once = beyond_caches(p);
   const NormCut cut = backward_cut(p);
   NormSums all = sums_layout(p, cut);
-  all.sums = reinterpret_cast<float2*>(p.ws);
+  const bool final = sums_are_final(p, cut);
+  all.sums = final ? nullptr : reinterpret_cast<float2*>(p.ws);
   float2* means = cut.split ? reinterpret_cast<float2*>(p.ws + sums_bytes(p, all)) : nullptr;
   // dweight and dbias come with the groups' means where all images do
   const bool one = batch(p) == p.B;
@@ -187,7 +193,7 @@ hipError_t launch_group_norm_backward(const GroupNormParams& in, hipStream_t s) 
     GroupNormParams q = images(p, b, std::min(batch(p), p.B - b));
     if (!one) q.dweight = q.dbias = nullptr;
     NormSums at = all;
-    at.sums += b * at.image;
+    if (at.sums) at.sums += b * at.image;
     at.means = means ? means + b * p.G : nullptr;
     const hipError_t e = for_type(p.dtype, [&](auto t) {
       using T = typename decltype(t)::type;
@@ -195,7 +201,7 @@ hipError_t launch_group_norm_backward(const GroupNormParams& in, hipStream_t s) 
     });
     if (e != hipSuccess) return e;
   }
-  return one && cut.split ? hipSuccess : launch_norm_join(p, all, s);
+  return final || (one && cut.split) ? hipSuccess : launch_norm_join(p, all, s);
 }
 
 hipError_t launch_group_norm_no_images(const GroupNormParams& p, hipStream_t s) {

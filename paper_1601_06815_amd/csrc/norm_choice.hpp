@@ -12,12 +12,17 @@ namespace oaa {
 
 inline size_t align_workspace(size_t v) { return (v + kWorkspaceAlign - 1) / kWorkspaceAlign * kWorkspaceAlign; }
 
-// Threads of the kernels that take slices, and the workgroups they aim for.
+// Threads of the kernels that take slices, and the workgroups they aim for: more
+// for a pass that writes, which likes its neighbours in time to be neighbours in
+// memory, than for sums, whose parts are to be joined. Measured on 389 MB
+// channels last, us, with 2048 / 4096 / 8192 / 24000: sums 73 / 78 / 89 / -,
+// forward result 136 / 131 / 127 / 147, input gradient 214 / 208 / 200 / 216.
 constexpr int kSplitThreads = 256;
 constexpr long kSlices = 2048;
 constexpr long kResultSlices = 8192;
 // Accesses of a thread loaded before the first of them is used, where values
-// stream.
+// stream. Eight change nothing channels last and spill in planes (1024 groups of
+// 409 KB forward 280 us against 212).
 constexpr int kAhead = 4;
 
 // ---- planes ----

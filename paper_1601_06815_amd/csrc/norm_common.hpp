@@ -112,6 +112,17 @@ __device__ __forceinline__ void gradient(float x, float dy, float mean, float rs
   dz = dy * act_slope<ACT>(fmaf(xh, w, b));
 }
 
+// Keeps the sums of dz and dz xh of channel c of an image: as sums[c] of that image,
+// or, where there is no other image, as dbias and dweight.
+__device__ __forceinline__ void keep_sums(const GroupNormParams& p, float2* sums, long c, double a, double d) {
+  if (sums) {
+    sums[c] = {float(a), float(d)};
+    return;
+  }
+  if (p.dbias) store_param(p.dbias, p.param_dtype, c, float(a));
+  if (p.dweight) store_param(p.dweight, p.param_dtype, c, float(d));
+}
+
 // What the input gradient takes of a channel: dx = rstd (w dz - m1 - xh m2).
 struct InputGradient {
   float w, m1, m2;

@@ -11,8 +11,14 @@
 // columns, which the access before it has too, count once.
 //
 // Every pass is bound by memory. Where a slab's rows fit the registers of one
-// workgroup, they are read once. Otherwise the rows are sliced over the device,
-// in three launches each way: sums, their join, the result.
+// workgroup, they are read once; neighbouring slabs, which share lines, run on
+// one die. Otherwise the rows are sliced over the device, in three launches each
+// way: sums, their join, and the result, which walks the images backwards, since
+// what was read last is still cached.
+//
+// Measured (bfloat16, SiLU, 64 images of 64 channels and 47524 positions): sums 76
+// us (5.1 TB/s) and result 129 us (6.0) forward, 139 (5.6) and 203 us (5.8)
+// backward; vector instructions issue in 41 to 59 % of the cycles.
 //
 // Statistics are summed in float64 about the group's first value x0: the
 // variance is E[d^2] - E[d]^2 of d = x - x0, which keeps its digits however far
@@ -420,7 +426,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_backward_k
       },
       [&](int c, double a, double d) {
         columns[sub][c] = {float(a), float(d)};
-        if (sums && active) sums[b * p.C + c0 + c] = {float(a), float(d)};
+        if (active) keep_sums(p, sums ? sums + b * p.C : nullptr, c0 + c, a, d);
       });
   if (!p.dx) return;
   __syncthreads();

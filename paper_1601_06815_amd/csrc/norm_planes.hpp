@@ -6,9 +6,15 @@
 //
 // Every pass is bound by memory, so a group's values are read once wherever
 // they fit in the registers of one workgroup: it loads them, sums, and writes
-// the result from the same registers. What does not fit is read again. Few
-// large groups are cut over the whole device instead, in two launches forward
-// and three backward.
+// the result from the same registers. What does not fit is read again, the last
+// first. Few large groups are cut over the whole device instead, in two launches
+// forward and three backward.
+//
+// Measured (float32, SiLU, inputs not in a cache): 4096 groups of 47 KB forward
+// 71 us (5.4 TB/s of what has to move), backward 117 us (4.9); 1024 groups of 409
+// KB, of which registers hold 48 % forward and 24 % backward, 196 us (4.3) and
+// 307 us (4.1), with 1.20 and 1.47 times what has to move through the caches of
+// the dies; four groups of 6.4 MB forward 8 + 13 us.
 //
 // A row is cut into accesses of V values from its start on, at whatever address
 // that is; the last access of a row whose length is no multiple of V is moved
@@ -431,7 +437,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void planes_backward
       a += row_sums[i * wpr + k].x;
       c += row_sums[i * wpr + k].y;
     }
-    if (sums) sums[b * p.C + c0 + i] = {float(a), float(c)};
+    keep_sums(p, sums ? sums + b * p.C : nullptr, c0 + i, a, c);
     ta += a * w[i];
     tb += c * w[i];
   }
@@ -572,6 +578,12 @@ hipError_t forward_groups(const GroupNormParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Threads and accesses in registers, by a group's accesses: as few threads as
+// hold it, since phases of several workgroups on a compute unit overlap. Where
+// none holds it, more accesses in registers cost waves or spill: 1024 groups of
+// 25544 accesses took 196 us with 12 a thread, 195 with 8, 212 with 16, 264 with
+// 20, and 309 with 512 threads of 50; 4096 groups of 2916 took 71 us on 512
+// threads of 8 and 75 on 256 of 16.
 template <typename T, int ACT, int V>
 hipError_t forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s) {
   const long units = p.D * accesses(p), groups = long(p.B) * p.G;
@@ -599,6 +611,9 @@ hipError_t backward_groups(const GroupNormParams& p, float2* sums, hipStream_t s
   return hipGetLastError();
 }
 
+// The same with x and dy: 4096 groups of 2916 accesses took 121 us on 256
+// threads of 12 and 153 on 512 of 6; 1024 of 25544 took 305 us on 1024 threads of
+// 6, 316 with 4, 322 with 8, 386 on 512 of 16.
 template <typename T, int ACT, int V>
 hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s) {
   const long units = p.D * accesses(p);
