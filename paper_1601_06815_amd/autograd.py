@@ -102,19 +102,22 @@ class GroupNormFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, num_groups, eps, activation):
-        y, mean, rstd = binding.group_norm_forward(x, num_groups, weight, bias, eps, activation)
-        ctx.num_groups, ctx.activation = num_groups, activation
-        ctx.save_for_backward(x, weight, bias, mean, rstd)
+        record = binding.GroupNormRecord(x, num_groups, weight, bias, eps, activation)
+        y, buffer = record.y, record.buffer
+        record.y = record.buffer = None  # autograd keeps what the backward pass needs
+        ctx.record = record
+        ctx.save_for_backward(x, weight, bias, buffer)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        x, weight, bias, mean, rstd = ctx.saved_tensors
+        x, weight, bias, buffer = ctx.saved_tensors
         if dy.stride() != x.stride():
             dy = _laid_out(dy, binding._norm_layout(x, "x")[0])
-        return (*binding.group_norm_backward(dy, x, ctx.num_groups, weight, bias, mean, rstd, ctx.activation,
-                                             *ctx.needs_input_grad[:3]), None, None, None)
+        need_x, need_weight, need_bias = ctx.needs_input_grad[:3]
+        dx, dweight, dbias = ctx.record.backward(dy, x, weight, bias, buffer, need_x, need_weight, need_bias)
+        return dx, dweight, dbias, None, None, None
 
 
 def group_norm(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none"):

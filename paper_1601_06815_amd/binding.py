@@ -528,6 +528,40 @@ def _like(x, call):
     return torch.empty((x.shape[0], *x.shape[2:], x.shape[1]), dtype=x.dtype, device=x.device).movedim(-1, 1)
 
 
+def _kinds(weight, bias):
+    return (None if weight is None else (weight.dtype, weight.shape),
+            None if bias is None else (bias.dtype, bias.shape))
+
+
+def _pointer(t):
+    return None if t is None else t.data_ptr()
+
+
+def _forward(call, index, x, weight, bias, y, mean, rstd):
+    """The launch; mean and rstd are addresses or None."""
+    need = call.forward_bytes
+    ws = _torch()[0].empty(need, dtype=_torch()[0].uint8, device=x.device) if need else None
+    _launch(load().oaa_group_norm_forward, index, call.address, x.data_ptr(), _pointer(weight), _pointer(bias),
+            y.data_ptr(), mean, rstd, _pointer(ws), need)
+
+
+def _backward(call, index, dy, x, weight, bias, mean, rstd, ws, need_x, need_weight, need_bias):
+    """The launch into new tensors; mean, rstd and ws (or None) are addresses."""
+    torch = _torch()[0]
+    dx = _like(x, call) if need_x else None
+    dweight = torch.empty_like(weight) if need_weight and weight is not None else None
+    dbias = torch.empty_like(bias) if need_bias and bias is not None else None
+    if dx is None and dweight is None and dbias is None:
+        return None, None, None
+    need = call.backward_bytes
+    if need and ws is None:
+        held = torch.empty(need, dtype=torch.uint8, device=x.device)  # until the launch
+        ws = held.data_ptr()
+    _launch(load().oaa_group_norm_backward, index, call.address, dy.data_ptr(), x.data_ptr(), _pointer(weight),
+            _pointer(bias), mean, rstd, _pointer(dx), _pointer(dweight), _pointer(dbias), ws, need)
+    return dx, dweight, dbias
+
+
 def group_norm_forward(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none", y=None, stats=True):
     """oaa_group_norm_forward on torch's current stream of x's device: (y, mean,
     rstd), the last two [B, G] float32 (None without ``stats``). x[B, C, ...]
@@ -536,21 +570,16 @@ def group_norm_forward(x, num_groups, weight=None, bias=None, eps=1e-5, activati
     index = _device_of(x, weight, bias)
     if y is not None and (y.shape != x.shape or y.dtype != x.dtype or y.get_device() != index):
         raise ValueError(f"y must be a {x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
-    call = _norm_call(x.shape, x.stride(), None if y is None else y.stride(), None, x.dtype,
-                      None if weight is None else (weight.dtype, weight.shape),
-                      None if bias is None else (bias.dtype, bias.shape), num_groups, eps, activation)
+    call = _norm_call(x.shape, x.stride(), None if y is None else y.stride(), None, x.dtype, *_kinds(weight, bias),
+                      num_groups, eps, activation)
     if y is None:
         y = _like(x, call)
-    mean = rstd = ws = None
-    if stats:
-        mean = torch.empty((x.shape[0], num_groups), dtype=torch.float32, device=x.device)
-        rstd = torch.empty_like(mean)
-    if call.forward_bytes:
-        ws = torch.empty(call.forward_bytes, dtype=torch.uint8, device=x.device)
-    _launch(load().oaa_group_norm_forward, index, call.address, x.data_ptr(), weight if weight is None else
-            weight.data_ptr(), bias if bias is None else bias.data_ptr(), y.data_ptr(), mean if mean is None else
-            mean.data_ptr(), rstd if rstd is None else rstd.data_ptr(), ws if ws is None else ws.data_ptr(),
-            call.forward_bytes)
+    if not stats:
+        _forward(call, index, x, weight, bias, y, None, None)
+        return y, None, None
+    mean = torch.empty((x.shape[0], num_groups), dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    _forward(call, index, x, weight, bias, y, mean.data_ptr(), rstd.data_ptr())
     return y, mean, rstd
 
 
@@ -563,24 +592,47 @@ def group_norm_backward(dy, x, num_groups, weight, bias, mean, rstd, activation=
     index = _device_of(x, weight, bias)
     if dy.shape != x.shape or dy.dtype != x.dtype or dy.get_device() != index:
         raise ValueError(f"dy must be a {x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
-    call = _norm_call(x.shape, x.stride(), None, dy.stride(), x.dtype,
-                      None if weight is None else (weight.dtype, weight.shape),
-                      None if bias is None else (bias.dtype, bias.shape), num_groups, 0.0, activation)
+    call = _norm_call(x.shape, x.stride(), None, dy.stride(), x.dtype, *_kinds(weight, bias), num_groups, 0.0,
+                      activation)
     groups = (x.shape[0], num_groups)
     for name, t in (("mean", mean), ("rstd", rstd)):
         if t.shape != groups or t.dtype != torch.float32 or t.get_device() != index or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous float32 tensor of shape {groups} on {x.device}")
-    dx = _like(x, call) if need_x else None
-    dweight = torch.empty_like(weight) if need_weight and weight is not None else None
-    dbias = torch.empty_like(bias) if need_bias and bias is not None else None
-    if dx is None and dweight is None and dbias is None:
-        return None, None, None
-    ws = torch.empty(call.backward_bytes, dtype=torch.uint8, device=x.device) if call.backward_bytes else None
-    _launch(load().oaa_group_norm_backward, index, call.address, dy.data_ptr(), x.data_ptr(), weight if weight is None
-            else weight.data_ptr(), bias if bias is None else bias.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-            dx if dx is None else dx.data_ptr(), dweight if dweight is None else dweight.data_ptr(),
-            dbias if dbias is None else dbias.data_ptr(), ws if ws is None else ws.data_ptr(), call.backward_bytes)
-    return dx, dweight, dbias
+    return _backward(call, index, dy, x, weight, bias, mean.data_ptr(), rstd.data_ptr(), None, need_x, need_weight,
+                     need_bias)
+
+
+# Most bytes of backward workspace that a recorded forward pass keeps beside its
+# statistics: allocating it then is cheaper than in autograd's backward thread.
+_KEPT_BYTES = 1 << 20
+
+
+class GroupNormRecord:
+    """A forward pass whose backward pass follows, for autograd: its output y, and
+    in one buffer the statistics and, if it is small, the backward workspace."""
+
+    def __init__(self, x, num_groups, weight, bias, eps, activation):
+        torch = _torch()[0]
+        self.index = _device_of(x, weight, bias)
+        # dy comes with x's strides, or is brought to them
+        self.args = (x.dtype, *_kinds(weight, bias), num_groups, eps, activation)
+        self.call = _norm_call(x.shape, x.stride(), None, x.stride(), *self.args)
+        self.row = 4 * x.shape[0] * num_groups
+        stats = (2 * self.row + 255) // 256 * 256
+        keep = self.call.backward_bytes if self.call.backward_bytes <= _KEPT_BYTES else 0
+        self.ws = stats if keep else None
+        self.buffer = torch.empty(stats + keep, dtype=torch.uint8, device=x.device)
+        self.y = _like(x, self.call)
+        at = self.buffer.data_ptr()
+        _forward(self.call, self.index, x, weight, bias, self.y, at, at + self.row)
+
+    def backward(self, dy, x, weight, bias, buffer, need_x, need_weight, need_bias):
+        """(dx, dweight, dbias) from the buffer as autograd kept it."""
+        call, at = self.call, buffer.data_ptr()
+        if dy.stride() != x.stride():
+            call = _norm_call(x.shape, x.stride(), None, dy.stride(), *self.args)
+        return _backward(call, self.index, dy, x, weight, bias, at, at + self.row,
+                         at + self.ws if self.ws is not None else None, need_x, need_weight, need_bias)
 
 
 NORM_TYPES = {1.0: NORM_SUM, 2.0: NORM_EUCLIDEAN, float("inf"): NORM_MAX}
