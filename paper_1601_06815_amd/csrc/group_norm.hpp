@@ -36,11 +36,15 @@ struct NormCut {
 // Where the backward pass leaves each channel's sums of dz and dz xh, in
 // `count` parts: part k of channel c of image b is sums[b image + c channel + k
 // slot]. means[B][G], the groups' means of t and t xh, are needed only where
-// groups are split: launch_norm_join makes them before dx.
+// groups are split: launch_norm_join makes them before dx, from the channels' sums
+// or, where group_parts is not 0, from sums of t and t xh that the kernel left in
+// as many parts a group, group_sums[B][group_parts][G].
 struct NormSums {
   float2* sums;
   float2* means;
   long count, image, channel, slot;
+  float2* group_sums;
+  long group_parts;
 };
 
 // One launch handles at most this many channels of images, so that its grid

@@ -13,11 +13,33 @@ constexpr int kThreads = 256;
 // rows where those run along the channels.
 constexpr int kColumns = 8;
 
-// Workgroups [0, groups): the means of t and t xh of a group each. The others:
-// dweight and dbias.
+// Workgroups [0, blocks): the groups' means of t and t xh, from the groups' own
+// parts a wave a group, from the channels' a workgroup a group. The others: dweight
+// and dbias.
 template <int kThreads>
-__global__ __launch_bounds__(kThreads) void norm_join_kernel(GroupNormParams p, NormSums at, int groups) {
-  if (int(blockIdx.x) < groups) {
+__global__ __launch_bounds__(kThreads) void norm_join_kernel(GroupNormParams p, NormSums at, int blocks) {
+  if (int(blockIdx.x) < blocks && at.group_parts) {
+    const long bg = long(blockIdx.x) * (kThreads / 64) + threadIdx.x / 64;
+    if (bg >= long(p.B) * p.G) return;
+    const long b = bg / p.G, g = bg - b * p.G;
+    const float2* sums = at.group_sums + b * at.group_parts * p.G + g;
+    double a = 0.0, d = 0.0;
+    for (long i = threadIdx.x % 64; i < at.group_parts; i += 64 * 8) {
+      float2 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = i + 64 * u < at.group_parts ? sums[(i + 64 * u) * p.G] : float2{0.0f, 0.0f};
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        a += v[u].x;
+        d += v[u].y;
+      }
+    }
+    lane_sum<64>(a, d);
+    const double n = double(p.D) * p.S;
+    if (threadIdx.x % 64 == 0) at.means[bg] = {float(a / n), float(d / n)};
+    return;
+  }
+  if (int(blockIdx.x) < blocks) {
     __shared__ double part[2 * kThreads / 64];
     const long bg = blockIdx.x, b = bg / p.G, c0 = (bg - b * p.G) * p.D;
     const float2* sums = at.sums + b * at.image + c0 * at.channel;
@@ -26,15 +48,24 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(GroupNormParams p, 
     long step = kThreads / p.D, k = threadIdx.x / p.D;
     int rest = kThreads % p.D, c = threadIdx.x % p.D;
     while (k < at.count) {
-      const float2 v = sums[c * at.channel + k * at.slot];
-      const double w = load_param(p.weight, p.param_dtype, c0 + c, 1.0f);
-      a = fma(w, double(v.x), a);
-      d = fma(w, double(v.y), d);
-      k += step;
-      c += rest;
-      if (c >= p.D) {
-        c -= p.D;
-        ++k;
+      float2 v[8];  // loaded together: the sums lie in another die's cache or in memory
+      float w[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const bool in = k < at.count;
+        v[u] = in ? sums[c * at.channel + k * at.slot] : float2{0.0f, 0.0f};
+        w[u] = in ? load_param(p.weight, p.param_dtype, c0 + c, 1.0f) : 0.0f;
+        k += step;
+        c += rest;
+        if (c >= p.D) {
+          c -= p.D;
+          ++k;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        a = fma(double(w[u]), double(v[u].x), a);
+        d = fma(double(w[u]), double(v[u].y), d);
       }
     }
     thread_sum<kThreads>(a, d, part);
@@ -45,7 +76,7 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(GroupNormParams p, 
   constexpr int kLanes = kThreads / kColumns;
   __shared__ double2 waves[kThreads / 64][kColumns];
   const int col = threadIdx.x % kColumns, lane = threadIdx.x / kColumns;
-  const long c = long(blockIdx.x - groups) * kColumns + col;
+  const long c = long(blockIdx.x - blocks) * kColumns + col;
   double a = 0.0, d = 0.0;
   if (c < p.C) {
     const float2* sums = at.sums + c * at.channel;
@@ -142,15 +173,21 @@ size_t sums_bytes(const GroupNormParams& p, const NormSums& at) {
 
 }  // namespace
 
-hipError_t launch_norm_join(const GroupNormParams& p, const NormSums& at, hipStream_t s) {
-  const int groups = at.means ? p.B * p.G : 0;
+template <int THREADS>
+static hipError_t join(const GroupNormParams& p, const NormSums& at, hipStream_t s) {
+  const long groups = at.means ? long(p.B) * p.G : 0;
+  const int blocks = int(at.group_parts ? (groups + THREADS / 64 - 1) / (THREADS / 64) : groups);
   const int columns = p.dweight || p.dbias ? (p.C + kColumns - 1) / kColumns : 0;
-  if (groups + columns == 0) return hipSuccess;
-  if (p.B * at.count <= 512)
-    norm_join_kernel<256><<<groups + columns, 256, 0, s>>>(p, at, groups);
-  else
-    norm_join_kernel<1024><<<groups + columns, 1024, 0, s>>>(p, at, groups);
+  if (blocks + columns == 0) return hipSuccess;
+  norm_join_kernel<THREADS><<<blocks + columns, THREADS, 0, s>>>(p, at, blocks);
   return hipGetLastError();
+}
+
+// More threads where a channel, or a group from its channels, has many parts.
+hipError_t launch_norm_join(const GroupNormParams& p, const NormSums& at, hipStream_t s) {
+  const bool from_channels = at.means && !at.group_parts;
+  return p.B * at.count <= 512 && (!from_channels || p.D * at.count <= 2048) ? join<256>(p, at, s)
+                                                                             : join<1024>(p, at, s);
 }
 
 size_t group_norm_forward_ws(const GroupNormParams& p) {
@@ -161,7 +198,9 @@ size_t group_norm_forward_ws(const GroupNormParams& p) {
 size_t group_norm_backward_ws(const GroupNormParams& p) {
   const NormCut cut = backward_cut(p);
   if (sums_are_final(p, cut)) return 0;
-  return sums_bytes(p, sums_layout(p, cut)) + (cut.split ? align_workspace(sizeof(float2) * p.B * p.G) : 0);
+  const NormSums at = sums_layout(p, cut);
+  const size_t means = align_workspace(sizeof(float2) * p.B * p.G);
+  return sums_bytes(p, at) + (cut.split ? means + at.group_parts * means : 0);
 }
 
 hipError_t launch_group_norm_forward(const GroupNormParams& in, hipStream_t s) {
@@ -187,6 +226,7 @@ hipError_t launch_group_norm_backward(const GroupNormParams& in, hipStream_t s) 
   const bool final = sums_are_final(p, cut);
   all.sums = final ? nullptr : reinterpret_cast<float2*>(p.ws);
   float2* means = cut.split ? reinterpret_cast<float2*>(p.ws + sums_bytes(p, all)) : nullptr;
+  all.group_sums = means ? means + align_workspace(sizeof(float2) * p.B * p.G) / sizeof(float2) : nullptr;
   // dweight and dbias come with the groups' means where all images do
   const bool one = batch(p) == p.B;
   for (long b = 0; b < p.B; b += batch(p)) {
@@ -195,6 +235,7 @@ hipError_t launch_group_norm_backward(const GroupNormParams& in, hipStream_t s) 
     NormSums at = all;
     if (at.sums) at.sums += b * at.image;
     at.means = means ? means + b * p.G : nullptr;
+    if (at.group_sums) at.group_sums += b * at.group_parts * p.G;
     const hipError_t e = for_type(p.dtype, [&](auto t) {
       using T = typename decltype(t)::type;
       return p.last ? launch_last_backward<T>(q, cut, at, s) : launch_planes_backward<T>(q, cut, at, s);

@@ -51,7 +51,8 @@ inline bool one_workgroup_can(const GroupNormParams& p) {
 // KB 8.8 / 8.4, of 256 KB 14.0 / 8.6; 128 groups of 128 KB 10.8 / 14.4, of 256 KB
 // 18.7 / 21.8; 1024 groups of 399 KB 195 / 260.
 inline bool forward_one_workgroup(const GroupNormParams& p) {
-  return one_workgroup_can(p) && (p.D * accesses(p) <= 6144 || long(p.B) * p.G >= 128);
+  const long units = p.D * accesses(p), groups = long(p.B) * p.G;
+  return one_workgroup_can(p) && (units <= 6144 || groups >= 192 || (groups >= 128 && units <= 8192));
 }
 
 // Backward. The alternative takes one launch more, but its lanes are not bound
@@ -104,7 +105,7 @@ inline NormCut planes_backward_cut(const GroupNormParams& p) {
 }
 
 inline NormSums planes_sums(const GroupNormParams& p, const NormCut& cut) {
-  return {nullptr, nullptr, cut.count, p.C * cut.count, cut.count, 1};
+  return {nullptr, nullptr, cut.count, p.C * cut.count, cut.count, 1, nullptr, 0};
 }
 
 // ---- channels last ----
@@ -146,6 +147,13 @@ inline long row_slice(const GroupNormParams& p, long slices) {
   return (slice + lanes * kAhead - 1) / (lanes * kAhead) * (lanes * kAhead);
 }
 
+// Slices of a pass that writes: of 48 KB or more, since a workgroup first loads
+// its columns' parameters and statistics.
+inline long result_slices(const GroupNormParams& p) {
+  const double bytes = double(p.B) * p.C * p.S * dtype_size(p.dtype);
+  return std::max(kSlices, std::min(kResultSlices, long(bytes / 49152)));
+}
+
 // Whether a slab goes to one workgroup. The alternative, slices of rows, reads
 // everything twice in two launches more. Measured, us, one workgroup first
 // (SiLU, D = 8 and S up to 8192 positions, slabs of one group up to 256 groups),
@@ -183,7 +191,7 @@ inline NormCut last_backward_cut(const GroupNormParams& p) { return cut_rows(p, 
 
 inline NormSums last_sums(const GroupNormParams& p, const NormCut& cut) {
   const long count = cut.split ? cut.count : 1;
-  return {nullptr, nullptr, count, p.C * count, 1, p.C};
+  return {nullptr, nullptr, count, p.C * count, 1, p.C, nullptr, cut.split ? parts(p, cut) : 0};
 }
 
 }  // namespace oaa

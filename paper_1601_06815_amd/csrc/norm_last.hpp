@@ -68,23 +68,47 @@ __device__ __forceinline__ void groups_of(int col, int first, int D, int (&g)[V]
 }
 
 // Sums over a slab's entries of each of its groups: entry (lane, column) lies at
-// entries[lane * pitch + column]. Lanes of a wave share a group. done(g, a, b)
-// is called once per group by one lane.
+// entries[lane * pitch + column]. A group goes to some lanes of a wave, or, where
+// groups are fewer than half the waves, to several waves. done(g, a, b) is called
+// once per group by one thread.
 template <int THREADS, typename E, typename Fn>
 __device__ __forceinline__ void group_sums(int tid, int lanes, int pitch, int width, int first, int D, E&& entry,
                                            Fn&& done) {
   const int groups = (first + width + D - 1) / D;
+  auto sum = [&](int g, int from, int step, double& a, double& b) {
+    a = b = 0.0;
+    if (g >= groups) return;
+    const int begin = max(g * D - first, 0), own = min((g + 1) * D - first, width) - begin;
+    for (int i = from; i < own * lanes; i += step) {
+      const int lane = i / own, c = begin + i - lane * own;
+      entry(lane * pitch + c, c, a, b);
+    }
+  };
+  double a, b;
+  constexpr int kWaves = THREADS / 64;
+  if constexpr (kWaves > 1) {
+    if (groups <= kWaves / 2) {
+      __shared__ double2 waves[kWaves];
+      const int each = kWaves / groups, wave = tid / 64;
+      sum(wave / each, wave % each * 64 + tid % 64, each * 64, a, b);
+      lane_sum<64>(a, b);
+      if (tid % 64 == 0) waves[wave] = {a, b};
+      __syncthreads();
+      if (tid >= groups) return;
+      a = b = 0.0;
+      for (int i = 0; i < each; ++i) {
+        a += waves[tid * each + i].x;
+        b += waves[tid * each + i].y;
+      }
+      done(tid, a, b);
+      return;
+    }
+  }
   int share = 64;  // lanes of a group
   while (share > 1 && share * groups > THREADS) share /= 2;
   for (int base = 0; base < groups; base += THREADS / share) {
     const int g = base + tid / share;
-    const int begin = max(g * D - first, 0), end = min((g + 1) * D - first, width), own = end - begin;
-    double a = 0.0, b = 0.0;
-    if (g < groups)
-      for (int i = tid % share; i < own * lanes; i += share) {
-        const int lane = i / own;
-        entry(lane * pitch + begin + i - lane * own, begin + i - lane * own, a, b);
-      }
+    sum(g, tid % share, share, a, b);
     for (int m = share / 2; m; m >>= 1) {
       a += __shfl_xor(a, m);
       b += __shfl_xor(b, m);
@@ -264,20 +288,27 @@ __global__ __launch_bounds__(kSplitThreads) void last_moments_kernel(GroupNormPa
       [&](int gi, double a, double q) { out[g0 + gi] = {a, q}; });
 }
 
-// mean and rstd of a group from the moments of its `count` parts.
+// mean and rstd of a group from the moments of its `count` parts, a wave a group.
 template <typename T>
 __global__ __launch_bounds__(kSplitThreads) void last_statistics_kernel(GroupNormParams p, int count,
                                                                         const double2* sums) {
-  __shared__ double part[2 * kSplitThreads / 64];
-  const long bg = blockIdx.x, b = bg / p.G, g = bg - b * p.G;
+  const long bg = long(blockIdx.x) * (kSplitThreads / 64) + threadIdx.x / 64;
+  if (bg >= long(p.B) * p.G) return;
+  const long b = bg / p.G, g = bg - b * p.G;
+  sums += b * count * p.G + g;
   double a = 0.0, q = 0.0;
-  for (int i = threadIdx.x; i < count; i += kSplitThreads) {
-    const double2 v = sums[(b * count + i) * p.G + g];
-    a += v.x;
-    q += v.y;
+  for (int i = threadIdx.x % 64; i < count; i += 64 * kAhead) {
+    double2 v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = i + 64 * u < count ? sums[long(i + 64 * u) * p.G] : double2{0.0, 0.0};
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      a += v[u].x;
+      q += v[u].y;
+    }
   }
-  thread_sum<kSplitThreads>(a, q, part);
-  if (threadIdx.x == 0) {
+  lane_sum<64>(a, q);
+  if (threadIdx.x % 64 == 0) {
     const T* x = static_cast<const T*>(p.x) + b * p.x_image + g * p.D;
     statistics(a, q, double(float(x[0])), double(p.D) * p.S, p.eps, p.mean[bg], p.rstd[bg]);
   }
@@ -457,11 +488,14 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_backward_k
   }
 }
 
-// sums[b][k][c] = (sum dz, sum dz xh) of channel c over slice k of image b's rows.
+// sums[b][k][c] = (sum dz, sum dz xh) of channel c over slice k of image b's rows;
+// group_sums[b][k slabs + j][g] = the same of t and t xh of the part of group g in
+// slab j.
 template <typename T, int ACT, int V>
 __global__ __launch_bounds__(kSplitThreads) void last_column_sums_kernel(GroupNormParams p, long slice, int count,
-                                                                         float2* sums) {
+                                                                         NormSums to) {
   __shared__ float2 entries[kSplitThreads * V];
+  __shared__ float2 columns[kSplitThreads * V];
   const SplitPlace<V> in(p, slice, count, blockIdx.x);
   const Place<V, kSplitThreads> at(threadIdx.x, in.width);
   if (at.active()) {
@@ -488,14 +522,30 @@ __global__ __launch_bounds__(kSplitThreads) void last_column_sums_kernel(GroupNo
       if (i >= at.dup) entries[at.lane * in.width + at.col + i] = {sa[i], sb[i]};
   }
   __syncthreads();
-  float2* out = sums + (in.b * count + in.k) * p.C + in.c0;
+  float2* out = to.sums + (in.b * count + in.k) * p.C + in.c0;
   group_sums<kSplitThreads>(
       threadIdx.x, at.lanes, in.width, in.width, 0, 1,
       [&](int e, int, double& a, double& d) {
         a += entries[e].x;
         d += entries[e].y;
       },
-      [&](int c, double a, double d) { out[c] = {float(a), float(d)}; });
+      [&](int c, double a, double d) {
+        columns[c] = {float(a), float(d)};
+        out[c] = {float(a), float(d)};
+      });
+  __syncthreads();
+  const int D = p.D, g0 = in.c0 / D, own = in.c0 - g0 * D, groups = (own + in.width + D - 1) / D;
+  float2* group_out = to.group_sums + ((in.b * count + in.k) * in.slabs + in.j) * p.G;
+  for (int i = threadIdx.x; i < p.G; i += kSplitThreads)
+    if (i < g0 || i >= g0 + groups) group_out[i] = {0.0f, 0.0f};
+  group_sums<kSplitThreads>(
+      threadIdx.x, 1, in.width, in.width, own, D,
+      [&](int e, int c, double& a, double& d) {
+        const double w = load_param(p.weight, p.param_dtype, in.c0 + c, 1.0f);
+        a = fma(w, double(columns[e].x), a);
+        d = fma(w, double(columns[e].y), d);
+      },
+      [&](int gi, double a, double d) { group_out[g0 + gi] = {float(a), float(d)}; });
 }
 
 template <typename T, int ACT, int V>
@@ -557,8 +607,9 @@ hipError_t forward(const GroupNormParams& in, const NormCut& cut, hipStream_t s)
   if (!p.rstd) p.rstd = stats + long(p.B) * p.G;
   const unsigned blocks = unsigned(p.B * parts(p, cut));
   last_moments_kernel<T, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), sums);
-  last_statistics_kernel<T><<<p.B * p.G, kSplitThreads, 0, s>>>(p, int(parts(p, cut)), sums);
-  const long slice = row_slice(p, kResultSlices), count = (p.S + slice - 1) / slice;
+  constexpr int kWaves = kSplitThreads / 64;
+  last_statistics_kernel<T><<<(p.B * p.G + kWaves - 1) / kWaves, kSplitThreads, 0, s>>>(p, int(parts(p, cut)), sums);
+  const long slice = row_slice(p, result_slices(p)), count = (p.S + slice - 1) / slice;
   last_apply_kernel<T, ACT, V>
       <<<unsigned(p.B * count * split_slabs(p.C, V)), kSplitThreads, 0, s>>>(p, slice, int(count));
   return hipGetLastError();
@@ -583,10 +634,10 @@ hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums
     return backward_slabs<T, ACT, V, kBackwardThreads, kBackwardRows>(p, slabs, at, s);
   }
   const unsigned blocks = unsigned(p.B * parts(p, cut));
-  last_column_sums_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at.sums);
+  last_column_sums_kernel<T, ACT, V><<<blocks, kSplitThreads, 0, s>>>(p, cut.slice, int(cut.count), at);
   if (hipError_t e = launch_norm_join(p, at, s)) return e;
   if (p.dx) {
-    const long slice = row_slice(p, kResultSlices), count = (p.S + slice - 1) / slice;
+    const long slice = row_slice(p, result_slices(p)), count = (p.S + slice - 1) / slice;
     last_input_gradient_kernel<T, ACT, V>
         <<<unsigned(p.B * count * split_slabs(p.C, V)), kSplitThreads, 0, s>>>(p, slice, int(count), at.means);
   }
