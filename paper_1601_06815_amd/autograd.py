@@ -160,4 +160,6 @@ def clip_grad_norm_(parameters, max_norm, norm_type=2.0):
     """Scale the gradients of the parameters in place so that their norm is at
     most max_norm; returns the norm before, a scalar on the device (nothing
     waits for it). Parameters without a gradient are left out."""
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
     return binding.grad_clip([p.grad for p in parameters if p.grad is not None], max_norm, norm_type)

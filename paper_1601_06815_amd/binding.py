@@ -703,6 +703,10 @@ def grad_clip(grads, max_norm, norm_type=2.0, out=None):
             if o.dtype != g.dtype or o.get_device() != index or o.shape != g.shape or o.stride() != g.stride():
                 raise ValueError(f"output {i} differs from its gradient in shape, strides, type or device")
         dst = array.array("Q", [t.data_ptr() for t in out])
+    if len(set(dst)) < len(dst):
+        written = [d for d, n in zip(dst, sizes) if n]
+        if len(set(written)) < len(written):
+            raise ValueError("a tensor is written twice: list each gradient once")
     _launch(load().oaa_grad_clip, index, len(grads), src.buffer_info()[0], dst.buffer_info()[0],
             sizes.buffer_info()[0], kinds.buffer_info()[0], NORM_TYPES[norm_type], max_norm, norm.data_ptr(),
             ws.data_ptr(), ws.numel())

@@ -171,10 +171,8 @@ size_t sums_bytes(const GroupNormParams& p, const NormSums& at) {
   return align_workspace(sizeof(float2) * p.B * p.C * at.count);
 }
 
-}  // namespace
-
 template <int THREADS>
-static hipError_t join(const GroupNormParams& p, const NormSums& at, hipStream_t s) {
+hipError_t join(const GroupNormParams& p, const NormSums& at, hipStream_t s) {
   const long groups = at.means ? long(p.B) * p.G : 0;
   const int blocks = int(at.group_parts ? (groups + THREADS / 64 - 1) / (THREADS / 64) : groups);
   const int columns = p.dweight || p.dbias ? (p.C + kColumns - 1) / kColumns : 0;
@@ -182,6 +180,8 @@ static hipError_t join(const GroupNormParams& p, const NormSums& at, hipStream_t
   norm_join_kernel<THREADS><<<blocks + columns, THREADS, 0, s>>>(p, at, blocks);
   return hipGetLastError();
 }
+
+}  // namespace
 
 // More threads where a channel, or a group from its channels, has many parts.
 hipError_t launch_norm_join(const GroupNormParams& p, const NormSums& at, hipStream_t s) {

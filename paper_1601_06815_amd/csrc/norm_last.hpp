@@ -17,7 +17,7 @@
 // what was read last is still cached.
 //
 // Measured (bfloat16, SiLU, 64 images of 64 channels and 47524 positions): sums 76
-// us (5.1 TB/s) and result 129 us (6.0) forward, 139 (5.6) and 203 us (5.8)
+// us (5.1 TB/s) and result 129 us (6.0) forward, 140 (5.6) and 209 us (5.6)
 // backward; vector instructions issue in 41 to 59 % of the cycles.
 //
 // Statistics are summed in float64 about the group's first value x0: the

@@ -11,7 +11,7 @@
 // forward and three backward.
 //
 // Measured (float32, SiLU, inputs not in a cache): 4096 groups of 47 KB forward
-// 71 us (5.4 TB/s of what has to move), backward 117 us (4.9); 1024 groups of 409
+// 71 us (5.4 TB/s of what has to move), backward 119 us (4.8); 1024 groups of 409
 // KB, of which registers hold 48 % forward and 24 % backward, 196 us (4.3) and
 // 307 us (4.1), with 1.20 and 1.47 times what has to move through the caches of
 // the dies; four groups of 6.4 MB forward 8 + 13 us.

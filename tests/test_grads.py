@@ -51,7 +51,7 @@ def check(grads, max_norm, p=2.0, out=None, in_place=False):
 
 LISTS = [
     [1], [300, 4, 4], [0], [0, 5, 0, 0, 7], [16384], [16385, 1], [16383, 16384, 3], [100003, 7, 65536, 1],
-    [(8, 3, 7, 7), 8, 8] * 5, [17] * 300, [40000] * 130, [3000000, 1, 5], [1 << 20] * 9,
+    [(8, 3, 7, 7), 8, 8] * 5, [17] * 300, [40000] * 130, [3000000, 1, 5], [1 << 20] * 9, [25000000, 7],
 ]
 
 
@@ -229,6 +229,14 @@ def test_binding_refuses(gpu_lib):
         binding.grad_clip([a], 1.0, out=[b])
     with pytest.raises(ValueError, match="output 0"):
         binding.grad_clip([a], 1.0, out=[a.bfloat16()])
+    with pytest.raises(ValueError, match="written twice"):
+        binding.grad_clip([a, b, a], 1.0)
+    assert float(binding.grad_norm([a, a])) > 0  # reading one twice is well defined
+    empty = a[:0]
+    binding.grad_clip([empty, a, empty], 1.0)
+    one = torch.nn.Parameter(torch.ones(4, device=DEV))
+    one.grad = torch.full((4,), 2.0, device=DEV)
+    assert float(autograd.clip_grad_norm_(one, 1.0)) == 4.0 and abs(float(one.grad[0]) - 0.5) < 1e-6
     for bad in (-1.0, float("nan")):
         with pytest.raises(binding.OaaError, match="max_norm"):
             binding.grad_clip([a], bad)

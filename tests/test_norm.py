@@ -128,6 +128,9 @@ REACH = [
     ("last", (40000, 64, 1, 2), 8, torch.bfloat16), ("last", (2, 3, 70, 71), 1, torch.float32),
     ("last", (2, 6, 31, 33), 2, torch.float16), ("last", (700, 20, 1, 1), 5, torch.float32),
     ("last", (4, 200, 90, 91), 200, torch.float16), ("last", (1200, 17, 12, 13), 1, torch.float32),
+    # outputs of 64 MB and more, stored past the caches
+    ("planes", (64, 32, 97, 97), 4, torch.float32), ("planes", (512, 32, 33, 65), 4, torch.bfloat16),
+    ("last", (128, 192, 28, 28), 16, torch.float32),
 ]
 
 
