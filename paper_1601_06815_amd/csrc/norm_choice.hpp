@@ -46,13 +46,17 @@ inline bool one_workgroup_can(const GroupNormParams& p) {
 }
 
 // Whether a group goes to one workgroup, forward. The alternative, slices of
-// groups over the device, reads everything twice in two launches. Measured, us,
-// one workgroup first (float32, D = 8, SiLU): 4 groups of 64 KB 5.6 / 8.4, of 128
-// KB 8.8 / 8.4, of 256 KB 14.0 / 8.6; 128 groups of 128 KB 10.8 / 14.4, of 256 KB
-// 18.7 / 21.8; 1024 groups of 399 KB 195 / 260.
+// groups over the device, reads everything twice in two launches. Few groups are
+// bound by one compute unit's arithmetic, so values count, not bytes. Measured,
+// us, one workgroup first (D = 8, SiLU): 4 groups of 16384 float32 values 5.6 /
+// 8.4, of 32768 8.8 / 8.4, of 65536 14.0 / 8.6; of 16384 bfloat16 values 5.7 /
+// 8.7, of 32768 7.7 / 8.8, with GELU 5 of 28855 10.5 / 8.9; 128 groups of 32768
+// float32 values 10.8 / 14.4, of 65536 bfloat16 ones 17.9 / 15.6; 256 of those
+// 22.9 / 23.2; 128 of 338560 float16 values 71 / 50; 1024 groups of 102152 float32
+// values 195 / 260.
 inline bool forward_one_workgroup(const GroupNormParams& p) {
-  const long units = p.D * accesses(p), groups = long(p.B) * p.G;
-  return one_workgroup_can(p) && (units <= 6144 || groups >= 192 || (groups >= 128 && units <= 8192));
+  const long values = p.D * p.S, groups = long(p.B) * p.G;
+  return one_workgroup_can(p) && (values <= 24576 || groups >= 192 || (groups >= 128 && values <= 32768));
 }
 
 // Backward. The alternative takes one launch more, but its lanes are not bound

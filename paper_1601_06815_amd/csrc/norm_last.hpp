@@ -168,11 +168,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void last_forward_ke
     if (works && s < S) held[k] = load<T, V>(xt + s * p.x_row);
   }
   float w[V], bias[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    w[i] = works ? load_param(p.weight, p.param_dtype, c0 + at.col + i, 1.0f) : 0.0f;
-    bias[i] = works ? load_param(p.bias, p.param_dtype, c0 + at.col + i, 0.0f) : 0.0f;
-  }
+  const long c = c0 + (works ? at.col : 0);
+  load_params<V>(p.weight, p.param_dtype, c, 1.0f, w);
+  load_params<V>(p.bias, p.param_dtype, c, 0.0f, bias);
   {
     if (!works) {
 #pragma unroll
@@ -325,9 +323,9 @@ struct Columns {
     for (int i = 0; i < V; ++i) {
       mean[i] = p.mean[b * p.G + g[i]];
       rstd[i] = p.rstd[b * p.G + g[i]];
-      w[i] = load_param(p.weight, p.param_dtype, c0 + i, 1.0f);
-      bias[i] = load_param(p.bias, p.param_dtype, c0 + i, 0.0f);
     }
+    load_params<V>(p.weight, p.param_dtype, c0, 1.0f, w);
+    load_params<V>(p.bias, p.param_dtype, c0, 0.0f, bias);
   }
 };
 

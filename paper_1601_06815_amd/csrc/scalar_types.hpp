@@ -76,6 +76,29 @@ __device__ __forceinline__ float load_param(const void* p, int dtype, long i, fl
   return float(static_cast<const f16*>(p)[i]);
 }
 
+// V neighbouring parameters, all loads issued before the first is converted.
+template <int V>
+__device__ __forceinline__ void load_params(const void* p, int dtype, long i, float absent, float (&out)[V]) {
+  auto all = [&](auto zero) {
+    const decltype(zero)* at = static_cast<const decltype(zero)*>(p) + i;
+    decltype(zero) v[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = at[k];
+#pragma unroll
+    for (int k = 0; k < V; ++k) out[k] = float(v[k]);
+  };
+  if (!p) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) out[k] = absent;
+  } else if (dtype == OAA_FLOAT32) {
+    all(float{});
+  } else if (dtype == OAA_BFLOAT16) {
+    all(bf16{});
+  } else {
+    all(f16{});
+  }
+}
+
 __device__ __forceinline__ void store_param(void* p, int dtype, long i, float f) {
   if (dtype == OAA_FLOAT32)
     static_cast<float*>(p)[i] = f;

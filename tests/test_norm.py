@@ -119,7 +119,8 @@ REACH = [
     ("planes", (50, 12, 137, 131), 4, torch.bfloat16), ("planes", (60, 12, 97, 199), 4, torch.float16),
     ("planes", (1, 4200, 1, 9), 2, torch.float32), ("planes", (40000, 64, 1, 2), 8, torch.float32),
     ("planes", (3, 20, 1, 5), 5, torch.float16), ("planes", (60, 40, 9, 9), 10, torch.bfloat16),
-    ("planes", (70, 30, 3, 700), 2, torch.float16), ("planes", (200, 6, 5, 7), 2, torch.float32),
+    ("planes", (3, 2000, 1, 3), 1, torch.float32), ("planes", (220, 2000, 1, 3), 1, torch.float32),
+    ("planes", (220, 1000, 1, 3), 1, torch.float32), ("planes", (70, 30, 3, 700), 2, torch.float16), ("planes", (200, 6, 5, 7), 2, torch.float32),
     ("last", (2, 8, 5, 5), 2, torch.float32), ("last", (2, 32, 24, 25), 4, torch.float32),
     ("last", (300, 32, 28, 28), 4, torch.float32), ("last", (300, 32, 28, 27), 4, torch.bfloat16),
     ("last", (150, 64, 40, 41), 8, torch.float32), ("last", (150, 64, 50, 51), 8, torch.bfloat16),
