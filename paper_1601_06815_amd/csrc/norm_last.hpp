@@ -25,8 +25,6 @@
 // the mean is from 0.
 #pragma once
 
-#include <algorithm>
-
 #include "norm_common.hpp"
 #include "tile_common.hpp"
 

@@ -26,8 +26,6 @@
 // the mean is from 0.
 #pragma once
 
-#include <algorithm>
-
 #include "norm_common.hpp"
 
 namespace oaa {
@@ -583,7 +581,8 @@ hipError_t forward_groups(const GroupNormParams& p, hipStream_t s) {
 // none holds it, more accesses in registers cost waves or spill: 1024 groups of
 // 25544 accesses took 196 us with 12 a thread, 195 with 8, 212 with 16, 264 with
 // 20, and 309 with 512 threads of 50; 4096 groups of 2916 took 71 us on 512
-// threads of 8 and 75 on 256 of 16.
+// threads of 8 and 75 on 256 of 16. In 16 bits, twice the values an access, 12
+// spill: 1024 groups of 12776 accesses took 132 us with 12, 115 with 8, 118 with 6.
 template <typename T, int ACT, int V>
 hipError_t forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s) {
   const long units = p.D * accesses(p), groups = long(p.B) * p.G;
@@ -591,7 +590,7 @@ hipError_t forward(const GroupNormParams& p, const NormCut& cut, hipStream_t s) 
     if (units <= 64 * 4) return forward_groups<T, ACT, V, 64, 4>(p, s);
     if (units <= 256 * 4) return forward_groups<T, ACT, V, 256, 4>(p, s);
     if (units <= 512 * 8) return forward_groups<T, ACT, V, 512, 8>(p, s);
-    return forward_groups<T, ACT, V, 1024, 12>(p, s);
+    return forward_groups<T, ACT, V, 1024, sizeof(T) == 4 ? 12 : 8>(p, s);
   }
   double2* sums = reinterpret_cast<double2*>(p.ws);
   const unsigned blocks = unsigned(cut.count * groups);
