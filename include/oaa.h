@@ -327,7 +327,8 @@ typedef enum {
 /* Element strides of one tensor: between images, and (channels last) between
  * positions. Both 0: dense. In planes row must be 0 or S. A tensor that is
  * written must not overlap itself; one that is read may (image = 0 repeats
- * one image). */
+ * one image, row = 0 one position; one position of one image for all, which
+ * would be 0 and 0, cannot be described). */
 typedef struct {
   long long image, row;
 } oaa_strides_t;

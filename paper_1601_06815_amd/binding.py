@@ -441,7 +441,8 @@ def _is_dense(shape, strides):
 def _layout_of(shape, strides, name, want=None):
     """(layout, S, image stride, row stride) of a tensor [B, C, ...], in planes or
     channels last with any strides between positions and images; `want`: only
-    this layout will do (one position or one channel is both)."""
+    this layout will do (one position or one channel is both). One vector over all
+    images and positions is refused: the description's strides 0 and 0 mean dense."""
     if len(shape) < 2:
         raise ValueError(f"{name} must have shape [B, C, ...], got {tuple(shape)}")
     C = shape[1]
@@ -462,7 +463,10 @@ def _layout_of(shape, strides, name, want=None):
     if want != LAYOUT_CHANNELS_LAST and step in (None, 1) and (C == 1 or strides[1] == S):
         return LAYOUT_PLANES, S, image, S
     if want != LAYOUT_PLANES and (C == 1 or strides[1] == 1):
-        return LAYOUT_CHANNELS_LAST, S, image, C if step is None else step
+        row = C if step is None else step
+        if image == 0 and row == 0 and S:
+            raise ValueError(f"{name}: strides {strides} of {tuple(shape)} repeat one position of one image everywhere")
+        return LAYOUT_CHANNELS_LAST, S, image, row
     kind = {None: "planes or channels last", LAYOUT_PLANES: "planes", LAYOUT_CHANNELS_LAST: "channels last"}[want]
     raise ValueError(f"{name}: strides {strides} of {tuple(shape)} are not {kind}")
 

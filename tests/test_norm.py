@@ -563,3 +563,57 @@ def test_binding_refuses_on_the_gpu(gpu_lib):
         binding.group_norm_backward(dy, x, 3, w, b, mean[:1], rstd)
     with pytest.raises(ValueError, match="rstd"):
         binding.group_norm_backward(dy, x, 3, w, b, mean, rstd.double())
+
+
+# ---- one vector over all images and positions --------------------------------------
+
+@pytest.mark.parametrize("want", [None, 1])
+@pytest.mark.parametrize("shape,strides", [((3, 6, 4, 5), (0, 1, 0, 0)), ((3, 1, 4, 5), (0, 0, 0, 0)),
+                                           ((3, 1, 4, 5), (0, 1, 0, 0)), ((2, 6, 7), (0, 1, 0)),
+                                           ((2, 3, 1, 5), (0, 1, 9, 0))])
+def test_a_broadcast_vector_is_no_description(shape, strides, want):
+    """Both strides 0 would be read as a dense tensor, past the vector's end."""
+    t = torch.empty(9).as_strided(shape, strides)
+    with pytest.raises(ValueError, match="everywhere"):
+        binding._norm_layout(t, "x", want)
+    x = (shape, (shape[1] * int(np.prod(shape[2:])), 1) + tuple(shape[1] * int(np.prod(shape[k + 1:]))
+                                                                for k in range(2, len(shape))))
+    for args in ((shape, strides, None, None), x + (strides, None), x + (None, strides)):
+        if want is None and shape[1] == 1 and args[1] != strides:
+            continue  # a dense x of one channel is in planes, which these strides are not either
+        with pytest.raises(ValueError):
+            binding._NormCall(*args, torch.float32, None, None, 1, 1e-5, "none")
+    laid = autograd._laid_out(t, want)
+    assert torch.equal(laid, t) and 0 not in [st for st, k in zip(laid.stride(), shape) if k > 1]
+    assert binding._norm_layout(laid, "x", want)[2] == shape[1] * int(np.prod(shape[2:]))
+
+
+def test_one_zero_stride_is_still_described():
+    for shape, strides, found in (((1, 6, 4, 5), (0, 1, 0, 0), (1, 20, 120, 0)), ((3, 6, 1, 1), (0, 1, 0, 0), (1, 1, 0, 6)),
+                                  ((3, 6, 4, 5), (6, 1, 0, 0), (1, 20, 6, 0)), ((3, 6, 4, 5), (0, 1, 30, 6), (1, 20, 0, 6))):
+        t = torch.empty(120).as_strided(shape, strides)
+        assert binding._norm_layout(t, "x", 1) == found
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("C,G", [(6, 3), (1, 1)])
+def test_broadcast_vectors(gpu_lib, C, G):
+    """As x, as the upstream gradient of a sum per channel, and refused as an output."""
+    shape = (3, C, 4, 5)
+    x, _, w, b = make(shape, G, "last", seed=53)
+    x = torch.empty((3, C + 1, 4, 5), device=DEV).to(memory_format=torch.channels_last)[:, :C].copy_(x)
+    weights = torch.linspace(-1.0, 2.0, C, device=DEV)
+    x.requires_grad_()
+    y = autograd.group_norm(x, G, w, b, activation="silu")
+    (got,) = torch.autograd.grad((y.sum((0, 2, 3)) * weights).sum(), x)
+    dy = weights.reshape(1, C, 1, 1).expand(shape)
+    ref = oracle.group_norm_backward(wide(dy), wide(x), G, wide(w), wide(b), activation="silu")[0]
+    rstd = oracle.group_norm_forward(wide(x), G)[2].max()
+    close(got, ref, torch.float32, scale=float(rstd * 1.2 * np.abs(wide(w)).max() * 2.0))
+    vector = torch.linspace(-2.0, 2.0, C, device=DEV).reshape(1, C, 1, 1).expand(shape)
+    close(autograd.group_norm(vector, G, w, b, activation="silu"),
+          oracle.group_norm_forward(wide(vector), G, wide(w), wide(b), activation="silu")[0], torch.float32)
+    for call in (lambda: binding.group_norm_forward(vector, G, w, b),
+                 lambda: binding.group_norm_forward(x.detach(), G, w, b, y=vector)):
+        with pytest.raises(ValueError, match="everywhere"):
+            call()
