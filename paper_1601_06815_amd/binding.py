@@ -618,25 +618,32 @@ class GroupNormRecord:
     def __init__(self, x, num_groups, weight, bias, eps, activation):
         torch = _torch()[0]
         self.index = _device_of(x, weight, bias)
-        # dy comes with x's strides, or is brought to them
+        # dy mostly comes with x's strides
+        self.strides = x.stride()
         self.args = (x.dtype, *_kinds(weight, bias), num_groups, eps, activation)
-        self.call = _norm_call(x.shape, x.stride(), None, x.stride(), *self.args)
+        self.call = _norm_call(x.shape, self.strides, None, self.strides, *self.args)
         self.row = 4 * x.shape[0] * num_groups
         stats = (2 * self.row + 255) // 256 * 256
-        keep = self.call.backward_bytes if self.call.backward_bytes <= _KEPT_BYTES else 0
-        self.ws = stats if keep else None
-        self.buffer = torch.empty(stats + keep, dtype=torch.uint8, device=x.device)
+        self.kept = self.call.backward_bytes if self.call.backward_bytes <= _KEPT_BYTES else 0
+        self.ws = stats
+        self.buffer = torch.empty(stats + self.kept, dtype=torch.uint8, device=x.device)
         self.y = _like(x, self.call)
         at = self.buffer.data_ptr()
         _forward(self.call, self.index, x, weight, bias, self.y, at, at + self.row)
 
     def backward(self, dy, x, weight, bias, buffer, need_x, need_weight, need_bias):
-        """(dx, dweight, dbias) from the buffer as autograd kept it."""
+        """(dx, dweight, dbias) from the tensors as autograd kept them: hooks on
+        saved tensors may bring x back with other strides than it had."""
+        if (x.dtype, *_kinds(weight, bias)) != self.args[:3] or x.shape != dy.shape:
+            raise ValueError("a saved tensor came back with another type or shape")
+        if _device_of(x, weight, bias) != self.index or buffer.get_device() != self.index:
+            raise ValueError(f"a saved tensor came back on another device than cuda:{self.index}")
         call, at = self.call, buffer.data_ptr()
-        if dy.stride() != x.stride():
+        if x.stride() != self.strides or dy.stride() != self.strides:
             call = _norm_call(x.shape, x.stride(), None, dy.stride(), *self.args)
-        return _backward(call, self.index, dy, x, weight, bias, at, at + self.row,
-                         at + self.ws if self.ws is not None else None, need_x, need_weight, need_bias)
+        # another layout may need a larger workspace than was kept
+        ws = at + self.ws if call.backward_bytes <= self.kept and (at + self.ws) % 256 == 0 else None
+        return _backward(call, self.index, dy, x, weight, bias, at, at + self.row, ws, need_x, need_weight, need_bias)
 
 
 NORM_TYPES = {1.0: NORM_SUM, 2.0: NORM_EUCLIDEAN, float("inf"): NORM_MAX}

@@ -617,3 +617,83 @@ def test_broadcast_vectors(gpu_lib, C, G):
                  lambda: binding.group_norm_forward(x.detach(), G, w, b, y=vector)):
         with pytest.raises(ValueError, match="everywhere"):
             call()
+
+
+# ---- saved tensors that come back changed ---------------------------------------------
+
+def slice_of(t):
+    """The same values as every second image's first channels in a larger tensor."""
+    B, C, H, W = t.shape
+    room = torch.zeros((2 * B, C + 3, H, W), dtype=t.dtype, device=t.device)
+    if t.stride(1) == 1:
+        room = room.to(memory_format=torch.channels_last)
+    return room[::2, :C].copy_(t)
+
+
+@pytest.mark.parametrize("before,after", [("last", "planes"), ("planes", "last"), ("slice", "planes"),
+                                          ("last slice", "last"), ("last", "last")])
+def test_backward_describes_the_tensor_it_gets(monkeypatch, lib, before, after):
+    """The description follows the strides of the x that autograd hands back, and
+    the workspace kept at the forward pass serves only what fits in it."""
+    calls = []
+    monkeypatch.setattr(binding, "_device_of", lambda *a: -1)
+    monkeypatch.setattr(binding, "_forward", lambda *a: None)
+    monkeypatch.setattr(binding, "_backward", lambda call, index, dy, x, w, b, mean, rstd, ws, *need: calls.append((call, ws)))
+    # a layer whose backward pass needs a workspace of another size in each layout
+    dense = torch.zeros(8, 16, 96, 96)
+    form = {"planes": dense, "last": lay(dense, "last"), "slice": slice_of(dense), "last slice": slice_of(lay(dense, "last"))}
+    record = binding.GroupNormRecord(form[before], 4, None, None, 1e-5, "silu")
+    x = form[after]
+    record.backward(torch.zeros_like(x), x, None, None, record.buffer, True, False, False)
+    (call, ws), = calls
+    layout, _, image, row = binding._norm_layout(x, "x")
+    assert (call.layout, call.desc.x.image, call.desc.x.row) == (layout, image, row)
+    assert (call.desc.dy.image, call.desc.dy.row) == (image, row)
+    sizes = {k: binding._norm_call(v.shape, v.stride(), None, v.stride(), v.dtype, None, None, 4, 1e-5, "silu").backward_bytes
+             for k, v in form.items()}
+    assert sizes["planes"] != sizes["last"] and call.backward_bytes == sizes[after]
+    at = record.buffer.data_ptr()
+    assert ws is None or at <= ws and ws + call.backward_bytes <= at + record.buffer.numel()
+
+
+def test_backward_refuses_another_tensor(monkeypatch, lib):
+    monkeypatch.setattr(binding, "_device_of", lambda *a: -1)
+    monkeypatch.setattr(binding, "_forward", lambda *a: None)
+    monkeypatch.setattr(binding, "_backward", lambda *a: pytest.fail("launched"))
+    x, w = torch.zeros(2, 6, 4, 4), torch.zeros(6)
+    record = binding.GroupNormRecord(x, 3, w, None, 1e-5, "silu")
+    for dy, bx, bw in ((x, x.bfloat16(), w), (x, x, w.bfloat16()), (x, x, w[:5]), (x, x[:1], w), (x, x, None)):
+        with pytest.raises(ValueError, match="came back"):
+            record.backward(dy, bx, bw, None, record.buffer, True, True, False)
+    with pytest.raises(ValueError, match="another device"):
+        record.index = 1
+        record.backward(x, x, w, None, record.buffer, True, True, False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", ["pinned", "pageable", "repacked"])
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("sliced", [False, True])
+@pytest.mark.parametrize("shape,G", [((3, 12, 11, 10), 4), ((8, 16, 96, 96), 4)], ids=str)
+def test_saved_tensors_elsewhere(gpu_lib, shape, G, layout, sliced, how):
+    """Gradients with the saved tensors moved to the host and back, or packed
+    into other memory at any address, are those without."""
+    x, dy, w, b = make(shape, G, layout, seed=59)
+    x = slice_of(x) if sliced else x
+    leaves = [t.requires_grad_() for t in (x, w, b)]
+    ref = torch.autograd.grad(autograd.group_norm(*leaves[:1], G, w, b, activation="gelu"), leaves, dy)
+
+    def pack(t):
+        room = torch.empty(t.numel() + 4, dtype=t.dtype, device=DEV)
+        return room[4:].view(t.shape).copy_(t)
+
+    hooks = {"pinned": lambda: torch.autograd.graph.save_on_cpu(pin_memory=True),
+             "pageable": lambda: torch.autograd.graph.save_on_cpu(),
+             "repacked": lambda: torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t)}[how]
+    with hooks():
+        y = autograd.group_norm(x, G, w, b, activation="gelu")
+    for upstream in (dy, lay(dy, "planes"), lay(dy, "last")):
+        got = torch.autograd.grad(y, leaves, upstream, retain_graph=True)
+        # the layouts sum in different orders; the sums of up to 74 thousand terms have either sign
+        for g, r in zip(got, ref):
+            close(g, wide(r), torch.float32, tol=3e-5)
