@@ -24,6 +24,7 @@ the gradients that the backward passes left in a network's parameters.
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 
@@ -127,8 +128,10 @@ def group_norm(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none
     last, and y like it; parameters are float32 or of x's type."""
     if not x.is_contiguous():
         x = _laid_out(x)
-    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
-                                    (bias is not None and bias.requires_grad)):
+    # forward-mode derivatives are refused by the function, not dropped
+    if forward_ad._current_level >= 0 or torch.is_grad_enabled() and (
+            x.requires_grad or (weight is not None and weight.requires_grad) or
+            (bias is not None and bias.requires_grad)):
         return GroupNormFunction.apply(x, weight, bias, num_groups, eps, activation)
     return binding.group_norm_forward(x, num_groups, weight, bias, eps, activation, stats=False)[0]
 

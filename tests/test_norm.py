@@ -12,6 +12,7 @@ rstd |t|, so that is its magnitude.
 import numpy as np
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from oracle import norm as oracle
 from paper_1601_06815_amd import autograd, binding
@@ -697,3 +698,34 @@ def test_saved_tensors_elsewhere(gpu_lib, shape, G, layout, sliced, how):
         # the layouts sum in different orders; the sums of up to 74 thousand terms have either sign
         for g, r in zip(got, ref):
             close(g, wide(r), torch.float32, tol=3e-5)
+
+
+# ---- forward-mode derivatives ----------------------------------------------------------
+
+def refuses_tangents(x, w, b):
+    with forward_ad.dual_level():
+        for k in range(3):
+            args = [x, w, b]
+            args[k] = forward_ad.make_dual(args[k], torch.ones_like(args[k]))
+            for grad in (False, True):
+                with torch.set_grad_enabled(grad), pytest.raises(NotImplementedError):
+                    autograd.group_norm(args[0], 3, args[1], args[2])
+        return autograd.group_norm(x, 3, w, b)
+
+
+def test_forward_mode_is_refused(monkeypatch):
+    """A dual tensor requires no gradient; its tangent must not get lost."""
+    class Record:
+        def __init__(self, x, *args):
+            self.y, self.buffer = x.clone(), x.new_empty(1)
+
+    monkeypatch.setattr(binding, "GroupNormRecord", Record)
+    monkeypatch.setattr(binding, "group_norm_forward", lambda x, *args, **kwargs: (x.clone(), None, None))
+    refuses_tangents(torch.zeros(2, 6, 4, 4), torch.ones(6), torch.ones(6))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_forward_mode(gpu_lib, layout):
+    x, _, w, b = make((2, 6, 5, 4), 3, layout, seed=61)
+    assert torch.equal(refuses_tangents(x, w, b), autograd.group_norm(x, 3, w, b))
