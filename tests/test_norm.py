@@ -729,3 +729,35 @@ def test_forward_mode_is_refused(monkeypatch):
 def test_forward_mode(gpu_lib, layout):
     x, _, w, b = make((2, 6, 5, 4), 3, layout, seed=61)
     assert torch.equal(refuses_tangents(x, w, b), autograd.group_norm(x, 3, w, b))
+
+
+# ---- the activations alone -------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_gelu_keeps_its_digits(gpu_lib, dtype, layout):
+    """With weights of 0 the pre-activation is the bias, exactly. In float32, Phi
+    adds roundings of 2^-25 (1 - Phi), 2^-25 (the exponential at 1/2), less than
+    that again for its exponent, and 6e-9 of its own: 1.2e-7 in all; below 0 it is
+    held to 3e-5 of itself down to 8 deviations. y and the slope add a rounding of
+    2^-24 each, and the slope's density (z^2 + 4) of them, by its exponent."""
+    from scipy.special import ndtr
+    C = 4096
+    z = torch.linspace(-8.0, 8.0, C, device=DEV)
+    x, dy, w, _ = make((1, C, 2, 2), 4, layout, dtype, seed=67)
+    w.zero_()
+    y, mean, rstd = binding.group_norm_forward(x, 4, w, z, activation="gelu")
+    Z = wide(z)
+    cdf = ndtr(Z)
+    off = np.minimum(1.2e-7, 3e-5 * cdf)
+    ref = (Z * cdf).reshape(1, C, 1, 1)
+    bound = (np.abs(Z) * off).reshape(ref.shape) + np.abs(ref) * (2.0 ** -24 + STEP[dtype] * 1.001) + LEAST[dtype]
+    assert np.all(np.abs(wide(y) - ref) <= bound), float(np.max(np.abs(wide(y) - ref) / bound))
+    dy.zero_()
+    dy[:, :, 0, 0] = 1.0
+    slope = wide(binding.group_norm_backward(dy, x, 4, w, z, mean, rstd, "gelu")[2])
+    density = np.exp(-0.5 * Z * Z) / np.sqrt(2.0 * np.pi)
+    exact = cdf + Z * density
+    bound = off + np.abs(Z) * density * (Z * Z + 4.0) * 2.0 ** -24 + np.abs(exact) * 2.0 ** -24
+    assert np.all(np.abs(slope - exact) <= bound), float(np.max(np.abs(slope - exact) / bound))
