@@ -428,6 +428,11 @@ def _launch(fn, index, *args):
         _check(status)
 
 
+def _written(tensors):
+    """Tell autograd that these tensors, which a graph may have saved, changed."""
+    _torch()[0].autograd.graph.increment_version(tensors)
+
+
 def _is_dense(shape, strides):
     expect = 1
     for k, st in zip(reversed(shape), reversed(strides)):
@@ -576,15 +581,15 @@ def group_norm_forward(x, num_groups, weight=None, bias=None, eps=1e-5, activati
         raise ValueError(f"y must be a {x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
     call = _norm_call(x.shape, x.stride(), None if y is None else y.stride(), None, x.dtype, *_kinds(weight, bias),
                       num_groups, eps, activation)
-    if y is None:
-        y = _like(x, call)
-    if not stats:
-        _forward(call, index, x, weight, bias, y, None, None)
-        return y, None, None
-    mean = torch.empty((x.shape[0], num_groups), dtype=torch.float32, device=x.device)
-    rstd = torch.empty_like(mean)
-    _forward(call, index, x, weight, bias, y, mean.data_ptr(), rstd.data_ptr())
-    return y, mean, rstd
+    out = _like(x, call) if y is None else y
+    mean = rstd = None
+    if stats:
+        mean = torch.empty((x.shape[0], num_groups), dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+    _forward(call, index, x, weight, bias, out, _pointer(mean), _pointer(rstd))
+    if y is not None:
+        _written(y)
+    return out, mean, rstd
 
 
 def group_norm_backward(dy, x, num_groups, weight, bias, mean, rstd, activation="none", need_x=True, need_weight=True,
@@ -721,4 +726,5 @@ def grad_clip(grads, max_norm, norm_type=2.0, out=None):
     _launch(load().oaa_grad_clip, index, len(grads), src.buffer_info()[0], dst.buffer_info()[0],
             sizes.buffer_info()[0], kinds.buffer_info()[0], NORM_TYPES[norm_type], max_norm, norm.data_ptr(),
             ws.data_ptr(), ws.numel())
+    _written(grads if out is None else out)
     return norm

@@ -312,3 +312,29 @@ def test_dense_in_any_order():
 def test_binding_refuses_on_the_cpu():
     with pytest.raises(ValueError, match="on the GPU"):
         binding.grad_norm([torch.zeros(3)])
+
+
+@pytest.mark.gpu
+def test_writes_are_seen_by_autograd(gpu_lib):
+    """A tensor that a graph has saved, clipped in place or written as an output,
+    must not be used changed."""
+    for write in (lambda h: binding.grad_clip([h], 0.01),
+                  lambda h: binding.grad_clip([torch.ones_like(h)], 0.01, out=[h]),
+                  lambda h: binding.group_norm_forward(torch.ones_like(h), 1, y=h)):
+        h = torch.ones((2, 3, 4), device=DEV, requires_grad=True) * 2
+        z = (h * h).sum()
+        version = h._version
+        write(h.detach())
+        assert h._version > version
+        with pytest.raises(RuntimeError, match="inplace"):
+            z.backward()
+    read = torch.ones(5, device=DEV)
+    version = read._version
+    binding.grad_norm([read])
+    binding.grad_clip([read], 1.0, out=[torch.empty_like(read)])
+    assert read._version == version
+    with torch.inference_mode():  # such tensors have no versions
+        inside = torch.ones(5, device=DEV)
+        binding.grad_clip([inside], 1.0)
+        binding.group_norm_forward(torch.ones((2, 3, 4), device=DEV), 1, y=torch.empty((2, 3, 4), device=DEV))
+    assert float(inside[0]) < 0.5
