@@ -389,7 +389,8 @@ oaa_status_t oaa_grad_norm(int count, const void* const* grads, const long long*
 
 /* The same norm, then out[i] = grads[i] k, each rounded once to the type of
  * grads[i]. out[i] is grads[i] (in place: with k = 1 nothing is written) or
- * memory that overlaps no gradient; no two outputs overlap. max_norm >= 0. */
+ * memory that overlaps no gradient; no two outputs overlap (both are checked).
+ * max_norm >= 0. */
 oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out, const long long* sizes,
                            const int* dtypes, oaa_norm_t type, float max_norm, float* norm, void* workspace,
                            size_t workspace_bytes, void* hip_stream);

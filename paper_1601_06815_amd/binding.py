@@ -707,7 +707,8 @@ def grad_norm(grads, norm_type=2.0):
 def grad_clip(grads, max_norm, norm_type=2.0, out=None):
     """oaa_grad_clip on torch's current stream: the tensors scaled by min(1,
     max_norm / (norm + 1e-6)), in place or into ``out`` (tensors of the same
-    shapes, types and strides). Returns the norm before clipping."""
+    shapes, types and strides that overlap neither each other nor a gradient; an
+    output may be its own gradient). Returns the norm before clipping."""
     grads = list(grads)
     index, (src, sizes, kinds), norm, ws = _grad_call(grads, norm_type)
     dst = src

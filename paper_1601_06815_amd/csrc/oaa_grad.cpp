@@ -6,6 +6,8 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <memory>
+#include <new>
 
 #include "grad.hpp"
 #include "oaa_status.hpp"
@@ -26,6 +28,44 @@ struct Lists {
   const long long* sizes;
   const int* dtypes;
 };
+
+// The memory of one output.
+struct Range {
+  uintptr_t begin, end;
+  int tensor;
+};
+
+uintptr_t end_of(const Lists& l, const void* begin, int i) {
+  return reinterpret_cast<uintptr_t>(begin) + uintptr_t(l.sizes[i]) * oaa::dtype_size(l.dtypes[i]);
+}
+
+// Whether no output overlaps another one, or a gradient other than its own in the
+// same place: a chunk could be written before it is read. Sorted by address, outputs
+// that are apart leave each gradient one neighbour to look at.
+oaa_status_t check_apart(const Lists& l) {
+  std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[l.count + 1]);
+  if (!ranges) return fail(OAA_ERR_UNSUPPORTED, "no host memory for %d tensors", l.count);
+  Range *first = ranges.get(), *last = first;
+  bool in_place = true;
+  for (int i = 0; i < l.count; ++i) {
+    if (!l.sizes[i]) continue;
+    *last++ = {reinterpret_cast<uintptr_t>(l.dst[i]), end_of(l, l.dst[i], i), i};
+    in_place = in_place && l.dst[i] == l.src[i];
+  }
+  std::sort(first, last, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  for (const Range* r = first; r + 1 < last; ++r)
+    if (r[1].begin < r->end)
+      return fail(OAA_ERR_INVALID_ARG, "outputs %d and %d overlap", r->tensor, r[1].tensor);
+  if (in_place) return OAA_OK;
+  for (int i = 0; i < l.count; ++i) {
+    if (!l.sizes[i]) continue;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(l.src[i]);
+    const Range* r = std::upper_bound(first, last, begin, [](uintptr_t at, const Range& a) { return at < a.end; });
+    if (r < last && r->begin < end_of(l, l.src[i], i) && !(r->tensor == i && r->begin == begin))
+      return fail(OAA_ERR_INVALID_ARG, "output %d overlaps gradient %d", r->tensor, i);
+  }
+  return OAA_OK;
+}
 
 oaa_status_t check(const Lists& l, oaa_norm_t type, const float* norm, void* ws, size_t ws_bytes) {
   if (l.count < 0) return fail(OAA_ERR_INVALID_ARG, "negative count %d", l.count);
@@ -54,7 +94,7 @@ oaa_status_t check(const Lists& l, oaa_norm_t type, const float* norm, void* ws,
                 need);
   if (reinterpret_cast<uintptr_t>(ws) % oaa::kWorkspaceAlign)
     return fail(OAA_ERR_INVALID_ARG, "workspace pointer is not %zu-byte aligned", oaa::kWorkspaceAlign);
-  return OAA_OK;
+  return l.dst ? check_apart(l) : OAA_OK;
 }
 
 long long chunks_of(long long size, int chunk) { return (size + chunk - 1) / chunk; }

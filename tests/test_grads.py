@@ -338,3 +338,42 @@ def test_writes_are_seen_by_autograd(gpu_lib):
         binding.grad_clip([inside], 1.0)
         binding.group_norm_forward(torch.ones((2, 3, 4), device=DEV), 1, y=torch.empty((2, 3, 4), device=DEV))
     assert float(inside[0]) < 0.5
+
+
+@pytest.mark.parametrize("src,out,sizes,kinds", [
+    ((4096, 8192), (8192, 4096), (4, 4), (0, 0)),  # exchanged
+    ((4096, 8192), (16384, 4096), (4, 4), (0, 0)),  # the second into the first
+    ((4096, 8192), (4096, 4096 + 8), (4, 4), (0, 1)),  # an output inside another
+    ((4096, 4096 + 12), (4096, 4096 + 12), (4, 4), (0, 0)),  # in place, one value in common
+    ((4096, 8192), (4096 + 4, 16384), (4, 4), (0, 0)),  # a step beside its own gradient
+    ((4096, 4096), (4096, 16384), (4, 4), (0, 0)),  # the same gradient, read once in place and once not
+    ((4096, 1 << 20, 8192), (1 << 21, 1 << 22, 4096 + 398), (100, 7, 3), (0, 0, 1)),  # the last value's half
+    ((1 << 20, 4096), (4096 + 8, 1 << 21), (64, 64), (1, 1)),
+    ((4096, 0, 8192), (1 << 20, 0, (1 << 20) + 14), (8, 0, 8), (1, 0, 1)),  # an empty one between
+])
+def test_refused_overlaps(lib, src, out, sizes, kinds):
+    """A tensor that one workgroup would write while another still reads it."""
+    count = len(sizes)
+    (a, n, k), o = arrays(src, sizes, kinds), arrays(out, (), ())[0]
+    with pytest.raises(binding.OaaError, match="overlap") as e:
+        binding.oaa_grad_clip(count, a.buffer_info()[0], o.buffer_info()[0], n.buffer_info()[0], k.buffer_info()[0], 2,
+                              1.0, 256, 512, 1 << 20, None)
+    assert e.value.status == 1
+
+
+@pytest.mark.gpu
+def test_neighbours_are_no_overlap(gpu_lib):
+    """Outputs right beside gradients and each other, in any order, some in place."""
+    room = make([64], [torch.float32], seed=19)[0]
+    refs = wide(room).copy()
+    grads = [room[40:48], room[8:16], room[24:24], room[16:23], room[8:16]]
+    out = [room[40:48], room[23:31], room[12:12], room[0:7], room[48:56]]
+    norm, clipped = oracle.grad_clip([wide(g) for g in grads], 0.1)
+    assert abs(float(binding.grad_clip(grads, 0.1, out=out)) - norm) <= 2e-7 * norm
+    for at, c in zip((40, 23, 12, 0, 48), clipped):
+        refs[at:at + len(c)] = c
+    assert np.all(np.abs(wide(room) - refs) <= 4e-7 * np.abs(refs))
+    with pytest.raises(binding.OaaError, match="overlap"):
+        binding.grad_clip([room[:8], room[8:16]], 0.1, out=[room[8:16], room[:8]])
+    with pytest.raises(binding.OaaError, match="overlap"):
+        binding.grad_clip([room[:8], room[4:12]], 0.1)
