@@ -9,6 +9,7 @@
 #include "group_norm.hpp"
 #include "oaa_status.hpp"
 #include "scalar_types.hpp"
+#include "strided.hpp"
 
 namespace {
 
@@ -32,10 +33,10 @@ oaa_status_t strides(const oaa_group_norm_t* d, const oaa_strides_t& in, bool wr
       return fail(OAA_ERR_UNSUPPORTED, "%s: planes must be dense (row stride %lld, %lld positions)", name, in.row, S);
     im = in.image;
     if (last) r = in.row;
-    const long long span = last ? (S - 1) * r + C : C * S;
     if (im > kMaxElems || r > kMaxElems || (d->B > 1 && im > kMaxElems / d->B) || (last && S > 1 && r > kMaxElems / S))
       return fail(OAA_ERR_UNSUPPORTED, "%s: strides too large (image %lld, row %lld)", name, im, r);
-    if (written && S > 0 && ((last && S > 1 && r < C) || (d->B > 1 && im < span)))
+    const oaa::Strided t = last ? oaa::Strided{d->B, im, S, r, C} : oaa::Strided{d->B, im, 1, 0, C * S};
+    if (written && S > 0 && d->B > 0 && !images_apart(t) && !rows_apart(t))
       return fail(OAA_ERR_INVALID_ARG, "%s is written but overlaps itself (image %lld, row %lld)", name, im, r);
   }
   *image = long(im);

@@ -761,3 +761,58 @@ def test_gelu_keeps_its_digits(gpu_lib, dtype, layout):
     exact = cdf + Z * density
     bound = off + np.abs(Z) * density * (Z * Z + 4.0) * 2.0 ** -24 + np.abs(exact) * 2.0 ** -24
     assert np.all(np.abs(slope - exact) <= bound), float(np.max(np.abs(slope - exact) / bound))
+
+
+# ---- images between each other's rows ----------------------------------------------------
+
+@pytest.fixture(scope="module")
+def strided(tmp_path_factory):
+    """Runs csrc/strided.hpp, plain C++: one line of output per line of input."""
+    import shutil
+    import subprocess
+
+    from paper_1601_06815_amd import build
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no g++")
+    at = tmp_path_factory.mktemp("strided")
+    (at / "t.cpp").write_text(
+        '#include "strided.hpp"\n#include <cstdio>\n'
+        'int main() { oaa::Strided t;\n'
+        '  while (std::scanf("%lld%lld%lld%lld%lld", &t.images, &t.image, &t.rows, &t.row, &t.columns) == 5)\n'
+        '    std::printf("%d\\n", oaa::images_apart(t) || oaa::rows_apart(t)); }\n')
+    subprocess.run([cxx, "-std=c++17", "-I", build.CSRC, str(at / "t.cpp"), "-o", str(at / "t")], check=True)
+    return lambda lines: subprocess.run([str(at / "t")], input="\n".join(" ".join(map(str, v)) for v in lines),
+                                        capture_output=True, text=True, check=True).stdout.split()
+
+
+def elements(images, image, rows, row, columns):
+    return [b * image + s * row + c for b in range(images) for s in range(rows) for c in range(columns)]
+
+
+def test_elements_apart(strided):
+    """What is taken as apart is, and so is every tensor whose images lie after each
+    other or between each other's rows."""
+    import itertools
+    all_ = list(itertools.product((1, 2, 3), range(14), (1, 2, 3), range(14), (1, 2, 3)))
+    for t, got in zip(all_, strided(all_)):
+        values = elements(*t)
+        distinct = len(set(values)) == len(values)
+        assert distinct or got == "0", t
+        B, image, S, row, C = t
+        regular = (S == 1 or row >= C) and (B == 1 or image >= C) and \
+            (B == 1 or S == 1 or image >= (S - 1) * row + C or row >= (B - 1) * image + C)
+        assert (got == "1") == regular, t
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("C", [6, 1])
+def test_images_between_rows(gpu_lib, C):
+    """x and y of shape [B, C, S] as views of [S, B, C], y with a gap of one channel."""
+    x, dy, w, b = make((4, C, 50), 1, "last", seed=71)
+    x, dy = (t.permute(2, 0, 1).contiguous().permute(1, 2, 0) for t in (x, dy))
+    room = torch.full((50, 4, C + 1), 7.0, device=DEV)
+    y = binding.group_norm_forward(x, 1, w, b, activation="silu", y=room[:, :, :C].permute(1, 2, 0))[0]
+    close(y, oracle.group_norm_forward(wide(x), 1, wide(w), wide(b), activation="silu")[0], torch.float32)
+    assert bool((room[:, :, C] == 7.0).all())
+    check(x, dy, 1, w, b, "silu")
