@@ -349,8 +349,10 @@ typedef struct {
  * invalid description, which the calls refuse. */
 size_t oaa_group_norm_workspace_bytes(const oaa_group_norm_t* d, int backward);
 
-/* y from x, into memory that does not overlap it. weight or bias NULL: 1 or 0. mean and rstd ([B][G] float32, for
- * the backward pass) may be NULL, each. The workspace (256-byte aligned; NULL
+/* y from x, into memory that does not overlap it (refused where the two surely
+ * share elements: exactly for equal strides, otherwise where one is dense and the
+ * other begins or ends in it). weight or bias NULL: 1 or 0. mean and rstd ([B][G]
+ * float32, for the backward pass) may be NULL, each. The workspace (256-byte aligned; NULL
  * if none is needed) holds nothing between calls and is free again once the
  * call's work on `stream` is done. Only enqueues work on the stream; validates
  * first. An empty x (B or S = 0) is no work. */
@@ -359,7 +361,7 @@ oaa_status_t oaa_group_norm_forward(const oaa_group_norm_t* d, const void* x, co
                                     void* hip_stream);
 
 /* dx, dweight and dbias from dy, the forward pass's x, weight and bias and its
- * mean and rstd; no output overlaps an input. Each of the three outputs may be NULL (at least one is not).
+ * mean and rstd; no output overlaps an input (dx is checked like y). Each of the three outputs may be NULL (at least one is not).
  * An empty x gives zeros in dweight and dbias. */
 oaa_status_t oaa_group_norm_backward(const oaa_group_norm_t* d, const void* dy, const void* x, const void* weight,
                                      const void* bias, const float* mean, const float* rstd, void* dx, void* dweight,

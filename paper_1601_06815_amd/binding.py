@@ -574,7 +574,7 @@ def _backward(call, index, dy, x, weight, bias, mean, rstd, ws, need_x, need_wei
 def group_norm_forward(x, num_groups, weight=None, bias=None, eps=1e-5, activation="none", y=None, stats=True):
     """oaa_group_norm_forward on torch's current stream of x's device: (y, mean,
     rstd), the last two [B, G] float32 (None without ``stats``). x[B, C, ...]
-    is laid out in planes or channels last, and so is y."""
+    is laid out in planes or channels last, and so is y, whose memory x does not share."""
     torch = _torch()[0]
     index = _device_of(x, weight, bias)
     if y is not None and (y.shape != x.shape or y.dtype != x.dtype or y.get_device() != index):

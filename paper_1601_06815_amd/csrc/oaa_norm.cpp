@@ -99,6 +99,25 @@ oaa_status_t aligned(const void* ptr, int dtype, const char* name) {
   return OAA_OK;
 }
 
+// The strides of one tensor of p.
+struct Tensor {
+  const void* ptr;
+  long image, row;
+  const char* name;
+};
+
+// An output that shares elements with an input would be read after it is written.
+oaa_status_t apart(const oaa::GroupNormParams& p, const Tensor& written, const Tensor& read) {
+  const bool rows = p.last && p.S > 1;
+  auto strided = [&](const Tensor& t) {
+    return rows ? oaa::Strided{p.B, t.image, p.S, t.row, p.C} : oaa::Strided{p.B, t.image, 1, 0, p.C * p.S};
+  };
+  const intptr_t bytes = reinterpret_cast<intptr_t>(read.ptr) - reinterpret_cast<intptr_t>(written.ptr);
+  if (oaa::overlap(strided(written), strided(read), bytes / intptr_t(oaa::dtype_size(p.dtype))))
+    return fail(OAA_ERR_INVALID_ARG, "%s overlaps %s", written.name, read.name);
+  return OAA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -123,6 +142,7 @@ oaa_status_t oaa_group_norm_forward(const oaa_group_norm_t* d, const void* x, co
   if (oaa_status_t st = aligned(rstd, OAA_FLOAT32, "rstd")) return st;
   if (oaa_status_t st = workspace(&p, oaa::group_norm_forward_ws(p), ws, ws_bytes)) return st;
   if (y == x) return fail(OAA_ERR_INVALID_ARG, "y is x: the input is read again after the first results are written");
+  if (oaa_status_t st = apart(p, {y, p.y_image, p.y_row, "y"}, {x, p.x_image, p.x_row, "x"})) return st;
   p.x = x;
   p.weight = weight;
   p.bias = bias;
@@ -158,6 +178,11 @@ oaa_status_t oaa_group_norm_backward(const oaa_group_norm_t* d, const void* dy, 
   if (oaa_status_t st = workspace(&p, oaa::group_norm_backward_ws(p), ws, ws_bytes)) return st;
   if (dx && (dx == x || dx == dy))
     return fail(OAA_ERR_INVALID_ARG, "dx is x or dy: both are read again after the first results are written");
+  if (dx) {
+    const Tensor out{dx, p.dx_image, p.dx_row, "dx"};
+    if (oaa_status_t st = apart(p, out, {x, p.x_image, p.x_row, "x"})) return st;
+    if (oaa_status_t st = apart(p, out, {dy, p.dy_image, p.dy_row, "dy"})) return st;
+  }
   p.x = x;
   p.dy = dy;
   p.weight = weight;

@@ -816,3 +816,87 @@ def test_images_between_rows(gpu_lib, C):
     close(y, oracle.group_norm_forward(wide(x), 1, wide(w), wide(b), activation="silu")[0], torch.float32)
     assert bool((room[:, :, C] == 7.0).all())
     check(x, dy, 1, w, b, "silu")
+
+
+# ---- outputs in the input's memory -------------------------------------------------------
+
+def test_overlap_by_strides(tmp_path):
+    """csrc/strided.hpp against lists of elements: equal strides exactly, others never
+    without an element in common."""
+    import itertools
+    import shutil
+    import subprocess
+
+    from paper_1601_06815_amd import build
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no g++")
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text('#include "strided.hpp"\n#include <cstdio>\n'
+                   'int main() { long long B, S, C, I, R, J, Q, at;\n'
+                   '  while (std::scanf("%lld%lld%lld%lld%lld%lld%lld%lld", &B, &S, &C, &I, &R, &J, &Q, &at) == 8)\n'
+                   '    std::printf("%d\\n", oaa::overlap({B, I, S, R, C}, {B, J, S, Q, C}, at)); }\n')
+    subprocess.run([cxx, "-std=c++17", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    rng = np.random.default_rng(73)
+    cases = []
+    for B, S, C in itertools.product((1, 2, 3), (1, 2, 4), (1, 2, 3)):
+        written = [(I, R) for I in range(16) for R in range(10)
+                   if len(set(elements(B, I, S, R, C))) == B * S * C
+                   and ((S == 1 or R >= C) and (B == 1 or I >= C)
+                        and (B == 1 or S == 1 or I >= (S - 1) * R + C or R >= (B - 1) * I + C))]
+        for I, R in (written[i] for i in rng.choice(len(written), min(12, len(written)), replace=False)):
+            others = [(I, R)] + [(int(rng.integers(0, 16)), int(rng.integers(0, 10))) for _ in range(3)]
+            cases += [(B, S, C, I, R, J, Q, at) for J, Q in others for at in range(-40, 41)]
+    out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True,
+                         text=True, check=True).stdout.split()
+    assert len(out) == len(cases)
+    for (B, S, C, I, R, J, Q, at), got in zip(cases, out):
+        shared = bool(set(elements(B, I, S, R, C)) & {at + e for e in elements(B, J, S, Q, C)})
+        assert shared or got == "0", (B, S, C, I, R, J, Q, at)
+        if (B == 1 or I == J) and (S == 1 or R == Q):
+            assert (got == "1") == shared, (B, S, C, I, R, J, Q, at)
+
+
+@pytest.mark.parametrize("change,x,y", [
+    (dict(), 4096, 4096 + 4), (dict(), 4096, 4096 - 4), (dict(), 4096, 4096 + 4 * 119),
+    (dict(layout=1), 4096, 4096 + 4), (dict(dtype=1), 4096, 4096 + 2 * 119),
+    (dict(x=(200, 10), y=(200, 10)), 4096, 4096 + 4 * 59),  # slices of one tensor, one channel in common
+    (dict(layout=1, x=(200, 20), y=(200, 20)), 4096, 4096 + 4 * 5),
+    (dict(layout=1, x=(12, 24), y=(12, 24)), 4096, 4096 + 4 * (12 + 3)),
+    (dict(S=1), 4096, 4096 + 4 * 11), (dict(x=(0, 10)), 4096, 4096 + 4 * 59), (dict(y=(90, 10)), 4096, 4096 + 4 * 119),
+])
+def test_refused_outputs_in_the_input(lib, change, x, y):
+    with pytest.raises(binding.OaaError, match="y overlaps x") as e:
+        binding.oaa_group_norm_forward(desc(**change), x, None, None, y, None, None, 1 << 20, 1 << 20, None)
+    assert e.value.status == 1
+    change = {("dx" if k == "y" else k): v for k, v in change.items()}
+    far = 1 << 22
+    for dy, x0, name in ((far, x, "x"), (x, far, "dy")):
+        given = dict(change) if name == "x" else {("dy" if k == "x" else k): v for k, v in change.items()}
+        with pytest.raises(binding.OaaError, match=f"dx overlaps {name}") as e:
+            binding.oaa_group_norm_backward(desc(**given), dy, x0, None, None, 256, 256, y, None, None, 1 << 20,
+                                            1 << 20, None)
+        assert e.value.status == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_outputs_beside_the_input(gpu_lib, layout):
+    """Channels, images and rows of one tensor between those of x."""
+    whole, _, w, b = make((6, 24, 7, 8), 1, layout, seed=79)
+    pairs = [(lambda t: t[:, :6], lambda t: t[:, 6:12]), (lambda t: t[:, 18:], lambda t: t[:, 3:9]),
+             (lambda t: t[::2, :6], lambda t: t[1::2, 2:8]), (lambda t: t[:3, :6], lambda t: t[3:, :6])]
+    if layout == "last":
+        pairs.append((lambda t: t[:, :6, :3], lambda t: t[:, 6:12, 2:5]))
+    for source, target in pairs:
+        room = whole.clone()
+        x, y = source(room), target(room)
+        ref = oracle.group_norm_forward(wide(x), 3, wide(w)[:6], wide(b)[:6], 1e-5, "silu")[0]
+        binding.group_norm_forward(x, 3, w[:6], b[:6], activation="silu", y=y)
+        close(y, ref, torch.float32)
+        target(room).copy_(target(whole))
+        assert torch.equal(room, whole)
+    x = whole[:, :6]
+    for y in (whole[:, 5:11], whole[:, 1:7]):
+        with pytest.raises(binding.OaaError, match="y overlaps x"):
+            binding.group_norm_forward(x, 3, w[:6], b[:6], y=y)
