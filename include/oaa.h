@@ -307,8 +307,9 @@ oaa_status_t oaa_conv_forward_noalloc(oaa_plan_t plan, const float* x, const flo
  *   dx = rstd (t - sum t / n - xh sum (t xh) / n)       (sums over the group)
  *
  * Statistics and sums are held in 32 bits or more whatever the types; every
- * output is rounded once. A value that is not finite makes its own group of
- * its own image NaN and, backward, dweight and dbias of that group's channels.
+ * output is rounded once. A value of x that is not finite makes its own group of
+ * its own image NaN and, backward, dweight of that group's channels and, with an
+ * activation, dbias (without one dbias does not depend on x).
  * The derivative of the ReLU at 0 is 0. */
 typedef enum {
   OAA_LAYOUT_PLANES = 0,       /* element (b, c, s) at b image + c S + s             */
@@ -376,7 +377,7 @@ oaa_status_t oaa_group_norm_backward(const oaa_group_norm_t* d, const void* dy, 
  *
  * Sums are held in 64 bits and added in a fixed order: equal calls give equal
  * bits. A NaN anywhere gives norm NaN and k NaN; an infinity gives norm
- * infinity and k 0. norm (one float32) stays on the device: nothing waits for
+ * infinity and k 0 (NaN where max_norm is infinite too). norm (one float32) stays on the device: nothing waits for
  * it. No tensors, or only empty ones, have norm 0. */
 typedef enum { OAA_NORM_SUM = 1, OAA_NORM_EUCLIDEAN = 2, OAA_NORM_MAX = 3 } oaa_norm_t;
 

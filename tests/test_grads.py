@@ -377,3 +377,16 @@ def test_neighbours_are_no_overlap(gpu_lib):
         binding.grad_clip([room[:8], room[8:16]], 0.1, out=[room[8:16], room[:8]])
     with pytest.raises(binding.OaaError, match="overlap"):
         binding.grad_clip([room[:8], room[4:12]], 0.1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[50, 60], [50000, 60, 70000]], ids=str)
+def test_infinite_bound(gpu_lib, sizes):
+    """No bound: nothing changes, unless the norm is infinite too, where inf / inf
+    has no value."""
+    grads = make(sizes, [torch.float32], seed=23)
+    before = [g.clone() for g in grads]
+    assert np.isfinite(float(binding.grad_clip(grads, INF)))
+    assert all(torch.equal(g, r) for g, r in zip(grads, before))
+    grads[1][2] = INF
+    assert float(binding.grad_clip(grads, INF)) == INF and all(bool(torch.isnan(g).all()) for g in grads)

@@ -900,3 +900,32 @@ def test_outputs_beside_the_input(gpu_lib, layout):
     for y in (whole[:, 5:11], whole[:, 1:7]):
         with pytest.raises(binding.OaaError, match="y overlaps x"):
             binding.group_norm_forward(x, 3, w[:6], b[:6], y=y)
+
+
+# ---- what is not finite, by activation ---------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,G", [((3, 8, 20, 21), 4), ((2, 8, 150, 151), 4), ((64, 32, 30, 30), 8)], ids=str)
+@pytest.mark.parametrize("act", ACTS)
+def test_what_one_bad_value_reaches(gpu_lib, act, shape, G, layout):
+    """Its group of its image, dweight of the group's channels and, where the
+    activation's slope depends on x, dbias."""
+    x, dy, w, b = make(shape, G, layout, seed=83)
+    D = shape[1] // G
+    clean = binding.group_norm_forward(x, G, w, b, activation=act)
+    cdx, cdw, cdb = binding.group_norm_backward(dy, x, G, w, b, clean[1], clean[2], act)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        bad = x.clone()
+        bad[1, D, 0, 0] = value
+        y, mean, rstd = binding.group_norm_forward(bad, G, w, b, activation=act)
+        dx, dw, db = binding.group_norm_backward(dy, bad, G, w, b, mean, rstd, act)
+        inside = torch.zeros_like(x, dtype=torch.bool)
+        inside[1, D:2 * D] = True
+        for got, ref in ((y, clean[0]), (dx, cdx)):
+            assert bool(torch.isnan(got[inside]).all()) and torch.equal(got[~inside], ref[~inside])
+        channels = slice(D, 2 * D)
+        assert bool(torch.isnan(dw[channels]).all())
+        assert torch.equal(db, cdb) if act == "none" else bool(torch.isnan(db[channels]).all())
+        for got, ref in ((dw, cdw), (db, cdb)):
+            assert torch.equal(got[2 * D:], ref[2 * D:]) and torch.equal(got[:D], ref[:D])
