@@ -307,7 +307,8 @@ oaa_status_t oaa_conv_forward_noalloc(oaa_plan_t plan, const float* x, const flo
  *   dx = rstd (t - sum t / n - xh sum (t xh) / n)       (sums over the group)
  *
  * Statistics and sums are held in 32 bits or more whatever the types; every
- * output is rounded once. A value of x that is not finite makes its own group of
+ * output is rounded once. x - mean is a float32: a value further than the largest
+ * one from its group's mean overflows. A value of x that is not finite makes its own group of
  * its own image NaN and, backward, dweight of that group's channels and, with an
  * activation, dbias (without one dbias does not depend on x).
  * The derivative of the ReLU at 0 is 0. */
