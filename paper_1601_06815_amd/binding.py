@@ -415,6 +415,14 @@ def _torch():
     return torch, torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
 
 
+@functools.lru_cache(maxsize=None)
+def _written():
+    """torch's call that tells autograd of tensors, which a graph may have saved,
+    that they changed."""
+    import torch
+    return torch.autograd.graph.increment_version
+
+
 def _launch(fn, index, *args):
     """fn(*args, stream) on the current stream of device `index`, with that
     device current: kernels are launched there."""
@@ -426,11 +434,6 @@ def _launch(fn, index, *args):
             status = fn(*args, raw_stream(index))
     if status != OAA_OK:
         _check(status)
-
-
-def _written(tensors):
-    """Tell autograd that these tensors, which a graph may have saved, changed."""
-    _torch()[0].autograd.graph.increment_version(tensors)
 
 
 def _is_dense(shape, strides):
@@ -588,7 +591,7 @@ def group_norm_forward(x, num_groups, weight=None, bias=None, eps=1e-5, activati
         rstd = torch.empty_like(mean)
     _forward(call, index, x, weight, bias, out, _pointer(mean), _pointer(rstd))
     if y is not None:
-        _written(y)
+        _written()(y)
     return out, mean, rstd
 
 
@@ -639,16 +642,21 @@ class GroupNormRecord:
     def backward(self, dy, x, weight, bias, buffer, need_x, need_weight, need_bias):
         """(dx, dweight, dbias) from the tensors as autograd kept them: hooks on
         saved tensors may bring x back with other strides than it had."""
-        if (x.dtype, *_kinds(weight, bias)) != self.args[:3] or x.shape != dy.shape:
+        index, C = self.index, self.call.desc.C
+        if x.dtype != self.args[0] or x.shape != dy.shape:
             raise ValueError("a saved tensor came back with another type or shape")
-        if _device_of(x, weight, bias) != self.index or buffer.get_device() != self.index:
-            raise ValueError(f"a saved tensor came back on another device than cuda:{self.index}")
+        if x.get_device() != index or buffer.get_device() != index:
+            raise ValueError(f"a saved tensor came back on another device than cuda:{index}")
+        for t, kind in ((weight, self.args[1]), (bias, self.args[2])):
+            if (t is None) != (kind is None) or t is not None and (
+                    t.dtype != kind[0] or t.numel() != C or t.get_device() != index or not t.is_contiguous()):
+                raise ValueError("a saved parameter came back with another type, shape, layout or device")
         call, at = self.call, buffer.data_ptr()
         if x.stride() != self.strides or dy.stride() != self.strides:
             call = _norm_call(x.shape, x.stride(), None, dy.stride(), *self.args)
         # another layout may need a larger workspace than was kept
         ws = at + self.ws if call.backward_bytes <= self.kept and (at + self.ws) % 256 == 0 else None
-        return _backward(call, self.index, dy, x, weight, bias, at, at + self.row, ws, need_x, need_weight, need_bias)
+        return _backward(call, index, dy, x, weight, bias, at, at + self.row, ws, need_x, need_weight, need_bias)
 
 
 NORM_TYPES = {1.0: NORM_SUM, 2.0: NORM_EUCLIDEAN, float("inf"): NORM_MAX}
@@ -727,5 +735,5 @@ def grad_clip(grads, max_norm, norm_type=2.0, out=None):
     _launch(load().oaa_grad_clip, index, len(grads), src.buffer_info()[0], dst.buffer_info()[0],
             sizes.buffer_info()[0], kinds.buffer_info()[0], NORM_TYPES[norm_type], max_norm, norm.data_ptr(),
             ws.data_ptr(), ws.numel())
-    _written(grads if out is None else out)
+    _written()(grads if out is None else out)
     return norm
