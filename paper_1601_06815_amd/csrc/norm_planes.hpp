@@ -11,10 +11,10 @@
 // forward and three backward.
 //
 // Measured (float32, SiLU, inputs not in a cache): 4096 groups of 47 KB forward
-// 71 us (5.4 TB/s of what has to move), backward 119 us (4.8); 1024 groups of 409
-// KB, of which registers hold 48 % forward and 24 % backward, 196 us (4.3) and
-// 307 us (4.1), with 1.20 and 1.47 times what has to move through the caches of
-// the dies; four groups of 6.4 MB forward 8 + 13 us.
+// 72 us (5.3 TB/s of what has to move), backward 119 to 124 us (4.6 to 4.8); 1024
+// groups of 409 KB, of which registers hold 48 % forward and 24 % backward, 196 us
+// (4.3) and 306 us (4.1), with 1.20 and 1.47 times what has to move through the
+// caches of the dies; four groups of 6.4 MB forward 8 + 13 us.
 //
 // A row is cut into accesses of V values from its start on, at whatever address
 // that is; the last access of a row whose length is no multiple of V is moved
@@ -610,9 +610,9 @@ hipError_t backward_groups(const GroupNormParams& p, float2* sums, hipStream_t s
   return hipGetLastError();
 }
 
-// The same with x and dy: 4096 groups of 2916 accesses took 121 us on 256
-// threads of 12 and 153 on 512 of 6; 1024 of 25544 took 305 us on 1024 threads of
-// 6, 316 with 4, 322 with 8, 386 on 512 of 16.
+// The same with x and dy, in float32 (16 bits were not measured): 4096 groups of
+// 2916 accesses took 121 us on 256 threads of 12 and 153 on 512 of 6; 1024 of 25544
+// took 305 us on 1024 threads of 6, 316 with 4, 322 with 8, 386 on 512 of 16.
 template <typename T, int ACT, int V>
 hipError_t backward(const GroupNormParams& p, const NormCut& cut, const NormSums& at, hipStream_t s) {
   const long units = p.D * accesses(p);
