@@ -399,6 +399,92 @@ oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out
                            const int* dtypes, oaa_norm_t type, float max_norm, float* norm, void* workspace,
                            size_t workspace_bytes, void* hip_stream);
 
+/* ---- Over the channels: the gated unit ---------------------------------------
+ *
+ * At each position of x (B images of C channels at S positions, or S = 1: B tokens),
+ * with two matrices Wg, Wu [F][C] and biases bg, bu [F]:
+ *
+ *   g = Wg x + bg     u = Wu x + bu     h = act(g) u                     (F channels)
+ *
+ * and, for the upstream gradient dh of h:
+ *
+ *   dg = dh u act'(g)     du = dh act(g)     dx = Wg^T dg + Wu^T du
+ *   dWg = sum dg x^T      dWu = sum du x^T   dbg = sum dg   dbu = sum du
+ *                                            (sums over images and positions)
+ *
+ * Products and sums are held in 32 bits or more whatever the types, and h and the
+ * gradients are rounded once. g and u stay in 32 bits for the backward pass. dg and du
+ * are rounded to the type of x where they enter the products dx and dW: the
+ * matrix cores take both operands in one type, and a rounding of each of many terms
+ * weighs less than that of the result. What is not finite at a position of x makes h and dx
+ * of that position, and dW, what the formulas do; nothing of other positions' h and dx.
+ * Equal calls give equal bits. */
+typedef struct {
+  int B, C, F;      /* images, channels of x, channels of h: B >= 0, C, F >= 1 (up to 2^20) */
+  long long S;      /* positions per image, >= 0 (in planes below 2^21)       */
+  int layout;       /* oaa_layout_t of x, h, dh and dx                        */
+  int dtype;        /* oaa_dtype_t of every tensor but gate and up            */
+  int activation;   /* oaa_activation_t                                       */
+  long long gate_row, up_row; /* elements between rows of Wg, Wu; 0: C, dense */
+  oaa_strides_t x, h, dh, dx;
+} oaa_gated_t;
+
+/* Device workspace a call needs at most, in bytes: of the forward pass, or with
+ * backward != 0 of the backward pass; with any_address == 0 if x and the weights begin
+ * at multiples of 4 bytes (16-bit tensors that do not are copied first, as are rows of
+ * odd length). 0 if none, and for a description that the calls refuse. */
+size_t oaa_gated_workspace_bytes(const oaa_gated_t* d, int backward, int any_address);
+
+/* h from x. gate_bias, up_bias: NULL for 0. gate and up (both, or both NULL): g and u
+ * for the backward pass, float32, dense in the layout of h ([B][F][S], or [B][S][F]). Outputs
+ * overlap neither an input nor each other (refused where their addresses meet,
+ * unless as columns beside each other of rows with the same strides). The
+ * workspace is as for oaa_group_norm_forward. Only enqueues work on the stream;
+ * validates first. An empty x (B or S = 0) is no work. */
+oaa_status_t oaa_gated_forward(const oaa_gated_t* d, const void* x, const void* gate_weight, const void* up_weight,
+                               const void* gate_bias, const void* up_bias, void* h, float* gate, float* up,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The gradients that are not NULL (one at least; both weights' or neither), dense for
+ * the weights and biases. x may be NULL without the weights' gradients, the
+ * weights without dx. An empty x gives zeros in the gradients of weights and biases. */
+oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void* x, const void* gate_weight,
+                                const void* up_weight, const float* gate, const float* up, void* dx,
+                                void* dgate_weight, void* dup_weight, void* dgate_bias, void* dup_bias,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- Dropout, with a mask that is never stored -------------------------------
+ *
+ *   y = residual + (kept ? x / (1 - p) : 0)
+ *
+ * Element i is kept if word i % 4 of the generator Philox4x32-10 at counter i / 4 is
+ * at least p 2^32 (rounded to a whole number). The generator's key is seed[0], and its counter's
+ * upper 64 bits are seed[1], the call's number; i is the element's index in the order
+ * of its layout, (b C + c) S + s in planes or (b S + s) C + c channels last,
+ * whatever the strides. The gradient is the same call on dy without a residual:
+ * dx = kept ? dy / (1 - p) : 0, and that of the residual is dy. A dropped element is
+ * 0 whatever x holds there. Computed in 32 bits and rounded once. */
+typedef struct {
+  int B, C;         /* as above: B >= 0, C >= 1                               */
+  long long S;      /* >= 0                                                   */
+  int layout;       /* oaa_layout_t of x, residual and y                      */
+  int x_dtype;      /* oaa_dtype_t of x                                       */
+  int y_dtype;      /* of residual and y: x_dtype, or one of the two OAA_FLOAT32 */
+  oaa_strides_t x, residual, y;
+} oaa_dropout_t;
+
+/* residual: NULL for none. p in [0, 1]. seed: DEVICE pointer to two 64-bit numbers,
+ * read when the kernel runs, so that a captured call draws another mask once they
+ * change. y may be x or residual itself (same type and strides); otherwise it shares
+ * no memory with them. Fewer than 2^34 - 2^12 elements. Only enqueues work on the
+ * stream; validates first. */
+oaa_status_t oaa_dropout(const oaa_dropout_t* d, const void* x, const void* residual, void* y, double p,
+                         const void* seed, void* hip_stream);
+
+/* used = state, then state's call number + 1, on the device: the seed of the next
+ * call, and of its gradient. Both are device pointers to two 64-bit numbers. */
+oaa_status_t oaa_dropout_next(void* state, void* used, void* hip_stream);
+
 /* Static text for a status code. */
 const char* oaa_status_string(oaa_status_t status);
 

@@ -33,6 +33,9 @@ norm
     Group normalisation with an activation, forward and backward, and the norm
     and clipping of gradients: what stands between such layers and at the end
     of a training step. Not from the paper; written from the formulas.
+block
+    The gated unit over channels, forward and backward, and dropout with its
+    generator: the parts of a feed-forward block. Not from the paper either.
 
 Every function of the layer states the passage it follows. Pins (tests/test_oracle.py)
 tie each function to library routines, closed forms and invariants that are
@@ -45,3 +48,4 @@ from .dft import dft_conv_forward  # noqa: F401
 from . import oaa  # noqa: F401
 from . import oas  # noqa: F401
 from . import norm  # noqa: F401
+from . import block  # noqa: F401

@@ -1,5 +1,6 @@
 """torch.autograd binding of the OaA convolution layer, of group normalisation
-with an activation, and the clipping of a network's gradients.
+with an activation, of the gated unit and dropout, and the clipping of a network's
+gradients.
 
 Training needs the forward convolution and the two backward convolutions
 (arXiv:1601.06815, Section 3.2); ``OaAConv2dFunction`` connects them to
@@ -17,8 +18,11 @@ advances, is unchanged), and recomputes them from the saved tensors
 otherwise.
 
 ``group_norm`` (``GroupNorm`` as a layer) takes the convolution's output in
-planes, or tensors in torch's channels_last layout; ``clip_grad_norm_`` clips
-the gradients that the backward passes left in a network's parameters.
+planes, or tensors in torch's channels_last layout, and so do ``gated``
+(``GatedUnit``), which mixes the channels at each position (tokens [T, C] are
+positions too), and ``dropout`` (``Dropout``), which adds a residual in the same
+pass; ``clip_grad_norm_`` clips the gradients that the backward passes left in a
+network's parameters.
 """
 
 import math
@@ -156,6 +160,129 @@ class GroupNorm(torch.nn.Module):
         if x.dim() < 2 or x.shape[1] != self.C:
             raise ValueError(f"expected x[B,{self.C},...], got {tuple(x.shape)}")
         return group_norm(x, self.G, self.weight, self.bias, self.eps, self.activation)
+
+
+def _rows(weight):
+    """weight[F, C], or a copy, with rows of neighbouring values."""
+    if weight.dim() == 2 and weight.stride(1) == 1 and weight.stride(0) >= weight.shape[1]:
+        return weight
+    return weight.contiguous()
+
+
+def _recorded(*tensors):
+    """Whether autograd has to see a call: forward-mode derivatives are refused by the
+    functions, not dropped."""
+    return forward_ad._current_level >= 0 or torch.is_grad_enabled() and any(
+        t is not None and t.requires_grad for t in tensors)
+
+
+class GatedFunction(torch.autograd.Function):
+    """h = act(gate_weight x + gate_bias) (up_weight x + up_bias)."""
+
+    @staticmethod
+    def forward(ctx, x, gate_weight, up_weight, gate_bias, up_bias, activation):
+        x = _laid_out(x)
+        h, gate, up = binding.gated_forward(x, gate_weight, up_weight, gate_bias, up_bias, activation)
+        ctx.activation = activation
+        ctx.save_for_backward(x, gate_weight, up_weight, gate, up)
+        return h
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh):
+        x, gate_weight, up_weight, gate, up = ctx.saved_tensors
+        # hooks on saved tensors may bring them back with other strides than they had
+        x = _laid_out(x)
+        layout = binding._norm_layout(x, "x")[0]
+        dh, gate, up = (_laid_out(t, layout) for t in (dh, gate, up))
+        need = ctx.needs_input_grad
+        grads = binding.gated_backward(dh, x, _rows(gate_weight), _rows(up_weight), gate, up, ctx.activation, need[0],
+                                       need[1] or need[2], need[3] or need[4])
+        return (*(g if n else None for g, n in zip(grads, need)), None)
+
+
+def gated(x, gate_weight, up_weight, gate_bias=None, up_bias=None, activation="silu"):
+    """act(gate_weight x + gate_bias) (up_weight x + up_bias) over the channels of
+    x[B, C, ...] at each position: [B, F, ...] for weights [F, C], in x's layout.
+    Tokens are x[T, C]. float32, bfloat16 or float16, all of one type."""
+    gate_weight, up_weight = _rows(gate_weight), _rows(up_weight)
+    if _recorded(x, gate_weight, up_weight, gate_bias, up_bias):
+        return GatedFunction.apply(x, gate_weight, up_weight, gate_bias, up_bias, activation)
+    return binding.gated_forward(_laid_out(x), gate_weight, up_weight, gate_bias, up_bias, activation, keep=False)[0]
+
+
+class GatedUnit(torch.nn.Module):
+    """The gated unit from in_channels to hidden_channels as a layer."""
+
+    def __init__(self, in_channels, hidden_channels, bias=True, activation="silu", device="cuda", dtype=torch.float32):
+        super().__init__()
+        if activation not in binding.ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(binding.ACTIVATIONS)}, got {activation!r}")
+        self.C, self.F, self.activation = in_channels, hidden_channels, activation
+        for name in ("gate", "up"):
+            weight = torch.randn(hidden_channels, in_channels, device=device) / math.sqrt(in_channels)
+            self.register_parameter(name + "_weight", torch.nn.Parameter(weight.to(dtype)))
+            self.register_parameter(name + "_bias", torch.nn.Parameter(
+                torch.zeros(hidden_channels, device=device, dtype=dtype)) if bias else None)
+
+    def forward(self, x):
+        if x.dim() < 2 or x.shape[1] != self.C:
+            raise ValueError(f"expected x[B,{self.C},...], got {tuple(x.shape)}")
+        return gated(x, self.gate_weight, self.up_weight, self.gate_bias, self.up_bias, self.activation)
+
+
+class DropoutFunction(torch.autograd.Function):
+    """y = residual + x / (1 - p) where the mask of seed keeps x."""
+
+    @staticmethod
+    def forward(ctx, x, p, seed, residual):
+        x = _laid_out(x)
+        ctx.layout = binding._norm_layout(x, "x")[0]
+        ctx.p, ctx.dtype = p, x.dtype
+        ctx.save_for_backward(seed)
+        return binding.dropout(x, p, seed, None if residual is None else _laid_out(residual, ctx.layout))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        seed, = ctx.saved_tensors
+        dx = None
+        if ctx.needs_input_grad[0]:
+            dx = binding.dropout(_laid_out(dy, ctx.layout), ctx.p, seed, dtype=ctx.dtype)
+        return dx, None, None, dy if ctx.needs_input_grad[3] else None
+
+
+def dropout(x, p, seed, residual=None):
+    """residual + x / (1 - p) where the mask of ``seed`` keeps x, residual elsewhere.
+    seed is an int64 tensor [key, call] on the device (``Dropout`` keeps one); equal
+    seeds give equal masks. x[B, C, ...] is float32, bfloat16 or float16 in planes or
+    channels last (element i of the mask is element i of that layout); residual and
+    the result are of x's type or float32."""
+    if _recorded(x, residual):
+        return DropoutFunction.apply(x, p, seed, residual)
+    x = _laid_out(x)
+    if residual is not None:
+        residual = _laid_out(residual, binding._norm_layout(x, "x")[0])
+    return binding.dropout(x, p, seed, residual)
+
+
+class Dropout(torch.nn.Module):
+    """Dropout with probability p while training. Its state (a key and the number of
+    calls) is a buffer on the device that every call advances there, so that a
+    captured graph draws another mask at each replay."""
+
+    def __init__(self, p=0.5, seed=None, device="cuda"):
+        super().__init__()
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"the probability must be in [0, 1], not {p!r}")
+        self.p = p
+        key = int(torch.randint(0, 1 << 62, (1,))) if seed is None else seed
+        self.register_buffer("state", torch.tensor([key, 0], dtype=torch.int64, device=device))
+
+    def forward(self, x, residual=None):
+        if self.training and self.p > 0.0:
+            return dropout(x, self.p, binding.dropout_next(self.state), residual)
+        return x if residual is None else dropout(x, 0.0, self.state, residual)
 
 
 @torch.no_grad()

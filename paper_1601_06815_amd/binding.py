@@ -1,7 +1,7 @@
 """ctypes binding of liboaa.so (include/oaa.h). Argument marshalling only.
 
 Functions carry the C names and take plain integers for device pointers and
-streams. ``Plan``, ``group_norm_*`` and ``grad_*`` wrap them for torch tensors:
+streams. ``Plan``, ``group_norm_*``, ``gated_*``, ``dropout`` and ``grad_*`` wrap them for torch tensors:
 torch supplies device memory (workspaces are uint8 tensors) and the current
 stream; every step of every pass runs in the library's HIP kernels. There is no fallback: if the library
 is missing, ``load()`` raises.
@@ -50,6 +50,21 @@ class GroupNormDesc(ctypes.Structure):
                 ("x", Strides), ("y", Strides), ("dy", Strides), ("dx", Strides)]
 
 
+class GatedDesc(ctypes.Structure):
+    """oaa_gated_t."""
+    _fields_ = [("B", ctypes.c_int), ("C", ctypes.c_int), ("F", ctypes.c_int), ("S", ctypes.c_longlong),
+                ("layout", ctypes.c_int), ("dtype", ctypes.c_int), ("activation", ctypes.c_int),
+                ("gate_row", ctypes.c_longlong), ("up_row", ctypes.c_longlong),
+                ("x", Strides), ("h", Strides), ("dh", Strides), ("dx", Strides)]
+
+
+class DropoutDesc(ctypes.Structure):
+    """oaa_dropout_t."""
+    _fields_ = [("B", ctypes.c_int), ("C", ctypes.c_int), ("S", ctypes.c_longlong), ("layout", ctypes.c_int),
+                ("x_dtype", ctypes.c_int), ("y_dtype", ctypes.c_int),
+                ("x", Strides), ("residual", Strides), ("y", Strides)]
+
+
 SIGNATURES = {
     "oaa_plan_create": (_c_int, [ctypes.POINTER(_vp), _c_int, _c_int, _c_int, _c_int, _c_int]),
     "oaa_plan_create_tiled": (_c_int, [ctypes.POINTER(_vp), _c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int]),
@@ -75,6 +90,11 @@ SIGNATURES = {
     "oaa_grad_workspace_bytes": (_c_size, [_c_int]),
     "oaa_grad_norm": (_c_int, [_c_int, _vp, _vp, _vp, _c_int, _vp, _vp, _c_size, _vp]),
     "oaa_grad_clip": (_c_int, [_c_int, _vp, _vp, _vp, _vp, _c_int, ctypes.c_float, _vp, _vp, _c_size, _vp]),
+    "oaa_gated_workspace_bytes": (_c_size, [_vp, _c_int, _c_int]),
+    "oaa_gated_forward": (_c_int, [_vp] * 10 + [_c_size, _vp]),
+    "oaa_gated_backward": (_c_int, [_vp] * 13 + [_c_size, _vp]),
+    "oaa_dropout": (_c_int, [_vp] * 4 + [ctypes.c_double, _vp, _vp]),
+    "oaa_dropout_next": (_c_int, [_vp] * 3),
     "oaa_status_string": (ctypes.c_char_p, [_c_int]),
     "oaa_last_error_detail": (ctypes.c_char_p, []),
 }
@@ -241,6 +261,32 @@ def oaa_grad_clip(count, grads, out, sizes, dtypes, norm_type, max_norm, norm, w
                                        workspace_bytes, stream))
 
 
+def oaa_gated_workspace_bytes(desc, backward, any_address):
+    """desc: a GatedDesc or its address."""
+    return load().oaa_gated_workspace_bytes(_address(desc), 1 if backward else 0, 1 if any_address else 0)
+
+
+def oaa_gated_forward(desc, x, gate_weight, up_weight, gate_bias, up_bias, h, gate, up, workspace, workspace_bytes,
+                      stream):
+    return _check(load().oaa_gated_forward(_address(desc), x, gate_weight, up_weight, gate_bias, up_bias, h, gate, up,
+                                           workspace, workspace_bytes, stream))
+
+
+def oaa_gated_backward(desc, dh, x, gate_weight, up_weight, gate, up, dx, dgate_weight, dup_weight, dgate_bias,
+                       dup_bias, workspace, workspace_bytes, stream):
+    return _check(load().oaa_gated_backward(_address(desc), dh, x, gate_weight, up_weight, gate, up, dx, dgate_weight,
+                                            dup_weight, dgate_bias, dup_bias, workspace, workspace_bytes, stream))
+
+
+def oaa_dropout(desc, x, residual, y, p, seed, stream):
+    """desc: a DropoutDesc or its address."""
+    return _check(load().oaa_dropout(_address(desc), x, residual, y, p, seed, stream))
+
+
+def oaa_dropout_next(state, used, stream):
+    return _check(load().oaa_dropout_next(state, used, stream))
+
+
 def _address(desc):
     return desc if isinstance(desc, int) or desc is None else ctypes.addressof(desc)
 
@@ -400,7 +446,7 @@ class Plan:
         return self.workspace[off:off + size].view(torch.complex64)
 
 
-# ---- group normalisation and gradients of torch tensors ------------------------
+# ---- group normalisation, the gated unit, dropout and gradients of torch tensors ---
 
 @functools.lru_cache(maxsize=None)
 def _dtype_codes():
@@ -657,6 +703,198 @@ class GroupNormRecord:
         # another layout may need a larger workspace than was kept
         ws = at + self.ws if call.backward_bytes <= self.kept and (at + self.ws) % 256 == 0 else None
         return _backward(call, index, dy, x, weight, bias, at, at + self.row, ws, need_x, need_weight, need_bias)
+
+
+class _GatedCall:
+    """What a call of the gated unit works out from shapes, strides and types
+    alone: the checks of them, the description and the workspaces' sizes."""
+
+    def __init__(self, shape, strides, dtype, weights, biases, out_strides, dh_strides, activation):
+        codes = _dtype_codes()
+        if dtype not in codes:
+            raise ValueError(f"x must be a float32, bfloat16 or float16 tensor on the GPU, got {dtype}")
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
+        self.layout, S, image, row = _layout_of(shape, strides, "x")
+        if max(shape[:2], default=0) >= 1 << 31:
+            raise ValueError(f"x has shape {tuple(shape)}: images and channels are counted in 32 bits")
+        C = shape[1]
+        F = weights[0][1][0] if len(weights[0][1]) == 2 else 0
+        rows = []
+        for name, (kind, size, stride) in zip(("gate_weight", "up_weight"), weights):
+            if kind != dtype or tuple(size) != (F, C) or F < 1 or F >= 1 << 31:
+                raise ValueError(f"{name} must be a {dtype} tensor of shape (F, {C}), like the other weight, "
+                                 f"got {kind} {tuple(size)}")
+            if (C > 1 and stride[1] != 1) or (F > 1 and stride[0] < C):
+                raise ValueError(f"{name}: strides {tuple(stride)} are not those of rows of {C} neighbouring values")
+            rows.append(stride[0] if F > 1 else C)
+        for name, bias in zip(("gate_bias", "up_bias"), biases):
+            if bias is not None and (bias[0] != dtype or tuple(bias[1]) != (F,)):
+                raise ValueError(f"{name} must be a {dtype} tensor of shape ({F},), got {bias[0]} {tuple(bias[1])}")
+        self.F = F
+        self.out_shape = (shape[0], F, *shape[2:])
+        self.gaps = (image, row) != (C * S, S if self.layout == LAYOUT_PLANES else C)
+        out, dh = ((0, 0) if st is None else _layout_of(self.out_shape, st, name, self.layout)[2:]
+                   for name, st in (("h", out_strides), ("dh", dh_strides)))
+        self.desc = GatedDesc(shape[0], C, F, S, self.layout, codes[dtype], ACTIVATIONS[activation], *rows,
+                              Strides(image, row), Strides(*out), Strides(*dh), Strides(0, 0))
+        self.address = ctypes.addressof(self.desc)
+        self.bytes = [[oaa_gated_workspace_bytes(self.desc, backward, any_address) for any_address in (False, True)]
+                      for backward in (False, True)]
+
+
+_gated_call = functools.lru_cache(maxsize=4096)(_GatedCall)
+
+
+def _gated_args(x, gate_weight, up_weight, gate_bias, up_bias):
+    """The index of the one device that all are on, and the types, shapes and strides
+    of weights and biases."""
+    index = x.get_device()
+    if index < 0:
+        raise ValueError(f"x must be a float32, bfloat16 or float16 tensor on the GPU, got {x.dtype} on {x.device}")
+    for name, t in (("gate_weight", gate_weight), ("up_weight", up_weight), ("gate_bias", gate_bias),
+                    ("up_bias", up_bias)):
+        if t is not None and (t.get_device() != index or (t.dim() == 1 and not t.is_contiguous())):
+            raise ValueError(f"{name} must be on {x.device}, and a bias contiguous")
+    return (index, ((gate_weight.dtype, gate_weight.shape, gate_weight.stride()),
+                    (up_weight.dtype, up_weight.shape, up_weight.stride())),
+            (None if gate_bias is None else (gate_bias.dtype, gate_bias.shape),
+             None if up_bias is None else (up_bias.dtype, up_bias.shape)))
+
+
+def _laid(shape, layout, dtype, device):
+    """A dense tensor of a shape [B, C, ...] in a layout."""
+    torch = _torch()[0]
+    if layout == LAYOUT_PLANES:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return torch.empty((shape[0], *shape[2:], shape[1]), dtype=dtype, device=device).movedim(-1, 1)
+
+
+def _gated_workspace(call, backward, x, gate_weight, up_weight):
+    """(tensor or None, its size)."""
+    odd = (x.data_ptr() | gate_weight.data_ptr() | up_weight.data_ptr()) % 4 != 0
+    need = call.bytes[backward][odd]
+    torch = _torch()[0]
+    return (torch.empty(need, dtype=torch.uint8, device=x.device) if need else None), need
+
+
+def gated_forward(x, gate_weight, up_weight, gate_bias=None, up_bias=None, activation="silu", h=None, keep=True):
+    """oaa_gated_forward on torch's current stream of x's device: (h, gate, up), the
+    last two float32 for the backward pass (None without ``keep``). x[B, C, ...] is laid
+    out in planes or channels last (tokens [T, C] are both), and so is h[B, F, ...];
+    the weights are [F, C] with rows of neighbouring values."""
+    torch = _torch()[0]
+    index, weights, biases = _gated_args(x, gate_weight, up_weight, gate_bias, up_bias)
+    call = _gated_call(x.shape, x.stride(), x.dtype, weights, biases, None if h is None else h.stride(), None,
+                       activation)
+    if h is not None and (tuple(h.shape) != call.out_shape or h.dtype != x.dtype or h.get_device() != index):
+        raise ValueError(f"h must be a {x.dtype} tensor of shape {call.out_shape} on {x.device}")
+    out = _laid(call.out_shape, call.layout, x.dtype, x.device) if h is None else h
+    gate = _laid(call.out_shape, call.layout, torch.float32, x.device) if keep else None
+    up = torch.empty_like(gate) if keep else None
+    ws, need = _gated_workspace(call, False, x, gate_weight, up_weight)
+    _launch(load().oaa_gated_forward, index, call.address, x.data_ptr(), gate_weight.data_ptr(), up_weight.data_ptr(),
+            _pointer(gate_bias), _pointer(up_bias), out.data_ptr(), _pointer(gate), _pointer(up), _pointer(ws), need)
+    if h is not None:
+        _written()(h)
+    return out, gate, up
+
+
+def gated_backward(dh, x, gate_weight, up_weight, gate, up, activation="silu", need_x=True, need_weights=True,
+                   need_biases=True):
+    """oaa_gated_backward on torch's current stream of x's device: (dx, dgate_weight,
+    dup_weight, dgate_bias, dup_bias), None for each that is not needed. gate and up are
+    the forward pass's."""
+    torch = _torch()[0]
+    index, weights, biases = _gated_args(x, gate_weight, up_weight, None, None)
+    call = _gated_call(x.shape, x.stride(), x.dtype, weights, biases, None, dh.stride(), activation)
+    if tuple(dh.shape) != call.out_shape or dh.dtype != x.dtype or dh.get_device() != index:
+        raise ValueError(f"dh must be a {x.dtype} tensor of shape {call.out_shape} on {x.device}")
+    for name, t in (("gate", gate), ("up", up)):
+        if tuple(t.shape) != call.out_shape or t.dtype != torch.float32 or t.get_device() != index or (
+                not (t.is_contiguous() if call.layout == LAYOUT_PLANES else t.movedim(1, -1).is_contiguous())):
+            raise ValueError(f"{name} must be a dense float32 tensor of shape {call.out_shape} on {x.device}, "
+                             "laid out like x")
+    if not (need_x or need_weights or need_biases):
+        return None, None, None, None, None
+    dx = _like(x, call) if need_x else None
+    dw = [torch.empty((call.F, x.shape[1]), dtype=x.dtype, device=x.device) if need_weights else None for _ in range(2)]
+    db = [torch.empty(call.F, dtype=x.dtype, device=x.device) if need_biases else None for _ in range(2)]
+    ws, need = _gated_workspace(call, True, x, gate_weight, up_weight)
+    _launch(load().oaa_gated_backward, index, call.address, dh.data_ptr(), x.data_ptr(), gate_weight.data_ptr(),
+            up_weight.data_ptr(), gate.data_ptr(), up.data_ptr(), _pointer(dx), *map(_pointer, dw), *map(_pointer, db),
+            _pointer(ws), need)
+    return (dx, *dw, *db)
+
+
+class _DropoutCall:
+    """What a call of dropout works out from shapes, strides and types alone."""
+
+    def __init__(self, shape, strides, dtype, residual, y_dtype, y_strides):
+        codes = _dtype_codes()
+        for name, kind in (("x", dtype), ("y", y_dtype)):
+            if kind not in codes:
+                raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor on the GPU, got {kind}")
+        if max(shape[:2], default=0) >= 1 << 31:
+            raise ValueError(f"x has shape {tuple(shape)}: images and channels are counted in 32 bits")
+        self.layout, S, image, row = _layout_of(shape, strides, "x")
+        if residual is not None and residual[0] != y_dtype:
+            raise ValueError(f"residual must be a {y_dtype} tensor like y, got {residual[0]}")
+        r, y = ((0, 0) if st is None else _layout_of(shape, st, name, self.layout)[2:]
+                for name, st in (("residual", residual and residual[1]), ("y", y_strides)))
+        self.desc = DropoutDesc(shape[0], shape[1], S, self.layout, codes[dtype], codes[y_dtype], Strides(image, row),
+                                Strides(*r), Strides(*y))
+        self.address = ctypes.addressof(self.desc)
+
+
+_dropout_call = functools.lru_cache(maxsize=4096)(_DropoutCall)
+
+
+def _check_seed(seed, index, name):
+    if (seed.dtype != _torch()[0].int64 or seed.get_device() != index or tuple(seed.shape) != (2,)
+            or not seed.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int64 tensor (key, call) on cuda:{index}")
+
+
+def dropout(x, p, seed, residual=None, y=None, dtype=None):
+    """oaa_dropout on torch's current stream of x's device: y = residual + x / (1 - p)
+    where the mask of ``seed`` (int64 [key, call] on the device) keeps x, residual
+    elsewhere. x[B, C, ...] is in planes or channels last, residual and y like it; y is
+    of residual's type, of ``dtype``, or of x's. The gradient of x is dropout(dy, p,
+    seed, dtype=x.dtype), with dy in x's layout."""
+    index = x.get_device()
+    if index < 0:
+        raise ValueError(f"x must be a float32, bfloat16 or float16 tensor on the GPU, got {x.dtype} on {x.device}")
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"the probability must be in [0, 1], not {p!r}")
+    _check_seed(seed, index, "seed")
+    for name, t in (("residual", residual), ("y", y)):
+        if t is not None and (t.shape != x.shape or t.get_device() != index):
+            raise ValueError(f"{name} must have x's shape {tuple(x.shape)} on {x.device}")
+    kind = y.dtype if y is not None else dtype or (x if residual is None else residual).dtype
+    if dtype not in (None, kind):
+        raise ValueError(f"y is {kind}, not {dtype}")
+    call = _dropout_call(x.shape, x.stride(), x.dtype, residual if residual is None else (residual.dtype, residual.stride()),
+                         kind, None if y is None else y.stride())
+    out = _laid(x.shape, call.layout, kind, x.device) if y is None else y
+    _launch(load().oaa_dropout, index, call.address, x.data_ptr(), _pointer(residual), out.data_ptr(), p,
+            seed.data_ptr())
+    if y is not None:
+        _written()(y)
+    return out
+
+
+def dropout_next(state):
+    """oaa_dropout_next on torch's current stream: the seed of the next call, a new
+    tensor; state's call number advances by one."""
+    index = state.get_device()
+    if index < 0:
+        raise ValueError(f"state must be on the GPU, not on {state.device}")
+    _check_seed(state, index, "state")
+    used = _torch()[0].empty_like(state)
+    _launch(load().oaa_dropout_next, index, state.data_ptr(), used.data_ptr())
+    _written()(state)
+    return used
 
 
 NORM_TYPES = {1.0: NORM_SUM, 2.0: NORM_EUCLIDEAN, float("inf"): NORM_MAX}

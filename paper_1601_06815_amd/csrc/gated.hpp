@@ -1,0 +1,107 @@
+// Parameter blocks and launchers of the gated unit, shared by the host code and
+// the kernels. Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+
+#include "oaa.h"
+
+namespace oaa {
+
+// One matrix product on the matrix cores, D[j][i] = sum over k of I[i][k] J[j][k],
+// i contiguous in D. The three products of the unit and its gradients, in either
+// layout of x (f: hidden channel, c: channel, t: position):
+//
+//                     i        j       k                              I             J
+//   unit, last        f pair   t       c                              W, k rows     x, k rows
+//   unit, planes      t        f pair  c                              x, k columns  W, k rows
+//   dx, last          c        t       f of gate, f of up             W, k columns  d, k rows
+//   dx, planes        t        c       f of gate, f of up             d, k columns  W, k columns
+//   dW, last          c        f       t of every image               x, k columns  d, k columns
+//   dW, planes        c        f       t of every image               x, k rows     d, k rows
+//
+// "k rows": k is the contiguous index of the operand; "k columns": i or j is.
+// Sums run over `segs` segments of K each (images; gate, then up).
+struct Operand {
+  const void* base;
+  long image;  // bytes between the images of the grid
+  long seg;    // bytes between the segments of the sum
+  long half;   // bytes from gate's operand to up's (the unit's W; d in dW)
+  int ld;      // bytes between rows
+};
+
+struct ProductParams {
+  Operand i, j;
+  int ni, nj;  // of one half
+  int images, halves;
+  int K, segs;
+  int splits;  // the sum's steps are cut into so many parts
+  // D: element strides; partial sums in 32 bits if splits > 1, dense [split][half][image][nj][ni]
+  void* out;
+  long out_image, out_half;
+  long out_ld;
+  // the unit: biases (or null), g and u in 32 bits (or null), [image][nj][ni] like D
+  const void *gate_bias, *up_bias;
+  float *gate, *up;
+  int act;
+};
+
+// Which operands have k contiguous, and which side the pair of W is on (the unit).
+enum ProductKind { kUnitLast, kUnitPlanes, kInputLast, kInputPlanes, kWeightLast, kWeightPlanes };
+
+// D's parts added up in order, rounded to T: `n` values in `outputs` tensors of n / outputs.
+struct JoinParams {
+  const float* part;
+  long n;
+  int splits;
+  void* out[2];
+  int outputs;
+};
+
+// dg and du from dh, g and u: rows x columns of every image, d with `ld` elements a
+// row, its last columns 0. sums: partial sums of dg and du over t (or null).
+struct SlopeParams {
+  int images;
+  long rows;    // last: t, planes: f
+  long columns; // last: f, planes: t
+  const void* dh;
+  long dh_image, dh_row;
+  const float *gate, *up;  // dense
+  void *dgate, *dup;
+  long ld;
+  int act;
+  bool last;
+  float* sums;     // [parts][2][F]
+  long parts;      // last: blocks of rows; planes: images
+  long part_rows;  // last: rows of a block
+};
+
+struct PackParams {  // a strided operand as dense rows of ld elements, 0 beyond its columns
+  const void* in[2];
+  void* out[2];
+  int count;
+  long images, image, rows, row, columns, ld;
+};
+
+// Operands a product can read in place: addresses and row strides of whole 4 bytes
+// (what a load into LDS takes), offsets within a tile below 2^31.
+template <typename T>
+hipError_t launch_product(const ProductParams& p, ProductKind kind, hipStream_t s);
+template <typename T>
+hipError_t launch_slope(const SlopeParams& p, hipStream_t s);
+// The partial sums of launch_slope, rounded to T, into whichever is not null.
+template <typename T>
+hipError_t launch_bias_join(const float* sums, long parts, int F, void* gate, void* up, hipStream_t s);
+template <typename T>
+hipError_t launch_join(const JoinParams& p, hipStream_t s);
+template <typename T>
+hipError_t launch_pack(const PackParams& p, hipStream_t s);
+template <typename T>
+hipError_t launch_zero(void* out, long n, hipStream_t s);
+
+// Parts that the sum of a product is cut into.
+int product_splits(int dtype, ProductKind kind, int ni, int nj, int images, int halves, int K, int segs);
+
+}  // namespace oaa

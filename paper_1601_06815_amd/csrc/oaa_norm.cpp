@@ -10,6 +10,7 @@
 #include "oaa_status.hpp"
 #include "scalar_types.hpp"
 #include "strided.hpp"
+#include "tensor_args.hpp"
 
 namespace {
 
@@ -17,31 +18,12 @@ using oaa::fail;
 using oaa::hip_status;
 
 constexpr long long kMaxInt = 0x7fffffffll;
-constexpr long long kMaxElems = 1ll << 46;  // of one tensor: byte offsets stay far inside 64 bits
+using oaa::kMaxElems;
 
-// The element strides of one tensor of d, or an error. `written`: it must not
-// overlap itself.
+// The element strides of one tensor of d, or an error.
 oaa_status_t strides(const oaa_group_norm_t* d, const oaa_strides_t& in, bool written, const char* name, long* image,
                      long* row) {
-  const bool last = d->layout == OAA_LAYOUT_CHANNELS_LAST;
-  const long long S = d->S, C = d->C;
-  long long r = last ? C : S, im = C * S;
-  if (in.image || in.row) {
-    if (in.image < 0 || in.row < 0)
-      return fail(OAA_ERR_INVALID_ARG, "%s: negative strides (image %lld, row %lld)", name, in.image, in.row);
-    if (!last && in.row && in.row != S)
-      return fail(OAA_ERR_UNSUPPORTED, "%s: planes must be dense (row stride %lld, %lld positions)", name, in.row, S);
-    im = in.image;
-    if (last) r = in.row;
-    if (im > kMaxElems || r > kMaxElems || (d->B > 1 && im > kMaxElems / d->B) || (last && S > 1 && r > kMaxElems / S))
-      return fail(OAA_ERR_UNSUPPORTED, "%s: strides too large (image %lld, row %lld)", name, im, r);
-    const oaa::Strided t = last ? oaa::Strided{d->B, im, S, r, C} : oaa::Strided{d->B, im, 1, 0, C * S};
-    if (written && S > 0 && d->B > 0 && !images_apart(t) && !rows_apart(t))
-      return fail(OAA_ERR_INVALID_ARG, "%s is written but overlaps itself (image %lld, row %lld)", name, im, r);
-  }
-  *image = long(im);
-  *row = long(r);
-  return OAA_OK;
+  return oaa::strides_of({d->B, d->C, d->S, d->layout}, in, written, name, image, row);
 }
 
 oaa_status_t describe(const oaa_group_norm_t* d, oaa::GroupNormParams* p) {
@@ -83,21 +65,11 @@ oaa_status_t describe(const oaa_group_norm_t* d, oaa::GroupNormParams* p) {
 bool empty(const oaa::GroupNormParams& p) { return p.B == 0 || p.S == 0; }
 
 oaa_status_t workspace(oaa::GroupNormParams* p, size_t need, void* ws, size_t bytes) {
-  if (need && (!ws || bytes < need))
-    return fail(OAA_ERR_NO_WORKSPACE, "workspace of %zu bytes is smaller than the %zu needed", ws ? bytes : size_t(0),
-                need);
-  if (need && reinterpret_cast<uintptr_t>(ws) % oaa::kWorkspaceAlign)
-    return fail(OAA_ERR_INVALID_ARG, "workspace pointer is not %zu-byte aligned", oaa::kWorkspaceAlign);
   p->ws = static_cast<char*>(ws);
-  return OAA_OK;
+  return oaa::workspace_fits(need, ws, bytes);
 }
 
-// Pointers address whole elements.
-oaa_status_t aligned(const void* ptr, int dtype, const char* name) {
-  if (reinterpret_cast<uintptr_t>(ptr) % oaa::dtype_size(dtype))
-    return fail(OAA_ERR_INVALID_ARG, "%s is not aligned to its type", name);
-  return OAA_OK;
-}
+using oaa::aligned;
 
 // The strides of one tensor of p.
 struct Tensor {
