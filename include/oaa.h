@@ -413,7 +413,7 @@ oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out
  *                                            (sums over images and positions)
  *
  * Products and sums are held in 32 bits or more whatever the types, and h and the
- * gradients are rounded once. g and u stay in 32 bits for the backward pass. dg and du
+ * gradients are rounded once. g and u are stored in 32 bits for the backward pass, or it makes them again. dg and du
  * are rounded to the type of x where they enter the products dx and dW: the
  * matrix cores take both operands in one type, and a rounding of each of many terms
  * weighs less than that of the result. What is not finite at a position of x makes h and dx
@@ -435,6 +435,11 @@ typedef struct {
  * odd length). 0 if none, and for a description that the calls refuse. */
 size_t oaa_gated_workspace_bytes(const oaa_gated_t* d, int backward, int any_address);
 
+/* Whether the two passes of such a unit take less time when the forward pass stores
+ * g and u (1), or when the backward pass makes them again from x, which also saves
+ * their memory (0). Either way is allowed. */
+int oaa_gated_keeps(const oaa_gated_t* d);
+
 /* h from x. gate_bias, up_bias: NULL for 0. gate and up (both, or both NULL): g and u
  * for the backward pass, float32, dense in the layout of h ([B][F][S], or [B][S][F]). Outputs
  * overlap neither an input nor each other (refused where their addresses meet,
@@ -446,12 +451,13 @@ oaa_status_t oaa_gated_forward(const oaa_gated_t* d, const void* x, const void* 
                                void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* The gradients that are not NULL (one at least; both weights' or neither), dense for
- * the weights and biases. x may be NULL without the weights' gradients, the
- * weights without dx. An empty x gives zeros in the gradients of weights and biases. */
+ * the weights and biases. gate and up: the forward pass's; both NULL: made again, with
+ * the same weights and biases (which are not read otherwise). With gate and up, x may
+ * be NULL without the weights' gradients, and the weights without dx. An empty x gives zeros in the gradients of weights and biases. */
 oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void* x, const void* gate_weight,
-                                const void* up_weight, const float* gate, const float* up, void* dx,
-                                void* dgate_weight, void* dup_weight, void* dgate_bias, void* dup_bias,
-                                void* workspace, size_t workspace_bytes, void* hip_stream);
+                                const void* up_weight, const void* gate_bias, const void* up_bias, const float* gate,
+                                const float* up, void* dx, void* dgate_weight, void* dup_weight, void* dgate_bias,
+                                void* dup_bias, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---- Dropout, with a mask that is never stored -------------------------------
  *

@@ -194,7 +194,7 @@ class GatedFunction(torch.autograd.Function):
         # hooks on saved tensors may bring them back with other strides than they had
         x = _laid_out(x)
         layout = binding._norm_layout(x, "x")[0]
-        dh, gate, up = (_laid_out(t, layout) for t in (dh, gate, up))
+        dh, gate, up = (t if t.dim() == 1 else _laid_out(t, layout) for t in (dh, gate, up))
         need = ctx.needs_input_grad
         grads = binding.gated_backward(dh, x, _rows(gate_weight), _rows(up_weight), gate, up, ctx.activation, need[0],
                                        need[1] or need[2], need[3] or need[4])

@@ -91,8 +91,9 @@ SIGNATURES = {
     "oaa_grad_norm": (_c_int, [_c_int, _vp, _vp, _vp, _c_int, _vp, _vp, _c_size, _vp]),
     "oaa_grad_clip": (_c_int, [_c_int, _vp, _vp, _vp, _vp, _c_int, ctypes.c_float, _vp, _vp, _c_size, _vp]),
     "oaa_gated_workspace_bytes": (_c_size, [_vp, _c_int, _c_int]),
+    "oaa_gated_keeps": (_c_int, [_vp]),
     "oaa_gated_forward": (_c_int, [_vp] * 10 + [_c_size, _vp]),
-    "oaa_gated_backward": (_c_int, [_vp] * 13 + [_c_size, _vp]),
+    "oaa_gated_backward": (_c_int, [_vp] * 15 + [_c_size, _vp]),
     "oaa_dropout": (_c_int, [_vp] * 4 + [ctypes.c_double, _vp, _vp]),
     "oaa_dropout_next": (_c_int, [_vp] * 3),
     "oaa_status_string": (ctypes.c_char_p, [_c_int]),
@@ -272,10 +273,15 @@ def oaa_gated_forward(desc, x, gate_weight, up_weight, gate_bias, up_bias, h, ga
                                            workspace, workspace_bytes, stream))
 
 
-def oaa_gated_backward(desc, dh, x, gate_weight, up_weight, gate, up, dx, dgate_weight, dup_weight, dgate_bias,
-                       dup_bias, workspace, workspace_bytes, stream):
-    return _check(load().oaa_gated_backward(_address(desc), dh, x, gate_weight, up_weight, gate, up, dx, dgate_weight,
-                                            dup_weight, dgate_bias, dup_bias, workspace, workspace_bytes, stream))
+def oaa_gated_keeps(desc):
+    return bool(load().oaa_gated_keeps(_address(desc)))
+
+
+def oaa_gated_backward(desc, dh, x, gate_weight, up_weight, gate_bias, up_bias, gate, up, dx, dgate_weight, dup_weight,
+                       dgate_bias, dup_bias, workspace, workspace_bytes, stream):
+    return _check(load().oaa_gated_backward(_address(desc), dh, x, gate_weight, up_weight, gate_bias, up_bias, gate, up,
+                                            dx, dgate_weight, dup_weight, dgate_bias, dup_bias, workspace,
+                                            workspace_bytes, stream))
 
 
 def oaa_dropout(desc, x, residual, y, p, seed, stream):
@@ -739,6 +745,7 @@ class _GatedCall:
         self.desc = GatedDesc(shape[0], C, F, S, self.layout, codes[dtype], ACTIVATIONS[activation], *rows,
                               Strides(image, row), Strides(*out), Strides(*dh), Strides(0, 0))
         self.address = ctypes.addressof(self.desc)
+        self.keeps = oaa_gated_keeps(self.desc)
         self.bytes = [[oaa_gated_workspace_bytes(self.desc, backward, any_address) for any_address in (False, True)]
                       for backward in (False, True)]
 
@@ -778,11 +785,19 @@ def _gated_workspace(call, backward, x, gate_weight, up_weight):
     return (torch.empty(need, dtype=torch.uint8, device=x.device) if need else None), need
 
 
+@functools.lru_cache(maxsize=None)
+def _no_bias(device):
+    """What stands for an absent bias among what a backward pass needs."""
+    return _torch()[0].empty(0, device=device)
+
+
 def gated_forward(x, gate_weight, up_weight, gate_bias=None, up_bias=None, activation="silu", h=None, keep=True):
     """oaa_gated_forward on torch's current stream of x's device: (h, gate, up), the
-    last two float32 for the backward pass (None without ``keep``). x[B, C, ...] is laid
-    out in planes or channels last (tokens [T, C] are both), and so is h[B, F, ...];
-    the weights are [F, C] with rows of neighbouring values."""
+    last two for the backward pass (None without ``keep``): g and u in float32 or, where
+    the backward pass is to make them again from x (oaa_gated_keeps), the biases, empty
+    tensors for absent ones. x[B, C, ...] is laid out in planes or channels last (tokens
+    [T, C] are both), and so is h[B, F, ...]; the weights are [F, C] with rows of
+    neighbouring values."""
     torch = _torch()[0]
     index, weights, biases = _gated_args(x, gate_weight, up_weight, gate_bias, up_bias)
     call = _gated_call(x.shape, x.stride(), x.dtype, weights, biases, None if h is None else h.stride(), None,
@@ -790,13 +805,17 @@ def gated_forward(x, gate_weight, up_weight, gate_bias=None, up_bias=None, activ
     if h is not None and (tuple(h.shape) != call.out_shape or h.dtype != x.dtype or h.get_device() != index):
         raise ValueError(f"h must be a {x.dtype} tensor of shape {call.out_shape} on {x.device}")
     out = _laid(call.out_shape, call.layout, x.dtype, x.device) if h is None else h
-    gate = _laid(call.out_shape, call.layout, torch.float32, x.device) if keep else None
-    up = torch.empty_like(gate) if keep else None
+    gate = up = None
+    if keep and call.keeps:
+        gate = _laid(call.out_shape, call.layout, torch.float32, x.device)
+        up = torch.empty_like(gate)
     ws, need = _gated_workspace(call, False, x, gate_weight, up_weight)
     _launch(load().oaa_gated_forward, index, call.address, x.data_ptr(), gate_weight.data_ptr(), up_weight.data_ptr(),
             _pointer(gate_bias), _pointer(up_bias), out.data_ptr(), _pointer(gate), _pointer(up), _pointer(ws), need)
     if h is not None:
         _written()(h)
+    if keep and not call.keeps:
+        gate, up = (_no_bias(x.device) if b is None else b for b in (gate_bias, up_bias))
     return out, gate, up
 
 
@@ -804,17 +823,22 @@ def gated_backward(dh, x, gate_weight, up_weight, gate, up, activation="silu", n
                    need_biases=True):
     """oaa_gated_backward on torch's current stream of x's device: (dx, dgate_weight,
     dup_weight, dgate_bias, dup_bias), None for each that is not needed. gate and up are
-    the forward pass's."""
+    the forward pass's; x, weights and biases as they were then."""
     torch = _torch()[0]
-    index, weights, biases = _gated_args(x, gate_weight, up_weight, None, None)
-    call = _gated_call(x.shape, x.stride(), x.dtype, weights, biases, None, dh.stride(), activation)
+    biases = (None, None)
+    if gate.dim() == 1 and up.dim() == 1:
+        biases = tuple(b if b.numel() else None for b in (gate, up))
+        gate = up = None
+    index, weights, kinds = _gated_args(x, gate_weight, up_weight, *biases)
+    call = _gated_call(x.shape, x.stride(), x.dtype, weights, kinds, None, dh.stride(), activation)
     if tuple(dh.shape) != call.out_shape or dh.dtype != x.dtype or dh.get_device() != index:
         raise ValueError(f"dh must be a {x.dtype} tensor of shape {call.out_shape} on {x.device}")
-    for name, t in (("gate", gate), ("up", up)):
-        if tuple(t.shape) != call.out_shape or t.dtype != torch.float32 or t.get_device() != index or (
-                not (t.is_contiguous() if call.layout == LAYOUT_PLANES else t.movedim(1, -1).is_contiguous())):
-            raise ValueError(f"{name} must be a dense float32 tensor of shape {call.out_shape} on {x.device}, "
-                             "laid out like x")
+    if gate is not None:
+        for name, t in (("gate", gate), ("up", up)):
+            if tuple(t.shape) != call.out_shape or t.dtype != torch.float32 or t.get_device() != index or (
+                    not (t.is_contiguous() if call.layout == LAYOUT_PLANES else t.movedim(1, -1).is_contiguous())):
+                raise ValueError(f"{name} must be a dense float32 tensor of shape {call.out_shape} on {x.device}, "
+                                 "laid out like x")
     if not (need_x or need_weights or need_biases):
         return None, None, None, None, None
     dx = _like(x, call) if need_x else None
@@ -822,8 +846,8 @@ def gated_backward(dh, x, gate_weight, up_weight, gate, up, activation="silu", n
     db = [torch.empty(call.F, dtype=x.dtype, device=x.device) if need_biases else None for _ in range(2)]
     ws, need = _gated_workspace(call, True, x, gate_weight, up_weight)
     _launch(load().oaa_gated_backward, index, call.address, dh.data_ptr(), x.data_ptr(), gate_weight.data_ptr(),
-            up_weight.data_ptr(), gate.data_ptr(), up.data_ptr(), _pointer(dx), *map(_pointer, dw), *map(_pointer, db),
-            _pointer(ws), need)
+            up_weight.data_ptr(), *map(_pointer, biases), _pointer(gate), _pointer(up), _pointer(dx),
+            *map(_pointer, dw), *map(_pointer, db), _pointer(ws), need)
     return (dx, *dw, *db)
 
 

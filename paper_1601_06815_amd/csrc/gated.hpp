@@ -46,6 +46,14 @@ struct ProductParams {
   const void *gate_bias, *up_bias;
   float *gate, *up;
   int act;
+  // the unit in the backward pass: from dh (strides of elements) dg and du, of `d_ld`
+  // elements a row, the last ones 0, instead of h; and (or null) their sums over the
+  // positions in parts [product_sum_parts()][2][F]
+  const void* dh;
+  long dh_image, dh_ld;
+  void *dgate, *dup;
+  long d_image, d_ld;
+  float* sums;
 };
 
 // Which operands have k contiguous, and which side the pair of W is on (the unit).
@@ -100,8 +108,5 @@ template <typename T>
 hipError_t launch_pack(const PackParams& p, hipStream_t s);
 template <typename T>
 hipError_t launch_zero(void* out, long n, hipStream_t s);
-
-// Parts that the sum of a product is cut into.
-int product_splits(int dtype, ProductKind kind, int ni, int nj, int images, int halves, int K, int segs);
 
 }  // namespace oaa

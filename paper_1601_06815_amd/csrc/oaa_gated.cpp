@@ -9,6 +9,7 @@
 
 #include "gated.hpp"
 #include "oaa_status.hpp"
+#include "product_choice.hpp"
 #include "scalar_types.hpp"
 #include "strided.hpp"
 #include "tensor_args.hpp"
@@ -122,12 +123,15 @@ struct Room {
   }
 };
 
-// Whether a product reads `rows` rows, `row` elements apart, of `columns` values from
-// `base` on in place; otherwise from a copy. k_rows: the sum goes along the columns.
-bool in_place(const Unit& u, uintptr_t base, long image, long rows, long row, long columns, bool k_rows) {
+// How products use an operand: the sum goes along its rows, or its columns, or both.
+enum Use { kRows = 1, kColumns = 2 };
+
+// Whether products read `rows` rows, `row` elements apart, of `columns` values from
+// `base` on in place; otherwise from a copy.
+bool in_place(const Unit& u, uintptr_t base, long image, long rows, long row, long columns, int use) {
   const long ld = row * u.size;
   if (base % 4 || ld % 4 || image * u.size % 4 || ld > 0x7fffffffl / (kTileOffset + 1)) return false;
-  return k_rows ? columns * u.size % 4 == 0 : row >= columns || rows == 1;
+  return (!(use & kRows) || columns * u.size % 4 == 0) && (!(use & kColumns) || row >= columns || rows == 1);
 }
 
 // An operand where it is, or copied to `room`, 0 in the padding of its rows.
@@ -138,9 +142,9 @@ struct Source {
 };
 
 Source place(const Unit& u, const void* base, long images, long image, long rows, long row,
-             long columns, bool k_rows, Room* room) {
+             long columns, int use, Room* room) {
   if (images == 1) image = 0;
-  if (in_place(u, reinterpret_cast<uintptr_t>(base), image, rows, row, columns, k_rows)) return {base, image, row, false};
+  if (in_place(u, reinterpret_cast<uintptr_t>(base), image, rows, row, columns, use)) return {base, image, row, false};
   const long ld = padded(columns);
   return {room->take(size_t(images) * rows * ld * u.size), rows * ld, ld, true};
 }
@@ -175,11 +179,11 @@ struct Layout {
 };
 
 // Weights are copied together: their rows then lie equally far apart.
-void place_weights(Layout* l, const void* gate_w, const void* up_w, bool k_rows, Room* room) {
+void place_weights(Layout* l, const void* gate_w, const void* up_w, int use, Room* room) {
   const Unit& u = l->u;
   const uintptr_t g = reinterpret_cast<uintptr_t>(gate_w), p = reinterpret_cast<uintptr_t>(up_w);
-  if (u.gate_row == u.up_row && in_place(u, g, 0, u.F, u.gate_row, u.C, k_rows) &&
-      in_place(u, p, 0, u.F, u.up_row, u.C, k_rows)) {
+  if (u.gate_row == u.up_row && in_place(u, g, 0, u.F, u.gate_row, u.C, use) &&
+      in_place(u, p, 0, u.F, u.up_row, u.C, use)) {
     l->gate_w = {gate_w, 0, u.gate_row, false};
     l->up_w = {up_w, 0, u.up_row, false};
     return;
@@ -190,15 +194,20 @@ void place_weights(Layout* l, const void* gate_w, const void* up_w, bool k_rows,
   l->up_w = {room->take(size_t(u.F) * ld * u.size), 0, ld, true};
 }
 
+void place_x(Layout* l, const void* x, int use, Room* room) {
+  const Unit& u = l->u;
+  l->x = u.last ? place(u, x, u.B, u.x_image, u.S, u.x_row, u.C, use, room)
+                : place(u, x, u.B, u.x_image, u.C, u.S, u.S, use, room);
+  l->copy_x = l->x.copied;
+}
+
 Layout forward_layout(const Unit& whole_unit, const void* x, const void* gate_w, const void* up_w, void* ws) {
   Layout l{};
   l.u = collapsed(whole_unit, false);
   const Unit& u = l.u;
   Room room{static_cast<char*>(ws), 0};
-  l.x = u.last ? place(u, x, u.B, u.x_image, u.S, u.x_row, u.C, true, &room)
-               : place(u, x, u.B, u.x_image, u.C, u.S, u.S, false, &room);
-  l.copy_x = l.x.copied;
-  place_weights(&l, gate_w, up_w, true, &room);
+  place_x(&l, x, u.last ? kRows : kColumns, &room);
+  place_weights(&l, gate_w, up_w, kRows, &room);
   l.need = room.used;
   return l;
 }
@@ -244,8 +253,9 @@ hipError_t make_copies(const Layout& l, const void* x, const void* gate_w, const
   return e != hipSuccess ? e : pack(u, &up_w, &l.up_w, 1, 1, 0, u.F, u.up_row, u.C, s);
 }
 
+// remake: g and u are made again from x.
 Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w, const void* up_w, bool need_x,
-                       bool need_w, bool need_b, void* ws) {
+                       bool need_w, bool need_b, bool remake, void* ws) {
   Layout l{};
   l.u = collapsed(whole_unit, true);
   const Unit& u = l.u;
@@ -257,36 +267,52 @@ Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w
   const size_t d_bytes = size_t(u.B) * l.d_image * u.size;
   l.dgate = room.take(d_bytes);
   l.dup = room.take(d_bytes);
+  l.part_rows = std::max(kPartRows, (rows * u.B + kMostParts - 1) / kMostParts);
   if (need_b) {
-    l.part_rows = rows;
-    l.parts = u.B;
-    if (u.last) {
-      l.part_rows = std::max(kPartRows, (rows * u.B + kMostParts - 1) / kMostParts);
-      l.parts = u.B * ((rows + l.part_rows - 1) / l.part_rows);
-    }
+    l.parts = remake ? oaa::product_sum_parts(int(u.size), u.last ? oaa::kUnitLast : oaa::kUnitPlanes, columns, rows, u.B)
+              : u.last ? u.B * ((rows + l.part_rows - 1) / l.part_rows)
+                       : u.B;
     l.sums = static_cast<float*>(room.take(size_t(l.parts) * 2 * u.F * 4));
-  } else {
-    l.part_rows = kPartRows;
   }
+  const int unit_x = u.last ? kRows : kColumns, dw_x = u.last ? kColumns : kRows;
+  if (need_x || remake) place_weights(&l, gate_w, up_w, (need_x ? kColumns : 0) | (remake ? kRows : 0), &room);
+  if (need_w || remake) place_x(&l, x, (need_w ? dw_x : 0) | (remake ? unit_x : 0), &room);
   size_t parts = 0;
   if (need_x) {
-    place_weights(&l, gate_w, up_w, false, &room);
     const ProductKind kind = u.last ? oaa::kInputLast : oaa::kInputPlanes;
     const int ni = int(u.last ? u.C : u.S), nj = int(u.last ? u.S : u.C);
-    l.dx_splits = oaa::product_splits(u.dtype, kind, ni, nj, u.B, 1, u.F, 2);
+    l.dx_splits = oaa::product_splits(int(u.size), kind, ni, nj, u.B, 1, u.F, 2);
     if (l.dx_splits > 1) parts = size_t(l.dx_splits) * u.B * ni * nj * 4;
   }
   if (need_w) {
-    l.x = u.last ? place(u, x, u.B, u.x_image, u.S, u.x_row, u.C, false, &room)
-                 : place(u, x, u.B, u.x_image, u.C, u.S, u.S, true, &room);
-    l.copy_x = l.x.copied;
-    l.dw_splits = oaa::product_splits(u.dtype, u.last ? oaa::kWeightLast : oaa::kWeightPlanes, u.C, u.F, 1, 2,
-                                      int(u.S), u.B);
+    l.dw_splits = oaa::product_splits(int(u.size), u.last ? oaa::kWeightLast : oaa::kWeightPlanes, u.C, u.F, 1, 2, u.S,
+                                      u.B);
     if (l.dw_splits > 1) parts = std::max(parts, size_t(l.dw_splits) * 2 * u.F * u.C * 4);
   }
   if (parts) l.product_parts = static_cast<float*>(room.take(parts));
   l.need = room.used;
   return l;
+}
+
+// The unit's product, forward or (p's dh set by the caller) again in the backward pass.
+ProductParams unit_product(const Layout& l, const void* gate_bias, const void* up_bias) {
+  const Unit& u = l.u;
+  ProductParams p{};
+  const Operand positions = operand(u, l.x, false, 0, 0);
+  const Operand weights = operand(u, l.gate_w, false, bytes_between(l.gate_w.base, l.up_w.base), 0);
+  p.i = u.last ? weights : positions;
+  p.j = u.last ? positions : weights;
+  p.ni = int(u.last ? u.F : u.S);
+  p.nj = int(u.last ? u.S : u.F);
+  p.images = u.B;
+  p.halves = 1;
+  p.K = u.C;
+  p.segs = 1;
+  p.splits = 1;
+  p.gate_bias = gate_bias;
+  p.up_bias = up_bias;
+  p.act = u.act;
+  return p;
 }
 
 // Whether every product has few enough tiles of 32 x 32, less than any uses; images
@@ -377,8 +403,14 @@ size_t oaa_gated_workspace_bytes(const oaa_gated_t* d, int backward, int any_add
   // addresses as far from what a product reads in place as the type allows
   char* const none = nullptr;
   const void* at = any_address && u.size == 2 ? none + 2 : none;
-  return backward ? backward_layout(u, at, at, at, true, true, true, nullptr).need
+  return backward ? std::max(backward_layout(u, at, at, at, true, true, true, false, nullptr).need,
+                             backward_layout(u, at, at, at, true, true, true, true, nullptr).need)
                   : forward_layout(u, at, at, at, nullptr).need;
+}
+
+int oaa_gated_keeps(const oaa_gated_t* d) {
+  Unit u;
+  return !check_size(d, &u) && !oaa::product_remakes(int(u.size), u.C);
 }
 
 oaa_status_t oaa_gated_forward(const oaa_gated_t* d, const void* x, const void* gate_weight, const void* up_weight,
@@ -407,35 +439,21 @@ oaa_status_t oaa_gated_forward(const oaa_gated_t* d, const void* x, const void* 
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (hipError_t e = make_copies(l, x, gate_weight, up_weight, s)) return hip_status(e, "gated unit, copies");
-  ProductParams p{};
-  const Operand tokens = operand(u, l.x, false, 0, 0);
-  const Operand weights = operand(u, l.gate_w, false, bytes_between(l.gate_w.base, l.up_w.base), 0);
-  p.i = u.last ? weights : tokens;
-  p.j = u.last ? tokens : weights;
-  p.ni = int(u.last ? u.F : u.S);
-  p.nj = int(u.last ? u.S : u.F);
-  p.images = u.B;
-  p.halves = 1;
-  p.K = u.C;
-  p.segs = 1;
-  p.splits = 1;
+  ProductParams p = unit_product(l, gate_bias, up_bias);
   p.out = h;
   p.out_image = u.h_image;
   p.out_ld = u.last ? u.h_row : u.S;
-  p.gate_bias = gate_bias;
-  p.up_bias = up_bias;
   p.gate = gate;
   p.up = up;
-  p.act = u.act;
   return hip_status(for_type(u.dtype, [&](auto t) {
     return oaa::launch_product<decltype(t)>(p, u.last ? oaa::kUnitLast : oaa::kUnitPlanes, s);
   }), "gated unit, forward");
 }
 
 oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void* x, const void* gate_weight,
-                                const void* up_weight, const float* gate, const float* up, void* dx,
-                                void* dgate_weight, void* dup_weight, void* dgate_bias, void* dup_bias, void* ws,
-                                size_t ws_bytes, void* stream) {
+                                const void* up_weight, const void* gate_bias, const void* up_bias, const float* gate,
+                                const float* up, void* dx, void* dgate_weight, void* dup_weight, void* dgate_bias,
+                                void* dup_bias, void* ws, size_t ws_bytes, void* stream) {
   Unit whole_unit;
   if (oaa_status_t st = check_size(d, &whole_unit)) return st;
   const Unit& w = whole_unit;
@@ -443,15 +461,18 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
     return fail(OAA_ERR_INVALID_ARG, "all five gradients are NULL");
   if (!dgate_weight != !dup_weight)
     return fail(OAA_ERR_INVALID_ARG, "dgate_weight and dup_weight are wanted together, or neither is");
-  const bool none = empty(w), need_x = dx, need_w = dgate_weight, need_b = dgate_bias || dup_bias;
-  const Pointer pointers[] = {{dh, !none, w.dtype, "dh"}, {x, !none && need_w, w.dtype, "x"},
-                              {gate_weight, !none && need_x, w.dtype, "gate_weight"},
-                              {up_weight, !none && need_x, w.dtype, "up_weight"}, {gate, !none, OAA_FLOAT32, "gate"},
-                              {up, !none, OAA_FLOAT32, "up"}, {dx, false, w.dtype, "dx"},
+  if (!gate != !up) return fail(OAA_ERR_INVALID_ARG, "gate and up are given together, or neither is");
+  const bool none = empty(w), need_x = dx, need_w = dgate_weight, need_b = dgate_bias || dup_bias, remake = !gate;
+  const bool uses_x = !none && (need_w || remake), uses_w = !none && (need_x || remake);
+  const Pointer pointers[] = {{dh, !none, w.dtype, "dh"}, {x, uses_x, w.dtype, "x"},
+                              {gate_weight, uses_w, w.dtype, "gate_weight"},
+                              {up_weight, uses_w, w.dtype, "up_weight"}, {gate_bias, false, w.dtype, "gate_bias"},
+                              {up_bias, false, w.dtype, "up_bias"}, {gate, false, OAA_FLOAT32, "gate"},
+                              {up, false, OAA_FLOAT32, "up"}, {dx, false, w.dtype, "dx"},
                               {dgate_weight, false, w.dtype, "dgate_weight"},
                               {dup_weight, false, w.dtype, "dup_weight"}, {dgate_bias, false, w.dtype, "dgate_bias"},
                               {dup_bias, false, w.dtype, "dup_bias"}};
-  if (oaa_status_t st = check(pointers, 11)) return st;
+  if (oaa_status_t st = check(pointers, 13)) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const long weights = long(w.F) * w.C;
   if (none) {
@@ -469,37 +490,55 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
                         dense(dup_weight, weights, w.size, "dup_weight"), dense(dgate_bias, w.F, w.size, "dgate_bias"),
                         dense(dup_bias, w.F, w.size, "dup_bias")};
   const Memory in[] = {tensor(w, dh, w.F, w.dh_image, w.dh_row, "dh"),
-                       tensor(w, need_w ? x : nullptr, w.C, w.x_image, w.x_row, "x"),
-                       weight(w, need_x ? gate_weight : nullptr, w.gate_row, "gate_weight"),
-                       weight(w, need_x ? up_weight : nullptr, w.up_row, "up_weight"), dense(gate, n, 4, "gate"),
+                       tensor(w, uses_x ? x : nullptr, w.C, w.x_image, w.x_row, "x"),
+                       weight(w, uses_w ? gate_weight : nullptr, w.gate_row, "gate_weight"),
+                       weight(w, uses_w ? up_weight : nullptr, w.up_row, "up_weight"),
+                       dense(remake ? gate_bias : nullptr, w.F, w.size, "gate_bias"),
+                       dense(remake ? up_bias : nullptr, w.F, w.size, "up_bias"), dense(gate, n, 4, "gate"),
                        dense(up, n, 4, "up")};
-  if (oaa_status_t st = apart(out, 5, in, 6)) return st;
-  const size_t need = backward_layout(w, x, gate_weight, up_weight, need_x, need_w, need_b, nullptr).need;
+  if (oaa_status_t st = apart(out, 5, in, 8)) return st;
+  const size_t need = backward_layout(w, x, gate_weight, up_weight, need_x, need_w, need_b, remake, nullptr).need;
   if (oaa_status_t st = oaa::workspace_fits(need, ws, ws_bytes)) return st;
-  const Layout l = backward_layout(w, x, gate_weight, up_weight, need_x, need_w, need_b, ws);
+  const Layout l = backward_layout(w, x, gate_weight, up_weight, need_x, need_w, need_b, remake, ws);
   const Unit& u = l.u;
   (void)hipGetLastError();
 
-  oaa::SlopeParams slope{};
-  slope.images = u.B;
-  slope.rows = u.last ? u.S : u.F;
-  slope.columns = u.last ? u.F : u.S;
-  slope.dh = dh;
-  slope.dh_image = u.dh_image;
-  slope.dh_row = u.last ? u.dh_row : u.S;
-  slope.gate = gate;
-  slope.up = up;
-  slope.dgate = l.dgate;
-  slope.dup = l.dup;
-  slope.ld = l.d_ld;
-  slope.act = u.act;
-  slope.last = u.last;
-  slope.sums = l.sums;
-  slope.parts = l.parts;
-  slope.part_rows = l.part_rows;
   hipError_t e = make_copies(l, x, gate_weight, up_weight, s);
   if (e != hipSuccess) return hip_status(e, "gated unit, copies");
-  e = for_type(u.dtype, [&](auto t) { return oaa::launch_slope<decltype(t)>(slope, s); });
+  const long dh_row = u.last ? u.dh_row : u.S;
+  if (remake) {
+    ProductParams p = unit_product(l, gate_bias, up_bias);
+    p.dh = dh;
+    p.dh_image = u.dh_image;
+    p.dh_ld = dh_row;
+    p.dgate = l.dgate;
+    p.dup = l.dup;
+    p.d_image = l.d_image;
+    p.d_ld = l.d_ld;
+    p.sums = l.sums;
+    e = for_type(u.dtype, [&](auto t) {
+      return oaa::launch_product<decltype(t)>(p, u.last ? oaa::kUnitLast : oaa::kUnitPlanes, s);
+    });
+  } else {
+    oaa::SlopeParams slope{};
+    slope.images = u.B;
+    slope.rows = u.last ? u.S : u.F;
+    slope.columns = u.last ? u.F : u.S;
+    slope.dh = dh;
+    slope.dh_image = u.dh_image;
+    slope.dh_row = dh_row;
+    slope.gate = gate;
+    slope.up = up;
+    slope.dgate = l.dgate;
+    slope.dup = l.dup;
+    slope.ld = l.d_ld;
+    slope.act = u.act;
+    slope.last = u.last;
+    slope.sums = l.sums;
+    slope.parts = l.parts;
+    slope.part_rows = l.part_rows;
+    e = for_type(u.dtype, [&](auto t) { return oaa::launch_slope<decltype(t)>(slope, s); });
+  }
   if (e != hipSuccess) return hip_status(e, "gated unit, slopes");
   if (need_b) {
     e = for_type(u.dtype, [&](auto t) {
@@ -564,15 +603,3 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
 }
 
 }  // extern "C"
-
-namespace oaa {
-
-int product_splits(int dtype, ProductKind, int ni, int nj, int images, int halves, int K, int segs) {
-  const long tiles = long((ni + 127) / 128) * ((nj + 127) / 128) * images * halves;
-  const long step = dtype == OAA_FLOAT32 ? 32 : 64;
-  const long steps = (K + step - 1) / step * segs;
-  const long want = (512 + tiles - 1) / tiles;
-  return int(std::max(1l, std::min({want, steps / 4, 64l})));
-}
-
-}  // namespace oaa

@@ -19,7 +19,9 @@
 
 #include "activation.hpp"
 #include "gated.hpp"
+#include "product_choice.hpp"
 #include "scalar_types.hpp"
+#include "tile_common.hpp"
 
 namespace oaa {
 namespace product {
@@ -90,10 +92,15 @@ struct Tile {
   static constexpr int kLine = R * int(sizeof(T));  // k columns: bytes of one k
   static constexpr int kBlock = sizeof(T) == 2 ? 32 : 64;
 
+  // This wave's loads differ by whole rows (lines), which go into the address of the
+  // memory described; a lane's own offset stays. (32 bits, k columns: the place of a
+  // block changes between lines.)
+  static constexpr int kOffsets = !KROWS && sizeof(T) == 4 ? kMine : 1;
+
   const char* at;  // of the tile's first row (k columns: first column), this segment and image
   long half, seg;
-  int ld, rows;    // rows from the tile's first on (of one half)
-  unsigned offset[kMine];
+  int ld, rows;  // rows from the tile's first on (of one half)
+  unsigned offset[kOffsets];
 
   __device__ __forceinline__ void init(const Operand& o, int image, int which, int first, int n, int wave, int lane) {
     at = static_cast<const char*>(o.base) + long(image) * o.image + long(which) * o.half +
@@ -103,15 +110,13 @@ struct Tile {
     ld = o.ld;
     rows = n - first;
 #pragma unroll
-    for (int m = 0; m < kMine; ++m) {
-      const int q = wave + m * WAVES;
+    for (int m = 0; m < kOffsets; ++m) {
       if constexpr (KROWS) {
-        const int row = min(row_of(8 * q + lane / 8), rows - 1);
-        offset[m] = unsigned(row) * unsigned(ld) + unsigned(((lane & 7) ^ (lane >> 3)) * 16);
+        offset[m] = unsigned(lane >> 3) * unsigned(ld) + unsigned(((lane & 7) ^ (lane >> 3)) * 16);
       } else {
-        const int byte = q * 1024 + lane * 16, k = byte / kLine, in = byte % kLine;
+        const int q = wave + m * WAVES, byte = q * 1024 + lane * 16, k = byte / kLine, in = byte % kLine;
         const int key = sizeof(T) == 2 ? k & 3 : (k >> 2) & 3;
-        offset[m] = unsigned(k) * unsigned(ld) + unsigned(((in / kBlock) ^ key) * kBlock + in % kBlock);
+        offset[m] = unsigned(k - first_line(q)) * unsigned(ld) + unsigned(((in / kBlock) ^ key) * kBlock + in % kBlock);
       }
     }
   }
@@ -120,43 +125,49 @@ struct Tile {
     if constexpr (PAIR) return r / GROUP * (GROUP / 2) + r % (GROUP / 2);
     return r;
   }
+  __device__ __forceinline__ long of_half(int q) const {
+    if constexpr (PAIR) return 8 * q % GROUP >= GROUP / 2 ? half : 0;
+    return 0;
+  }
+  static __device__ __forceinline__ int first_line(int q) { return q * 1024 / kLine; }
 
-  // Loads the step from k0 on of segment s to LDS at `lds`.
-  __device__ __forceinline__ void load(unsigned lds, int s, int k0, int K, int wave, int lane) const {
-    if constexpr (KROWS) {
-      const char* from = at + long(s) * seg + long(k0) * long(sizeof(T));
-      const bool whole = k0 + kStep<T> <= K;
+  // A step to load: from k0 on of segment s.
+  struct Step {
+    const char* from;
+    int left;  // k rows: bytes of a row that the segment still has; k columns: lines
+  };
+  __device__ __forceinline__ Step step(int s, int k0, int K) const {
+    if constexpr (KROWS) return {at + long(s) * seg + long(k0) * long(sizeof(T)), (K - k0) * int(sizeof(T))};
+    return {at + long(s) * seg + long(k0) * ld, K - k0};
+  }
+  static __device__ __forceinline__ bool whole(const Step& t) { return !KROWS || t.left >= kStepBytes; }
+  // Load m of this wave's, of a whole step, to LDS. Rows or lines that there are not, and
+  // what lies beyond the last one's end, come as 0.
+  __device__ __forceinline__ void piece(unsigned lds, const Step& t, int m, int wave) const {
+    const int q = wave + m * WAVES;
+    if (kLoads % WAVES && q >= kLoads) return;
+    const int skip = KROWS ? row_of(8 * q) : first_line(q);
+    const int there = (KROWS ? rows : t.left) - skip;
+    const long bytes = long(there - 1) * ld + (KROWS ? t.left : (rows * int(sizeof(T)) + 3) / 4 * 4);
+    load_16(lds + q * 1024, offset[kOffsets > 1 ? m : 0],
+            resource(t.from + of_half(q) + long(skip) * ld, there > 0 ? bytes : 0));
+  }
+  // All of this wave's of any step.
+  __device__ __forceinline__ void load(unsigned lds, const Step& t, int wave, int lane) const {
+    if (whole(t)) {
 #pragma unroll
-      for (int m = 0; m < kMine; ++m) {
-        const int q = wave + m * WAVES;
-        if (kLoads % WAVES && q >= kLoads) break;
-        const char* base = from;
-        if constexpr (PAIR) base += 8 * q % GROUP >= GROUP / 2 ? half : 0;
-        const intx4 rs = resource(base, 0x7ffffffcl);
-        if (whole) {
-          load_16(lds + q * 1024, offset[m], rs);
-        } else {
-          // the last values of a segment, 4 bytes a lane: nothing beyond K is read
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int word = lane + 64 * e, r = word / 32, piece = (word % 32 / 4) ^ (r & 7);
-            const int k = piece * 16 + word % 4 * 4;
-            const int row = min(row_of(8 * q + r), rows - 1);
-            const bool in = k0 * int(sizeof(T)) + k < K * int(sizeof(T));
-            load_4(lds + q * 1024 + 256 * e, in ? unsigned(row) * unsigned(ld) + unsigned(k) : kNowhere, rs);
-          }
-        }
-      }
-    } else {
-      const char* from = at + long(s) * seg + long(k0) * ld;
-      // to the end of the segment's last line: what lies beyond comes as 0
-      const long bytes = long(K - 1 - k0) * ld + (long(rows) * long(sizeof(T)) + 3) / 4 * 4;
-      const intx4 rs = resource(from, bytes);
-#pragma unroll
-      for (int m = 0; m < kMine; ++m) {
-        const int q = wave + m * WAVES;
-        if (kLoads % WAVES && q >= kLoads) break;
-        load_16(lds + q * 1024, offset[m], rs);
+      for (int m = 0; m < kMine; ++m) piece(lds, t, m, wave);
+      return;
+    }
+    // the last values of a segment, 4 bytes a lane: nothing beyond K is read
+#pragma unroll 1
+    for (int q = wave; q < kLoads; q += WAVES) {
+      const intx4 rs = resource(t.from + of_half(q), 0x7ffffffcl);
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e) {
+        const int word = lane + 64 * e, r = word / 32, k = ((word % 32 / 4) ^ r) * 16 + word % 4 * 4;
+        const int row = min(row_of(8 * q + r), rows - 1);
+        load_4(lds + q * 1024 + 256 * e, k < t.left ? unsigned(row) * unsigned(ld) + unsigned(k) : kNowhere, rs);
       }
     }
   }
@@ -193,9 +204,224 @@ __device__ __forceinline__ floatx4 fragment(unsigned tile, int row, int sub, int
   }
 }
 
+// Rows of RI values in LDS: piece c (16 bytes) of row r is at place c ^ (r % pieces), so
+// that neither 16 rows nor one row's pieces meet in a bank. put: four values of 32 bits
+// (or 16), number `four` of the row.
+template <int RI>
+__device__ __forceinline__ unsigned place(unsigned slab, int r, int c) {
+  constexpr int kPieces = RI / 4;
+  return slab + unsigned(r) * (RI * 4) + unsigned(c ^ (r & (kPieces - 1))) * 16;
+}
+template <int RI>
+__device__ __forceinline__ void put(unsigned slab, int r, int four, floatx4 v) {
+  *reinterpret_cast<__attribute__((address_space(3))) floatx4*>(place<RI>(slab, r, four)) = v;
+}
+template <typename E, int RI>
+__device__ __forceinline__ void put_16(unsigned slab, int r, int four, floatx4 v) {
+  typedef E vec __attribute__((ext_vector_type(4)));
+  constexpr int kPieces = RI / 8;
+  vec w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = E(v[e]);
+  *reinterpret_cast<__attribute__((address_space(3))) vec*>(
+      slab + unsigned(r) * (RI * 2) + unsigned((four / 2) ^ (r & (kPieces - 1))) * 16 + (four & 1) * 8) = w;
+}
+
+template <typename E>
+__device__ __forceinline__ void store_values(E* to, int n, const E (&v)[16 / sizeof(E)]) {
+  constexpr int V = 16 / int(sizeof(E));
+  if (n >= V) {
+    Vec<E, V> w;
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[e] = v[e];
+    *reinterpret_cast<Vec<E, V>*>(to) = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < n) to[e] = v[e];
+  }
+}
+
+// ROWS rows of RI values from LDS to rows j, j + 1, ... < nj of `out`, the first `ni`
+// values of each.
+template <typename E, int RI, int ROWS>
+__device__ __forceinline__ void store_rows(unsigned slab, E* out, long ld, int j, int nj, int ni, int lane) {
+  constexpr int V = 16 / int(sizeof(E)), kPieces = RI / V, kRows = 64 / kPieces;
+  const int c = lane % kPieces, r0 = lane / kPieces;
+#pragma unroll 2
+  for (int r = r0; r < ROWS; r += kRows) {
+    const floatx4 v = *reinterpret_cast<lds_floatx4*>(slab + unsigned(r) * (RI * int(sizeof(E))) +
+                                                      unsigned(c ^ (r & (kPieces - 1))) * 16);
+    if (j + r < nj && c * V < ni) {
+      struct {
+        E e[V];
+      } w = __builtin_bit_cast(decltype(w), v);
+      store_values<E>(out + long(j + r) * ld + c * V, ni - c * V, w.e);
+    }
+  }
+}
+
+// The end of the unit: rows of g and u from LDS become h (and g and u in memory, if the
+// call keeps them), or with dh, in the backward pass, dg and du with their sums over
+// the positions.
+template <typename T, int RI, int ROWS, int PAIR>
+struct UnitEnd {
+  static constexpr int V = 16 / int(sizeof(T)), kPieces = RI / V, kRows = 64 / kPieces;
+  static constexpr int kType = sizeof(T) == 4 ? OAA_FLOAT32 : __is_same(T, bf16) ? OAA_BFLOAT16 : OAA_FLOAT16;
+  const ProductParams& p;
+  const int image, lane;
+  const int c, r0;  // this lane's piece of every row, and its first row
+  const int i, n;   // its first value, and how many there are from there on
+  float gate_bias[V], up_bias[V];  // PAIR 1
+  float sum_g[V], sum_u[V];
+  long part = 0;  // which part of the sums over the positions this wave's are
+
+  __device__ __forceinline__ UnitEnd(const ProductParams& p_, int image_, int first, int lane_)
+      : p(p_), image(image_), lane(lane_), c(lane_ % kPieces), r0(lane_ / kPieces), i(first + c * V), n(p_.ni - i) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      sum_g[e] = sum_u[e] = 0.0f;
+      if constexpr (PAIR == 1) {
+        gate_bias[e] = e < n ? load_param(p.gate_bias, kType, i + e, 0.0f) : 0.0f;
+        up_bias[e] = e < n ? load_param(p.up_bias, kType, i + e, 0.0f) : 0.0f;
+      }
+    }
+  }
+
+  __device__ __forceinline__ void rows(unsigned slab, int j) {
+    switch (p.act) {
+      case OAA_ACT_RELU: return rows_of<OAA_ACT_RELU>(slab, j);
+      case OAA_ACT_SILU: return rows_of<OAA_ACT_SILU>(slab, j);
+      case OAA_ACT_GELU: return rows_of<OAA_ACT_GELU>(slab, j);
+      default: return rows_of<OAA_ACT_NONE>(slab, j);
+    }
+  }
+
+  template <int ACT>
+  __device__ __forceinline__ void rows_of(unsigned slab, int j0) {
+#pragma unroll 1
+    for (int r = r0; r < ROWS; r += kRows) {
+      const int j = j0 + r;
+      float g[V], u[V];
+#pragma unroll
+      for (int k = 0; k < V / 4; ++k) {
+        const floatx4 a = *reinterpret_cast<lds_floatx4*>(place<RI>(slab, r, c * (V / 4) + k));
+        const floatx4 b = *reinterpret_cast<lds_floatx4*>(place<RI>(slab + ROWS * RI * 4, r, c * (V / 4) + k));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          g[4 * k + e] = a[e];
+          u[4 * k + e] = b[e];
+        }
+      }
+      const bool in = j < p.nj && n > 0;
+      if constexpr (PAIR == 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          g[e] += gate_bias[e];
+          u[e] += up_bias[e];
+        }
+      } else {
+        const float bg = in ? load_param(p.gate_bias, kType, j, 0.0f) : 0.0f;
+        const float bu = in ? load_param(p.up_bias, kType, j, 0.0f) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          g[e] += bg;
+          u[e] += bu;
+        }
+      }
+      if (p.dh) {
+        float a = 0.0f, b = 0.0f;  // PAIR 2: of this row
+        if (in) {
+          const T* from = static_cast<const T*>(p.dh) + long(image) * p.dh_image + long(j) * p.dh_ld + i;
+          T dg[V], du[V];
+          float d[V];
+          if (n >= V) {
+            const Vec<T, V> v = load<T, V>(from);
+#pragma unroll
+            for (int e = 0; e < V; ++e) d[e] = float(v[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) d[e] = e < n ? float(from[e]) : 0.0f;
+          }
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float y = e < n ? d[e] * u[e] * act_slope<ACT>(g[e]) : 0.0f, z = e < n ? d[e] * act<ACT>(g[e]) : 0.0f;
+            dg[e] = T(y);
+            du[e] = T(z);
+            if constexpr (PAIR == 1) {
+              sum_g[e] += y;
+              sum_u[e] += z;
+            } else {
+              a += y;
+              b += z;
+            }
+          }
+          // whole pieces: the padding of d's rows is 0
+          const long at = long(image) * p.d_image + long(j) * p.d_ld + i;
+          store_values<T>(static_cast<T*>(p.dgate) + at, V, dg);
+          store_values<T>(static_cast<T*>(p.dup) + at, V, du);
+        }
+        if constexpr (PAIR == 2) {
+          if (p.sums) {
+#pragma unroll
+            for (int m = 1; m < kPieces; m *= 2) {
+              a += __shfl_xor(a, m);
+              b += __shfl_xor(b, m);
+            }
+            if (c == 0 && j < p.nj) {
+              p.sums[(part * 2) * p.nj + j] = a;
+              p.sums[(part * 2 + 1) * p.nj + j] = b;
+            }
+          }
+        }
+      } else if (in) {
+        T h[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[e] = T(act<ACT>(g[e]) * u[e]);
+        store_values<T>(static_cast<T*>(p.out) + long(image) * p.out_image + long(j) * p.out_ld + i, n, h);
+        if (p.gate) {
+          const long at = (long(image) * p.nj + j) * p.ni + i;
+#pragma unroll
+          for (int k = 0; k < V / 4; ++k) {
+            const float a[4] = {g[4 * k], g[4 * k + 1], g[4 * k + 2], g[4 * k + 3]};
+            const float b[4] = {u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]};
+            store_values<float>(p.gate + at + 4 * k, n - 4 * k, a);
+            store_values<float>(p.up + at + 4 * k, n - 4 * k, b);
+          }
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void end() {
+    if constexpr (PAIR == 1) {
+      if (!p.dh || !p.sums) return;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+#pragma unroll
+        for (int m = kPieces; m < 64; m *= 2) {
+          sum_g[e] += __shfl_xor(sum_g[e], m);
+          sum_u[e] += __shfl_xor(sum_u[e], m);
+        }
+        if (r0 == 0 && e < n) {
+          p.sums[(part * 2) * p.ni + i + e] = sum_g[e];
+          p.sums[(part * 2 + 1) * p.ni + i + e] = sum_u[e];
+        }
+      }
+    }
+  }
+};
+
+// Workgroups go to the eight dies in turn; here each die takes a stretch of tiles.
+__device__ __forceinline__ int xcd_order(unsigned block, unsigned blocks) {
+  const unsigned each = blocks / 8, more = blocks % 8, die = block % 8;
+  return int(die * each + min(die, more) + block / 8);
+}
+constexpr int kGroup = 8;
+
 // PAIR: 0 none, 1 on i, 2 on j.
 template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR>
-__global__ void __launch_bounds__(64 * WI * WJ) kernel(ProductParams p) {
+__global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 ? 1 : 2) kernel(ProductParams p) {
   constexpr int WAVES = WI * WJ, GI = TI / WI, GJ = TJ / WJ;  // a wave's part of the tile
   constexpr int NI = GI / 16, NJ = GJ / 16;
   constexpr int kStage = (TI + TJ) * kStepBytes;
@@ -206,15 +432,15 @@ __global__ void __launch_bounds__(64 * WI * WJ) kernel(ProductParams p) {
 
   // this workgroup's tile, and its part of the sum
   constexpr int FI = PAIR == 1 ? TI / 2 : TI, FJ = PAIR == 2 ? TJ / 2 : TJ;
-  const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ;
-  int t = blockIdx.x;
-  const int ti = t % tiles_i;
-  t /= tiles_i;
-  const int tj = t % tiles_j;
-  t /= tiles_j;
-  const int which = t % p.halves;
-  t /= p.halves;
-  const int image = t % p.images, split = t / p.images;
+  const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ, all_j = tiles_j * p.halves;
+  const int plane = tiles_i * all_j;
+  int t = xcd_order(blockIdx.x, gridDim.x);
+  const int image = t / plane % p.images, split = t / plane / p.images;
+  t %= plane;
+  // groups of kGroup tiles along j, in each i by i
+  const int group = t / (kGroup * tiles_i) * kGroup, rows = min(kGroup, all_j - group);
+  t %= kGroup * tiles_i;
+  const int ti = t / rows, tj = (group + t % rows) % tiles_j, which = (group + t % rows) / tiles_j;
   const int i0 = ti * FI, j0 = tj * FJ;
   const int steps = (p.K + kStep<T> - 1) / kStep<T>;
   const long total = long(steps) * p.segs;
@@ -225,14 +451,17 @@ __global__ void __launch_bounds__(64 * WI * WJ) kernel(ProductParams p) {
   a.init(p.i, image, PAIR == 0 && p.i.half ? which : 0, i0, p.ni, wave, lane);
   b.init(p.j, image, PAIR == 0 ? which : 0, j0, p.nj, wave, lane);
   int s = int(first / steps), k0 = int(first % steps) * kStep<T>;
-  auto load = [&](int stage) {
-    a.load(lds + stage * kStage, s, k0, p.K, wave, lane);
-    b.load(lds + stage * kStage + TI * kStepBytes, s, k0, p.K, wave, lane);
+  auto advance = [&]() {
     k0 += kStep<T>;
     if (k0 >= p.K) {
       k0 = 0;
       ++s;
     }
+  };
+  auto load = [&](int stage) {
+    a.load(lds + stage * kStage, a.step(s, k0, p.K), wave, lane);
+    b.load(lds + stage * kStage + TI * kStepBytes, b.step(s, k0, p.K), wave, lane);
+    advance();
   };
 
   floatx4 acc[NI][NJ];
@@ -241,98 +470,119 @@ __global__ void __launch_bounds__(64 * WI * WJ) kernel(ProductParams p) {
 #pragma unroll
     for (int y = 0; y < NJ; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  if (first < end) load(0);
-  int stage = 0;
-  for (long n = first; n < end; ++n) {
+  // A step's two halves of k follow each other without a pause: while the products of
+  // one run, row by row, the fragments of the next take the place of those that are
+  // done with. At the barrier between them every wave has read all of this stage, and the
+  // stage after it, asked for a step ago, has landed; so what comes after that goes
+  // where this one was, asked for among the products of the second half.
+  floatx4 fa[NI], fb[2][NJ];
+  auto read_a = [&](int stage, int sub, int x) {
+    fa[x] = fragment<T, TI, IK>(lds + stage * kStage, wi * GI + 16 * x, sub, lane);
+  };
+  auto read_b = [&](int stage, int sub, int y) {
+    fb[sub][y] = fragment<T, TJ, JK>(lds + stage * kStage + TI * kStepBytes, wj * GJ + 16 * y, sub, lane);
+  };
+  auto half = [&](int sub, int stage, auto&& between) {  // products of `sub`; reads the other of `stage`
+#pragma unroll
+    for (int x = 0; x < NI; ++x) {
+#pragma unroll
+      for (int y = 0; y < NJ; ++y) acc[x][y] = multiply<T>(fa[x], fb[sub][y], acc[x][y]);
+      read_a(stage, sub ^ 1, x);
+#pragma unroll
+      for (int y = x * NJ / NI; y < (x + 1) * NJ / NI; ++y) read_b(stage, sub ^ 1, y);
+      between(x);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (first < end) {
+    load(0);
+    if (first + 1 < end) load(1);
     wait_for_loads();
-    if (n + 1 < end) load(stage ^ 1);
-    const unsigned ta = lds + stage * kStage, tb = ta + TI * kStepBytes;
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      floatx4 fa[NI], fb[NJ];
+    for (int x = 0; x < NI; ++x) read_a(0, 0, x);
 #pragma unroll
-      for (int x = 0; x < NI; ++x) fa[x] = fragment<T, TI, IK>(ta, wi * GI + 16 * x, sub, lane);
+    for (int y = 0; y < NJ; ++y) read_b(0, 0, y);
+  }
+  int stage = 0;
+#pragma unroll 1
+  for (long n = first; n < end; ++n) {
+    half(0, stage, [](int) {});
+    wait_for_loads();
+    const bool more = n + 2 < end;
+    const auto sa = a.step(s, k0, p.K);
+    const auto sb = b.step(s, k0, p.K);
+    const bool whole = more && a.whole(sa) && b.whole(sb);
+    const unsigned la = lds + stage * kStage, lb = la + TI * kStepBytes;
+    // (after the last step these reads find old values, which nothing uses)
+    half(1, stage ^ 1, [&](int x) {
+      if (!whole) return;
 #pragma unroll
-      for (int y = 0; y < NJ; ++y) fb[y] = fragment<T, TJ, JK>(tb, wj * GJ + 16 * y, sub, lane);
+      for (int m = x * a.kMine / NI; m < (x + 1) * a.kMine / NI; ++m) a.piece(la, sa, m, wave);
 #pragma unroll
-      for (int x = 0; x < NI; ++x)
-#pragma unroll
-        for (int y = 0; y < NJ; ++y) acc[x][y] = multiply<T>(fa[x], fb[y], acc[x][y]);
+      for (int m = x * b.kMine / NI; m < (x + 1) * b.kMine / NI; ++m) b.piece(lb, sb, m, wave);
+    });
+    if (more) {
+      if (!whole) {
+        a.load(la, sa, wave, lane);
+        b.load(lb, sb, wave, lane);
+      }
+      advance();
     }
     stage ^= 1;
   }
 
-  // lane: column j of 16, four neighbours along i
-  const int ii = i0 + wi * (PAIR == 1 ? GI / 2 : GI) + 4 * (lane >> 4), jj = j0 + wj * (PAIR == 2 ? GJ / 2 : GJ) + (lane & 15);
-  auto put = [&](auto* to, int i, floatx4 v) {
-    using E = std::remove_reference_t<decltype(*to)>;
-    Vec<E, 4> w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) set_element<E, 4>(w, e, v[e]);
-    if (i + 4 <= p.ni) {
-      *reinterpret_cast<Vec<E, 4>*>(to) = w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (i + e < p.ni) to[e] = E(v[e]);
-    }
-  };
+  // The results leave through LDS, each wave's through a slab of its own: what a lane
+  // holds (column j of 16, four neighbours along i) becomes rows along i, which are
+  // then read back, finished and stored 16 bytes or more a lane by a loop that is short to fetch.
+  constexpr unsigned kSlab = 2 * kStage / WAVES;
+  __syncthreads();
+  const unsigned slab = lds + wave * kSlab;
+  const int row = lane & 15, quad = lane >> 4;
   if constexpr (PAIR != 0) {
-    constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ;
-    const int type = sizeof(T) == 4 ? OAA_FLOAT32 : __is_same(T, bf16) ? OAA_BFLOAT16 : OAA_FLOAT16;
+    constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ, RI = 16 * MI;
+    constexpr int kRows = int(kSlab / (2 * RI * 4)) < 16 * MJ ? int(kSlab / (2 * RI * 4)) : 16 * MJ;  // of a pass
+    static_assert(kRows % 16 == 0 && 16 * MJ % kRows == 0, "");
+    UnitEnd<T, RI, kRows, PAIR> finish(p, image, i0 + wi * RI, lane);
+    finish.part = PAIR == 1 ? long(image) * tiles_j * WJ + tj * WJ + wj : long(image) * tiles_i * WI + ti * WI + wi;
+    const int jw = j0 + wj * 16 * MJ;
 #pragma unroll
-    for (int x = 0; x < MI; ++x) {
-      const int i = ii + 16 * x;
-      if (i >= p.ni) continue;
+    for (int pass = 0; pass < 16 * MJ / kRows; ++pass) {
 #pragma unroll
-      for (int y = 0; y < MJ; ++y) {
-        const int j = jj + 16 * y;
-        if (j >= p.nj) continue;
-        floatx4 g = acc[x][y], u = acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? y + MJ : y], h;
-        if (p.gate_bias || p.up_bias) {
+      for (int y = 0; y < kRows / 16; ++y)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int f = PAIR == 1 ? min(i + e, p.ni - 1) : j;
-            g[e] += load_param(p.gate_bias, type, f, 0.0f);
-            u[e] += load_param(p.up_bias, type, f, 0.0f);
-          }
+        for (int x = 0; x < MI; ++x) {
+          const int yy = pass * kRows / 16 + y;
+          put<RI>(slab, 16 * y + row, 4 * x + quad, acc[x][yy]);
+          put<RI>(slab + kRows * RI * 4, 16 * y + row, 4 * x + quad, acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? yy + MJ : yy]);
         }
-        auto gated = [&](auto value) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = oaa::act<decltype(value)::value>(g[e]) * u[e];
-        };
-        switch (p.act) {
-          case OAA_ACT_RELU: gated(std::integral_constant<int, OAA_ACT_RELU>{}); break;
-          case OAA_ACT_SILU: gated(std::integral_constant<int, OAA_ACT_SILU>{}); break;
-          case OAA_ACT_GELU: gated(std::integral_constant<int, OAA_ACT_GELU>{}); break;
-          default: gated(std::integral_constant<int, OAA_ACT_NONE>{});
-        }
-        put(static_cast<T*>(p.out) + long(image) * p.out_image + long(j) * p.out_ld + i, i, h);
-        if (p.gate) {
-          const long at = (long(image) * p.nj + j) * p.ni + i;
-          put(p.gate + at, i, g);
-          put(p.up + at, i, u);
-        }
-      }
+      finish.rows(slab, jw + pass * kRows);
     }
+    finish.end();
   } else {
+    const long part = (long(split) * p.halves + which) * p.images + image;
+    auto rows = [&](auto zero, auto* out, long ld) {
+      using E = decltype(zero);
+      constexpr int kRows = int(kSlab / (GI * sizeof(E))) < GJ ? int(kSlab / (GI * sizeof(E))) : GJ;
+      static_assert(kRows % 16 == 0 && GJ % kRows == 0, "");
 #pragma unroll
-    for (int x = 0; x < NI; ++x) {
-      const int i = ii + 16 * x;
-      if (i >= p.ni) continue;
+      for (int pass = 0; pass < GJ / kRows; ++pass) {
 #pragma unroll
-      for (int y = 0; y < NJ; ++y) {
-        const int j = jj + 16 * y;
-        if (j >= p.nj) continue;
-        if (p.splits > 1) {
-          const long part = (long(split) * p.halves + which) * p.images + image;
-          put(static_cast<float*>(p.out) + (part * p.nj + j) * p.ni + i, i, acc[x][y]);
-        } else {
-          put(static_cast<T*>(p.out) + long(image) * p.out_image + long(which) * p.out_half + long(j) * p.out_ld + i, i,
-              acc[x][y]);
-        }
+        for (int y = 0; y < kRows / 16; ++y)
+#pragma unroll
+          for (int x = 0; x < NI; ++x) {
+            const floatx4 v = acc[x][pass * kRows / 16 + y];
+            if constexpr (sizeof(E) == 4)
+              put<GI>(slab, 16 * y + row, 4 * x + quad, v);
+            else
+              put_16<E, GI>(slab, 16 * y + row, 4 * x + quad, v);
+          }
+        store_rows<E, GI, kRows>(slab, out + i0 + wi * GI, ld, j0 + wj * GJ + pass * kRows, p.nj, p.ni - (i0 + wi * GI), lane);
       }
-    }
+    };
+    if (p.splits > 1)
+      rows(0.0f, static_cast<float*>(p.out) + part * p.nj * p.ni, p.ni);
+    else
+      rows(T(0.0f), static_cast<T*>(p.out) + long(image) * p.out_image + long(which) * p.out_half, p.out_ld);
   }
 }
 
@@ -344,12 +594,19 @@ hipError_t launch(const ProductParams& p, hipStream_t s) {
   if (tiles * (64 * WI * WJ) >= 1l << 32 || tiles >= 1l << 31) return hipErrorInvalidValue;  // refused before
   auto kern = kernel<T, TI, TJ, WI, WJ, IK, JK, PAIR>;
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+    const hipError_t e = tile::allow_lds(kern, lds);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(kern, dim3(unsigned(tiles)), dim3(64 * WI * WJ), lds, s, p);
   return hipGetLastError();
+}
+
+template <typename T, bool IK, bool JK, int PAIR>
+hipError_t launch_sized(const ProductParams& p, ProductKind kind, hipStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (product_tile(2, kind, p.ni, p.nj, p.images, p.halves, p.splits) == 256)
+      return launch<T, 256, 256, kWaves256.i, kWaves256.j, IK, JK, PAIR>(p, s);
+  return launch<T, 128, 128, kWaves128.i, kWaves128.j, IK, JK, PAIR>(p, s);
 }
 
 }  // namespace product
@@ -358,12 +615,12 @@ template <typename T>
 hipError_t launch_product(const ProductParams& p, ProductKind kind, hipStream_t s) {
   using namespace product;
   switch (kind) {
-    case kUnitLast: return launch<T, 128, 128, 2, 2, true, true, 1>(p, s);
-    case kUnitPlanes: return launch<T, 128, 128, 2, 2, false, true, 2>(p, s);
-    case kInputLast: return launch<T, 128, 128, 2, 2, false, true, 0>(p, s);
-    case kInputPlanes: return launch<T, 128, 128, 2, 2, false, false, 0>(p, s);
-    case kWeightLast: return launch<T, 128, 128, 2, 2, false, false, 0>(p, s);
-    case kWeightPlanes: return launch<T, 128, 128, 2, 2, true, true, 0>(p, s);
+    case kUnitLast: return launch_sized<T, true, true, 1>(p, kind, s);
+    case kUnitPlanes: return launch_sized<T, false, true, 2>(p, kind, s);
+    case kInputLast: return launch_sized<T, false, true, 0>(p, kind, s);
+    case kInputPlanes: return launch_sized<T, false, false, 0>(p, kind, s);
+    case kWeightLast: return launch_sized<T, false, false, 0>(p, kind, s);
+    case kWeightPlanes: return launch_sized<T, true, true, 0>(p, kind, s);
   }
   return hipErrorInvalidValue;
 }
