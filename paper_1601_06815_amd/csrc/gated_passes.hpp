@@ -145,26 +145,25 @@ __global__ void __launch_bounds__(kThreads) slope_planes_kernel(SlopeParams p) {
   }
 }
 
-// 64 hidden channels by 4 shares of the parts a workgroup.
+// 16 hidden channels of gate's or up's by 64 shares of the parts a workgroup: the parts
+// are many and the channels few, and what takes time is how many loads follow each other.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) bias_join_kernel(const float* sums, long parts, int F, T* gate, T* up) {
-  const int cl = threadIdx.x & 63, pl = threadIdx.x >> 6;
-  const int f = blockIdx.x * 64 + cl;
-  __shared__ double share[2][4][64];
-  double a[2] = {};
+__global__ void __launch_bounds__(1024) bias_join_kernel(const float* sums, long parts, int F, T* gate, T* up) {
+  const int cl = threadIdx.x & 15, pl = threadIdx.x >> 4, f = blockIdx.x * 16 + cl, half = blockIdx.y;
+  T* const out = half ? up : gate;
+  if (!out) return;
+  __shared__ double share[64][16];
+  double a = 0.0;
   if (f < F)
-#pragma unroll 4
-    for (long k = pl; k < parts; k += 4) {
-      a[0] += sums[(2 * k) * F + f];
-      a[1] += sums[(2 * k + 1) * F + f];
-    }
-  share[0][pl][cl] = a[0];
-  share[1][pl][cl] = a[1];
+#pragma unroll 8
+    for (long k = pl; k < parts; k += 64) a += sums[(2 * k + half) * F + f];
+  share[pl][cl] = a;
   __syncthreads();
-  if (pl < 2 && f < F) {
-    T* out = pl ? up : gate;
-    if (out) out[f] = T(float((share[pl][0][cl] + share[pl][1][cl]) + (share[pl][2][cl] + share[pl][3][cl])));
+  for (int m = 32; m; m /= 2) {
+    if (pl < m) share[pl][cl] += share[pl + m][cl];
+    __syncthreads();
   }
+  if (pl == 0 && f < F) out[f] = T(float(share[0][cl]));
 }
 
 template <typename T>
@@ -232,7 +231,7 @@ hipError_t launch_slope(const SlopeParams& p, hipStream_t s) {
 template <typename T>
 hipError_t launch_bias_join(const float* sums, long parts, int F, void* gate, void* up, hipStream_t s) {
   using namespace passes;
-  hipLaunchKernelGGL((bias_join_kernel<T>), dim3((F + 63) / 64), dim3(kThreads), 0, s, sums, parts, F,
+  hipLaunchKernelGGL((bias_join_kernel<T>), dim3((F + 15) / 16, 2), dim3(1024), 0, s, sums, parts, F,
                      static_cast<T*>(gate), static_cast<T*>(up));
   return hipGetLastError();
 }

@@ -36,7 +36,6 @@ typedef __attribute__((address_space(3))) const floatx4 lds_floatx4;
 typedef __attribute__((address_space(3))) const float lds_float;
 
 constexpr int kStepBytes = 128;
-constexpr unsigned kNowhere = 0x80000000u;  // an offset outside every resource: the load brings 0
 
 template <typename T>
 constexpr int kStep = kStepBytes / int(sizeof(T));
@@ -67,14 +66,10 @@ __device__ __forceinline__ intx4 resource(const char* base, long bytes) {
   return r;
 }
 
-// 16 bytes (or 4) a lane from memory to LDS at `lds` + lane x 16 (or 4). The
-// compiler knows nothing of the load: wait_for_loads() does.
+// 16 bytes a lane from memory to LDS at `lds` + lane x 16. The compiler knows nothing
+// of the load: wait_for_loads() does.
 __device__ __forceinline__ void load_16(unsigned lds, unsigned offset, intx4 rs) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(rs)
-               : "memory");
-}
-__device__ __forceinline__ void load_4(unsigned lds, unsigned offset, intx4 rs) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(rs)
                : "memory");
 }
 // Every load into LDS of this wave has landed and every read of LDS is done, in all
@@ -85,30 +80,47 @@ __device__ __forceinline__ void wait_for_loads() {
 
 // One operand's tile: R rows, loaded by WAVES waves. PAIR: rows come in groups of
 // GROUP, the first half of each from gate's operand, the second from up's.
+//
+// Load m of a wave (1 KB: 8 rows, or the lines of k columns that fit) lies a fixed
+// number of rows (lines) after the one before, so a lane's offset in it is the same for all,
+// and what differs goes into the scalar description of the memory: its address, and its
+// size, past which there are no more rows (lines, values) and the load brings 0.
 template <typename T, int R, int WAVES, bool KROWS, bool PAIR, int GROUP>
 struct Tile {
-  static constexpr int kLoads = R * kStepBytes / 1024;  // of 1 KB each
-  static constexpr int kMine = (kLoads + WAVES - 1) / WAVES;
-  static constexpr int kLine = R * int(sizeof(T));  // k columns: bytes of one k
+  static constexpr int kMine = R * kStepBytes / 1024 / WAVES;  // loads of a wave in a step
+  static constexpr int kLine = R * int(sizeof(T));             // k columns: bytes of one k
   static constexpr int kBlock = sizeof(T) == 2 ? 32 : 64;
-
-  // This wave's loads differ by whole rows (lines), which go into the address of the
-  // memory described; a lane's own offset stays. (32 bits, k columns: the place of a
-  // block changes between lines.)
+  static_assert(R * kStepBytes % (1024 * WAVES) == 0, "");
+  static_assert(!PAIR || 8 * WAVES == GROUP || 8 * WAVES == GROUP / 2, "");
+  // rows or lines between a wave's loads (of a pair's: between those of one half)
+  static constexpr int kApart = !KROWS ? WAVES * 1024 / kLine : !PAIR ? 8 * WAVES : GROUP / 2;
+  // whether a wave's loads are of gate's and up's rows in turn (or all of one of them)
+  static constexpr bool kTurns = PAIR && 8 * WAVES < GROUP;
+  // (32 bits, k columns: the place of a block changes between a wave's loads)
   static constexpr int kOffsets = !KROWS && sizeof(T) == 4 ? kMine : 1;
 
-  const char* at;  // of the tile's first row (k columns: first column), this segment and image
-  long half, seg;
-  int ld, rows;  // rows from the tile's first on (of one half)
+  const char* from;  // the wave's first row (line) of the step to load next
+  const char* base;  // of segment 0, k = 0
+  long half, seg, hop;
+  int ld, rows, apart;
+  int size;  // k rows: bytes from there to the end of the last row at k = 0; k columns: of a line
   unsigned offset[kOffsets];
 
-  __device__ __forceinline__ void init(const Operand& o, int image, int which, int first, int n, int wave, int lane) {
-    at = static_cast<const char*>(o.base) + long(image) * o.image + long(which) * o.half +
-         (KROWS ? long(first) * o.ld : long(first) * long(sizeof(T)));
+  __device__ __forceinline__ void init(const Operand& o, int image, int which, int first, int n, int K, int wave,
+                                       int lane) {
+    ld = o.ld;
+    rows = n - first;  // from the tile's first on (of one half)
     half = o.half;
     seg = o.seg;
-    ld = o.ld;
-    rows = n - first;
+    hop = KROWS ? kStepBytes : long(kStep<T>) * ld;
+    apart = kApart * ld;
+    const int skip = KROWS ? row_of(8 * wave) : wave * 1024 / kLine;
+    base = static_cast<const char*>(o.base) + long(image) * o.image + long(which) * o.half + long(skip) * ld +
+           (KROWS ? long(first) * ld : long(first) * long(sizeof(T)));
+    if constexpr (PAIR && !kTurns) base += 8 * wave % GROUP >= GROUP / 2 ? half : 0;
+    from = base;
+    size = KROWS ? (min(rows, PAIR ? R / 2 : R) - skip - 1) * ld + (K * int(sizeof(T)) + 3) / 4 * 4
+                 : (min(rows, R) * int(sizeof(T)) + 3) / 4 * 4 - (skip + 1) * ld;
 #pragma unroll
     for (int m = 0; m < kOffsets; ++m) {
       if constexpr (KROWS) {
@@ -116,7 +128,7 @@ struct Tile {
       } else {
         const int q = wave + m * WAVES, byte = q * 1024 + lane * 16, k = byte / kLine, in = byte % kLine;
         const int key = sizeof(T) == 2 ? k & 3 : (k >> 2) & 3;
-        offset[m] = unsigned(k - first_line(q)) * unsigned(ld) + unsigned(((in / kBlock) ^ key) * kBlock + in % kBlock);
+        offset[m] = unsigned(lane * 16 / kLine) * unsigned(ld) + unsigned(((in / kBlock) ^ key) * kBlock + in % kBlock);
       }
     }
   }
@@ -125,84 +137,95 @@ struct Tile {
     if constexpr (PAIR) return r / GROUP * (GROUP / 2) + r % (GROUP / 2);
     return r;
   }
-  __device__ __forceinline__ long of_half(int q) const {
-    if constexpr (PAIR) return 8 * q % GROUP >= GROUP / 2 ? half : 0;
-    return 0;
+  // To step k0 of segment s: the next one, or (k0 = 0) the next segment's first.
+  __device__ __forceinline__ void go(int s, int k0) {
+    from = k0 ? from + hop : base + long(s) * seg;
   }
-  static __device__ __forceinline__ int first_line(int q) { return q * 1024 / kLine; }
+  __device__ __forceinline__ void start(int s, int k0) { from = base + long(s) * seg + long(k0 / kStep<T>) * hop; }
 
-  // A step to load: from k0 on of segment s.
-  struct Step {
-    const char* from;
-    int left;  // k rows: bytes of a row that the segment still has; k columns: lines
-  };
-  __device__ __forceinline__ Step step(int s, int k0, int K) const {
-    if constexpr (KROWS) return {at + long(s) * seg + long(k0) * long(sizeof(T)), (K - k0) * int(sizeof(T))};
-    return {at + long(s) * seg + long(k0) * ld, K - k0};
+  // Load m of this wave's to LDS. What a row has beyond K of the segment's last step is
+  // the next row's start (or 0 after the last): cut() clears it.
+  __device__ __forceinline__ void piece(unsigned lds, int k0, int K, int m, int wave) const {
+    const int rest = KROWS ? size - k0 * int(sizeof(T)) : size + min(K - k0, kStep<T>) * ld;
+    const char* at = from + (kTurns ? long(m / 2 * apart) + (m % 2 ? half : 0) : long(m * apart));
+    const int bytes = rest - (kTurns ? m / 2 : m) * apart;
+    load_16(lds + (wave + m * WAVES) * 1024, offset[kOffsets > 1 ? m : 0], resource(at, max(bytes, 0)));
   }
-  static __device__ __forceinline__ bool whole(const Step& t) { return !KROWS || t.left >= kStepBytes; }
-  // Load m of this wave's, of a whole step, to LDS. Rows or lines that there are not, and
-  // what lies beyond the last one's end, come as 0.
-  __device__ __forceinline__ void piece(unsigned lds, const Step& t, int m, int wave) const {
-    const int q = wave + m * WAVES;
-    if (kLoads % WAVES && q >= kLoads) return;
-    const int skip = KROWS ? row_of(8 * q) : first_line(q);
-    const int there = (KROWS ? rows : t.left) - skip;
-    const long bytes = long(there - 1) * ld + (KROWS ? t.left : (rows * int(sizeof(T)) + 3) / 4 * 4);
-    load_16(lds + q * 1024, offset[kOffsets > 1 ? m : 0],
-            resource(t.from + of_half(q) + long(skip) * ld, there > 0 ? bytes : 0));
-  }
-  // All of this wave's of any step.
-  __device__ __forceinline__ void load(unsigned lds, const Step& t, int wave, int lane) const {
-    if (whole(t)) {
-#pragma unroll
-      for (int m = 0; m < kMine; ++m) piece(lds, t, m, wave);
-      return;
-    }
-    // the last values of a segment, 4 bytes a lane: nothing beyond K is read
+  // Clears the values of a tile in LDS from the first `left` bytes of each row on.
+  static __device__ __forceinline__ void cut(unsigned lds, int left) {
+    if constexpr (KROWS) {
+      int t = threadIdx.x;
+      asm volatile("" : "+v"(t));  // nothing of this is worked out ahead, and held, by the loop around it
 #pragma unroll 1
-    for (int q = wave; q < kLoads; q += WAVES) {
-      const intx4 rs = resource(t.from + of_half(q), 0x7ffffffcl);
-#pragma unroll 1
-      for (int e = 0; e < 4; ++e) {
-        const int word = lane + 64 * e, r = word / 32, k = ((word % 32 / 4) ^ r) * 16 + word % 4 * 4;
-        const int row = min(row_of(8 * q + r), rows - 1);
-        load_4(lds + q * 1024 + 256 * e, k < t.left ? unsigned(row) * unsigned(ld) + unsigned(k) : kNowhere, rs);
+      for (int w = t; w < R * 32; w += 64 * WAVES) {
+        const int piece = (w % 32 / 4) ^ (w / 32 & 7);
+        if (piece * 16 + w % 4 * 4 >= left) *reinterpret_cast<__attribute__((address_space(3))) int*>(lds + w * 4) = 0;
       }
     }
   }
 };
 
-// Fragment of 16 rows from `row` on (a multiple of 16), part `sub` (0, 1) of the step.
+// Where a lane finds its fragments of 16 rows in a tile: fragment x from row `first` (a
+// multiple of 64) on, half `sub` of the step. LDS addresses without the tile's own.
 template <typename T, int R, bool KROWS>
-__device__ __forceinline__ floatx4 fragment(unsigned tile, int row, int sub, int lane) {
-  if constexpr (KROWS) {
-    const int r = row + (lane & 15), piece = (4 * sub + (lane >> 4)) ^ (r & 7);
-    return *reinterpret_cast<lds_floatx4*>(tile + r * kStepBytes + piece * 16);
-  } else if constexpr (sizeof(T) == 2) {
-    constexpr int kLine = R * 2;
-    const int r = (lane & 15) >> 2;
-    const unsigned a = tile + (32 * sub + 8 * (lane >> 4) + r) * kLine + ((row / 16) ^ r) * 32 + (lane & 3) * 8;
-    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        const_cast<__attribute__((address_space(3))) shortx4*>(reinterpret_cast<lds_shortx4*>(a)));
-    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        const_cast<__attribute__((address_space(3))) shortx4*>(reinterpret_cast<lds_shortx4*>(a + 4 * kLine)));
-    shortx8 v;
+struct Fragments {
+  unsigned at[KROWS ? 2 : 4];
+
+  __device__ __forceinline__ void init(int first, int lane) {
+    if constexpr (KROWS) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = lo[e];
-      v[e + 4] = hi[e];
+      for (int sub = 0; sub < 2; ++sub)
+        at[sub] = (first + (lane & 15)) * kStepBytes + ((4 * sub + (lane >> 4)) ^ (lane & 7)) * 16;
+    } else if constexpr (sizeof(T) == 2) {
+      const int r = (lane & 15) >> 2;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) at[x] = (8 * (lane >> 4) + r) * (R * 2) + first * 2 + (x ^ r) * 32 + (lane & 3) * 8;
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        at[x] = 4 * (lane >> 4) * (R * 4) + first * 4 + (x ^ (lane >> 4)) * 64 + (lane & 15) * 4;
     }
-    return __builtin_bit_cast(floatx4, v);
-  } else {
-    constexpr int kLine = R * 4;
-    const unsigned a = tile + (16 * sub + 4 * (lane >> 4)) * kLine + ((row / 16) ^ (lane >> 4)) * 64 + (lane & 15) * 4;
-    floatx4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<lds_float*>(a + e * kLine);
-    return v;
   }
-}
+  // The same in one tile, for half `sub` of the step.
+  struct Base {
+    unsigned at[KROWS ? 1 : 4];
+  };
+  __device__ __forceinline__ Base base(unsigned tile, int sub) const {
+    Base b;
+#pragma unroll
+    for (int x = 0; x < (KROWS ? 1 : 4); ++x) {
+      b.at[x] = tile + at[KROWS ? sub : x];
+      // one address, and each fragment's distance in its instruction: not one each
+      asm volatile("" : "+v"(b.at[x]));
+    }
+    return b;
+  }
+  static __device__ __forceinline__ floatx4 read(const Base& b, int x, int sub) {
+    if constexpr (KROWS) {
+      return *reinterpret_cast<lds_floatx4*>(b.at[0] + x * 16 * kStepBytes);
+    } else if constexpr (sizeof(T) == 2) {
+      constexpr int kLine = R * 2;
+      const unsigned a = b.at[x & 3] + (x >> 2) * 128 + 32 * sub * kLine;
+      typedef __attribute__((address_space(3))) shortx4 lds_short;
+      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_short*>(a));
+      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_short*>(a + 4 * kLine));
+      shortx8 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = lo[e];
+        v[e + 4] = hi[e];
+      }
+      return __builtin_bit_cast(floatx4, v);
+    } else {
+      constexpr int kLine = R * 4;
+      const unsigned a = b.at[x & 3] + (x >> 2) * 256 + 16 * sub * kLine;
+      floatx4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<lds_float*>(a + e * kLine);
+      return v;
+    }
+  }
+};
 
 // Rows of RI values in LDS: piece c (16 bytes) of row r is at place c ^ (r % pieces), so
 // that neither 16 rows nor one row's pieces meet in a bank. put: four values of 32 bits
@@ -443,26 +466,40 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   const int ti = t / rows, tj = (group + t % rows) % tiles_j, which = (group + t % rows) / tiles_j;
   const int i0 = ti * FI, j0 = tj * FJ;
   const int steps = (p.K + kStep<T> - 1) / kStep<T>;
-  const long total = long(steps) * p.segs;
-  const long first = total * split / p.splits, end = total * (split + 1) / p.splits;
+  const long total = long(steps) * p.segs;  // below 2^31
+  const int first = int(total * split / p.splits), end = int(total * (split + 1) / p.splits);
 
+  int s = first / steps, k0 = first % steps * kStep<T>;
   Tile<T, TI, WAVES, IK, PAIR == 1, GI> a;
   Tile<T, TJ, WAVES, JK, PAIR == 2, GJ> b;
-  a.init(p.i, image, PAIR == 0 && p.i.half ? which : 0, i0, p.ni, wave, lane);
-  b.init(p.j, image, PAIR == 0 ? which : 0, j0, p.nj, wave, lane);
-  int s = int(first / steps), k0 = int(first % steps) * kStep<T>;
+  a.init(p.i, image, which, i0, p.ni, p.K, wave, lane);
+  b.init(p.j, image, which, j0, p.nj, p.K, wave, lane);
+  a.start(s, k0);
+  b.start(s, k0);
   auto advance = [&]() {
     k0 += kStep<T>;
     if (k0 >= p.K) {
       k0 = 0;
       ++s;
     }
+    a.go(s, k0);
+    b.go(s, k0);
   };
   auto load = [&](int stage) {
-    a.load(lds + stage * kStage, a.step(s, k0, p.K), wave, lane);
-    b.load(lds + stage * kStage + TI * kStepBytes, b.step(s, k0, p.K), wave, lane);
+#pragma unroll
+    for (int m = 0; m < a.kMine; ++m) a.piece(lds + stage * kStage, k0, p.K, m, wave);
+#pragma unroll
+    for (int m = 0; m < b.kMine; ++m) b.piece(lds + stage * kStage + TI * kStepBytes, k0, p.K, m, wave);
     advance();
   };
+  // The last values of a segment, once they have landed.
+  const int left = p.K % kStep<T> * int(sizeof(T));
+  auto cut = [&](int stage) {
+    a.cut(lds + stage * kStage, left);
+    b.cut(lds + stage * kStage + TI * kStepBytes, left);
+    wait_for_loads();
+  };
+  const bool ragged = (IK || JK) && left;
 
   floatx4 acc[NI][NJ];
 #pragma unroll
@@ -476,58 +513,54 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   // stage after it, asked for a step ago, has landed; so what comes after that goes
   // where this one was, asked for among the products of the second half.
   floatx4 fa[NI], fb[2][NJ];
-  auto read_a = [&](int stage, int sub, int x) {
-    fa[x] = fragment<T, TI, IK>(lds + stage * kStage, wi * GI + 16 * x, sub, lane);
-  };
-  auto read_b = [&](int stage, int sub, int y) {
-    fb[sub][y] = fragment<T, TJ, JK>(lds + stage * kStage + TI * kStepBytes, wj * GJ + 16 * y, sub, lane);
-  };
+  Fragments<T, TI, IK> at_a;
+  Fragments<T, TJ, JK> at_b;
+  at_a.init(wi * GI, lane);
+  at_b.init(wj * GJ, lane);
   auto half = [&](int sub, int stage, auto&& between) {  // products of `sub`; reads the other of `stage`
+    const auto ba = at_a.base(lds + stage * kStage, sub ^ 1);
+    const auto bb = at_b.base(lds + stage * kStage + TI * kStepBytes, sub ^ 1);
 #pragma unroll
     for (int x = 0; x < NI; ++x) {
 #pragma unroll
       for (int y = 0; y < NJ; ++y) acc[x][y] = multiply<T>(fa[x], fb[sub][y], acc[x][y]);
-      read_a(stage, sub ^ 1, x);
+      fa[x] = at_a.read(ba, x, sub ^ 1);
 #pragma unroll
-      for (int y = x * NJ / NI; y < (x + 1) * NJ / NI; ++y) read_b(stage, sub ^ 1, y);
+      for (int y = x * NJ / NI; y < (x + 1) * NJ / NI; ++y) fb[sub ^ 1][y] = at_b.read(bb, y, sub ^ 1);
       between(x);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   if (first < end) {
     load(0);
+    const bool last = k0 == 0;
     if (first + 1 < end) load(1);
     wait_for_loads();
+    if (ragged && last) cut(0);
+    const auto ba = at_a.base(lds, 0);
+    const auto bb = at_b.base(lds + TI * kStepBytes, 0);
 #pragma unroll
-    for (int x = 0; x < NI; ++x) read_a(0, 0, x);
+    for (int x = 0; x < NI; ++x) fa[x] = at_a.read(ba, x, 0);
 #pragma unroll
-    for (int y = 0; y < NJ; ++y) read_b(0, 0, y);
+    for (int y = 0; y < NJ; ++y) fb[0][y] = at_b.read(bb, y, 0);
   }
   int stage = 0;
 #pragma unroll 1
-  for (long n = first; n < end; ++n) {
+  for (int n = first; n < end; ++n) {
     half(0, stage, [](int) {});
     wait_for_loads();
+    if (ragged && k0 == 0 && n + 1 < end) cut(stage ^ 1);
     const bool more = n + 2 < end;
-    const auto sa = a.step(s, k0, p.K);
-    const auto sb = b.step(s, k0, p.K);
-    const bool whole = more && a.whole(sa) && b.whole(sb);
     const unsigned la = lds + stage * kStage, lb = la + TI * kStepBytes;
     // (after the last step these reads find old values, which nothing uses)
     half(1, stage ^ 1, [&](int x) {
-      if (!whole) return;
+      if (!more) return;
 #pragma unroll
-      for (int m = x * a.kMine / NI; m < (x + 1) * a.kMine / NI; ++m) a.piece(la, sa, m, wave);
+      for (int m = x * a.kMine / NI; m < (x + 1) * a.kMine / NI; ++m) a.piece(la, k0, p.K, m, wave);
 #pragma unroll
-      for (int m = x * b.kMine / NI; m < (x + 1) * b.kMine / NI; ++m) b.piece(lb, sb, m, wave);
+      for (int m = x * b.kMine / NI; m < (x + 1) * b.kMine / NI; ++m) b.piece(lb, k0, p.K, m, wave);
     });
-    if (more) {
-      if (!whole) {
-        a.load(la, sa, wave, lane);
-        b.load(lb, sb, wave, lane);
-      }
-      advance();
-    }
+    if (more) advance();
     stage ^= 1;
   }
 
