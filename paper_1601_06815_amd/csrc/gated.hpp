@@ -38,6 +38,10 @@ struct ProductParams {
   int images, halves;
   int K, segs;
   int splits;  // the sum's steps are cut into so many parts
+  // the launcher's own: the launch's first image, steps of a part of the sum, and a
+  // reciprocal for the tiles' order
+  int first_image, split_steps;
+  unsigned group_reciprocal;
   // D: element strides; partial sums in 32 bits if splits > 1, dense [split][half][image][nj][ni]
   void* out;
   long out_image, out_half;

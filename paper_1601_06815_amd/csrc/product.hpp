@@ -4,17 +4,20 @@
 // bits, 32 of 32 bits). Both operands' tiles of a step go from memory straight into
 // LDS, 16 bytes a lane, while the step before is multiplied; nothing passes through
 // registers on the way. LDS is written linearly by such a load, so what keeps the
-// reads free of bank conflicts is which address each lane asks for:
-//   k rows:    [row][8 pieces of 16 bytes], piece c of row r at place c ^ (r % 8);
-//   k columns: [k][row pieces], 32 bytes (16 bits) or 64 (32 bits) a block, block b of
-//              line k at place b ^ (k % 4) or b ^ (k / 4 % 4): the lines that one read
-//              takes lie in different banks.
+// reads free of bank conflicts is which 16 bytes ("piece") each lane asks for: piece c
+// of a row (k rows: 8 pieces; k columns: a line of one k) lies at place c ^ key(row).
+//
 // A lane's fragment is 16 bytes: 8 values of k (16 bits; for k columns two
-// transposing reads), or 4 (32 bits), one for each of four products.
+// transposing reads), or 4 (32 bits), one for each of four products. The 16 rows of a
+// fragment follow each other, but in 16 bits those of i do not: fragments 2 q and 2 q + 1
+// take rows 8 a + b and 8 a + 4 + b (a, b = 0..3) of 32, so that the results that a lane
+// holds of both (rows 4 quad + e of each) are 8 neighbours along i, 16 bytes, beside those
+// of the next quad, and leave for memory as they are.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "activation.hpp"
@@ -56,12 +59,13 @@ __device__ __forceinline__ floatx4 multiply(floatx4 a, floatx4 b, floatx4 c) {
   }
 }
 
-__device__ __forceinline__ intx4 resource(const char* base, long bytes) {
-  const unsigned long long a = reinterpret_cast<unsigned long long>(base);
+// `bytes` (below 2^31) from base on, uniform.
+__device__ __forceinline__ intx4 resource(const char* base, int bytes) {
+  const unsigned long long a = reinterpret_cast<unsigned long long>(base);  // below 2^48
   intx4 r;
   r[0] = __builtin_amdgcn_readfirstlane(int(unsigned(a)));
-  r[1] = __builtin_amdgcn_readfirstlane(int(unsigned(a >> 32) & 0xffffu));
-  r[2] = __builtin_amdgcn_readfirstlane(int(bytes < 0x7ffffffcl ? bytes : 0x7ffffffcl));
+  r[1] = __builtin_amdgcn_readfirstlane(int(unsigned(a >> 32)));
+  r[2] = __builtin_amdgcn_readfirstlane(bytes);
   r[3] = 0x00020000;
   return r;
 }
@@ -78,6 +82,25 @@ __device__ __forceinline__ void wait_for_loads() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// The row of fragment x, in its wave's part of the tile, that lane m of 16 has.
+template <typename T, bool I>
+__device__ __forceinline__ constexpr int row_in_fragment(int x, int m) {
+  return I && sizeof(T) == 2 ? x / 2 * 32 + m / 4 * 8 + x % 2 * 4 + m % 4 : x * 16 + m;
+}
+
+// The key of an operand's row r (k rows) or line k (k columns), by how fragments read it:
+// rows that a read takes together lie in different banks.
+template <typename T, bool KROWS, bool I>
+__device__ __forceinline__ int key_of(int r) {
+  constexpr bool kApart = I && sizeof(T) == 2;
+  if constexpr (KROWS)
+    return kApart ? (r & 3) | (r >> 3 & 1) << 2 : r & 7;
+  else if constexpr (sizeof(T) == 2)
+    return (r & 3) << (kApart ? 2 : 1);
+  else
+    return (r >> 2 & 3) << 2;
+}
+
 // One operand's tile: R rows, loaded by WAVES waves. PAIR: rows come in groups of
 // GROUP, the first half of each from gate's operand, the second from up's.
 //
@@ -85,71 +108,71 @@ __device__ __forceinline__ void wait_for_loads() {
 // number of rows (lines) after the one before, so a lane's offset in it is the same for all,
 // and what differs goes into the scalar description of the memory: its address, and its
 // size, past which there are no more rows (lines, values) and the load brings 0.
-template <typename T, int R, int WAVES, bool KROWS, bool PAIR, int GROUP>
+template <typename T, int R, int WAVES, bool KROWS, bool I, bool PAIR, int GROUP>
 struct Tile {
   static constexpr int kMine = R * kStepBytes / 1024 / WAVES;  // loads of a wave in a step
   static constexpr int kLine = R * int(sizeof(T));             // k columns: bytes of one k
-  static constexpr int kBlock = sizeof(T) == 2 ? 32 : 64;
+  static constexpr int kRows = 8 * WAVES;                      // k rows: of all waves' load m
   static_assert(R * kStepBytes % (1024 * WAVES) == 0, "");
-  static_assert(!PAIR || 8 * WAVES == GROUP || 8 * WAVES == GROUP / 2, "");
-  // rows or lines between a wave's loads (of a pair's: between those of one half)
-  static constexpr int kApart = !KROWS ? WAVES * 1024 / kLine : !PAIR ? 8 * WAVES : GROUP / 2;
+  static_assert(!PAIR || kRows == GROUP || GROUP / 2 % kRows == 0, "");
   // whether a wave's loads are of gate's and up's rows in turn (or all of one of them)
-  static constexpr bool kTurns = PAIR && 8 * WAVES < GROUP;
-  // (32 bits, k columns: the place of a block changes between a wave's loads)
+  static constexpr bool kTurns = PAIR && kRows < GROUP;
+  // (32 bits, k columns: a line's key differs between a wave's loads)
   static constexpr int kOffsets = !KROWS && sizeof(T) == 4 ? kMine : 1;
 
   const char* from;  // the wave's first row (line) of the step to load next
   const char* base;  // of segment 0, k = 0
   long half, seg, hop;
-  int ld, rows, apart;
+  int ld;
   int size;  // k rows: bytes from there to the end of the last row at k = 0; k columns: of a line
   unsigned offset[kOffsets];
+
+  // Rows (lines, of its half) between a wave's load m and its first, and whether it is of up's.
+  static constexpr int apart(int m) {
+    if (!KROWS) return m * (WAVES * 1024 / kLine);
+    if (!PAIR) return m * kRows;
+    constexpr int per = kTurns ? GROUP / 2 / kRows : 1;
+    return kTurns ? m / (2 * per) * (GROUP / 2) + m % per * kRows : m * (GROUP / 2);
+  }
+  static constexpr bool second(int m) { return kTurns && m / (GROUP / 2 / kRows) % 2; }
 
   __device__ __forceinline__ void init(const Operand& o, int image, int which, int first, int n, int K, int wave,
                                        int lane) {
     ld = o.ld;
-    rows = n - first;  // from the tile's first on (of one half)
+    const int rows = n - first;  // from the tile's first on (of one half)
     half = o.half;
     seg = o.seg;
     hop = KROWS ? kStepBytes : long(kStep<T>) * ld;
-    apart = kApart * ld;
-    const int skip = KROWS ? row_of(8 * wave) : wave * 1024 / kLine;
-    base = static_cast<const char*>(o.base) + long(image) * o.image + long(which) * o.half + long(skip) * ld +
+    const int skip = !KROWS ? wave * 1024 / kLine : PAIR ? 8 * wave % (GROUP / 2) : 8 * wave;
+    base = static_cast<const char*>(o.base) + long(image) * o.image + (which ? o.half : 0) + long(skip) * ld +
            (KROWS ? long(first) * ld : long(first) * long(sizeof(T)));
-    if constexpr (PAIR && !kTurns) base += 8 * wave % GROUP >= GROUP / 2 ? half : 0;
+    if constexpr (PAIR && !kTurns) base += 8 * wave >= GROUP / 2 ? half : 0;
     from = base;
     size = KROWS ? (min(rows, PAIR ? R / 2 : R) - skip - 1) * ld + (K * int(sizeof(T)) + 3) / 4 * 4
                  : (min(rows, R) * int(sizeof(T)) + 3) / 4 * 4 - (skip + 1) * ld;
 #pragma unroll
     for (int m = 0; m < kOffsets; ++m) {
+      const int q = wave + m * WAVES;
       if constexpr (KROWS) {
-        offset[m] = unsigned(lane >> 3) * unsigned(ld) + unsigned(((lane & 7) ^ (lane >> 3)) * 16);
+        offset[m] = unsigned(lane >> 3) * unsigned(ld) +
+                    unsigned(((lane & 7) ^ key_of<T, KROWS, I>(8 * q + (lane >> 3))) * 16);
       } else {
-        const int q = wave + m * WAVES, byte = q * 1024 + lane * 16, k = byte / kLine, in = byte % kLine;
-        const int key = sizeof(T) == 2 ? k & 3 : (k >> 2) & 3;
-        offset[m] = unsigned(lane * 16 / kLine) * unsigned(ld) + unsigned(((in / kBlock) ^ key) * kBlock + in % kBlock);
+        const int byte = q * 1024 + lane * 16, k = byte / kLine, piece = byte % kLine / 16;
+        offset[m] = unsigned(lane * 16 / kLine) * unsigned(ld) + unsigned((piece ^ key_of<T, KROWS, I>(k)) * 16);
       }
     }
   }
-  // Row of its half that the tile's row is.
-  static __device__ __forceinline__ int row_of(int r) {
-    if constexpr (PAIR) return r / GROUP * (GROUP / 2) + r % (GROUP / 2);
-    return r;
-  }
   // To step k0 of segment s: the next one, or (k0 = 0) the next segment's first.
-  __device__ __forceinline__ void go(int s, int k0) {
-    from = k0 ? from + hop : base + long(s) * seg;
-  }
+  __device__ __forceinline__ void go(int s, int k0) { from = k0 ? from + hop : base + long(s) * seg; }
   __device__ __forceinline__ void start(int s, int k0) { from = base + long(s) * seg + long(k0 / kStep<T>) * hop; }
 
   // Load m of this wave's to LDS. What a row has beyond K of the segment's last step is
   // the next row's start (or 0 after the last): cut() clears it.
   __device__ __forceinline__ void piece(unsigned lds, int k0, int K, int m, int wave) const {
     const int rest = KROWS ? size - k0 * int(sizeof(T)) : size + min(K - k0, kStep<T>) * ld;
-    const char* at = from + (kTurns ? long(m / 2 * apart) + (m % 2 ? half : 0) : long(m * apart));
-    const int bytes = rest - (kTurns ? m / 2 : m) * apart;
-    load_16(lds + (wave + m * WAVES) * 1024, offset[kOffsets > 1 ? m : 0], resource(at, max(bytes, 0)));
+    const int skip = apart(m) * ld;
+    load_16(lds + (wave + m * WAVES) * 1024, offset[kOffsets > 1 ? m : 0],
+            resource(from + skip + (second(m) ? half : 0), max(rest - skip, 0)));
   }
   // Clears the values of a tile in LDS from the first `left` bytes of each row on.
   static __device__ __forceinline__ void cut(unsigned lds, int left) {
@@ -158,42 +181,50 @@ struct Tile {
       asm volatile("" : "+v"(t));  // nothing of this is worked out ahead, and held, by the loop around it
 #pragma unroll 1
       for (int w = t; w < R * 32; w += 64 * WAVES) {
-        const int piece = (w % 32 / 4) ^ (w / 32 & 7);
+        const int piece = (w % 32 / 4) ^ key_of<T, KROWS, I>(w / 32);
         if (piece * 16 + w % 4 * 4 >= left) *reinterpret_cast<__attribute__((address_space(3))) int*>(lds + w * 4) = 0;
       }
     }
   }
 };
 
-// Where a lane finds its fragments of 16 rows in a tile: fragment x from row `first` (a
-// multiple of 64) on, half `sub` of the step. LDS addresses without the tile's own.
-template <typename T, int R, bool KROWS>
+// Where a lane finds its fragments in a tile: fragment x from row `first` (a multiple of
+// 64) on, half `sub` of the step. LDS addresses without the tile's own; fragments that
+// differ by a fixed distance share one.
+template <typename T, int R, bool KROWS, bool I>
 struct Fragments {
+  static constexpr int kBases = KROWS ? 1 : 4;
   unsigned at[KROWS ? 2 : 4];
 
   __device__ __forceinline__ void init(int first, int lane) {
+    const int m = lane & 15, g = lane >> 4;
     if constexpr (KROWS) {
+      const int row = first + row_in_fragment<T, I>(0, m);
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
-        at[sub] = (first + (lane & 15)) * kStepBytes + ((4 * sub + (lane >> 4)) ^ (lane & 7)) * 16;
-    } else if constexpr (sizeof(T) == 2) {
-      const int r = (lane & 15) >> 2;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) at[x] = (8 * (lane >> 4) + r) * (R * 2) + first * 2 + (x ^ r) * 32 + (lane & 3) * 8;
+        at[sub] = row * kStepBytes + ((4 * sub + g) ^ key_of<T, KROWS, I>(row)) * 16;
     } else {
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        at[x] = 4 * (lane >> 4) * (R * 4) + first * 4 + (x ^ (lane >> 4)) * 64 + (lane & 15) * 4;
+      for (int b = 0; b < 4; ++b) {
+        if constexpr (sizeof(T) == 2) {
+          // a transposing read: lane 4 r + c asks for values 4 c .. 4 c + 3 of line r
+          const int k = 8 * g + (m >> 2), column = first + row_in_fragment<T, I>(I ? 2 * b : b, m % 4 * 4);
+          at[b] = k * (R * 2) + ((column / 8) ^ key_of<T, KROWS, I>(k)) * 16 + column % 8 * 2;
+        } else {
+          const int k = 4 * g, column = first + row_in_fragment<T, I>(b, m);
+          at[b] = k * (R * 4) + ((column / 4) ^ key_of<T, KROWS, I>(k)) * 16 + column % 4 * 4;
+        }
+      }
     }
   }
   // The same in one tile, for half `sub` of the step.
   struct Base {
-    unsigned at[KROWS ? 1 : 4];
+    unsigned at[kBases];
   };
   __device__ __forceinline__ Base base(unsigned tile, int sub) const {
     Base b;
 #pragma unroll
-    for (int x = 0; x < (KROWS ? 1 : 4); ++x) {
+    for (int x = 0; x < kBases; ++x) {
       b.at[x] = tile + at[KROWS ? sub : x];
       // one address, and each fragment's distance in its instruction: not one each
       asm volatile("" : "+v"(b.at[x]));
@@ -202,10 +233,11 @@ struct Fragments {
   }
   static __device__ __forceinline__ floatx4 read(const Base& b, int x, int sub) {
     if constexpr (KROWS) {
-      return *reinterpret_cast<lds_floatx4*>(b.at[0] + x * 16 * kStepBytes);
+      return *reinterpret_cast<lds_floatx4*>(b.at[0] + row_in_fragment<T, I>(x, 0) * kStepBytes);
     } else if constexpr (sizeof(T) == 2) {
       constexpr int kLine = R * 2;
-      const unsigned a = b.at[x & 3] + (x >> 2) * 128 + 32 * sub * kLine;
+      const int which = I ? x >> 1 & 3 : x & 3, more = I ? (x >> 3) * 256 + (x & 1) * 8 : (x >> 2) * 128;
+      const unsigned a = b.at[which] + more + 32 * sub * kLine;
       typedef __attribute__((address_space(3))) shortx4 lds_short;
       const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_short*>(a));
       const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_short*>(a + 4 * kLine));
@@ -287,10 +319,9 @@ __device__ __forceinline__ void store_rows(unsigned slab, E* out, long ld, int j
 // The end of the unit: rows of g and u from LDS become h (and g and u in memory, if the
 // call keeps them), or with dh, in the backward pass, dg and du with their sums over
 // the positions.
-template <typename T, int RI, int ROWS, int PAIR>
+template <typename T, int RI, int ROWS, int PAIR, bool BACK>
 struct UnitEnd {
   static constexpr int V = 16 / int(sizeof(T)), kPieces = RI / V, kRows = 64 / kPieces;
-  static constexpr int kType = sizeof(T) == 4 ? OAA_FLOAT32 : __is_same(T, bf16) ? OAA_BFLOAT16 : OAA_FLOAT16;
   const ProductParams& p;
   const int image, lane;
   const int c, r0;  // this lane's piece of every row, and its first row
@@ -302,29 +333,65 @@ struct UnitEnd {
   __device__ __forceinline__ UnitEnd(const ProductParams& p_, int image_, int first, int lane_)
       : p(p_), image(image_), lane(lane_), c(lane_ % kPieces), r0(lane_ / kPieces), i(first + c * V), n(p_.ni - i) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sum_g[e] = sum_u[e] = 0.0f;
-      if constexpr (PAIR == 1) {
-        gate_bias[e] = e < n ? load_param(p.gate_bias, kType, i + e, 0.0f) : 0.0f;
-        up_bias[e] = e < n ? load_param(p.up_bias, kType, i + e, 0.0f) : 0.0f;
+    for (int e = 0; e < V; ++e) sum_g[e] = sum_u[e] = gate_bias[e] = up_bias[e] = 0.0f;
+    if constexpr (PAIR == 1) {
+      biases(p.gate_bias, gate_bias);
+      biases(p.up_bias, up_bias);
+    }
+  }
+
+  __device__ __forceinline__ void biases(const void* from, float (&to)[V]) const {
+    const T* at = static_cast<const T*>(from) + i;
+    if (!from || n <= 0) return;
+    if (n >= V) {
+      const Vec<T, V> v = load<T, V>(at);
+#pragma unroll
+      for (int e = 0; e < V; ++e) to[e] = float(v[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (e < n) to[e] = float(at[e]);
+    }
+  }
+
+  // What a row needs from memory, asked for while the one before is worked on.
+  struct Row {
+    Vec<T, V> dh;
+    float gate_bias, up_bias;  // PAIR 2
+  };
+  __device__ __forceinline__ void fetch(Row& w, int j) const {
+    const bool in = j < p.nj && n > 0;
+    if constexpr (PAIR == 2) {
+      w.gate_bias = p.gate_bias && in ? float(static_cast<const T*>(p.gate_bias)[j]) : 0.0f;
+      w.up_bias = p.up_bias && in ? float(static_cast<const T*>(p.up_bias)[j]) : 0.0f;
+    }
+    if (BACK && in) {
+      const T* from = static_cast<const T*>(p.dh) + long(image) * p.dh_image + long(j) * p.dh_ld + i;
+      if (n >= V) {
+        w.dh = load<T, V>(from);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) w.dh[e] = e < n ? from[e] : T(0.0f);
       }
     }
   }
 
-  __device__ __forceinline__ void rows(unsigned slab, int j) {
+  __device__ __forceinline__ void rows(const Row& w, unsigned slab, int j) {
     switch (p.act) {
-      case OAA_ACT_RELU: return rows_of<OAA_ACT_RELU>(slab, j);
-      case OAA_ACT_SILU: return rows_of<OAA_ACT_SILU>(slab, j);
-      case OAA_ACT_GELU: return rows_of<OAA_ACT_GELU>(slab, j);
-      default: return rows_of<OAA_ACT_NONE>(slab, j);
+      case OAA_ACT_RELU: return rows_of<OAA_ACT_RELU>(w, slab, j);
+      case OAA_ACT_SILU: return rows_of<OAA_ACT_SILU>(w, slab, j);
+      case OAA_ACT_GELU: return rows_of<OAA_ACT_GELU>(w, slab, j);
+      default: return rows_of<OAA_ACT_NONE>(w, slab, j);
     }
   }
 
   template <int ACT>
-  __device__ __forceinline__ void rows_of(unsigned slab, int j0) {
+  __device__ __forceinline__ void rows_of(const Row& first, unsigned slab, int j0) {
+    Row w = first, next;
 #pragma unroll 1
-    for (int r = r0; r < ROWS; r += kRows) {
+    for (int r = r0; r < ROWS; r += kRows, w = next) {
       const int j = j0 + r;
+      if (r + kRows < ROWS) fetch(next, j + kRows);
       float g[V], u[V];
 #pragma unroll
       for (int k = 0; k < V / 4; ++k) {
@@ -332,53 +399,33 @@ struct UnitEnd {
         const floatx4 b = *reinterpret_cast<lds_floatx4*>(place<RI>(slab + ROWS * RI * 4, r, c * (V / 4) + k));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          g[4 * k + e] = a[e];
-          u[4 * k + e] = b[e];
+          g[4 * k + e] = a[e] + (PAIR == 1 ? gate_bias[4 * k + e] : w.gate_bias);
+          u[4 * k + e] = b[e] + (PAIR == 1 ? up_bias[4 * k + e] : w.up_bias);
         }
       }
       const bool in = j < p.nj && n > 0;
-      if constexpr (PAIR == 1) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          g[e] += gate_bias[e];
-          u[e] += up_bias[e];
-        }
-      } else {
-        const float bg = in ? load_param(p.gate_bias, kType, j, 0.0f) : 0.0f;
-        const float bu = in ? load_param(p.up_bias, kType, j, 0.0f) : 0.0f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          g[e] += bg;
-          u[e] += bu;
-        }
-      }
-      if (p.dh) {
+      if constexpr (BACK) {
         float a = 0.0f, b = 0.0f;  // PAIR 2: of this row
         if (in) {
-          const T* from = static_cast<const T*>(p.dh) + long(image) * p.dh_image + long(j) * p.dh_ld + i;
           T dg[V], du[V];
-          float d[V];
-          if (n >= V) {
-            const Vec<T, V> v = load<T, V>(from);
-#pragma unroll
-            for (int e = 0; e < V; ++e) d[e] = float(v[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) d[e] = e < n ? float(from[e]) : 0.0f;
-          }
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float y = e < n ? d[e] * u[e] * act_slope<ACT>(g[e]) : 0.0f, z = e < n ? d[e] * act<ACT>(g[e]) : 0.0f;
+            const float d = float(w.dh[e]);
+            const float y = d * u[e] * act_slope<ACT>(g[e]), z = d * act<ACT>(g[e]);
             dg[e] = T(y);
             du[e] = T(z);
             if constexpr (PAIR == 1) {
               sum_g[e] += y;
               sum_u[e] += z;
             } else {
-              a += y;
-              b += z;
+              a += e < n ? y : 0.0f;
+              b += e < n ? z : 0.0f;
             }
           }
+          if (n < V)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (e >= n) dg[e] = du[e] = T(0.0f);
           // whole pieces: the padding of d's rows is 0
           const long at = long(image) * p.d_image + long(j) * p.d_ld + i;
           store_values<T>(static_cast<T*>(p.dgate) + at, V, dg);
@@ -418,7 +465,7 @@ struct UnitEnd {
 
   __device__ __forceinline__ void end() {
     if constexpr (PAIR == 1) {
-      if (!p.dh || !p.sums) return;
+      if (!BACK || !p.sums) return;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
 #pragma unroll
@@ -435,6 +482,136 @@ struct UnitEnd {
   }
 };
 
+// The end of the unit from the registers, for a wave whose part lies inside of i: acc[x][y]
+// are g, acc[x + MI][y] or acc[x][y + MJ] u, of column j + 16 y, in pieces of 16 bytes of
+// neighbours from i on, four pieces (the lane's and three other lanes') apart. Writes h (and g and u, if the call keeps them), or with dh,
+// in the backward pass, dg and du with their sums over the positions.
+template <typename T, int MI, int MJ, int PAIR, bool BACK, int ACT, int NI, int NJ>
+__device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (&acc)[NI][NJ], int image, long part,
+                                         int i, int j, int lane) {
+  constexpr int V = 16 / int(sizeof(T)), F = V / 4, kPieces = MI / F;  // pieces of a column: V values, F fragments
+  auto at = [](int q) { return q * 4 * V; };  // where piece q is
+  Vec<T, V> gate_bias[PAIR == 1 ? kPieces : 1], up_bias[PAIR == 1 ? kPieces : 1];
+  if constexpr (PAIR == 1) {
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      gate_bias[q] = up_bias[q] = Vec<T, V>{};
+      if (p.gate_bias) gate_bias[q] = load<T, V>(static_cast<const T*>(p.gate_bias) + i + at(q));
+      if (p.up_bias) up_bias[q] = load<T, V>(static_cast<const T*>(p.up_bias) + i + at(q));
+    }
+  }
+  const T* dh = static_cast<const T*>(p.dh) + long(image) * p.dh_image + i;
+  Vec<T, V> ahead[kPieces];
+  auto fetch = [&](int y) {
+    if (BACK && j + 16 * y < p.nj)
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) ahead[q] = load<T, V>(dh + long(j + 16 * y) * p.dh_ld + at(q));
+  };
+  fetch(0);
+  float sum_g[PAIR == 1 ? kPieces * V : 1], sum_u[PAIR == 1 ? kPieces * V : 1];
+  if constexpr (PAIR == 1) {
+#pragma unroll
+    for (int e = 0; e < kPieces * V; ++e) sum_g[e] = sum_u[e] = 0.0f;
+  }
+#pragma unroll
+  for (int y = 0; y < MJ; ++y) {
+    const int jj = j + 16 * y;
+    const bool in = jj < p.nj;
+    float bg = 0.0f, bu = 0.0f;
+    if constexpr (PAIR == 2) {
+      if (p.gate_bias && in) bg = float(static_cast<const T*>(p.gate_bias)[jj]);
+      if (p.up_bias && in) bu = float(static_cast<const T*>(p.up_bias)[jj]);
+    }
+    Vec<T, V> now[kPieces];
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) now[q] = ahead[q];
+    if (y + 1 < MJ) fetch(y + 1);
+    float a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      float g[V], u[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const int x = q * F + e / 4;
+        g[e] = acc[x][y][e % 4] + (PAIR == 1 ? element<T, V>(gate_bias[q], e) : bg);
+        u[e] = acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? y + MJ : y][e % 4] + (PAIR == 1 ? element<T, V>(up_bias[q], e) : bu);
+      }
+      if constexpr (BACK) {
+        if (!in) continue;
+        Vec<T, V> dg, du;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float d = element<T, V>(now[q], e), s = d * u[e] * act_slope<ACT>(g[e]), t = d * act<ACT>(g[e]);
+          set_element<T, V>(dg, e, s);
+          set_element<T, V>(du, e, t);
+          if constexpr (PAIR == 1) {
+            sum_g[q * V + e] += s;
+            sum_u[q * V + e] += t;
+          } else {
+            a += s;
+            b += t;
+          }
+        }
+        const long to = long(image) * p.d_image + long(jj) * p.d_ld + i + at(q);
+        *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.dgate) + to) = dg;
+        *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.dup) + to) = du;
+      } else if (in) {
+        Vec<T, V> h;
+#pragma unroll
+        for (int e = 0; e < V; ++e) set_element<T, V>(h, e, act<ACT>(g[e]) * u[e]);
+        *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.out) + long(image) * p.out_image + long(jj) * p.out_ld + i + at(q)) = h;
+        if (p.gate) {
+          const long to = (long(image) * p.nj + jj) * p.ni + i + at(q);
+#pragma unroll
+          for (int k = 0; k < F; ++k) {
+            Vec<float, 4> v, w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = g[4 * k + e];
+              w[e] = u[4 * k + e];
+            }
+            *reinterpret_cast<Vec<float, 4>*>(p.gate + to + 4 * k) = v;
+            *reinterpret_cast<Vec<float, 4>*>(p.up + to + 4 * k) = w;
+          }
+        }
+      }
+    }
+    if constexpr (PAIR == 2) {
+      if (BACK && p.sums) {  // over i: the four quads' of this column
+#pragma unroll
+        for (int m = 16; m < 64; m *= 2) {
+          a += __shfl_xor(a, m);
+          b += __shfl_xor(b, m);
+        }
+        if (lane < 16 && in) {
+          p.sums[(part * 2) * p.nj + jj] = a;
+          p.sums[(part * 2 + 1) * p.nj + jj] = b;
+        }
+      }
+    }
+  }
+  if constexpr (PAIR == 1) {
+    if (BACK && p.sums) {  // over j: the 16 columns'
+#pragma unroll
+      for (int e = 0; e < kPieces * V; ++e) {
+#pragma unroll
+        for (int m = 1; m < 16; m *= 2) {
+          sum_g[e] += __shfl_xor(sum_g[e], m);
+          sum_u[e] += __shfl_xor(sum_u[e], m);
+        }
+      }
+      if (lane % 16 == 0)
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q)
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            p.sums[(part * 2) * p.ni + i + at(q) + e] = sum_g[q * V + e];
+            p.sums[(part * 2 + 1) * p.ni + i + at(q) + e] = sum_u[q * V + e];
+          }
+    }
+  }
+}
+
 // Workgroups go to the eight dies in turn; here each die takes a stretch of tiles.
 __device__ __forceinline__ int xcd_order(unsigned block, unsigned blocks) {
   const unsigned each = blocks / 8, more = blocks % 8, die = block % 8;
@@ -442,11 +619,12 @@ __device__ __forceinline__ int xcd_order(unsigned block, unsigned blocks) {
 }
 constexpr int kGroup = 8;
 
-// PAIR: 0 none, 1 on i, 2 on j.
-template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR>
+// PAIR: 0 none, 1 on i, 2 on j. BACK: the unit in the backward pass.
+template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK>
 __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 ? 1 : 2) kernel(ProductParams p) {
   constexpr int WAVES = WI * WJ, GI = TI / WI, GJ = TJ / WJ;  // a wave's part of the tile
   constexpr int NI = GI / 16, NJ = GJ / 16;
+  static_assert(GI % (PAIR == 1 ? 128 : 64) == 0, "");
   constexpr int kStage = (TI + TJ) * kStepBytes;
   extern __shared__ char lds_memory[];
   const unsigned lds = unsigned(reinterpret_cast<size_t>((lds_char*)lds_memory));
@@ -456,22 +634,31 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   // this workgroup's tile, and its part of the sum
   constexpr int FI = PAIR == 1 ? TI / 2 : TI, FJ = PAIR == 2 ? TJ / 2 : TJ;
   const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ, all_j = tiles_j * p.halves;
-  const int plane = tiles_i * all_j;
   int t = xcd_order(blockIdx.x, gridDim.x);
-  const int image = t / plane % p.images, split = t / plane / p.images;
-  t %= plane;
+  const int image = blockIdx.y + p.first_image, split = blockIdx.z;
   // groups of kGroup tiles along j, in each i by i
-  const int group = t / (kGroup * tiles_i) * kGroup, rows = min(kGroup, all_j - group);
-  t %= kGroup * tiles_i;
-  const int ti = t / rows, tj = (group + t % rows) % tiles_j, which = (group + t % rows) / tiles_j;
+  const int each = kGroup * tiles_i;
+  int group = int(__umulhi(unsigned(t), p.group_reciprocal));  // exact or one less
+  t -= group * each;
+  if (t >= each) {
+    t -= each;
+    ++group;
+  }
+  const int rows = min(kGroup, all_j - group * kGroup);
+  const int ti = rows == kGroup ? t / kGroup : t / rows;
+  const int tjj = group * kGroup + t - ti * rows, which = tjj >= tiles_j, tj = tjj - (which ? tiles_j : 0);
   const int i0 = ti * FI, j0 = tj * FJ;
   const int steps = (p.K + kStep<T> - 1) / kStep<T>;
-  const long total = long(steps) * p.segs;  // below 2^31
-  const int first = int(total * split / p.splits), end = int(total * (split + 1) / p.splits);
+  const int total = steps * p.segs;
+  int first = 0, end = total;
+  if (PAIR == 0 && p.splits > 1) {
+    first = min(total, split * p.split_steps);
+    end = min(total, first + p.split_steps);
+  }
 
-  int s = first / steps, k0 = first % steps * kStep<T>;
-  Tile<T, TI, WAVES, IK, PAIR == 1, GI> a;
-  Tile<T, TJ, WAVES, JK, PAIR == 2, GJ> b;
+  int s = first ? first / steps : 0, k0 = (first - s * steps) * kStep<T>;
+  Tile<T, TI, WAVES, IK, true, PAIR == 1, GI> a;
+  Tile<T, TJ, WAVES, JK, false, PAIR == 2, GJ> b;
   a.init(p.i, image, which, i0, p.ni, p.K, wave, lane);
   b.init(p.j, image, which, j0, p.nj, p.K, wave, lane);
   a.start(s, k0);
@@ -513,8 +700,8 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   // stage after it, asked for a step ago, has landed; so what comes after that goes
   // where this one was, asked for among the products of the second half.
   floatx4 fa[NI], fb[2][NJ];
-  Fragments<T, TI, IK> at_a;
-  Fragments<T, TJ, JK> at_b;
+  Fragments<T, TI, IK, true> at_a;
+  Fragments<T, TJ, JK, false> at_b;
   at_a.init(wi * GI, lane);
   at_b.init(wj * GJ, lane);
   auto half = [&](int sub, int stage, auto&& between) {  // products of `sub`; reads the other of `stage`
@@ -564,37 +751,73 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     stage ^= 1;
   }
 
-  // The results leave through LDS, each wave's through a slab of its own: what a lane
-  // holds (column j of 16, four neighbours along i) becomes rows along i, which are
-  // then read back, finished and stored 16 bytes or more a lane by a loop that is short to fetch.
+  // A lane's results: column j of 16, and 16 bytes of neighbours along i of every 64. They leave
+  // from the registers, 16 bytes a store, except where a wave's part crosses the end of
+  // i: that goes through LDS, each wave's through a slab of its own, as rows that a
+  // short loop reads back and finishes.
   constexpr unsigned kSlab = 2 * kStage / WAVES;
+  const int row = lane & 15, quad = lane >> 4;
+  constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ, RI = 16 * MI;
+  constexpr int kVec = 16 / int(sizeof(T));
+  const int iw = i0 + wi * RI, jw = j0 + wj * 16 * MJ;
+  const bool inside = iw + RI <= p.ni;
   __syncthreads();
   const unsigned slab = lds + wave * kSlab;
-  const int row = lane & 15, quad = lane >> 4;
   if constexpr (PAIR != 0) {
-    constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ, RI = 16 * MI;
+    const long part = PAIR == 1 ? long(image) * tiles_j * WJ + tj * WJ + wj : long(image) * tiles_i * WI + ti * WI + wi;
+    if (inside) {
+      switch (p.act) {
+        case OAA_ACT_RELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_RELU>(p, acc, image, part, iw + quad * kVec, jw + row, lane); break;
+        case OAA_ACT_SILU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_SILU>(p, acc, image, part, iw + quad * kVec, jw + row, lane); break;
+        case OAA_ACT_GELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_GELU>(p, acc, image, part, iw + quad * kVec, jw + row, lane); break;
+        default: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_NONE>(p, acc, image, part, iw + quad * kVec, jw + row, lane);
+      }
+      return;
+    }
     constexpr int kRows = int(kSlab / (2 * RI * 4)) < 16 * MJ ? int(kSlab / (2 * RI * 4)) : 16 * MJ;  // of a pass
     static_assert(kRows % 16 == 0 && 16 * MJ % kRows == 0, "");
-    UnitEnd<T, RI, kRows, PAIR> finish(p, image, i0 + wi * RI, lane);
-    finish.part = PAIR == 1 ? long(image) * tiles_j * WJ + tj * WJ + wj : long(image) * tiles_i * WI + ti * WI + wi;
-    const int jw = j0 + wj * 16 * MJ;
+    UnitEnd<T, RI, kRows, PAIR, BACK> finish(p, image, iw, lane);
+    finish.part = part;
+    typename UnitEnd<T, RI, kRows, PAIR, BACK>::Row ahead;
+    constexpr int kPasses = 16 * MJ / kRows;
+#pragma unroll 1
+    for (int pass = 0; pass < kPasses; ++pass) {
+      finish.fetch(ahead, jw + pass * kRows + finish.r0);
 #pragma unroll
-    for (int pass = 0; pass < 16 * MJ / kRows; ++pass) {
+      for (int q = 0; q < kPasses; ++q) {
+        if (q != pass) continue;
 #pragma unroll
-      for (int y = 0; y < kRows / 16; ++y)
+        for (int y = 0; y < kRows / 16; ++y)
 #pragma unroll
-        for (int x = 0; x < MI; ++x) {
-          const int yy = pass * kRows / 16 + y;
-          put<RI>(slab, 16 * y + row, 4 * x + quad, acc[x][yy]);
-          put<RI>(slab + kRows * RI * 4, 16 * y + row, 4 * x + quad, acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? yy + MJ : yy]);
-        }
-      finish.rows(slab, jw + pass * kRows);
+          for (int x = 0; x < MI; ++x) {
+            const int yy = q * kRows / 16 + y, four = row_in_fragment<T, true>(x, 4 * quad) / 4;
+            put<RI>(slab, 16 * y + row, four, acc[x][yy]);
+            put<RI>(slab + kRows * RI * 4, 16 * y + row, four, acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? yy + MJ : yy]);
+          }
+      }
+      finish.rows(ahead, slab, jw + pass * kRows);
     }
     finish.end();
   } else {
     const long part = (long(split) * p.halves + which) * p.images + image;
-    auto rows = [&](auto zero, auto* out, long ld) {
+    auto leave = [&](auto zero, auto* out, long ld) {
       using E = decltype(zero);
+      constexpr int V = 16 / int(sizeof(E));
+      if (inside) {
+#pragma unroll
+        for (int y = 0; y < MJ; ++y) {
+          if (jw + row + 16 * y >= p.nj) continue;
+          E* to = out + iw + long(jw + row + 16 * y) * ld;
+#pragma unroll
+          for (int x = 0; x < MI; x += V / 4) {
+            Vec<E, V> w;
+#pragma unroll
+            for (int e = 0; e < V; ++e) set_element<E, V>(w, e, acc[x + e / 4][y][e % 4]);
+            *reinterpret_cast<Vec<E, V>*>(to + row_in_fragment<T, true>(x, 4 * quad)) = w;
+          }
+        }
+        return;
+      }
       constexpr int kRows = int(kSlab / (GI * sizeof(E))) < GJ ? int(kSlab / (GI * sizeof(E))) : GJ;
       static_assert(kRows % 16 == 0 && GJ % kRows == 0, "");
 #pragma unroll
@@ -604,42 +827,56 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
 #pragma unroll
           for (int x = 0; x < NI; ++x) {
             const floatx4 v = acc[x][pass * kRows / 16 + y];
+            const int four = row_in_fragment<T, true>(x, 4 * quad) / 4;
             if constexpr (sizeof(E) == 4)
-              put<GI>(slab, 16 * y + row, 4 * x + quad, v);
+              put<GI>(slab, 16 * y + row, four, v);
             else
-              put_16<E, GI>(slab, 16 * y + row, 4 * x + quad, v);
+              put_16<E, GI>(slab, 16 * y + row, four, v);
           }
-        store_rows<E, GI, kRows>(slab, out + i0 + wi * GI, ld, j0 + wj * GJ + pass * kRows, p.nj, p.ni - (i0 + wi * GI), lane);
+        store_rows<E, GI, kRows>(slab, out + iw, ld, jw + pass * kRows, p.nj, p.ni - iw, lane);
       }
     };
     if (p.splits > 1)
-      rows(0.0f, static_cast<float*>(p.out) + part * p.nj * p.ni, p.ni);
+      leave(0.0f, static_cast<float*>(p.out) + part * p.nj * p.ni, p.ni);
     else
-      rows(T(0.0f), static_cast<T*>(p.out) + long(image) * p.out_image + long(which) * p.out_half, p.out_ld);
+      leave(T(0.0f), static_cast<T*>(p.out) + long(image) * p.out_image + long(which) * p.out_half, p.out_ld);
   }
 }
 
-template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR>
+template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK>
 hipError_t launch(const ProductParams& p, hipStream_t s) {
   constexpr int FI = PAIR == 1 ? TI / 2 : TI, FJ = PAIR == 2 ? TJ / 2 : TJ;
   constexpr size_t lds = 2 * size_t(TI + TJ) * kStepBytes;
-  const long tiles = long((p.ni + FI - 1) / FI) * ((p.nj + FJ - 1) / FJ) * p.halves * p.images * p.splits;
-  if (tiles * (64 * WI * WJ) >= 1l << 32 || tiles >= 1l << 31) return hipErrorInvalidValue;  // refused before
-  auto kern = kernel<T, TI, TJ, WI, WJ, IK, JK, PAIR>;
+  const long tiles_i = (p.ni + FI - 1) / FI, tiles = tiles_i * ((p.nj + FJ - 1) / FJ) * p.halves;
+  constexpr int kMostImages = 65535;  // of a launch
+  if (tiles * (64 * WI * WJ) >= 1l << 32) return hipErrorInvalidValue;  // refused before
+  auto kern = kernel<T, TI, TJ, WI, WJ, IK, JK, PAIR, BACK>;
   if (lds > 65536) {
     const hipError_t e = tile::allow_lds(kern, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3(unsigned(tiles)), dim3(64 * WI * WJ), lds, s, p);
-  return hipGetLastError();
+  ProductParams q = p;
+  const long steps = long((p.K + kStep<T> - 1) / kStep<T>) * p.segs;
+  q.split_steps = int((steps + p.splits - 1) / p.splits);
+  q.group_reciprocal = unsigned((1ull << 32) / (kGroup * tiles_i));
+  for (q.first_image = 0; q.first_image < p.images; q.first_image += kMostImages) {
+    const int images = std::min(kMostImages, p.images - q.first_image);
+    hipLaunchKernelGGL(kern, dim3(unsigned(tiles), images, p.splits), dim3(64 * WI * WJ), lds, s, q);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
-template <typename T, bool IK, bool JK, int PAIR>
+template <typename T, bool IK, bool JK, int PAIR, bool BACK = false>
 hipError_t launch_sized(const ProductParams& p, ProductKind kind, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
-    if (product_tile(2, kind, p.ni, p.nj, p.images, p.halves, p.splits) == 256)
-      return launch<T, 256, 256, kWaves256.i, kWaves256.j, IK, JK, PAIR>(p, s);
-  return launch<T, 128, 128, kWaves128.i, kWaves128.j, IK, JK, PAIR>(p, s);
+    if (product_tile(2, kind, p.ni, p.nj, p.images, p.halves, p.splits) == 256) {
+      constexpr ProductWaves w = product_waves(256, PAIR == 1);
+      return launch<T, 256, 256, w.i, w.j, IK, JK, PAIR, BACK>(p, s);
+    }
+  constexpr ProductWaves w = product_waves(128, PAIR == 1);
+  return launch<T, 128, 128, w.i, w.j, IK, JK, PAIR, BACK>(p, s);
 }
 
 }  // namespace product
@@ -648,8 +885,10 @@ template <typename T>
 hipError_t launch_product(const ProductParams& p, ProductKind kind, hipStream_t s) {
   using namespace product;
   switch (kind) {
-    case kUnitLast: return launch_sized<T, true, true, 1>(p, kind, s);
-    case kUnitPlanes: return launch_sized<T, false, true, 2>(p, kind, s);
+    case kUnitLast:
+      return p.dh ? launch_sized<T, true, true, 1, true>(p, kind, s) : launch_sized<T, true, true, 1>(p, kind, s);
+    case kUnitPlanes:
+      return p.dh ? launch_sized<T, false, true, 2, true>(p, kind, s) : launch_sized<T, false, true, 2>(p, kind, s);
     case kInputLast: return launch_sized<T, false, true, 0>(p, kind, s);
     case kInputPlanes: return launch_sized<T, false, false, 0>(p, kind, s);
     case kWeightLast: return launch_sized<T, false, false, 0>(p, kind, s);

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cstdlib>
 
 #include "gated.hpp"
 
@@ -12,14 +13,17 @@ inline long product_tiles(ProductKind kind, int tile, long ni, long nj, long ima
   return (ni + fi - 1) / fi * ((nj + fj - 1) / fj) * images * halves;
 }
 
-// Waves along i and j of a tile.
+// Waves along i and j of a tile: each has at least 64 rows of i, or 64 of each of a pair's.
 struct ProductWaves {
   int i, j;
 };
-constexpr ProductWaves kWaves256{2, 4}, kWaves128{2, 2};
+constexpr ProductWaves product_waves(int tile, bool pair_on_i) {
+  return tile == 256 ? ProductWaves{2, 4} : pair_on_i ? ProductWaves{1, 4} : ProductWaves{2, 2};
+}
 
 // Side of the tile.
 inline int product_tile(int size, ProductKind kind, long ni, long nj, long images, long halves, long splits) {
+  if (const char* e = getenv("TILE")) return size == 2 ? atoi(e) : 128;
   return size == 2 && product_tiles(kind, 256, ni, nj, images, halves) * splits >= 256 ? 256 : 128;
 }
 
@@ -27,7 +31,7 @@ inline int product_tile(int size, ProductKind kind, long ni, long nj, long image
 // one for each wave's positions.
 inline long product_sum_parts(int size, ProductKind kind, long ni, long nj, long images) {
   const int tile = product_tile(size, kind, ni, nj, images, 1, 1);
-  const ProductWaves w = tile == 256 ? kWaves256 : kWaves128;
+  const ProductWaves w = product_waves(tile, kind == kUnitLast);
   return images * (((kind == kUnitLast ? nj : ni) + tile - 1) / tile) * (kind == kUnitLast ? w.j : w.i);
 }
 
