@@ -166,15 +166,31 @@ __global__ void __launch_bounds__(1024) bias_join_kernel(const float* sums, long
   if (pl == 0 && f < F) out[f] = T(float(share[0][cl]));
 }
 
-template <typename T>
+// LANES threads an output, each with its share of the parts; added up in a fixed order.
+template <typename T, int LANES>
 __global__ void __launch_bounds__(kThreads) join_kernel(JoinParams p) {
+  constexpr int WIDE = kThreads / LANES;  // outputs of a workgroup
+  __shared__ float share[LANES][WIDE];
   const long each = p.n / p.outputs;
-  for (long i = long(blockIdx.x) * kThreads + threadIdx.x; i < p.n; i += long(gridDim.x) * kThreads) {
-    float a = p.part[i];
-#pragma unroll 4
-    for (int k = 1; k < p.splits; ++k) a += p.part[k * p.n + i];
-    const int which = i >= each;
-    static_cast<T*>(p.out[which])[i - which * each] = T(a);
+  const int o = threadIdx.x % WIDE, l = threadIdx.x / WIDE;
+  for (long first = long(blockIdx.x) * WIDE; first < p.n; first += long(gridDim.x) * WIDE) {
+    const long i = first + o;
+    float a = 0.0f;
+    if (i < p.n)
+#pragma unroll 8
+      for (int k = l; k < p.splits; k += LANES) a += p.part[k * p.n + i];
+    if constexpr (LANES > 1) {
+      share[l][o] = a;
+      __syncthreads();
+      if (l == 0)
+#pragma unroll
+        for (int k = 1; k < LANES; ++k) a += share[k][o];
+      __syncthreads();
+    }
+    if (l == 0 && i < p.n) {
+      const int which = i >= each;
+      static_cast<T*>(p.out[which])[i - which * each] = T(a);
+    }
   }
 }
 
@@ -239,7 +255,12 @@ hipError_t launch_bias_join(const float* sums, long parts, int F, void* gate, vo
 template <typename T>
 hipError_t launch_join(const JoinParams& p, hipStream_t s) {
   using namespace passes;
-  hipLaunchKernelGGL((join_kernel<T>), dim3(blocks_for((p.n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
+  // few outputs leave most of the device to the parts: what takes time is how many loads
+  // follow each other
+  if (p.n < 100000 && p.splits > 8)
+    hipLaunchKernelGGL((join_kernel<T, 16>), dim3(blocks_for((p.n + 15) / 16)), dim3(kThreads), 0, s, p);
+  else
+    hipLaunchKernelGGL((join_kernel<T, 1>), dim3(blocks_for((p.n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 

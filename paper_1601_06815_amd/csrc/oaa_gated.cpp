@@ -269,7 +269,7 @@ Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w
   l.dup = room.take(d_bytes);
   l.part_rows = std::max(kPartRows, (rows * u.B + kMostParts - 1) / kMostParts);
   if (need_b) {
-    l.parts = remake ? oaa::product_sum_parts(int(u.size), u.last ? oaa::kUnitLast : oaa::kUnitPlanes, columns, rows, u.B)
+    l.parts = remake ? oaa::product_sum_parts(int(u.size), u.last ? oaa::kUnitLast : oaa::kUnitPlanes, columns, rows, u.B, u.C)
               : u.last ? u.B * ((rows + l.part_rows - 1) / l.part_rows)
                        : u.B;
     l.sums = static_cast<float*>(room.take(size_t(l.parts) * 2 * u.F * 4));

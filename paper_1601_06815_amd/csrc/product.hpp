@@ -89,14 +89,14 @@ __device__ __forceinline__ constexpr int row_in_fragment(int x, int m) {
 }
 
 // The key of an operand's row r (k rows) or line k (k columns), by how fragments read it:
-// rows that a read takes together lie in different banks.
-template <typename T, bool KROWS, bool I>
+// rows that a read takes together lie in different banks. R: rows of the tile.
+template <typename T, int R, bool KROWS, bool I>
 __device__ __forceinline__ int key_of(int r) {
   constexpr bool kApart = I && sizeof(T) == 2;
   if constexpr (KROWS)
     return kApart ? (r & 3) | (r >> 3 & 1) << 2 : r & 7;
   else if constexpr (sizeof(T) == 2)
-    return (r & 3) << (kApart ? 2 : 1);
+    return !kApart ? (r & 3) << 1 : R == 64 ? (r >> 1 & 1) << 2 : (r & 3) << 2;
   else
     return (r >> 2 & 3) << 2;
 }
@@ -155,10 +155,10 @@ struct Tile {
       const int q = wave + m * WAVES;
       if constexpr (KROWS) {
         offset[m] = unsigned(lane >> 3) * unsigned(ld) +
-                    unsigned(((lane & 7) ^ key_of<T, KROWS, I>(8 * q + (lane >> 3))) * 16);
+                    unsigned(((lane & 7) ^ key_of<T, R, KROWS, I>(8 * q + (lane >> 3))) * 16);
       } else {
         const int byte = q * 1024 + lane * 16, k = byte / kLine, piece = byte % kLine / 16;
-        offset[m] = unsigned(lane * 16 / kLine) * unsigned(ld) + unsigned((piece ^ key_of<T, KROWS, I>(k)) * 16);
+        offset[m] = unsigned(lane * 16 / kLine) * unsigned(ld) + unsigned((piece ^ key_of<T, R, KROWS, I>(k)) * 16);
       }
     }
   }
@@ -181,7 +181,7 @@ struct Tile {
       asm volatile("" : "+v"(t));  // nothing of this is worked out ahead, and held, by the loop around it
 #pragma unroll 1
       for (int w = t; w < R * 32; w += 64 * WAVES) {
-        const int piece = (w % 32 / 4) ^ key_of<T, KROWS, I>(w / 32);
+        const int piece = (w % 32 / 4) ^ key_of<T, R, KROWS, I>(w / 32);
         if (piece * 16 + w % 4 * 4 >= left) *reinterpret_cast<__attribute__((address_space(3))) int*>(lds + w * 4) = 0;
       }
     }
@@ -189,7 +189,7 @@ struct Tile {
 };
 
 // Where a lane finds its fragments in a tile: fragment x from row `first` (a multiple of
-// 64) on, half `sub` of the step. LDS addresses without the tile's own; fragments that
+// 32 for i, 16 for j) on, half `sub` of the step. LDS addresses without the tile's own; fragments that
 // differ by a fixed distance share one.
 template <typename T, int R, bool KROWS, bool I>
 struct Fragments {
@@ -202,17 +202,17 @@ struct Fragments {
       const int row = first + row_in_fragment<T, I>(0, m);
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
-        at[sub] = row * kStepBytes + ((4 * sub + g) ^ key_of<T, KROWS, I>(row)) * 16;
+        at[sub] = row * kStepBytes + ((4 * sub + g) ^ key_of<T, R, KROWS, I>(row)) * 16;
     } else {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         if constexpr (sizeof(T) == 2) {
           // a transposing read: lane 4 r + c asks for values 4 c .. 4 c + 3 of line r
           const int k = 8 * g + (m >> 2), column = first + row_in_fragment<T, I>(I ? 2 * b : b, m % 4 * 4);
-          at[b] = k * (R * 2) + ((column / 8) ^ key_of<T, KROWS, I>(k)) * 16 + column % 8 * 2;
+          at[b] = k * (R * 2) + ((column / 8) ^ key_of<T, R, KROWS, I>(k)) * 16 + column % 8 * 2;
         } else {
           const int k = 4 * g, column = first + row_in_fragment<T, I>(b, m);
-          at[b] = k * (R * 4) + ((column / 4) ^ key_of<T, KROWS, I>(k)) * 16 + column % 4 * 4;
+          at[b] = k * (R * 4) + ((column / 4) ^ key_of<T, R, KROWS, I>(k)) * 16 + column % 4 * 4;
         }
       }
     }
@@ -624,7 +624,7 @@ template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR
 __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 ? 1 : 2) kernel(ProductParams p) {
   constexpr int WAVES = WI * WJ, GI = TI / WI, GJ = TJ / WJ;  // a wave's part of the tile
   constexpr int NI = GI / 16, NJ = GJ / 16;
-  static_assert(GI % (PAIR == 1 ? 128 : 64) == 0, "");
+  static_assert(GI % (PAIR == 1 ? 64 : 32) == 0 && GJ % (PAIR == 2 ? 32 : 16) == 0, "");
   constexpr int kStage = (TI + TJ) * kStepBytes;
   extern __shared__ char lds_memory[];
   const unsigned lds = unsigned(reinterpret_cast<size_t>((lds_char*)lds_memory));
@@ -870,13 +870,18 @@ hipError_t launch(const ProductParams& p, hipStream_t s) {
 
 template <typename T, bool IK, bool JK, int PAIR, bool BACK = false>
 hipError_t launch_sized(const ProductParams& p, ProductKind kind, hipStream_t s) {
+  const int tile = product_tile(sizeof(T), kind, p.ni, p.nj, p.images, p.halves, p.K, p.segs);
   if constexpr (sizeof(T) == 2)
-    if (product_tile(2, kind, p.ni, p.nj, p.images, p.halves, p.splits) == 256) {
+    if (tile == 256) {
       constexpr ProductWaves w = product_waves(256, PAIR == 1);
       return launch<T, 256, 256, w.i, w.j, IK, JK, PAIR, BACK>(p, s);
     }
-  constexpr ProductWaves w = product_waves(128, PAIR == 1);
-  return launch<T, 128, 128, w.i, w.j, IK, JK, PAIR, BACK>(p, s);
+  if (tile == 128) {
+    constexpr ProductWaves w = product_waves(128, PAIR == 1);
+    return launch<T, 128, 128, w.i, w.j, IK, JK, PAIR, BACK>(p, s);
+  }
+  constexpr ProductWaves w = product_waves(64, PAIR == 1);
+  return launch<T, 64, 64, w.i, w.j, IK, JK, PAIR, BACK>(p, s);
 }
 
 }  // namespace product
