@@ -38,10 +38,10 @@ struct ProductParams {
   int images, halves;
   int K, segs;
   int splits;  // the sum's steps are cut into so many parts
-  // the launcher's own: the launch's first image, steps of a part of the sum, and a
-  // reciprocal for the tiles' order
-  int first_image, split_steps;
-  unsigned group_reciprocal;
+  // the launcher's own: tiles in all, steps of a part of the sum, and 2^32 over the tiles of
+  // an image and over those of a group
+  int tiles, split_steps;
+  unsigned plane_reciprocal, group_reciprocal;
   // D: element strides; partial sums in 32 bits if splits > 1, dense [split][half][image][nj][ni]
   void* out;
   long out_image, out_half;
@@ -61,7 +61,21 @@ struct ProductParams {
 };
 
 // Which operands have k contiguous, and which side the pair of W is on (the unit).
-enum ProductKind { kUnitLast, kUnitPlanes, kInputLast, kInputPlanes, kWeightLast, kWeightPlanes };
+// ("again": the unit in the backward pass.)
+enum ProductKind {
+  kUnitLast, kUnitPlanes, kUnitLastAgain, kUnitPlanesAgain, kInputLast, kInputPlanes, kWeightLast, kWeightPlanes
+};
+
+// The unit of few positions: rows of x, h and the weights at any address, with their
+// elements apart; g and u dense.
+struct FewParams {
+  long T, C, F;
+  const void *x, *gate_weight, *up_weight, *gate_bias, *up_bias;
+  long x_row, gate_row, up_row, h_row;
+  void* h;
+  float *gate, *up;  // or null
+  int act;
+};
 
 // D's parts added up in order, rounded to T: `n` values in `outputs` tensors of n / outputs.
 struct JoinParams {
@@ -101,6 +115,8 @@ struct PackParams {  // a strided operand as dense rows of ld elements, 0 beyond
 // (what a load into LDS takes), offsets within a tile below 2^31.
 template <typename T>
 hipError_t launch_product(const ProductParams& p, ProductKind kind, hipStream_t s);
+template <typename T>
+hipError_t launch_few(const FewParams& p, hipStream_t s);
 template <typename T>
 hipError_t launch_slope(const SlopeParams& p, hipStream_t s);
 // The partial sums of launch_slope, rounded to T, into whichever is not null.

@@ -167,6 +167,7 @@ long bytes_between(const void* a, const void* b) {
 // weights say which need copies.
 struct Layout {
   Unit u;
+  bool few;  // forward: few positions, nothing is copied
   Source x, gate_w, up_w;
   bool copy_x, copy_w;
   void *dgate, *dup;
@@ -205,6 +206,8 @@ Layout forward_layout(const Unit& whole_unit, const void* x, const void* gate_w,
   Layout l{};
   l.u = collapsed(whole_unit, false);
   const Unit& u = l.u;
+  l.few = u.last && u.B == 1 && u.S <= oaa::kFewPositions;
+  if (l.few) return l;
   Room room{static_cast<char*>(ws), 0};
   place_x(&l, x, u.last ? kRows : kColumns, &room);
   place_weights(&l, gate_w, up_w, kRows, &room);
@@ -269,7 +272,7 @@ Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w
   l.dup = room.take(d_bytes);
   l.part_rows = std::max(kPartRows, (rows * u.B + kMostParts - 1) / kMostParts);
   if (need_b) {
-    l.parts = remake ? oaa::product_sum_parts(int(u.size), u.last ? oaa::kUnitLast : oaa::kUnitPlanes, columns, rows, u.B, u.C)
+    l.parts = remake ? oaa::product_sum_parts(int(u.size), u.last ? oaa::kUnitLastAgain : oaa::kUnitPlanesAgain, columns, rows, u.B, u.C)
               : u.last ? u.B * ((rows + l.part_rows - 1) / l.part_rows)
                        : u.B;
     l.sums = static_cast<float*>(room.take(size_t(l.parts) * 2 * u.F * 4));
@@ -438,6 +441,12 @@ oaa_status_t oaa_gated_forward(const oaa_gated_t* d, const void* x, const void* 
   const Unit& u = l.u;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
+  if (l.few) {
+    const oaa::FewParams f{u.S, u.C, u.F, x, gate_weight, up_weight, gate_bias, up_bias, u.x_row, u.gate_row, u.up_row,
+                           u.h_row, h, gate, up, u.act};
+    return hip_status(for_type(u.dtype, [&](auto t) { return oaa::launch_few<decltype(t)>(f, s); }),
+                      "gated unit, forward");
+  }
   if (hipError_t e = make_copies(l, x, gate_weight, up_weight, s)) return hip_status(e, "gated unit, copies");
   ProductParams p = unit_product(l, gate_bias, up_bias);
   p.out = h;
@@ -517,7 +526,7 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
     p.d_ld = l.d_ld;
     p.sums = l.sums;
     e = for_type(u.dtype, [&](auto t) {
-      return oaa::launch_product<decltype(t)>(p, u.last ? oaa::kUnitLast : oaa::kUnitPlanes, s);
+      return oaa::launch_product<decltype(t)>(p, u.last ? oaa::kUnitLastAgain : oaa::kUnitPlanesAgain, s);
     });
   } else {
     oaa::SlopeParams slope{};

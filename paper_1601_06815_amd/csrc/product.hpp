@@ -101,6 +101,12 @@ __device__ __forceinline__ int key_of(int r) {
     return (r >> 2 & 3) << 2;
 }
 
+// The same, but for the last N memory operations of this wave.
+template <int N>
+__device__ __forceinline__ void wait_but_for() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 // One operand's tile: R rows, loaded by WAVES waves. PAIR: rows come in groups of
 // GROUP, the first half of each from gate's operand, the second from up's.
 //
@@ -482,32 +488,74 @@ struct UnitEnd {
   }
 };
 
-// The end of the unit from the registers, for a wave whose part lies inside of i: acc[x][y]
-// are g, acc[x + MI][y] or acc[x][y + MJ] u, of column j + 16 y, in pieces of 16 bytes of
-// neighbours from i on, four pieces (the lane's and three other lanes') apart. Writes h (and g and u, if the call keeps them), or with dh,
-// in the backward pass, dg and du with their sums over the positions.
-template <typename T, int MI, int MJ, int PAIR, bool BACK, int ACT, int NI, int NJ>
-__device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (&acc)[NI][NJ], int image, long part,
-                                         int i, int j, int lane) {
-  constexpr int V = 16 / int(sizeof(T)), F = V / 4, kPieces = MI / F;  // pieces of a column: V values, F fragments
-  auto at = [](int q) { return q * 4 * V; };  // where piece q is
-  Vec<T, V> gate_bias[PAIR == 1 ? kPieces : 1], up_bias[PAIR == 1 ? kPieces : 1];
-  if constexpr (PAIR == 1) {
+// What the end of the unit needs from memory, for a wave whose part lies inside of i:
+// biases and, in the backward pass, dh. Columns j + 16 y; pieces of 16 bytes from i on, four
+// pieces (the lane's and three other lanes') apart.
+template <typename T, int MI, int MJ, int PAIR, bool BACK>
+struct UnitNeeds {
+  static constexpr int V = 16 / int(sizeof(T)), F = V / 4, kPieces = MI / F;  // a piece: V values, F fragments
+  static constexpr int kBiases = PAIR == 1 ? kPieces : MJ;
+  using Bias = std::conditional_t<PAIR == 1, Vec<T, V>, T>;
+  Bias gate_bias[kBiases], up_bias[kBiases];
+  Vec<T, V> dh[BACK ? MJ * kPieces : 1];
+
+  static constexpr int at(int q) { return q * 4 * V; }  // where piece q is
+  __device__ __forceinline__ void fetch(const ProductParams& p, int image, int i, int j) {
 #pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-      gate_bias[q] = up_bias[q] = Vec<T, V>{};
-      if (p.gate_bias) gate_bias[q] = load<T, V>(static_cast<const T*>(p.gate_bias) + i + at(q));
-      if (p.up_bias) up_bias[q] = load<T, V>(static_cast<const T*>(p.up_bias) + i + at(q));
+    for (int k = 0; k < kBiases; ++k) {
+      gate_bias[k] = up_bias[k] = Bias{};
+      const int f = PAIR == 1 ? i + at(k) : j + 16 * k;
+      if (PAIR == 2 && f >= p.nj) continue;
+      if (p.gate_bias) gate_bias[k] = *reinterpret_cast<const Bias*>(static_cast<const T*>(p.gate_bias) + f);
+      if (p.up_bias) up_bias[k] = *reinterpret_cast<const Bias*>(static_cast<const T*>(p.up_bias) + f);
+    }
+    if constexpr (BACK) {
+      const T* from = static_cast<const T*>(p.dh) + long(image) * p.dh_image + i;
+#pragma unroll
+      for (int y = 0; y < MJ; ++y)
+        if (j + 16 * y < p.nj)
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q) dh[y * kPieces + q] = load<T, V>(from + long(j + 16 * y) * p.dh_ld + at(q));
     }
   }
-  const T* dh = static_cast<const T*>(p.dh) + long(image) * p.dh_image + i;
-  Vec<T, V> ahead[kPieces];
-  auto fetch = [&](int y) {
-    if (BACK && j + 16 * y < p.nj)
+  // All of it is here: the compiler's waits for it come before this, not among what follows.
+  __device__ __forceinline__ void arrive() {
 #pragma unroll
-      for (int q = 0; q < kPieces; ++q) ahead[q] = load<T, V>(dh + long(j + 16 * y) * p.dh_ld + at(q));
-  };
-  fetch(0);
+    for (int k = 0; k < kBiases; ++k) {
+      hold(gate_bias[k]);
+      hold(up_bias[k]);
+    }
+    if constexpr (BACK) {
+#pragma unroll
+      for (int k = 0; k < MJ * kPieces; ++k) hold(dh[k]);
+    }
+  }
+  template <typename E>
+  static __device__ __forceinline__ void hold(E& e) {
+    if constexpr (sizeof(E) == 16) {
+      floatx4 v = __builtin_bit_cast(floatx4, e);
+      asm volatile("" : "+v"(v));
+      e = __builtin_bit_cast(E, v);
+    } else if constexpr (sizeof(E) == 4) {
+      asm volatile("" : "+v"(e));
+    } else {
+      int v = __builtin_bit_cast(unsigned short, e);
+      asm volatile("" : "+v"(v));
+      e = __builtin_bit_cast(E, static_cast<unsigned short>(v));
+    }
+  }
+};
+
+// The end of the unit from the registers, for such a wave: acc[x][y] are g, acc[x +
+// MI][y] or acc[x][y + MJ] u. Writes h (and g and u, if the call keeps them), or in the
+// backward pass dg and du with their sums over the positions.
+template <typename T, int MI, int MJ, int PAIR, bool BACK, int ACT, int NI, int NJ>
+__device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (&acc)[NI][NJ],
+                                         const UnitNeeds<T, MI, MJ, PAIR, BACK>& needs, int image, long part, int i,
+                                         int j, int lane) {
+  using Needs = UnitNeeds<T, MI, MJ, PAIR, BACK>;
+  constexpr int V = Needs::V, F = Needs::F, kPieces = Needs::kPieces;
+  auto at = [](int q) { return Needs::at(q); };
   float sum_g[PAIR == 1 ? kPieces * V : 1], sum_u[PAIR == 1 ? kPieces * V : 1];
   if constexpr (PAIR == 1) {
 #pragma unroll
@@ -517,15 +565,6 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
   for (int y = 0; y < MJ; ++y) {
     const int jj = j + 16 * y;
     const bool in = jj < p.nj;
-    float bg = 0.0f, bu = 0.0f;
-    if constexpr (PAIR == 2) {
-      if (p.gate_bias && in) bg = float(static_cast<const T*>(p.gate_bias)[jj]);
-      if (p.up_bias && in) bu = float(static_cast<const T*>(p.up_bias)[jj]);
-    }
-    Vec<T, V> now[kPieces];
-#pragma unroll
-    for (int q = 0; q < kPieces; ++q) now[q] = ahead[q];
-    if (y + 1 < MJ) fetch(y + 1);
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
@@ -533,15 +572,23 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const int x = q * F + e / 4;
-        g[e] = acc[x][y][e % 4] + (PAIR == 1 ? element<T, V>(gate_bias[q], e) : bg);
-        u[e] = acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? y + MJ : y][e % 4] + (PAIR == 1 ? element<T, V>(up_bias[q], e) : bu);
+        float bg, bu;
+        if constexpr (PAIR == 1) {
+          bg = element<T, V>(needs.gate_bias[q], e);
+          bu = element<T, V>(needs.up_bias[q], e);
+        } else {
+          bg = float(needs.gate_bias[y]);
+          bu = float(needs.up_bias[y]);
+        }
+        g[e] = acc[x][y][e % 4] + bg;
+        u[e] = acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? y + MJ : y][e % 4] + bu;
       }
       if constexpr (BACK) {
         if (!in) continue;
         Vec<T, V> dg, du;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float d = element<T, V>(now[q], e), s = d * u[e] * act_slope<ACT>(g[e]), t = d * act<ACT>(g[e]);
+          const float d = element<T, V>(needs.dh[y * kPieces + q], e), s = d * u[e] * act_slope<ACT>(g[e]), t = d * act<ACT>(g[e]);
           set_element<T, V>(dg, e, s);
           set_element<T, V>(du, e, t);
           if constexpr (PAIR == 1) {
@@ -576,6 +623,7 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
         }
       }
     }
+    __builtin_amdgcn_sched_barrier(0);  // one column's values in registers at a time
     if constexpr (PAIR == 2) {
       if (BACK && p.sums) {  // over i: the four quads' of this column
 #pragma unroll
@@ -619,75 +667,130 @@ __device__ __forceinline__ int xcd_order(unsigned block, unsigned blocks) {
 }
 constexpr int kGroup = 8;
 
+// t / d, given 2^32 / d.
+__device__ __forceinline__ int divide(int t, int d, unsigned reciprocal) {
+  int q = int(__umulhi(unsigned(t), reciprocal));  // exact or one less
+  return q + (t - q * d >= d);
+}
+
+// The kernel's arguments, and the lane, as the compiler has not seen them before: what is
+// worked out from them for one tile is not held in registers for the next.
+__device__ __forceinline__ const ProductParams& again(const ProductParams& args) {
+  typedef __attribute__((address_space(4))) const ProductParams constant_params;
+  constant_params* p = (constant_params*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const ProductParams*)p;
+}
+__device__ __forceinline__ int lane_again() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t & 63;
+}
+
 // PAIR: 0 none, 1 on i, 2 on j. BACK: the unit in the backward pass.
 template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK>
-__global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 ? 1 : 2) kernel(ProductParams p) {
+__global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 ? 1 : 2) kernel(ProductParams args) {
   constexpr int WAVES = WI * WJ, GI = TI / WI, GJ = TJ / WJ;  // a wave's part of the tile
   constexpr int NI = GI / 16, NJ = GJ / 16;
   static_assert(GI % (PAIR == 1 ? 64 : 32) == 0 && GJ % (PAIR == 2 ? 32 : 16) == 0, "");
   constexpr int kStage = (TI + TJ) * kStepBytes;
   extern __shared__ char lds_memory[];
   const unsigned lds = unsigned(reinterpret_cast<size_t>((lds_char*)lds_memory));
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
-
-  // this workgroup's tile, and its part of the sum
   constexpr int FI = PAIR == 1 ? TI / 2 : TI, FJ = PAIR == 2 ? TJ / 2 : TJ;
-  const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ, all_j = tiles_j * p.halves;
-  int t = xcd_order(blockIdx.x, gridDim.x);
-  const int image = blockIdx.y + p.first_image, split = blockIdx.z;
-  // groups of kGroup tiles along j, in each i by i
-  const int each = kGroup * tiles_i;
-  int group = int(__umulhi(unsigned(t), p.group_reciprocal));  // exact or one less
-  t -= group * each;
-  if (t >= each) {
-    t -= each;
-    ++group;
-  }
-  const int rows = min(kGroup, all_j - group * kGroup);
-  const int ti = rows == kGroup ? t / kGroup : t / rows;
-  const int tjj = group * kGroup + t - ti * rows, which = tjj >= tiles_j, tj = tjj - (which ? tiles_j : 0);
-  const int i0 = ti * FI, j0 = tj * FJ;
-  const int steps = (p.K + kStep<T> - 1) / kStep<T>;
-  const int total = steps * p.segs;
-  int first = 0, end = total;
-  if (PAIR == 0 && p.splits > 1) {
-    first = min(total, split * p.split_steps);
-    end = min(total, first + p.split_steps);
-  }
 
-  int s = first ? first / steps : 0, k0 = (first - s * steps) * kStep<T>;
+  // A tile of D (or of its parts), and its part of the sum.
+  struct Place {
+    int image, split, which, ti, tj, first, end;
+  };
+  auto place = [&](unsigned number) {
+    const ProductParams& p = again(args);
+    const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ, all_j = tiles_j * p.halves;
+    const int total = (p.K + kStep<T> - 1) / kStep<T> * p.segs;
+    Place w;
+    const int plane = tiles_i * all_j;
+    int t = xcd_order(number, p.tiles), rest = divide(t, plane, p.plane_reciprocal);
+    t -= rest * plane;
+    w.split = 0;
+    w.first = 0;
+    w.end = total;
+    if (PAIR == 0 && p.splits > 1) {
+      w.split = p.images > 1 ? rest / p.images : rest;
+      rest -= w.split * p.images;
+      w.first = min(total, w.split * p.split_steps);
+      w.end = min(total, w.first + p.split_steps);
+    }
+    w.image = rest;
+    // groups of kGroup tiles along j, in each i by i
+    const int each = kGroup * tiles_i, group = divide(t, each, p.group_reciprocal);
+    t -= group * each;
+    const int rows = min(kGroup, all_j - group * kGroup);
+    w.ti = rows == kGroup ? t / kGroup : t / rows;
+    w.tj = group * kGroup + t - w.ti * rows;
+    w.which = w.tj >= tiles_j;
+    w.tj -= w.which ? tiles_j : 0;
+    return w;
+  };
+
+  int s = 0, k0 = 0;  // of the step to load next
   Tile<T, TI, WAVES, IK, true, PAIR == 1, GI> a;
   Tile<T, TJ, WAVES, JK, false, PAIR == 2, GJ> b;
-  a.init(p.i, image, which, i0, p.ni, p.K, wave, lane);
-  b.init(p.j, image, which, j0, p.nj, p.K, wave, lane);
-  a.start(s, k0);
-  b.start(s, k0);
-  auto advance = [&]() {
+  auto advance = [&](int K) {
     k0 += kStep<T>;
-    if (k0 >= p.K) {
+    if (k0 >= K) {
       k0 = 0;
       ++s;
     }
     a.go(s, k0);
     b.go(s, k0);
   };
-  auto load = [&](int stage) {
+  auto load = [&](const ProductParams& p, int stage) {
 #pragma unroll
     for (int m = 0; m < a.kMine; ++m) a.piece(lds + stage * kStage, k0, p.K, m, wave);
 #pragma unroll
     for (int m = 0; m < b.kMine; ++m) b.piece(lds + stage * kStage + TI * kStepBytes, k0, p.K, m, wave);
-    advance();
+    advance(p.K);
+  };
+  // The first two steps of a tile to LDS; whether the first is a segment's last.
+  auto begin = [&](const Place& w) {
+    const ProductParams& p = again(args);
+    const int lane = lane_again(), steps = (p.K + kStep<T> - 1) / kStep<T>;
+    s = w.first ? w.first / steps : 0;
+    k0 = (w.first - s * steps) * kStep<T>;
+    a.init(p.i, w.image, w.which, w.ti * FI, p.ni, p.K, wave, lane);
+    b.init(p.j, w.image, w.which, w.tj * FJ, p.nj, p.K, wave, lane);
+    a.start(s, k0);
+    b.start(s, k0);
+    if (w.first >= w.end) return false;
+    load(p, 0);
+    const bool last = k0 == 0;
+    if (w.first + 1 < w.end) load(p, 1);
+    return last;
   };
   // The last values of a segment, once they have landed.
-  const int left = p.K % kStep<T> * int(sizeof(T));
-  auto cut = [&](int stage) {
+  auto cut = [&](int stage, int left) {
     a.cut(lds + stage * kStage, left);
     b.cut(lds + stage * kStage + TI * kStepBytes, left);
-    wait_for_loads();
+    wait_but_for<63>();
   };
-  const bool ragged = (IK || JK) && left;
 
+  // A workgroup takes one tile after the other. The first steps of the next are asked for
+  // before the results of this one leave.
+  unsigned number = blockIdx.x;
+  Place w = place(number);
+  bool last = begin(w), another, late;
+  constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ, RI = 16 * MI;
+  constexpr int kVec = 16 / int(sizeof(T));
+  // Stores that a wave inside of i and j ends a tile with: they are younger than the loads
+  // of the next tile's first steps, which therefore need not wait for them.
+  constexpr int kStores = MI * MJ * 4 / kVec * (BACK ? 2 : 1);
+  constexpr bool kEarly = PAIR != 0 && TI * TJ <= 128 * 128;  // registers for the unit's needs while it multiplies
+  bool stored = false;
+  for (;;) {
+  const ProductParams& p = again(args);
+  const int lane = lane_again(), left = p.K % kStep<T> * int(sizeof(T));
+  const bool ragged = (IK || JK) && left;
   floatx4 acc[NI][NJ];
 #pragma unroll
   for (int x = 0; x < NI; ++x)
@@ -718,12 +821,22 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  const int first = w.first, end = w.end;
+  std::conditional_t<PAIR != 0, UnitNeeds<T, MI, MJ, PAIR ? PAIR : 1, BACK>, int> needs;
+  auto fetch = [&](const ProductParams& p, int lane) {
+    if constexpr (PAIR != 0)
+      needs.fetch(p, w.image, w.ti * FI + wi * RI + lane / 16 * kVec, w.tj * FJ + wj * 16 * MJ + lane % 16);
+  };
+  auto landed = [&]() {
+    if (stored)
+      wait_but_for<kStores>();
+    else
+      wait_for_loads();
+  };
   if (first < end) {
-    load(0);
-    const bool last = k0 == 0;
-    if (first + 1 < end) load(1);
-    wait_for_loads();
-    if (ragged && last) cut(0);
+    landed();
+    if (kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
+    if (ragged && last) cut(0, left);
     const auto ba = at_a.base(lds, 0);
     const auto bb = at_b.base(lds + TI * kStepBytes, 0);
 #pragma unroll
@@ -735,8 +848,13 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
 #pragma unroll 1
   for (int n = first; n < end; ++n) {
     half(0, stage, [](int) {});
-    wait_for_loads();
-    if (ragged && k0 == 0 && n + 1 < end) cut(stage ^ 1);
+    // this stage is read by all waves; the next has landed: of the first two steps both
+    // had, and after the last there is none
+    if (n > first && n + 1 < end)
+      wait_for_loads();
+    else
+      wait_but_for<63>();
+    if (ragged && k0 == 0 && n + 1 < end) cut(stage ^ 1, left);
     const bool more = n + 2 < end;
     const unsigned la = lds + stage * kStage, lb = la + TI * kStepBytes;
     // (after the last step these reads find old values, which nothing uses)
@@ -747,7 +865,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
 #pragma unroll
       for (int m = x * b.kMine / NI; m < (x + 1) * b.kMine / NI; ++m) b.piece(lb, k0, p.K, m, wave);
     });
-    if (more) advance();
+    if (more) advance(p.K);
     stage ^= 1;
   }
 
@@ -756,24 +874,41 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   // i: that goes through LDS, each wave's through a slab of its own, as rows that a
   // short loop reads back and finishes.
   constexpr unsigned kSlab = 2 * kStage / WAVES;
-  const int row = lane & 15, quad = lane >> 4;
-  constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ, RI = 16 * MI;
-  constexpr int kVec = 16 / int(sizeof(T));
-  const int iw = i0 + wi * RI, jw = j0 + wj * 16 * MJ;
+  {
+  const ProductParams& p = again(args);
+  const int lane = lane_again(), row = lane & 15, quad = lane >> 4;
+  const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ;
+  const int image = w.image, which = w.which, i0 = w.ti * FI;
+  const int iw = i0 + wi * RI, jw = w.tj * FJ + wj * 16 * MJ;
   const bool inside = iw + RI <= p.ni;
+  const long part = PAIR == 1   ? (long(image) * tiles_j + w.tj) * WJ + wj
+                    : PAIR == 2 ? (long(image) * tiles_i + w.ti) * WI + wi
+                                : (long(w.split) * p.halves + which) * p.images + image;
   __syncthreads();
+  number += gridDim.x;
+  another = number < unsigned(p.tiles);
+  // (where LDS is not needed any more, and registers last)
+  const bool early = (PAIR == 0 || kEarly) && i0 + FI <= p.ni;
+  late = another && !early;
+  stored = another && early && inside && jw + 16 * MJ <= p.nj;
+  if constexpr (PAIR != 0) {
+    if (inside) {
+      if (!kEarly || first >= end) fetch(p, lane);
+      needs.arrive();
+    }
+  }
+  if (another) w = place(number);
+  if (another && early) last = begin(w);
   const unsigned slab = lds + wave * kSlab;
   if constexpr (PAIR != 0) {
-    const long part = PAIR == 1 ? long(image) * tiles_j * WJ + tj * WJ + wj : long(image) * tiles_i * WI + ti * WI + wi;
     if (inside) {
       switch (p.act) {
-        case OAA_ACT_RELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_RELU>(p, acc, image, part, iw + quad * kVec, jw + row, lane); break;
-        case OAA_ACT_SILU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_SILU>(p, acc, image, part, iw + quad * kVec, jw + row, lane); break;
-        case OAA_ACT_GELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_GELU>(p, acc, image, part, iw + quad * kVec, jw + row, lane); break;
-        default: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_NONE>(p, acc, image, part, iw + quad * kVec, jw + row, lane);
+        case OAA_ACT_RELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_RELU>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane); break;
+        case OAA_ACT_SILU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_SILU>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane); break;
+        case OAA_ACT_GELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_GELU>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane); break;
+        default: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_NONE>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane);
       }
-      return;
-    }
+    } else {
     constexpr int kRows = int(kSlab / (2 * RI * 4)) < 16 * MJ ? int(kSlab / (2 * RI * 4)) : 16 * MJ;  // of a pass
     static_assert(kRows % 16 == 0 && 16 * MJ % kRows == 0, "");
     UnitEnd<T, RI, kRows, PAIR, BACK> finish(p, image, iw, lane);
@@ -798,8 +933,8 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
       finish.rows(ahead, slab, jw + pass * kRows);
     }
     finish.end();
+    }
   } else {
-    const long part = (long(split) * p.halves + which) * p.images + image;
     auto leave = [&](auto zero, auto* out, long ld) {
       using E = decltype(zero);
       constexpr int V = 16 / int(sizeof(E));
@@ -841,15 +976,22 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     else
       leave(T(0.0f), static_cast<T*>(p.out) + long(image) * p.out_image + long(which) * p.out_half, p.out_ld);
   }
+  }
+  if (!another) break;
+  if (late) {
+    __syncthreads();
+    last = begin(w);
+  }
+  }
 }
 
 template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK>
 hipError_t launch(const ProductParams& p, hipStream_t s) {
   constexpr int FI = PAIR == 1 ? TI / 2 : TI, FJ = PAIR == 2 ? TJ / 2 : TJ;
   constexpr size_t lds = 2 * size_t(TI + TJ) * kStepBytes;
-  const long tiles_i = (p.ni + FI - 1) / FI, tiles = tiles_i * ((p.nj + FJ - 1) / FJ) * p.halves;
-  constexpr int kMostImages = 65535;  // of a launch
-  if (tiles * (64 * WI * WJ) >= 1l << 32) return hipErrorInvalidValue;  // refused before
+  const long tiles_i = (p.ni + FI - 1) / FI, plane = tiles_i * ((p.nj + FJ - 1) / FJ) * p.halves;
+  const long tiles = plane * p.images * p.splits;
+  if (tiles >= 1l << 31) return hipErrorInvalidValue;  // refused before
   auto kern = kernel<T, TI, TJ, WI, WJ, IK, JK, PAIR, BACK>;
   if (lds > 65536) {
     const hipError_t e = tile::allow_lds(kern, lds);
@@ -857,21 +999,20 @@ hipError_t launch(const ProductParams& p, hipStream_t s) {
   }
   ProductParams q = p;
   const long steps = long((p.K + kStep<T> - 1) / kStep<T>) * p.segs;
+  q.tiles = int(tiles);
   q.split_steps = int((steps + p.splits - 1) / p.splits);
-  q.group_reciprocal = unsigned((1ull << 32) / (kGroup * tiles_i));
-  for (q.first_image = 0; q.first_image < p.images; q.first_image += kMostImages) {
-    const int images = std::min(kMostImages, p.images - q.first_image);
-    hipLaunchKernelGGL(kern, dim3(unsigned(tiles), images, p.splits), dim3(64 * WI * WJ), lds, s, q);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  q.plane_reciprocal = unsigned(std::min((1ll << 32) / plane, (1ll << 32) - 1));
+  q.group_reciprocal = unsigned((1ll << 32) / (kGroup * tiles_i));
+  // as many workgroups as the device holds: a multiple of its dies
+  const long most = kTilesAtOnce[TI / 128];
+  hipLaunchKernelGGL(kern, dim3(unsigned(std::min(tiles, most))), dim3(64 * WI * WJ), lds, s, q);
+  return hipGetLastError();
 }
 
 template <typename T, bool IK, bool JK, int PAIR, bool BACK = false>
 hipError_t launch_sized(const ProductParams& p, ProductKind kind, hipStream_t s) {
   const int tile = product_tile(sizeof(T), kind, p.ni, p.nj, p.images, p.halves, p.K, p.segs);
-  if constexpr (sizeof(T) == 2)
+  if constexpr (sizeof(T) == 2 && !BACK)
     if (tile == 256) {
       constexpr ProductWaves w = product_waves(256, PAIR == 1);
       return launch<T, 256, 256, w.i, w.j, IK, JK, PAIR, BACK>(p, s);
@@ -890,10 +1031,10 @@ template <typename T>
 hipError_t launch_product(const ProductParams& p, ProductKind kind, hipStream_t s) {
   using namespace product;
   switch (kind) {
-    case kUnitLast:
-      return p.dh ? launch_sized<T, true, true, 1, true>(p, kind, s) : launch_sized<T, true, true, 1>(p, kind, s);
-    case kUnitPlanes:
-      return p.dh ? launch_sized<T, false, true, 2, true>(p, kind, s) : launch_sized<T, false, true, 2>(p, kind, s);
+    case kUnitLast: return launch_sized<T, true, true, 1>(p, kind, s);
+    case kUnitPlanes: return launch_sized<T, false, true, 2>(p, kind, s);
+    case kUnitLastAgain: return launch_sized<T, true, true, 1, true>(p, kind, s);
+    case kUnitPlanesAgain: return launch_sized<T, false, true, 2, true>(p, kind, s);
     case kInputLast: return launch_sized<T, false, true, 0>(p, kind, s);
     case kInputPlanes: return launch_sized<T, false, false, 0>(p, kind, s);
     case kWeightLast: return launch_sized<T, false, false, 0>(p, kind, s);

@@ -601,8 +601,8 @@ def test_refused_workspaces(lib):
     # float32 is read in place; 16 bits with rows of odd length, or at odd addresses, are not
     assert binding.oaa_gated_workspace_bytes(d, False, True) == 0
     assert binding.oaa_gated_workspace_bytes(desc(dtype=1), False, False) == 0
-    assert binding.oaa_gated_workspace_bytes(desc(dtype=1), False, True) > 0
-    assert binding.oaa_gated_workspace_bytes(desc(dtype=1, C=7), False, False) > 0
+    assert binding.oaa_gated_workspace_bytes(desc(dtype=1, S=20), False, True) > 0
+    assert binding.oaa_gated_workspace_bytes(desc(dtype=1, C=7, S=20), False, False) > 0
     with pytest.raises(binding.OaaError) as e:
         forward(desc(dtype=2), x=M + 2, ws=None, size=0)
     assert e.value.status == 3
@@ -611,8 +611,8 @@ def test_refused_workspaces(lib):
 def test_slices_beside_each_other(lib):
     """x and h as columns of one tensor pass the check of overlaps (and then fail for
     want of a workspace); one column in common does not."""
-    for layout, strides, width in ((0, (160, 10), 50), (1, (160, 16), 5)):
-        d = desc(layout=layout, dtype=1, C=5, x=strides, h=strides)
+    for layout, strides, width in ((0, (320, 20), 100), (1, (320, 16), 5)):
+        d = desc(layout=layout, dtype=1, C=5, S=20, x=strides, h=strides)
         x = M + 2
         with pytest.raises(binding.OaaError) as e:
             forward(d, x=x, h=x + 2 * width, ws=None, size=0)
