@@ -413,11 +413,14 @@ oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out
  *                                            (sums over images and positions)
  *
  * Products and sums are held in 32 bits or more whatever the types, and h and the
- * gradients are rounded once. g and u are stored in 32 bits for the backward pass, or it makes them again. dg and du
- * are rounded to the type of x where they enter the products dx and dW: the
- * matrix cores take both operands in one type, and a rounding of each of many terms
- * weighs less than that of the result. What is not finite at a position of x makes h and dx
- * of that position, and dW, what the formulas do; nothing of other positions' h and dx.
+ * gradients are rounded once. g and u are stored in 32 bits for the backward pass, or it
+ * makes them again. dg and du are rounded to the type of x where they enter the products
+ * dx and dW: the matrix cores take both operands in one type, and a rounding of each of
+ * many terms weighs less than that of the result. float32 values are multiplied as sums of
+ * three bfloat16 values, which is exact to float32's rounding for magnitudes from 2^-110
+ * (below, digits are lost) to 3.39e38 (above, as infinite). What is not finite at a position
+ * of x, or in a weight, makes what the formulas sum over it infinite or NaN (NaN, in float32,
+ * where they may say infinite), and nothing else: other positions' h and dx stay as they are.
  * Equal calls give equal bits. */
 typedef struct {
   int B, C, F;      /* images, channels of x, channels of h: B >= 0, C, F >= 1 (up to 2^20) */

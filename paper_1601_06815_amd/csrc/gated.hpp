@@ -77,13 +77,16 @@ struct FewParams {
   int act;
 };
 
-// D's parts added up in order, rounded to T: `n` values in `outputs` tensors of n / outputs.
+// D's parts added up in order, rounded to T: `n` values in `outputs` tensors of n / outputs,
+// dense or (ld != 0) as images of nj rows of ni.
 struct JoinParams {
   const float* part;
   long n;
   int splits;
   void* out[2];
   int outputs;
+  int ni, nj;
+  long ld, image;
 };
 
 // dg and du from dh, g and u: rows x columns of every image, d with `ld` elements a
@@ -99,8 +102,7 @@ struct SlopeParams {
   long ld;
   int act;
   bool last;
-  float* sums;     // [parts][2][F]
-  long parts;      // last: blocks of rows; planes: images
+  float* sums;     // [blocks of rows (last), or images (planes)][2][F]
   long part_rows;  // last: rows of a block
 };
 

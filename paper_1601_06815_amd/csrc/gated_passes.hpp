@@ -189,7 +189,12 @@ __global__ void __launch_bounds__(kThreads) join_kernel(JoinParams p) {
     }
     if (l == 0 && i < p.n) {
       const int which = i >= each;
-      static_cast<T*>(p.out[which])[i - which * each] = T(a);
+      long at = i - which * each;
+      if (p.ld) {
+        const long row = at / p.ni, image = row / p.nj;
+        at = image * p.image + (row - image * p.nj) * p.ld + (at - row * p.ni);
+      }
+      static_cast<T*>(p.out[which])[at] = T(a);
     }
   }
 }

@@ -284,12 +284,12 @@ Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w
   if (need_x) {
     const ProductKind kind = u.last ? oaa::kInputLast : oaa::kInputPlanes;
     const int ni = int(u.last ? u.C : u.S), nj = int(u.last ? u.S : u.C);
-    l.dx_splits = oaa::product_splits(int(u.size), kind, ni, nj, u.B, 1, u.F, 2);
+    l.dx_splits = oaa::product_choice(int(u.size), kind, ni, nj, u.B, 1, u.F, 2).splits;
     if (l.dx_splits > 1) parts = size_t(l.dx_splits) * u.B * ni * nj * 4;
   }
   if (need_w) {
-    l.dw_splits = oaa::product_splits(int(u.size), u.last ? oaa::kWeightLast : oaa::kWeightPlanes, u.C, u.F, 1, 2, u.S,
-                                      u.B);
+    l.dw_splits = oaa::product_choice(int(u.size), u.last ? oaa::kWeightLast : oaa::kWeightPlanes, u.C, u.F, 1, 2, u.S, u.B)
+                      .splits;
     if (l.dw_splits > 1) parts = std::max(parts, size_t(l.dw_splits) * 2 * u.F * u.C * 4);
   }
   if (parts) l.product_parts = static_cast<float*>(room.take(parts));
@@ -544,7 +544,6 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
     slope.act = u.act;
     slope.last = u.last;
     slope.sums = l.sums;
-    slope.parts = l.parts;
     slope.part_rows = l.part_rows;
     e = for_type(u.dtype, [&](auto t) { return oaa::launch_slope<decltype(t)>(slope, s); });
   }
@@ -571,6 +570,12 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
       j.splits = p.splits;
       j.out[0] = first;
       j.out[1] = second;
+      j.ni = p.ni;
+      j.nj = p.nj;
+      if (p.out_ld != p.ni || (p.images > 1 && p.out_image != long(p.ni) * p.nj)) {
+        j.ld = p.out_ld;
+        j.image = p.out_image;
+      }
       return oaa::launch_join<T>(j, s);
     });
   };

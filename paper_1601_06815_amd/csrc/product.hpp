@@ -7,8 +7,8 @@
 // reads free of bank conflicts is which 16 bytes ("piece") each lane asks for: piece c
 // of a row (k rows: 8 pieces; k columns: a line of one k) lies at place c ^ key(row).
 //
-// A lane's fragment is 16 bytes: 8 values of k (16 bits; for k columns two
-// transposing reads), or 4 (32 bits), one for each of four products. The 16 rows of a
+// A lane's fragment is 16 bytes: 8 values of k (16 bits; for k columns two transposing
+// reads), or 4 of 32 bits, of which two make one product's (see Pieces). The 16 rows of a
 // fragment follow each other, but in 16 bits those of i do not: fragments 2 q and 2 q + 1
 // take rows 8 a + b and 8 a + 4 + b (a, b = 0..3) of 32, so that the results that a lane
 // holds of both (rows 4 quad + e of each) are 8 neighbours along i, 16 bytes, beside those
@@ -58,6 +58,39 @@ __device__ __forceinline__ floatx4 multiply(floatx4 a, floatx4 b, floatx4 c) {
       return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
   }
 }
+
+// float32 on the bf16 matrix cores, which are 16 times as fast as those of float32: every
+// value is the sum of three bf16 values (the nearest, the nearest to what is left, and to
+// what is left then: 24 bits), and of the nine products of two values' pieces the six
+// above 2^-24 of the whole are taken, the smallest first. That is exact to float32's own
+// rounding for magnitudes between 2^-110 (below, the third piece runs out of exponents) and
+// 3.38e38 (above, the first is infinite and the rest NaN, as for infinities).
+struct Pieces {
+  typedef bf16 vec __attribute__((ext_vector_type(8)));
+  typedef bf16 two __attribute__((ext_vector_type(2)));
+  typedef float wide __attribute__((ext_vector_type(2)));
+  vec p[3];
+  __device__ __forceinline__ Pieces() {}
+  // of lo and hi, with their signs changed where `sign` has its highest bit set
+  __device__ __forceinline__ Pieces(floatx4 lo, floatx4 hi, unsigned sign = 0) {
+    unsigned packed[3][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float a = e < 2 ? lo[2 * e] : hi[2 * e - 4], b = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
+      a = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, a) ^ sign);
+      b = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, b) ^ sign);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const wide w = {a, b};
+        packed[k][e] = __builtin_bit_cast(unsigned, __builtin_convertvector(w, two));
+        a -= __builtin_bit_cast(float, packed[k][e] << 16);
+        b -= __builtin_bit_cast(float, packed[k][e] & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) p[k] = __builtin_bit_cast(vec, packed[k]);
+  }
+};
 
 // `bytes` (below 2^31) from base on, uniform.
 __device__ __forceinline__ intx4 resource(const char* base, int bytes) {
@@ -802,11 +835,91 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   // done with. At the barrier between them every wave has read all of this stage, and the
   // stage after it, asked for a step ago, has landed; so what comes after that goes
   // where this one was, asked for among the products of the second half.
-  floatx4 fa[NI], fb[2][NJ];
+  const int first = w.first, end = w.end;
+  std::conditional_t<PAIR != 0, UnitNeeds<T, MI, MJ, PAIR ? PAIR : 1, BACK>, int> needs;
+  auto fetch = [&](const ProductParams& p, int lane) {
+    if constexpr (PAIR != 0)
+      needs.fetch(p, w.image, w.ti * FI + wi * RI + lane / 16 * kVec, w.tj * FJ + wj * 16 * MJ + lane % 16);
+  };
+  auto landed = [&]() {
+    if (stored)
+      wait_but_for<kStores>();
+    else
+      wait_for_loads();
+  };
   Fragments<T, TI, IK, true> at_a;
   Fragments<T, TJ, JK, false> at_b;
   at_a.init(wi * GI, lane);
   at_b.init(wj * GJ, lane);
+  if constexpr (sizeof(T) == 4) {
+    // The matrix cores round toward one side, an error of one sign that a long sum gathers:
+    // every eight steps the sums change their sign, and j's values with them.
+    unsigned sign = 0;
+    int stage = 0;
+#pragma unroll 1
+    for (int n = first; n < end; ++n) {
+      if (n == first)
+        landed();
+      else
+        wait_for_loads();
+      if (n == first && kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
+      if (ragged && (n == first ? last : k0 == 0)) cut(stage, left);
+      if (n > first && n + 1 < end) load(p, stage ^ 1);
+      const unsigned ta = lds + stage * kStage, tb = ta + TI * kStepBytes;
+      const auto a0 = at_a.base(ta, 0), a1 = at_a.base(ta, 1);
+      Pieces pb[NJ], pa;
+      {
+        const auto b0 = at_b.base(tb, 0), b1 = at_b.base(tb, 1);
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) pb[y] = Pieces(at_b.read(b0, y, 0), at_b.read(b1, y, 1), sign);
+      }
+      pa = Pieces(at_a.read(a0, 0, 0), at_a.read(a1, 0, 1));
+      floatx4 raw[2];
+      if (NI > 1) {
+        raw[0] = at_a.read(a0, 1, 0);
+        raw[1] = at_a.read(a1, 1, 1);
+      }
+      // among the products of one row, the next one's values are taken apart
+#pragma unroll
+      for (int x = 0; x < NI; ++x) {
+        __builtin_amdgcn_sched_barrier(0);
+        Pieces next;
+        if (x + 1 < NI) next = Pieces(raw[0], raw[1]);
+        if (x + 2 < NI) {
+          raw[0] = at_a.read(a0, x + 2, 0);
+          raw[1] = at_a.read(a1, x + 2, 1);
+        }
+        constexpr int order[6][2] = {{2, 0}, {1, 1}, {0, 2}, {1, 0}, {0, 1}, {0, 0}};
+#pragma unroll
+        for (int t = 0; t < 6; ++t)
+#pragma unroll
+          for (int y = 0; y < NJ; ++y)
+            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa.p[order[t][0]], pb[y].p[order[t][1]], acc[x][y], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < 6 * NJ; ++t) {  // (44 instructions take a row apart)
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, 44 / (6 * NJ) + 1, 0);
+        }
+        pa = next;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      stage ^= 1;
+      if ((n - first) % 8 == 7) {
+        sign ^= 0x80000000u;
+#pragma unroll
+        for (int x = 0; x < NI; ++x)
+#pragma unroll
+          for (int y = 0; y < NJ; ++y) acc[x][y] = -acc[x][y];
+      }
+    }
+    if (sign) {
+#pragma unroll
+      for (int x = 0; x < NI; ++x)
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) acc[x][y] = -acc[x][y];
+    }
+  } else {
+  floatx4 fa[NI], fb[2][NJ];
   auto half = [&](int sub, int stage, auto&& between) {  // products of `sub`; reads the other of `stage`
     const auto ba = at_a.base(lds + stage * kStage, sub ^ 1);
     const auto bb = at_b.base(lds + stage * kStage + TI * kStepBytes, sub ^ 1);
@@ -820,18 +933,6 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
       between(x);
       __builtin_amdgcn_sched_barrier(0);
     }
-  };
-  const int first = w.first, end = w.end;
-  std::conditional_t<PAIR != 0, UnitNeeds<T, MI, MJ, PAIR ? PAIR : 1, BACK>, int> needs;
-  auto fetch = [&](const ProductParams& p, int lane) {
-    if constexpr (PAIR != 0)
-      needs.fetch(p, w.image, w.ti * FI + wi * RI + lane / 16 * kVec, w.tj * FJ + wj * 16 * MJ + lane % 16);
-  };
-  auto landed = [&]() {
-    if (stored)
-      wait_but_for<kStores>();
-    else
-      wait_for_loads();
   };
   if (first < end) {
     landed();
@@ -867,6 +968,8 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     });
     if (more) advance(p.K);
     stage ^= 1;
+  }
+
   }
 
   // A lane's results: column j of 16, and 16 bytes of neighbours along i of every 64. They leave
@@ -1011,8 +1114,8 @@ hipError_t launch(const ProductParams& p, hipStream_t s) {
 
 template <typename T, bool IK, bool JK, int PAIR, bool BACK = false>
 hipError_t launch_sized(const ProductParams& p, ProductKind kind, hipStream_t s) {
-  const int tile = product_tile(sizeof(T), kind, p.ni, p.nj, p.images, p.halves, p.K, p.segs);
-  if constexpr (sizeof(T) == 2 && !BACK)
+  const int tile = product_choice(sizeof(T), kind, p.ni, p.nj, p.images, p.halves, p.K, p.segs).tile;
+  if constexpr (!BACK)
     if (tile == 256) {
       constexpr ProductWaves w = product_waves(256, PAIR == 1);
       return launch<T, 256, 256, w.i, w.j, IK, JK, PAIR, BACK>(p, s);

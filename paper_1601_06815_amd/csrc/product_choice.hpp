@@ -2,7 +2,6 @@
 #pragma once
 
 #include <algorithm>
-#include <cstdlib>
 
 #include "gated.hpp"
 
@@ -27,51 +26,51 @@ constexpr ProductWaves product_waves(int tile, bool pair_i) {
 constexpr int kMostSplits = 128;
 constexpr int kTilesAtOnce[] = {1280, 512, 256};  // of side 64, 128, 256 that the device holds
 
-// Parts that the sum of a product on tiles of a side is cut into, where too few tiles
-// would leave the device idle.
-inline int splits_on(int size, ProductKind kind, int tile, long ni, long nj, long images, long halves, long K,
-                     long segs) {
-  if (pair_on_i(kind) || pair_on_j(kind)) return 1;
-  const long tiles = product_tiles(kind, tile, ni, nj, images, halves);
-  const long step = 128 / size, steps = (K + step - 1) / step * segs;
-  return int(std::max(1l, std::min({512 / tiles, steps / 3, long(kMostSplits)})));
-}
+// The side of a product's tiles, and the parts that its sum is cut into.
+struct ProductChoice {
+  int tile, splits;
+};
 
-// Side of the tile: the least of the rounds of tiles that the device holds at once, times
-// what a round takes (a tile's products at a rate that larger tiles come nearer to, and
-// the wait for its first operands).
-inline int product_tile(int size, ProductKind kind, long ni, long nj, long images, long halves, long K, long segs) {
-  const bool again = kind == kUnitLastAgain || kind == kUnitPlanesAgain;
-  if (const char* e = getenv("TILE")) return (size == 2 && !again) || atoi(e) < 256 ? atoi(e) : 128;
-  int best = 64;
+// The least of: the rounds of tiles that the device holds at once, times what a round takes
+// (the wait for a tile's first operands, its results, and its steps), and the parts' way
+// through memory. Large tiles read least, but take longest alone, and their last round may
+// be nearly empty. Measured, us by side 64, 128, 256 (bfloat16 unit forward): 512 positions 512 ->
+// 2048 9.5, 10.5, 21.8; 2048 positions 1024 -> 4096 67, 40, 40; 16 images of 64 x 64 planes,
+// 256 -> 512 95, 58, 50. (A unit has to have its whole sums: it is not cut. In the backward pass
+// it has no tile of 256: its registers do not hold what it needs besides the sums.)
+inline ProductChoice product_choice(int size, ProductKind kind, long ni, long nj, long images, long halves, long K,
+                                    long segs) {
+  // ns of a step: of a tile that has a compute unit to itself, and at the full rate
+  static constexpr double alone[2][3] = {{400, 500, 1000}, {1100, 2100, 4400}};
+  static constexpr double full[2][3] = {{200, 450, 1600}, {660, 1830, 5600}};
+  static constexpr double around[] = {3000, 3000, 6000};  // a tile's steps
+  const bool again = kind == kUnitLastAgain || kind == kUnitPlanesAgain, pair = pair_on_i(kind) || pair_on_j(kind);
+  const long step = 128 / size, steps = (K + step - 1) / step * segs;
+  const long most = pair ? 1 : std::max(1l, std::min(steps / 3, long(kMostSplits)));
+  ProductChoice best{64, 1};
   double least = 0;
-  for (int i = 0; i < (size == 2 && !again ? 3 : 2); ++i) {
-    const int tile = 64 << i;
-    const int splits = splits_on(size, kind, tile, ni, nj, images, halves, K, segs);
-    const double tiles = double(product_tiles(kind, tile, ni, nj, images, halves)) * splits;
-    const double step = 128.0 / size, steps = ((K + step - 1) / step * segs + splits - 1) / splits;
-    const double rounds = std::max(1.0, tiles / kTilesAtOnce[i]);
-    const double slow[] = {1.7, 1.3, 1.0};
-    // ns: a step of a tile to itself; tiles that share a compute unit share its rate
-    const double products = (size == 2 ? 1.0 : 14.0) * slow[i] * tile * tile * 0.0135 * std::min(tiles / 256, kTilesAtOnce[i] / 256.0);
-    const double time = rounds * (3000 + steps * std::max(products, 400.0));
-    if (i == 0 || time < least) {
-      best = tile;
-      least = time;
+  for (int i = 0; i < (again ? 2 : 3); ++i) {
+    const long tiles = product_tiles(kind, 64 << i, ni, nj, images, halves);
+    for (long splits = 1; splits <= most; splits *= 2) {
+      const double all = double(tiles) * splits, each = double((steps + splits - 1) / splits);
+      const double rounds = std::max(1.0, all / kTilesAtOnce[i]);
+      const double shared = std::min(all, double(kTilesAtOnce[i])) / 256;
+      double time = rounds * (around[i] + each * std::max(alone[size > 2][i], shared * full[size > 2][i]));
+      // parts are written and read at 4 TB/s by one launch more
+      if (splits > 1) time += 4000 + double(ni) * nj * images * halves * splits * 8 / 4000;
+      if (least == 0 || time < least) {
+        best = {64 << i, int(splits)};
+        least = time;
+      }
     }
   }
   return best;
 }
 
-inline int product_splits(int size, ProductKind kind, long ni, long nj, long images, long halves, long K, long segs) {
-  return splits_on(size, kind, product_tile(size, kind, ni, nj, images, halves, K, segs), ni, nj, images, halves, K,
-                   segs);
-}
-
 // Parts that the unit, in the backward pass, leaves the sums over the positions in:
 // one for each wave's positions.
 inline long product_sum_parts(int size, ProductKind kind, long ni, long nj, long images, long K) {
-  const int tile = product_tile(size, kind, ni, nj, images, 1, K, 1);
+  const int tile = product_choice(size, kind, ni, nj, images, 1, K, 1).tile;
   const ProductWaves w = product_waves(tile, pair_on_i(kind));
   return images * (((pair_on_i(kind) ? nj : ni) + tile - 1) / tile) * (pair_on_i(kind) ? w.j : w.i);
 }
@@ -79,7 +78,12 @@ inline long product_sum_parts(int size, ProductKind kind, long ni, long nj, long
 // Positions up to which the forward unit reads its weights without tiles.
 constexpr long kFewPositions = 32;
 
-// Whether the backward pass makes g and u again from x rather than having them stored.
+// Whether the backward pass makes g and u again from x rather than having them stored: the
+// product grows with C, what storing them moves (16 bytes a hidden value and position) does
+// not. us of both passes, stored and made again: float32, 8 planes of 56 x 56, 64 -> 256 102 and
+// 103, 16384 positions 256 -> 1024 394 and 441; bfloat16, 16384 positions, 512 -> 2048 495
+// and 405, 1024 -> 4096 1174 and 1218 (and 512 positions 86 and 75), 2048 -> 8192 3302 and
+// 4096. Of equals the one that needs no memory.
 inline bool product_remakes(int size, long C) { return size == 2 ? C <= 1024 : C <= 64; }
 
 }  // namespace oaa

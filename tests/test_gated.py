@@ -234,6 +234,30 @@ def test_weights_in_one_tensor(gpu_lib, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("S,F", [(7, 900), (150, 700), (150, 12)])
+def test_input_gradient_with_gaps(gpu_lib, S, F, layout, dtype):
+    """dx with values between its rows and images, left as they were: in one piece, and
+    joined from parts of a long sum."""
+    B, C, last = 3, 20, layout == "last"
+    x, dh, gw, uw, *_ = make((B, C, S, 1), F, layout, dtype, bias=False, seed=21)
+    h, gate, up = binding.gated_forward(x, gw, uw, keep=False)
+    row, image = (C + 3, S * (C + 3) + 5) if last else (S, C * S + 6)
+    d = desc(B=B, C=C, F=F, S=S, layout=int(last), dtype=binding._dtype_codes()[dtype], dx=(image, row))
+    flat = torch.full((B * image,), 3.0, dtype=dtype, device=DEV)
+    ws = torch.empty(binding.oaa_gated_workspace_bytes(d, 1, 0), dtype=torch.uint8, device=DEV)
+    binding.oaa_gated_backward(d, dh.data_ptr(), x.data_ptr(), gw.data_ptr(), uw.data_ptr(), None, None, None, None,
+                               flat.data_ptr(), None, None, None, None, ws.data_ptr(), ws.numel(),
+                               torch.cuda.current_stream().cuda_stream)
+    got = flat.as_strided((B, S, C) if last else (B, C, S), (image, row, 1))
+    b = Bounds(wide(x), wide(gw), wide(uw), None, None, "silu", dtype, wide(dh))
+    near((got.movedim(-1, 1) if last else got)[..., None], b.grads[0], b.offs[0], dtype, "dx", 2 * F)
+    got.fill_(3.0)
+    assert bool((flat == 3.0).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["planes", "last"])
 def test_nothing_to_do(gpu_lib, layout):
     for shape in ((0, 6, 3, 2), (2, 6, 0, 4), (0, 6)):
