@@ -456,7 +456,8 @@ oaa_status_t oaa_gated_forward(const oaa_gated_t* d, const void* x, const void* 
 /* The gradients that are not NULL (one at least; both weights' or neither), dense for
  * the weights and biases. gate and up: the forward pass's; both NULL: made again, with
  * the same weights and biases (which are not read otherwise). With gate and up, x may
- * be NULL without the weights' gradients, and the weights without dx. An empty x gives zeros in the gradients of weights and biases. */
+ * be NULL without the weights' gradients, and the weights without dx. An empty x gives
+ * zeros in the gradients of weights and biases. */
 oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void* x, const void* gate_weight,
                                 const void* up_weight, const void* gate_bias, const void* up_bias, const float* gate,
                                 const float* up, void* dx, void* dgate_weight, void* dup_weight, void* dgate_bias,

@@ -25,6 +25,7 @@ pass; ``clip_grad_norm_`` clips the gradients that the backward passes left in a
 network's parameters.
 """
 
+import functools
 import math
 
 import torch
@@ -90,16 +91,24 @@ class OaAConv2d(torch.nn.Module):
         return OaAConv2dFunction.apply(x, self.weight, self.plan_for(B, N))
 
 
+@functools.lru_cache(maxsize=4096)
+def _layout(shape, strides, want=None):
+    """The layout (`want`, if one is given) of a tensor's strides; None if the library
+    does not take them."""
+    try:
+        return binding._layout_of(shape, strides, "x", want)[0]
+    except ValueError:
+        return None
+
+
 def _laid_out(t, layout=None):
     """t if the library takes its strides (in `layout`, if one is given), or a
     dense copy of it."""
-    try:
-        binding._norm_layout(t, "x", layout)
-    except ValueError:
-        if layout == binding.LAYOUT_CHANNELS_LAST:
-            return t.movedim(1, -1).contiguous().movedim(-1, 1)
-        return t.contiguous()
-    return t
+    if _layout(t.shape, t.stride(), layout) is not None:
+        return t
+    if layout == binding.LAYOUT_CHANNELS_LAST:
+        return t.movedim(1, -1).contiguous().movedim(-1, 1)
+    return t.contiguous()
 
 
 class GroupNormFunction(torch.autograd.Function):
@@ -193,7 +202,7 @@ class GatedFunction(torch.autograd.Function):
         x, gate_weight, up_weight, gate, up = ctx.saved_tensors
         # hooks on saved tensors may bring them back with other strides than they had
         x = _laid_out(x)
-        layout = binding._norm_layout(x, "x")[0]
+        layout = _layout(x.shape, x.stride())
         dh, gate, up = (t if t.dim() == 1 else _laid_out(t, layout) for t in (dh, gate, up))
         need = ctx.needs_input_grad
         grads = binding.gated_backward(dh, x, _rows(gate_weight), _rows(up_weight), gate, up, ctx.activation, need[0],
@@ -237,7 +246,7 @@ class DropoutFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, p, seed, residual):
         x = _laid_out(x)
-        ctx.layout = binding._norm_layout(x, "x")[0]
+        ctx.layout = _layout(x.shape, x.stride())
         ctx.p, ctx.dtype = p, x.dtype
         ctx.save_for_backward(seed)
         return binding.dropout(x, p, seed, None if residual is None else _laid_out(residual, ctx.layout))
@@ -262,14 +271,16 @@ def dropout(x, p, seed, residual=None):
         return DropoutFunction.apply(x, p, seed, residual)
     x = _laid_out(x)
     if residual is not None:
-        residual = _laid_out(residual, binding._norm_layout(x, "x")[0])
+        residual = _laid_out(residual, _layout(x.shape, x.stride()))
     return binding.dropout(x, p, seed, residual)
 
 
 class Dropout(torch.nn.Module):
     """Dropout with probability p while training. Its state (a key and the number of
     calls) is a buffer on the device that every call advances there, so that a
-    captured graph draws another mask at each replay."""
+    captured graph draws another mask at each replay. A call that is made again for the
+    backward pass, as by torch.utils.checkpoint, draws another one too: there, draw the
+    seed once (``binding.dropout_next(state)``) and call ``dropout`` with it."""
 
     def __init__(self, p=0.5, seed=None, device="cuda"):
         super().__init__()

@@ -788,7 +788,9 @@ def _gated_workspace(call, backward, x, gate_weight, up_weight):
 @functools.lru_cache(maxsize=None)
 def _no_bias(device):
     """What stands for an absent bias among what a backward pass needs."""
-    return _torch()[0].empty(0, device=device)
+    torch = _torch()[0]
+    with torch.inference_mode(False):  # autograd is to keep it
+        return torch.empty(0, device=device)
 
 
 def gated_forward(x, gate_weight, up_weight, gate_bias=None, up_bias=None, activation="silu", h=None, keep=True):
@@ -898,8 +900,8 @@ def dropout(x, p, seed, residual=None, y=None, dtype=None):
     kind = y.dtype if y is not None else dtype or (x if residual is None else residual).dtype
     if dtype not in (None, kind):
         raise ValueError(f"y is {kind}, not {dtype}")
-    call = _dropout_call(x.shape, x.stride(), x.dtype, residual if residual is None else (residual.dtype, residual.stride()),
-                         kind, None if y is None else y.stride())
+    added = None if residual is None else (residual.dtype, residual.stride())
+    call = _dropout_call(x.shape, x.stride(), x.dtype, added, kind, None if y is None else y.stride())
     out = _laid(x.shape, call.layout, kind, x.device) if y is None else y
     _launch(load().oaa_dropout, index, call.address, x.data_ptr(), _pointer(residual), out.data_ptr(), p,
             seed.data_ptr())

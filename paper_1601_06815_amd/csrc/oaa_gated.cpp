@@ -272,9 +272,11 @@ Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w
   l.dup = room.take(d_bytes);
   l.part_rows = std::max(kPartRows, (rows * u.B + kMostParts - 1) / kMostParts);
   if (need_b) {
-    l.parts = remake ? oaa::product_sum_parts(int(u.size), u.last ? oaa::kUnitLastAgain : oaa::kUnitPlanesAgain, columns, rows, u.B, u.C)
-              : u.last ? u.B * ((rows + l.part_rows - 1) / l.part_rows)
-                       : u.B;
+    if (remake)
+      l.parts = oaa::product_sum_parts(int(u.size), u.last ? oaa::kUnitLastAgain : oaa::kUnitPlanesAgain, columns, rows,
+                                       u.B, u.C);
+    else
+      l.parts = u.last ? u.B * ((rows + l.part_rows - 1) / l.part_rows) : u.B;
     l.sums = static_cast<float*>(room.take(size_t(l.parts) * 2 * u.F * 4));
   }
   const int unit_x = u.last ? kRows : kColumns, dw_x = u.last ? kColumns : kRows;
@@ -288,8 +290,8 @@ Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w
     if (l.dx_splits > 1) parts = size_t(l.dx_splits) * u.B * ni * nj * 4;
   }
   if (need_w) {
-    l.dw_splits = oaa::product_choice(int(u.size), u.last ? oaa::kWeightLast : oaa::kWeightPlanes, u.C, u.F, 1, 2, u.S, u.B)
-                      .splits;
+    const ProductKind kind = u.last ? oaa::kWeightLast : oaa::kWeightPlanes;
+    l.dw_splits = oaa::product_choice(int(u.size), kind, u.C, u.F, 1, 2, u.S, u.B).splits;
     if (l.dw_splits > 1) parts = std::max(parts, size_t(l.dw_splits) * 2 * u.F * u.C * 4);
   }
   if (parts) l.product_parts = static_cast<float*>(room.take(parts));
@@ -486,7 +488,10 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
   const long weights = long(w.F) * w.C;
   if (none) {
     (void)hipGetLastError();
-    const struct { void* at; long n; } zeros[] = {{dgate_weight, weights}, {dup_weight, weights}, {dgate_bias, w.F}, {dup_bias, w.F}};
+    const struct {
+      void* at;
+      long n;
+    } zeros[] = {{dgate_weight, weights}, {dup_weight, weights}, {dgate_bias, w.F}, {dup_bias, w.F}};
     for (const auto& z : zeros) {
       if (!z.at) continue;
       const hipError_t e = for_type(w.dtype, [&](auto t) { return oaa::launch_zero<decltype(t)>(z.at, z.n, s); });
@@ -495,7 +500,8 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
     return OAA_OK;
   }
   const long long n = (long long)w.B * w.S * w.F;
-  const Memory out[] = {tensor(w, dx, w.C, w.dx_image, w.dx_row, "dx"), dense(dgate_weight, weights, w.size, "dgate_weight"),
+  const Memory out[] = {tensor(w, dx, w.C, w.dx_image, w.dx_row, "dx"),
+                        dense(dgate_weight, weights, w.size, "dgate_weight"),
                         dense(dup_weight, weights, w.size, "dup_weight"), dense(dgate_bias, w.F, w.size, "dgate_bias"),
                         dense(dup_bias, w.F, w.size, "dup_bias")};
   const Memory in[] = {tensor(w, dh, w.F, w.dh_image, w.dh_row, "dh"),

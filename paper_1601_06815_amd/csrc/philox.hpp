@@ -13,7 +13,8 @@ struct Words {
 };
 
 // The words of counter (lo, hi of `at`, lo, hi of `call`) under `key`.
-__host__ __device__ __forceinline__ Words philox(unsigned long long at, unsigned long long call, unsigned long long key) {
+__host__ __device__ __forceinline__ Words philox(unsigned long long at, unsigned long long call,
+                                                 unsigned long long key) {
   unsigned a = unsigned(at), b = unsigned(at >> 32), c = unsigned(call), d = unsigned(call >> 32);
   unsigned k0 = unsigned(key), k1 = unsigned(key >> 32);
 #pragma unroll

@@ -43,6 +43,7 @@ constexpr int kStepBytes = 128;
 template <typename T>
 constexpr int kStep = kStepBytes / int(sizeof(T));
 
+// (float32: where loads take the time, gated_few.hpp; elsewhere see Pieces)
 template <typename T>
 __device__ __forceinline__ floatx4 multiply(floatx4 a, floatx4 b, floatx4 c) {
   if constexpr (sizeof(T) == 4) {
@@ -621,7 +622,8 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
         Vec<T, V> dg, du;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float d = element<T, V>(needs.dh[y * kPieces + q], e), s = d * u[e] * act_slope<ACT>(g[e]), t = d * act<ACT>(g[e]);
+          const float d = element<T, V>(needs.dh[y * kPieces + q], e);
+          const float s = d * u[e] * act_slope<ACT>(g[e]), t = d * act<ACT>(g[e]);
           set_element<T, V>(dg, e, s);
           set_element<T, V>(du, e, t);
           if constexpr (PAIR == 1) {
@@ -639,7 +641,8 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
         Vec<T, V> h;
 #pragma unroll
         for (int e = 0; e < V; ++e) set_element<T, V>(h, e, act<ACT>(g[e]) * u[e]);
-        *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.out) + long(image) * p.out_image + long(jj) * p.out_ld + i + at(q)) = h;
+        T* to = static_cast<T*>(p.out) + long(image) * p.out_image + long(jj) * p.out_ld + i + at(q);
+        *reinterpret_cast<Vec<T, V>*>(to) = h;
         if (p.gate) {
           const long to = (long(image) * p.nj + jj) * p.ni + i + at(q);
 #pragma unroll
@@ -821,270 +824,274 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   constexpr bool kEarly = PAIR != 0 && TI * TJ <= 128 * 128;  // registers for the unit's needs while it multiplies
   bool stored = false;
   for (;;) {
-  const ProductParams& p = again(args);
-  const int lane = lane_again(), left = p.K % kStep<T> * int(sizeof(T));
-  const bool ragged = (IK || JK) && left;
-  floatx4 acc[NI][NJ];
+    const ProductParams& p = again(args);
+    const int lane = lane_again(), left = p.K % kStep<T> * int(sizeof(T));
+    const bool ragged = (IK || JK) && left;
+    floatx4 acc[NI][NJ];
 #pragma unroll
-  for (int x = 0; x < NI; ++x)
+    for (int x = 0; x < NI; ++x)
 #pragma unroll
-    for (int y = 0; y < NJ; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int y = 0; y < NJ; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  // A step's two halves of k follow each other without a pause: while the products of
-  // one run, row by row, the fragments of the next take the place of those that are
-  // done with. At the barrier between them every wave has read all of this stage, and the
-  // stage after it, asked for a step ago, has landed; so what comes after that goes
-  // where this one was, asked for among the products of the second half.
-  const int first = w.first, end = w.end;
-  std::conditional_t<PAIR != 0, UnitNeeds<T, MI, MJ, PAIR ? PAIR : 1, BACK>, int> needs;
-  auto fetch = [&](const ProductParams& p, int lane) {
-    if constexpr (PAIR != 0)
-      needs.fetch(p, w.image, w.ti * FI + wi * RI + lane / 16 * kVec, w.tj * FJ + wj * 16 * MJ + lane % 16);
-  };
-  auto landed = [&]() {
-    if (stored)
-      wait_but_for<kStores>();
-    else
-      wait_for_loads();
-  };
-  Fragments<T, TI, IK, true> at_a;
-  Fragments<T, TJ, JK, false> at_b;
-  at_a.init(wi * GI, lane);
-  at_b.init(wj * GJ, lane);
-  if constexpr (sizeof(T) == 4) {
-    // The matrix cores round toward one side, an error of one sign that a long sum gathers:
-    // every eight steps the sums change their sign, and j's values with them.
-    unsigned sign = 0;
-    int stage = 0;
-#pragma unroll 1
-    for (int n = first; n < end; ++n) {
-      if (n == first)
-        landed();
+    // A step's two halves of k follow each other without a pause: while the products of
+    // one run, row by row, the fragments of the next take the place of those that are
+    // done with. At the barrier between them every wave has read all of this stage, and the
+    // stage after it, asked for a step ago, has landed; so what comes after that goes
+    // where this one was, asked for among the products of the second half.
+    const int first = w.first, end = w.end;
+    std::conditional_t<PAIR != 0, UnitNeeds<T, MI, MJ, PAIR ? PAIR : 1, BACK>, int> needs;
+    auto fetch = [&](const ProductParams& p, int lane) {
+      if constexpr (PAIR != 0)
+        needs.fetch(p, w.image, w.ti * FI + wi * RI + lane / 16 * kVec, w.tj * FJ + wj * 16 * MJ + lane % 16);
+    };
+    auto landed = [&]() {
+      if (stored)
+        wait_but_for<kStores>();
       else
         wait_for_loads();
-      if (n == first && kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
-      if (ragged && (n == first ? last : k0 == 0)) cut(stage, left);
-      if (n > first && n + 1 < end) load(p, stage ^ 1);
-      const unsigned ta = lds + stage * kStage, tb = ta + TI * kStepBytes;
-      const auto a0 = at_a.base(ta, 0), a1 = at_a.base(ta, 1);
-      Pieces pb[NJ], pa;
-      {
-        const auto b0 = at_b.base(tb, 0), b1 = at_b.base(tb, 1);
+    };
+    Fragments<T, TI, IK, true> at_a;
+    Fragments<T, TJ, JK, false> at_b;
+    at_a.init(wi * GI, lane);
+    at_b.init(wj * GJ, lane);
+    if constexpr (sizeof(T) == 4) {
+      // The matrix cores round toward one side, an error of one sign that a long sum gathers:
+      // every eight steps the sums change their sign, and j's values with them.
+      unsigned sign = 0;
+      int stage = 0;
+#pragma unroll 1
+      for (int n = first; n < end; ++n) {
+        if (n == first)
+          landed();
+        else
+          wait_for_loads();
+        if (n == first && kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
+        if (ragged && (n == first ? last : k0 == 0)) cut(stage, left);
+        if (n > first && n + 1 < end) load(p, stage ^ 1);
+        const unsigned ta = lds + stage * kStage, tb = ta + TI * kStepBytes;
+        const auto a0 = at_a.base(ta, 0), a1 = at_a.base(ta, 1);
+        Pieces pb[NJ], pa;
+        {
+          const auto b0 = at_b.base(tb, 0), b1 = at_b.base(tb, 1);
 #pragma unroll
-        for (int y = 0; y < NJ; ++y) pb[y] = Pieces(at_b.read(b0, y, 0), at_b.read(b1, y, 1), sign);
-      }
-      pa = Pieces(at_a.read(a0, 0, 0), at_a.read(a1, 0, 1));
-      floatx4 raw[2];
-      if (NI > 1) {
-        raw[0] = at_a.read(a0, 1, 0);
-        raw[1] = at_a.read(a1, 1, 1);
-      }
-      // among the products of one row, the next one's values are taken apart
+          for (int y = 0; y < NJ; ++y) pb[y] = Pieces(at_b.read(b0, y, 0), at_b.read(b1, y, 1), sign);
+        }
+        pa = Pieces(at_a.read(a0, 0, 0), at_a.read(a1, 0, 1));
+        floatx4 raw[2];
+        if (NI > 1) {
+          raw[0] = at_a.read(a0, 1, 0);
+          raw[1] = at_a.read(a1, 1, 1);
+        }
+        // among the products of one row, the next one's values are taken apart
 #pragma unroll
-      for (int x = 0; x < NI; ++x) {
+        for (int x = 0; x < NI; ++x) {
+          __builtin_amdgcn_sched_barrier(0);
+          Pieces next;
+          if (x + 1 < NI) next = Pieces(raw[0], raw[1]);
+          if (x + 2 < NI) {
+            raw[0] = at_a.read(a0, x + 2, 0);
+            raw[1] = at_a.read(a1, x + 2, 1);
+          }
+          constexpr int order[6][2] = {{2, 0}, {1, 1}, {0, 2}, {1, 0}, {0, 1}, {0, 0}};
+#pragma unroll
+          for (const auto& t : order)
+#pragma unroll
+            for (int y = 0; y < NJ; ++y)
+              acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa.p[t[0]], pb[y].p[t[1]], acc[x][y], 0, 0, 0);
+#pragma unroll
+          for (int t = 0; t < 6 * NJ; ++t) {  // (44 instructions take a row apart)
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 44 / (6 * NJ) + 1, 0);
+          }
+          pa = next;
+        }
         __builtin_amdgcn_sched_barrier(0);
-        Pieces next;
-        if (x + 1 < NI) next = Pieces(raw[0], raw[1]);
-        if (x + 2 < NI) {
-          raw[0] = at_a.read(a0, x + 2, 0);
-          raw[1] = at_a.read(a1, x + 2, 1);
+        stage ^= 1;
+        if ((n - first) % 8 == 7) {
+          sign ^= 0x80000000u;
+#pragma unroll
+          for (int x = 0; x < NI; ++x)
+#pragma unroll
+            for (int y = 0; y < NJ; ++y) acc[x][y] = -acc[x][y];
         }
-        constexpr int order[6][2] = {{2, 0}, {1, 1}, {0, 2}, {1, 0}, {0, 1}, {0, 0}};
-#pragma unroll
-        for (int t = 0; t < 6; ++t)
-#pragma unroll
-          for (int y = 0; y < NJ; ++y)
-            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa.p[order[t][0]], pb[y].p[order[t][1]], acc[x][y], 0, 0, 0);
-#pragma unroll
-        for (int t = 0; t < 6 * NJ; ++t) {  // (44 instructions take a row apart)
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x002, 44 / (6 * NJ) + 1, 0);
-        }
-        pa = next;
       }
-      __builtin_amdgcn_sched_barrier(0);
-      stage ^= 1;
-      if ((n - first) % 8 == 7) {
-        sign ^= 0x80000000u;
+      if (sign) {
 #pragma unroll
         for (int x = 0; x < NI; ++x)
 #pragma unroll
           for (int y = 0; y < NJ; ++y) acc[x][y] = -acc[x][y];
       }
-    }
-    if (sign) {
-#pragma unroll
-      for (int x = 0; x < NI; ++x)
-#pragma unroll
-        for (int y = 0; y < NJ; ++y) acc[x][y] = -acc[x][y];
-    }
-  } else {
-  floatx4 fa[NI], fb[2][NJ];
-  auto half = [&](int sub, int stage, auto&& between) {  // products of `sub`; reads the other of `stage`
-    const auto ba = at_a.base(lds + stage * kStage, sub ^ 1);
-    const auto bb = at_b.base(lds + stage * kStage + TI * kStepBytes, sub ^ 1);
-#pragma unroll
-    for (int x = 0; x < NI; ++x) {
-#pragma unroll
-      for (int y = 0; y < NJ; ++y) acc[x][y] = multiply<T>(fa[x], fb[sub][y], acc[x][y]);
-      fa[x] = at_a.read(ba, x, sub ^ 1);
-#pragma unroll
-      for (int y = x * NJ / NI; y < (x + 1) * NJ / NI; ++y) fb[sub ^ 1][y] = at_b.read(bb, y, sub ^ 1);
-      between(x);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  if (first < end) {
-    landed();
-    if (kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
-    if (ragged && last) cut(0, left);
-    const auto ba = at_a.base(lds, 0);
-    const auto bb = at_b.base(lds + TI * kStepBytes, 0);
-#pragma unroll
-    for (int x = 0; x < NI; ++x) fa[x] = at_a.read(ba, x, 0);
-#pragma unroll
-    for (int y = 0; y < NJ; ++y) fb[0][y] = at_b.read(bb, y, 0);
-  }
-  int stage = 0;
-#pragma unroll 1
-  for (int n = first; n < end; ++n) {
-    half(0, stage, [](int) {});
-    // this stage is read by all waves; the next has landed: of the first two steps both
-    // had, and after the last there is none
-    if (n > first && n + 1 < end)
-      wait_for_loads();
-    else
-      wait_but_for<63>();
-    if (ragged && k0 == 0 && n + 1 < end) cut(stage ^ 1, left);
-    const bool more = n + 2 < end;
-    const unsigned la = lds + stage * kStage, lb = la + TI * kStepBytes;
-    // (after the last step these reads find old values, which nothing uses)
-    half(1, stage ^ 1, [&](int x) {
-      if (!more) return;
-#pragma unroll
-      for (int m = x * a.kMine / NI; m < (x + 1) * a.kMine / NI; ++m) a.piece(la, k0, p.K, m, wave);
-#pragma unroll
-      for (int m = x * b.kMine / NI; m < (x + 1) * b.kMine / NI; ++m) b.piece(lb, k0, p.K, m, wave);
-    });
-    if (more) advance(p.K);
-    stage ^= 1;
-  }
-
-  }
-
-  // A lane's results: column j of 16, and 16 bytes of neighbours along i of every 64. They leave
-  // from the registers, 16 bytes a store, except where a wave's part crosses the end of
-  // i: that goes through LDS, each wave's through a slab of its own, as rows that a
-  // short loop reads back and finishes.
-  constexpr unsigned kSlab = 2 * kStage / WAVES;
-  {
-  const ProductParams& p = again(args);
-  const int lane = lane_again(), row = lane & 15, quad = lane >> 4;
-  const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ;
-  const int image = w.image, which = w.which, i0 = w.ti * FI;
-  const int iw = i0 + wi * RI, jw = w.tj * FJ + wj * 16 * MJ;
-  const bool inside = iw + RI <= p.ni;
-  const long part = PAIR == 1   ? (long(image) * tiles_j + w.tj) * WJ + wj
-                    : PAIR == 2 ? (long(image) * tiles_i + w.ti) * WI + wi
-                                : (long(w.split) * p.halves + which) * p.images + image;
-  __syncthreads();
-  number += gridDim.x;
-  another = number < unsigned(p.tiles);
-  // (where LDS is not needed any more, and registers last)
-  const bool early = (PAIR == 0 || kEarly) && i0 + FI <= p.ni;
-  late = another && !early;
-  stored = another && early && inside && jw + 16 * MJ <= p.nj;
-  if constexpr (PAIR != 0) {
-    if (inside) {
-      if (!kEarly || first >= end) fetch(p, lane);
-      needs.arrive();
-    }
-  }
-  if (another) w = place(number);
-  if (another && early) last = begin(w);
-  const unsigned slab = lds + wave * kSlab;
-  if constexpr (PAIR != 0) {
-    if (inside) {
-      switch (p.act) {
-        case OAA_ACT_RELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_RELU>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane); break;
-        case OAA_ACT_SILU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_SILU>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane); break;
-        case OAA_ACT_GELU: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_GELU>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane); break;
-        default: unit_end<T, MI, MJ, PAIR, BACK, OAA_ACT_NONE>(p, acc, needs, image, part, iw + quad * kVec, jw + row, lane);
-      }
     } else {
-    constexpr int kRows = int(kSlab / (2 * RI * 4)) < 16 * MJ ? int(kSlab / (2 * RI * 4)) : 16 * MJ;  // of a pass
-    static_assert(kRows % 16 == 0 && 16 * MJ % kRows == 0, "");
-    UnitEnd<T, RI, kRows, PAIR, BACK> finish(p, image, iw, lane);
-    finish.part = part;
-    typename UnitEnd<T, RI, kRows, PAIR, BACK>::Row ahead;
-    constexpr int kPasses = 16 * MJ / kRows;
-#pragma unroll 1
-    for (int pass = 0; pass < kPasses; ++pass) {
-      finish.fetch(ahead, jw + pass * kRows + finish.r0);
+      floatx4 fa[NI], fb[2][NJ];
+      auto half = [&](int sub, int stage, auto&& between) {  // products of `sub`; reads the other of `stage`
+        const auto ba = at_a.base(lds + stage * kStage, sub ^ 1);
+        const auto bb = at_b.base(lds + stage * kStage + TI * kStepBytes, sub ^ 1);
 #pragma unroll
-      for (int q = 0; q < kPasses; ++q) {
-        if (q != pass) continue;
+        for (int x = 0; x < NI; ++x) {
 #pragma unroll
-        for (int y = 0; y < kRows / 16; ++y)
+          for (int y = 0; y < NJ; ++y) acc[x][y] = multiply<T>(fa[x], fb[sub][y], acc[x][y]);
+          fa[x] = at_a.read(ba, x, sub ^ 1);
 #pragma unroll
-          for (int x = 0; x < MI; ++x) {
-            const int yy = q * kRows / 16 + y, four = row_in_fragment<T, true>(x, 4 * quad) / 4;
-            put<RI>(slab, 16 * y + row, four, acc[x][yy]);
-            put<RI>(slab + kRows * RI * 4, 16 * y + row, four, acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? yy + MJ : yy]);
-          }
-      }
-      finish.rows(ahead, slab, jw + pass * kRows);
-    }
-    finish.end();
-    }
-  } else {
-    auto leave = [&](auto zero, auto* out, long ld) {
-      using E = decltype(zero);
-      constexpr int V = 16 / int(sizeof(E));
-      if (inside) {
-#pragma unroll
-        for (int y = 0; y < MJ; ++y) {
-          if (jw + row + 16 * y >= p.nj) continue;
-          E* to = out + iw + long(jw + row + 16 * y) * ld;
-#pragma unroll
-          for (int x = 0; x < MI; x += V / 4) {
-            Vec<E, V> w;
-#pragma unroll
-            for (int e = 0; e < V; ++e) set_element<E, V>(w, e, acc[x + e / 4][y][e % 4]);
-            *reinterpret_cast<Vec<E, V>*>(to + row_in_fragment<T, true>(x, 4 * quad)) = w;
-          }
+          for (int y = x * NJ / NI; y < (x + 1) * NJ / NI; ++y) fb[sub ^ 1][y] = at_b.read(bb, y, sub ^ 1);
+          between(x);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        return;
+      };
+      if (first < end) {
+        landed();
+        if (kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
+        if (ragged && last) cut(0, left);
+        const auto ba = at_a.base(lds, 0);
+        const auto bb = at_b.base(lds + TI * kStepBytes, 0);
+#pragma unroll
+        for (int x = 0; x < NI; ++x) fa[x] = at_a.read(ba, x, 0);
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) fb[0][y] = at_b.read(bb, y, 0);
       }
-      constexpr int kRows = int(kSlab / (GI * sizeof(E))) < GJ ? int(kSlab / (GI * sizeof(E))) : GJ;
-      static_assert(kRows % 16 == 0 && GJ % kRows == 0, "");
+      int stage = 0;
+#pragma unroll 1
+      for (int n = first; n < end; ++n) {
+        half(0, stage, [](int) {});
+        // this stage is read by all waves; the next has landed: of the first two steps both
+        // had, and after the last there is none
+        if (n > first && n + 1 < end)
+          wait_for_loads();
+        else
+          wait_but_for<63>();
+        if (ragged && k0 == 0 && n + 1 < end) cut(stage ^ 1, left);
+        const bool more = n + 2 < end;
+        const unsigned la = lds + stage * kStage, lb = la + TI * kStepBytes;
+        // (after the last step these reads find old values, which nothing uses)
+        half(1, stage ^ 1, [&](int x) {
+          if (!more) return;
 #pragma unroll
-      for (int pass = 0; pass < GJ / kRows; ++pass) {
+          for (int m = x * a.kMine / NI; m < (x + 1) * a.kMine / NI; ++m) a.piece(la, k0, p.K, m, wave);
 #pragma unroll
-        for (int y = 0; y < kRows / 16; ++y)
-#pragma unroll
-          for (int x = 0; x < NI; ++x) {
-            const floatx4 v = acc[x][pass * kRows / 16 + y];
-            const int four = row_in_fragment<T, true>(x, 4 * quad) / 4;
-            if constexpr (sizeof(E) == 4)
-              put<GI>(slab, 16 * y + row, four, v);
-            else
-              put_16<E, GI>(slab, 16 * y + row, four, v);
+          for (int m = x * b.kMine / NI; m < (x + 1) * b.kMine / NI; ++m) b.piece(lb, k0, p.K, m, wave);
+        });
+        if (more) advance(p.K);
+        stage ^= 1;
+      }
+    }
+
+    // A lane's results: column j of 16, and 16 bytes of neighbours along i of every 64. They leave
+    // from the registers, 16 bytes a store, except where a wave's part crosses the end of
+    // i: that goes through LDS, each wave's through a slab of its own, as rows that a
+    // short loop reads back and finishes.
+    constexpr unsigned kSlab = 2 * kStage / WAVES;
+    {
+      const ProductParams& p = again(args);
+      const int lane = lane_again(), row = lane & 15, quad = lane >> 4;
+      const int tiles_i = (p.ni + FI - 1) / FI, tiles_j = (p.nj + FJ - 1) / FJ;
+      const int image = w.image, which = w.which, i0 = w.ti * FI;
+      const int iw = i0 + wi * RI, jw = w.tj * FJ + wj * 16 * MJ;
+      const bool inside = iw + RI <= p.ni;
+      const long part = PAIR == 1   ? (long(image) * tiles_j + w.tj) * WJ + wj
+                        : PAIR == 2 ? (long(image) * tiles_i + w.ti) * WI + wi
+                                    : (long(w.split) * p.halves + which) * p.images + image;
+      __syncthreads();
+      number += gridDim.x;
+      another = number < unsigned(p.tiles);
+      // (where LDS is not needed any more, and registers last)
+      const bool early = (PAIR == 0 || kEarly) && i0 + FI <= p.ni;
+      late = another && !early;
+      stored = another && early && inside && jw + 16 * MJ <= p.nj;
+      if constexpr (PAIR != 0) {
+        if (inside) {
+          if (!kEarly || first >= end) fetch(p, lane);
+          needs.arrive();
+        }
+      }
+      if (another) w = place(number);
+      if (another && early) last = begin(w);
+      const unsigned slab = lds + wave * kSlab;
+      if constexpr (PAIR != 0) {
+        if (inside) {
+          auto end_with = [&](auto which_act) {
+            unit_end<T, MI, MJ, PAIR, BACK, decltype(which_act)::value>(p, acc, needs, image, part, iw + quad * kVec,
+                                                                        jw + row, lane);
+          };
+          switch (p.act) {
+            case OAA_ACT_RELU: end_with(std::integral_constant<int, OAA_ACT_RELU>{}); break;
+            case OAA_ACT_SILU: end_with(std::integral_constant<int, OAA_ACT_SILU>{}); break;
+            case OAA_ACT_GELU: end_with(std::integral_constant<int, OAA_ACT_GELU>{}); break;
+            default: end_with(std::integral_constant<int, OAA_ACT_NONE>{});
           }
-        store_rows<E, GI, kRows>(slab, out + iw, ld, jw + pass * kRows, p.nj, p.ni - iw, lane);
+        } else {
+          constexpr int kRows = int(kSlab / (2 * RI * 4)) < 16 * MJ ? int(kSlab / (2 * RI * 4)) : 16 * MJ;  // of a pass
+          static_assert(kRows % 16 == 0 && 16 * MJ % kRows == 0, "");
+          UnitEnd<T, RI, kRows, PAIR, BACK> finish(p, image, iw, lane);
+          finish.part = part;
+          typename UnitEnd<T, RI, kRows, PAIR, BACK>::Row ahead;
+          constexpr int kPasses = 16 * MJ / kRows;
+#pragma unroll 1
+          for (int pass = 0; pass < kPasses; ++pass) {
+            finish.fetch(ahead, jw + pass * kRows + finish.r0);
+#pragma unroll
+            for (int q = 0; q < kPasses; ++q) {
+              if (q != pass) continue;
+#pragma unroll
+              for (int y = 0; y < kRows / 16; ++y)
+#pragma unroll
+                for (int x = 0; x < MI; ++x) {
+                  const int yy = q * kRows / 16 + y, four = row_in_fragment<T, true>(x, 4 * quad) / 4;
+                  put<RI>(slab, 16 * y + row, four, acc[x][yy]);
+                  const floatx4 u = acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? yy + MJ : yy];
+                put<RI>(slab + kRows * RI * 4, 16 * y + row, four, u);
+                }
+            }
+            finish.rows(ahead, slab, jw + pass * kRows);
+        }
+        finish.end();
+        }
+      } else {
+        auto leave = [&](auto zero, auto* out, long ld) {
+          using E = decltype(zero);
+          constexpr int V = 16 / int(sizeof(E));
+          if (inside) {
+#pragma unroll
+            for (int y = 0; y < MJ; ++y) {
+              if (jw + row + 16 * y >= p.nj) continue;
+              E* to = out + iw + long(jw + row + 16 * y) * ld;
+#pragma unroll
+              for (int x = 0; x < MI; x += V / 4) {
+                Vec<E, V> w;
+#pragma unroll
+                for (int e = 0; e < V; ++e) set_element<E, V>(w, e, acc[x + e / 4][y][e % 4]);
+                *reinterpret_cast<Vec<E, V>*>(to + row_in_fragment<T, true>(x, 4 * quad)) = w;
+              }
+            }
+            return;
+          }
+          constexpr int kRows = int(kSlab / (GI * sizeof(E))) < GJ ? int(kSlab / (GI * sizeof(E))) : GJ;
+          static_assert(kRows % 16 == 0 && GJ % kRows == 0, "");
+#pragma unroll
+          for (int pass = 0; pass < GJ / kRows; ++pass) {
+#pragma unroll
+            for (int y = 0; y < kRows / 16; ++y)
+#pragma unroll
+              for (int x = 0; x < NI; ++x) {
+                const floatx4 v = acc[x][pass * kRows / 16 + y];
+                const int four = row_in_fragment<T, true>(x, 4 * quad) / 4;
+                if constexpr (sizeof(E) == 4)
+                  put<GI>(slab, 16 * y + row, four, v);
+                else
+                  put_16<E, GI>(slab, 16 * y + row, four, v);
+              }
+            store_rows<E, GI, kRows>(slab, out + iw, ld, jw + pass * kRows, p.nj, p.ni - iw, lane);
+          }
+        };
+        if (p.splits > 1)
+          leave(0.0f, static_cast<float*>(p.out) + part * p.nj * p.ni, p.ni);
+        else
+          leave(T(0.0f), static_cast<T*>(p.out) + long(image) * p.out_image + long(which) * p.out_half, p.out_ld);
       }
-    };
-    if (p.splits > 1)
-      leave(0.0f, static_cast<float*>(p.out) + part * p.nj * p.ni, p.ni);
-    else
-      leave(T(0.0f), static_cast<T*>(p.out) + long(image) * p.out_image + long(which) * p.out_half, p.out_ld);
-  }
-  }
-  if (!another) break;
-  if (late) {
-    __syncthreads();
-    last = begin(w);
-  }
+    }
+    if (!another) break;
+    if (late) {
+      __syncthreads();
+      last = begin(w);
+    }
   }
 }
 
