@@ -552,6 +552,17 @@ struct UnitNeeds {
           for (int q = 0; q < kPieces; ++q) dh[y * kPieces + q] = load<T, V>(from + long(j + 16 * y) * p.dh_ld + at(q));
     }
   }
+  // The biases from LDS, gate's and up's of a tile's `n` rows or columns, of which the lane's
+  // first is number `first`.
+  __device__ __forceinline__ void take(unsigned lds, int n, int first) {
+    typedef __attribute__((address_space(3))) const Bias lds_bias;
+#pragma unroll
+    for (int k = 0; k < kBiases; ++k) {
+      const unsigned from = lds + unsigned(first + (PAIR == 1 ? at(k) : 16 * k)) * unsigned(sizeof(T));
+      gate_bias[k] = *reinterpret_cast<lds_bias*>(from);
+      up_bias[k] = *reinterpret_cast<lds_bias*>(from + n * unsigned(sizeof(T)));
+    }
+  }
   // All of it is here: the compiler's waits for it come before this, not among what follows.
   __device__ __forceinline__ void arrive() {
 #pragma unroll
@@ -821,7 +832,11 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   // Stores that a wave inside of i and j ends a tile with: they are younger than the loads
   // of the next tile's first steps, which therefore need not wait for them.
   constexpr int kStores = MI * MJ * 4 / kVec * (BACK ? 2 : 1);
-  constexpr bool kEarly = PAIR != 0 && TI * TJ <= 128 * 128;  // registers for the unit's needs while it multiplies
+  // The unit's needs are asked for while it multiplies. Large tiles have no registers for
+  // them: a thread asks for one bias, and they meet in LDS behind the stages.
+  constexpr bool kEarly = PAIR != 0 && TI * TJ <= 128 * 128, kShared = PAIR != 0 && !kEarly;
+  constexpr int kOwn = PAIR == 2 ? FJ : FI;  // biases of gate's or up's that a tile needs
+  static_assert(!kShared || (!BACK && 2 * kOwn <= 64 * WAVES), "");
   bool stored = false;
   for (;;) {
     const ProductParams& p = again(args);
@@ -843,6 +858,14 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     auto fetch = [&](const ProductParams& p, int lane) {
       if constexpr (PAIR != 0)
         needs.fetch(p, w.image, w.ti * FI + wi * RI + lane / 16 * kVec, w.tj * FJ + wj * 16 * MJ + lane % 16);
+    };
+    T bias{};
+    auto fetch_shared = [&](const ProductParams& p) {
+      if constexpr (kShared) {
+        const int t = threadIdx.x, k = (PAIR == 2 ? w.tj * FJ : w.ti * FI) + t % kOwn;
+        const T* from = static_cast<const T*>(t < kOwn ? p.gate_bias : p.up_bias);
+        if (from && t < 2 * kOwn && k < (PAIR == 2 ? p.nj : p.ni)) bias = from[k];
+      }
     };
     auto landed = [&]() {
       if (stored)
@@ -866,6 +889,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
         else
           wait_for_loads();
         if (n == first && kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
+        if (n == first) fetch_shared(p);
         if (ragged && (n == first ? last : k0 == 0)) cut(stage, left);
         if (n > first && n + 1 < end) load(p, stage ^ 1);
         const unsigned ta = lds + stage * kStage, tb = ta + TI * kStepBytes;
@@ -940,6 +964,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
       if (first < end) {
         landed();
         if (kEarly && w.ti * FI + wi * RI + RI <= p.ni) fetch(p, lane);
+        fetch_shared(p);
         if (ragged && last) cut(0, left);
         const auto ba = at_a.base(lds, 0);
         const auto bb = at_b.base(lds + TI * kStepBytes, 0);
@@ -989,21 +1014,21 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
       const long part = PAIR == 1   ? (long(image) * tiles_j + w.tj) * WJ + wj
                         : PAIR == 2 ? (long(image) * tiles_i + w.ti) * WI + wi
                                     : (long(w.split) * p.halves + which) * p.images + image;
+      if constexpr (kShared)
+        if (threadIdx.x < 2 * kOwn)
+          *reinterpret_cast<__attribute__((address_space(3))) T*>(lds + 2 * kStage + threadIdx.x * sizeof(T)) = bias;
       __syncthreads();
       number += gridDim.x;
       another = number < unsigned(p.tiles);
-      // (where LDS is not needed any more, and registers last)
-      const bool early = (PAIR == 0 || kEarly) && i0 + FI <= p.ni;
+      const bool early = i0 + FI <= p.ni;  // where the stages are not needed any more
       late = another && !early;
       stored = another && early && inside && jw + 16 * MJ <= p.nj;
-      if constexpr (PAIR != 0) {
-        if (inside) {
-          if (!kEarly || first >= end) fetch(p, lane);
-          needs.arrive();
-        }
+      if constexpr (kEarly) {
+        if (inside) needs.arrive();
       }
       if (another) w = place(number);
       if (another && early) last = begin(w);
+      if constexpr (kShared) needs.take(lds + 2 * kStage, kOwn, PAIR == 2 ? wj * 16 * MJ + row : wi * RI + quad * kVec);
       const unsigned slab = lds + wave * kSlab;
       if constexpr (PAIR != 0) {
         if (inside) {
@@ -1098,7 +1123,8 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
 template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK>
 hipError_t launch(const ProductParams& p, hipStream_t s) {
   constexpr int FI = PAIR == 1 ? TI / 2 : TI, FJ = PAIR == 2 ? TJ / 2 : TJ;
-  constexpr size_t lds = 2 * size_t(TI + TJ) * kStepBytes;
+  // (the biases of large tiles' units)
+  constexpr size_t lds = 2 * size_t(TI + TJ) * kStepBytes + (PAIR && TI * TJ > 128 * 128 ? TI * sizeof(T) : 0);
   const long tiles_i = (p.ni + FI - 1) / FI, plane = tiles_i * ((p.nj + FJ - 1) / FJ) * p.halves;
   const long tiles = plane * p.images * p.splits;
   if (tiles >= 1l << 31) return hipErrorInvalidValue;  // refused before
