@@ -35,15 +35,16 @@ struct ProductChoice {
 // (the wait for a tile's first operands, its results, and its steps), and the parts' way
 // through memory. Large tiles read least, but take longest alone, and their last round may
 // be nearly empty. Measured, us by side 64, 128, 256 (bfloat16 unit forward): 512 positions 512 ->
-// 2048 9.5, 10.5, 21.8; 2048 positions 1024 -> 4096 67, 40, 40; 16 images of 64 x 64 planes,
-// 256 -> 512 95, 58, 50. (A unit has to have its whole sums: it is not cut. In the backward pass
+// 2048 9.5, 10.5, 21.8; 2048 positions 1024 -> 4096 65, 37, 34; 16 images of 64 x 64 planes,
+// 256 -> 512 93, 58, 48. (A unit has to have its whole sums: it is not cut. In the backward pass
 // it has no tile of 256: its registers do not hold what it needs besides the sums.)
 inline ProductChoice product_choice(int size, ProductKind kind, long ni, long nj, long images, long halves, long K,
                                     long segs) {
   // ns of a step: of a tile that has a compute unit to itself, and at the full rate
   static constexpr double alone[2][3] = {{400, 500, 1000}, {1100, 2100, 4400}};
   static constexpr double full[2][3] = {{200, 450, 1600}, {660, 1830, 5600}};
-  static constexpr double around[] = {3000, 3000, 6000};  // a tile's steps
+  // around a tile's steps; small tiles' results in planes, many short pieces, take longer
+  const double planes = kind == kUnitPlanes ? 1500 : 0, around[] = {3000 + planes, 3000 + planes, 6000};
   const bool again = kind == kUnitLastAgain || kind == kUnitPlanesAgain, pair = pair_on_i(kind) || pair_on_j(kind);
   const long step = 128 / size, steps = (K + step - 1) / step * segs;
   const long most = pair ? 1 : std::max(1l, std::min(steps / 3, long(kMostSplits)));
