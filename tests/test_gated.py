@@ -188,6 +188,81 @@ def test_sizes(gpu_lib, layout, shape, F, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,F", [((12, 1001, 40, 41), 770), ((2, 2045, 19, 27), 4091)])
+def test_large_tiles(gpu_lib, shape, F, layout, dtype):
+    """Sizes that are multiples of nothing at which each product takes its largest tiles: h
+    and dx at some positions, the weights' and biases' gradients of some hidden channels,
+    which need nothing of the others."""
+    x, dh, gw, uw, gb, ub = make(shape, F, layout, dtype, seed=31)
+    B, C, H, W = shape
+    h, gate, up = binding.gated_forward(x, gw, uw, gb, ub)
+    dx, dgw, duw, dgb, dub = binding.gated_backward(dh, x, gw, uw, gate, up)
+    T = B * H * W
+    rng = np.random.default_rng(1)
+    some = np.unique(np.concatenate([rng.integers(0, T, 40), [0, 1, T - 2, T - 1]]))
+
+    def rows(t):
+        return t.movedim(1, -1).reshape(T, -1)[torch.from_numpy(some).to(DEV)].contiguous()
+
+    b = Bounds(wide(rows(x)), *map(wide, (gw, uw, gb, ub)), "silu", dtype, wide(rows(dh)))
+    near(rows(h), b.h, b.h_off, dtype, "h", C)
+    near(rows(dx), b.grads[0], b.offs[0], dtype, "dx", 2 * F)
+    few = torch.tensor([0, 1, 63, 64, 255, 256, F - 2, F - 1], device=DEV)
+    b = Bounds(wide(x), *(wide(t[few]) for t in (gw, uw, gb, ub)), "silu", dtype, wide(dh[:, few]))
+    for name, got, ref, off in zip(NAMES[1:], (dgw, duw, dgb, dub), b.grads[1:], b.offs[1:]):
+        near(got[few], ref, off, dtype, name, T)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,F", [((3, 40, 9, 8), 56), ((2, 70, 31, 5), 150), ((1, 260, 21, 1), 131)])
+def test_stored_or_made_again(gpu_lib, shape, F, layout, dtype):
+    """Both ways of the backward pass, whichever is the faster: g and u that the forward
+    pass stored, and made again."""
+    x, dh, gw, uw, gb, ub = make(shape, F, layout, dtype, seed=33)
+    B, C, H, W = shape
+    last = layout == "last"
+    d = desc(B=B, C=C, F=F, S=H * W, layout=int(last), dtype=binding._dtype_codes()[dtype])
+    stream = torch.cuda.current_stream().cuda_stream
+    ws = [torch.empty(max(1, binding.oaa_gated_workspace_bytes(d, back, 0)), dtype=torch.uint8, device=DEV)
+          for back in (0, 1)]
+    h = torch.empty_like(dh)
+    kept = [torch.full(dh.shape, float("nan"), device=DEV) for _ in range(2)]
+    weights = [t.data_ptr() for t in (gw, uw, gb, ub)]
+    binding.oaa_gated_forward(d, x.data_ptr(), *weights, h.data_ptr(), *(t.data_ptr() for t in kept),
+                              ws[0].data_ptr(), ws[0].numel(), stream)
+    assert torch.equal(h, binding.gated_forward(x, gw, uw, gb, ub, keep=False)[0])
+    b = Bounds(wide(x), *map(wide, (gw, uw, gb, ub)), "silu", dtype, wide(dh))
+    for addresses in ([t.data_ptr() for t in kept], [None, None]):
+        grads = [torch.empty_like(t) for t in (x, gw, uw, gb, ub)]
+        binding.oaa_gated_backward(d, dh.data_ptr(), x.data_ptr(), *weights, *addresses, *(t.data_ptr() for t in grads),
+                                   ws[1].data_ptr(), ws[1].numel(), stream)
+        terms = (2 * F, *[x.numel() // C] * 4)
+        for name, got, ref, off, n in zip(NAMES, grads, b.grads, b.offs, terms):
+            near(got, ref, off, dtype, name, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,F", [((150, 300), 260), ((2, 40, 31, 5), 66), ((9, 100), 130)])
+@pytest.mark.parametrize("k", [-55, 60])
+def test_range_of_float32(gpu_lib, shape, F, k):
+    """x times 2^k and the weights over 2^k give the same g and u, and gradients that
+    differ by those factors: scaling by a power of two rounds nowhere."""
+    x, dh, gw, uw, gb, ub = make(shape, F, dtype=torch.float32, seed=35)
+    ref = binding.gated_forward(x, gw, uw, gb, ub)
+    grads = binding.gated_backward(dh, x, gw, uw, *ref[1:])
+    s = 2.0 ** k
+    far = binding.gated_forward(x * s, gw / s, uw / s, gb, ub)
+    assert all(torch.equal(a, b) for a, b in zip(ref, far))
+    for got, want, scale in zip(binding.gated_backward(dh, x * s, gw / s, uw / s, *far[1:]), grads,
+                                (1 / s, s, s, 1.0, 1.0)):
+        assert torch.equal(got, want * scale)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
 @pytest.mark.parametrize("view", ["channels", "channels last", "rows last", "images", "one image many times",
                                   "one position many times", "odd address", "odd address last"])
