@@ -19,7 +19,9 @@ __device__ __forceinline__ float kept(const DropoutParams& p, unsigned word, flo
 }
 
 // Dense tensors of n elements: V neighbours a thread, loaded before their words
-// are made.
+// are made, which takes less time than the loads do. Bound by memory: float32 without a
+// residual, 105 million values 133 us (6.3 TB/s); bfloat16 with a float32 one, 195 million 350
+// us (5.6), and the gradient 195 us (6.0); 3136 values 2.5 us.
 template <typename TX, typename TY, int V>
 __global__ void __launch_bounds__(kThreads) dense_kernel(DropoutParams p, long n) {
   const long at = (long(blockIdx.x) * kThreads + threadIdx.x) * V;
