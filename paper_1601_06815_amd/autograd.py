@@ -215,6 +215,7 @@ def gated(x, gate_weight, up_weight, gate_bias=None, up_bias=None, activation="s
     x[B, C, ...] at each position: [B, F, ...] for weights [F, C], in x's layout.
     Tokens are x[T, C]. float32, bfloat16 or float16, all of one type."""
     gate_weight, up_weight = _rows(gate_weight), _rows(up_weight)
+    gate_bias, up_bias = (b if b is None or b.is_contiguous() else b.contiguous() for b in (gate_bias, up_bias))
     if _recorded(x, gate_weight, up_weight, gate_bias, up_bias):
         return GatedFunction.apply(x, gate_weight, up_weight, gate_bias, up_bias, activation)
     return binding.gated_forward(_laid_out(x), gate_weight, up_weight, gate_bias, up_bias, activation, keep=False)[0]
@@ -248,7 +249,8 @@ class DropoutFunction(torch.autograd.Function):
         x = _laid_out(x)
         ctx.layout = _layout(x.shape, x.stride())
         ctx.p, ctx.dtype = p, x.dtype
-        ctx.save_for_backward(seed)
+        # (without a mask any seed will do, and one that a layer advances would be found changed)
+        ctx.save_for_backward(seed if p > 0.0 else seed.clone())
         return binding.dropout(x, p, seed, None if residual is None else _laid_out(residual, ctx.layout))
 
     @staticmethod
@@ -280,7 +282,8 @@ class Dropout(torch.nn.Module):
     calls) is a buffer on the device that every call advances there, so that a
     captured graph draws another mask at each replay. A call that is made again for the
     backward pass, as by torch.utils.checkpoint, draws another one too: there, draw the
-    seed once (``binding.dropout_next(state)``) and call ``dropout`` with it."""
+    seed once (``binding.dropout_next(state)``) and call ``dropout`` with it. Copies of a
+    layer have its key and draw the same masks."""
 
     def __init__(self, p=0.5, seed=None, device="cuda"):
         super().__init__()

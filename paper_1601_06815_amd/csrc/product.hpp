@@ -150,7 +150,7 @@ __device__ __forceinline__ int key_of(int r) {
     return (r >> 2 & 3) << 2;
 }
 
-// The same, but for the last N memory operations of this wave.
+// As wait_for_loads(), but not for the last N memory operations of this wave.
 template <int N>
 __device__ __forceinline__ void wait_but_for() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");

@@ -244,6 +244,19 @@ def test_seed_that_changed(gpu_lib):
 
 
 @pytest.mark.gpu
+def test_layer_between_modes(gpu_lib):
+    """The gradient of a call in evaluation mode, after the layer has trained on."""
+    layer = autograd.Dropout(0.5, seed=3, device=DEV).eval()
+    x, r = (make((4, 6), seed=n).requires_grad_() for n in (1, 2))
+    y = layer(x, r)
+    layer.train()
+    layer(x.detach())
+    dy = make((4, 6), seed=5)
+    dx, dr = torch.autograd.grad(y, (x, r), dy)
+    assert torch.equal(dx, dy) and torch.equal(dr, dy) and torch.equal(y, x + r)
+
+
+@pytest.mark.gpu
 def test_forward_mode_is_refused(gpu_lib):
     x = make((3, 50), seed=19)
     with forward_ad.dual_level():

@@ -493,6 +493,26 @@ def test_saved_tensors_elsewhere(gpu_lib, layout, how):
 
 
 @pytest.mark.gpu
+def test_biases_of_any_strides(gpu_lib):
+    """Columns of a matrix, and one value for all channels: with their gradients."""
+    x, dh, gw, uw, gb, ub = make((70, 12), 40, seed=17)
+    both = torch.stack((gb, ub), 1).requires_grad_()
+    one = torch.full((1,), 0.25, device=DEV, requires_grad=True)
+    h = autograd.gated(x, gw, uw, both[:, 0], both[:, 1])
+    assert torch.equal(h, autograd.gated(x, gw, uw, gb, ub))
+    (grad,) = torch.autograd.grad(h, both, dh)
+    ref = binding.gated_backward(dh, x, gw, uw, *binding.gated_forward(x, gw, uw, gb, ub)[1:])[3:]
+    assert torch.equal(grad, torch.stack(ref, 1))
+    full = one.detach().repeat(40)
+    h = autograd.gated(x, gw, uw, one.expand(40), ub)
+    assert torch.equal(h, autograd.gated(x, gw, uw, full, ub))
+    (grad,) = torch.autograd.grad(h, one, dh)
+    ref = binding.gated_backward(dh, x, gw, uw, *binding.gated_forward(x, gw, uw, full, ub)[1:])[3]
+    # torch adds the 40 values up in float32
+    torch.testing.assert_close(grad[0].double(), ref.double().sum(), rtol=0, atol=40 * E * float(ref.abs().sum()))
+
+
+@pytest.mark.gpu
 def test_writes_are_seen(gpu_lib):
     """A saved tensor that changed before the backward pass is an error, not a wrong
     gradient; writing through h is announced."""
