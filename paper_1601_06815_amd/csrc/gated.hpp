@@ -38,9 +38,9 @@ struct ProductParams {
   int images, halves;
   int K, segs;
   int splits;  // the sum's steps are cut into so many parts
-  // the launcher's own: tiles in all, steps of a part of the sum, and 2^32 over the tiles of
-  // an image and over those of a group
-  int tiles, split_steps;
+  // the launcher's own: tiles in all, steps of a part of the sum, tiles that a workgroup takes
+  // one beside the other (or 0), and 2^32 over the tiles of an image and over those of a group
+  int tiles, split_steps, run;
   unsigned plane_reciprocal, group_reciprocal;
   // D: element strides; partial sums in 32 bits if splits > 1, dense [split][half][image][nj][ni]
   void* out;

@@ -22,9 +22,10 @@
 //   float32, 32 planes of 113 x 113, 256 -> 512: six matrix instructions a product, busy 36 to
 //   58 %; unit with g and u stored 1.75 ms, dx 1.26 (170 TFLOP/s), dW 1.15 (186).
 //   bfloat16, 128 planes of 54 x 54, 128 -> 512: two steps a tile, so what is around them: a
-//   tile of 256 waits for its operands (4200 cycles), multiplies (6600), asks for the next
-//   one's (3500) and turns sums into h (7400), of 23800; unit 0.30 ms, made again with dg and
-//   du 0.48 (2.6 TB/s), dx 0.23 and dW 0.24 (3.8 and 3.6 TB/s).
+//   tile of 256 that loads both operands waits for them (4200 cycles), multiplies (6600), asks
+//   for the next one's (3500) and turns sums into h (7400), of 23800; unit 0.28 ms (0.31 if
+//   every tile does), made again with dg and du 0.48 (2.6 TB/s), dx 0.23 and dW 0.24 (3.8 and
+//   3.6 TB/s).
 // Transposing reads meet in pairs in the banks (40 to 50 % of LDS's cycles). Rows and keys
 // that avoid it, with the sums exchanged between lanes' registers at the end, brought no time
 // (dx 1.00 and 1.04 ms, dW 0.93 and 1.01): LDS is busy for half of the cycles only.
@@ -749,8 +750,13 @@ __device__ __forceinline__ int lane_again() {
   return t & 63;
 }
 
-// PAIR: 0 none, 1 on i, 2 on j. BACK: the unit in the backward pass.
-template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK>
+// Whether a workgroup may take tiles beside each other.
+template <typename T, int PAIR, bool BACK>
+constexpr bool kRuns = PAIR != 0 && !BACK && sizeof(T) == 2;
+
+// PAIR: 0 none, 1 on i, 2 on j. BACK: the unit in the backward pass. RUN: a workgroup takes
+// p.run tiles beside each other.
+template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK, bool RUN>
 __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 ? 1 : 2) kernel(ProductParams args) {
   constexpr int WAVES = WI * WJ, GI = TI / WI, GJ = TJ / WJ;  // a wave's part of the tile
   constexpr int NI = GI / 16, NJ = GJ / 16;
@@ -772,7 +778,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     const int total = (p.K + kStep<T> - 1) / kStep<T> * p.segs;
     Place w;
     const int plane = tiles_i * all_j;
-    int t = xcd_order(number, p.tiles), rest = divide(t, plane, p.plane_reciprocal);
+    int t = RUN ? int(number) : xcd_order(number, p.tiles), rest = divide(t, plane, p.plane_reciprocal);
     t -= rest * plane;
     w.split = 0;
     w.first = 0;
@@ -807,15 +813,17 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     a.go(s, k0);
     b.go(s, k0);
   };
-  auto load = [&](const ProductParams& p, int stage) {
+  auto load = [&](const ProductParams& p, int stage, bool with_a = true) {
+    if (with_a)
 #pragma unroll
-    for (int m = 0; m < a.kMine; ++m) a.piece(lds + stage * kStage, k0, p.K, m, wave);
+      for (int m = 0; m < a.kMine; ++m) a.piece(lds + stage * kStage, k0, p.K, m, wave);
 #pragma unroll
     for (int m = 0; m < b.kMine; ++m) b.piece(lds + stage * kStage + TI * kStepBytes, k0, p.K, m, wave);
     advance(p.K);
   };
-  // The first two steps of a tile to LDS; whether the first is a segment's last.
-  auto begin = [&](const Place& w) {
+  // The first two steps of a tile to LDS; whether the first is a segment's last. with_a: or i's
+  // operand is there already.
+  auto begin = [&](const Place& w, bool with_a) {
     const ProductParams& p = again(args);
     const int lane = lane_again(), steps = (p.K + kStep<T> - 1) / kStep<T>;
     s = w.first ? w.first / steps : 0;
@@ -825,9 +833,9 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     a.start(s, k0);
     b.start(s, k0);
     if (w.first >= w.end) return false;
-    load(p, 0);
+    load(p, 0, with_a);
     const bool last = k0 == 0;
-    if (w.first + 1 < w.end) load(p, 1);
+    if (w.first + 1 < w.end) load(p, 1, with_a);
     return last;
   };
   // The last values of a segment, once they have landed.
@@ -839,9 +847,19 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
 
   // A workgroup takes one tile after the other. The first steps of the next are asked for
   // before the results of this one leave.
-  unsigned number = blockIdx.x;
+  // Where a sum is no longer than the two stages, these are tiles beside each other, and i's
+  // operand stays for those of the same rows (bfloat16, 128 images of 54 x 54, 128 -> 512, us:
+  // channels last 271 and 213, planes 297 and 268; but made again in the backward pass, in
+  // planes, 455 and 540: pieces of d's rows that meet in a line are then written at other
+  // times; float32 49 and 52).
+  unsigned number = blockIdx.x, stop = args.tiles;
+  if constexpr (RUN) {
+    number = unsigned(xcd_order(blockIdx.x, gridDim.x)) * args.run;
+    stop = min(number + args.run, stop);
+    if (number >= stop) return;
+  }
   Place w = place(number);
-  bool last = begin(w), another, late;
+  bool last = begin(w, true), another, late;
   constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ, RI = 16 * MI;
   constexpr int kVec = 16 / int(sizeof(T));
   // Stores that a wave inside of i and j ends a tile with: they are younger than the loads
@@ -1033,8 +1051,8 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
         if (threadIdx.x < 2 * kOwn)
           *reinterpret_cast<__attribute__((address_space(3))) T*>(lds + 2 * kStage + threadIdx.x * sizeof(T)) = bias;
       __syncthreads();
-      number += gridDim.x;
-      another = number < unsigned(p.tiles);
+      number += RUN ? 1 : gridDim.x;
+      another = number < stop;
       const bool early = i0 + FI <= p.ni;  // where the stages are not needed any more
       late = another && !early;
       stored = another && early && inside && jw + 16 * MJ <= p.nj;
@@ -1042,7 +1060,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
         if (inside) needs.arrive();
       }
       if (another) w = place(number);
-      if (another && early) last = begin(w);
+      if (another && early) last = begin(w, !RUN || w.image != image || w.ti * FI != i0);
       if constexpr (kShared) needs.take(lds + 2 * kStage, kOwn, PAIR == 2 ? wj * 16 * MJ + row : wi * RI + quad * kVec);
       const unsigned slab = lds + wave * kSlab;
       if constexpr (PAIR != 0) {
@@ -1130,7 +1148,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     if (!another) break;
     if (late) {
       __syncthreads();
-      last = begin(w);
+      last = begin(w, true);
     }
   }
 }
@@ -1143,20 +1161,26 @@ hipError_t launch(const ProductParams& p, hipStream_t s) {
   const long tiles_i = (p.ni + FI - 1) / FI, plane = tiles_i * ((p.nj + FJ - 1) / FJ) * p.halves;
   const long tiles = plane * p.images * p.splits;
   if (tiles >= 1l << 31) return hipErrorInvalidValue;  // refused before
-  auto kern = kernel<T, TI, TJ, WI, WJ, IK, JK, PAIR, BACK>;
+  // as many workgroups as the device holds: a multiple of its dies
+  const long steps = long((p.K + kStep<T> - 1) / kStep<T>) * p.segs;
+  const long blocks = std::min(tiles, long(kTilesAtOnce[TI / 128]));
+  auto kern = kernel<T, TI, TJ, WI, WJ, IK, JK, PAIR, BACK, false>;
+  bool beside = false;
+  if constexpr (kRuns<T, PAIR, BACK>) {
+    beside = steps <= 2 && tiles > blocks;
+    if (beside) kern = kernel<T, TI, TJ, WI, WJ, IK, JK, PAIR, BACK, true>;
+  }
   if (lds > 65536) {
     const hipError_t e = tile::allow_lds(kern, lds);
     if (e != hipSuccess) return e;
   }
   ProductParams q = p;
-  const long steps = long((p.K + kStep<T> - 1) / kStep<T>) * p.segs;
   q.tiles = int(tiles);
   q.split_steps = int((steps + p.splits - 1) / p.splits);
   q.plane_reciprocal = unsigned(std::min((1ll << 32) / plane, (1ll << 32) - 1));
   q.group_reciprocal = unsigned((1ll << 32) / (kGroup * tiles_i));
-  // as many workgroups as the device holds: a multiple of its dies
-  const long most = kTilesAtOnce[TI / 128];
-  hipLaunchKernelGGL(kern, dim3(unsigned(std::min(tiles, most))), dim3(64 * WI * WJ), lds, s, q);
+  q.run = beside ? int((tiles + blocks - 1) / blocks) : 0;
+  hipLaunchKernelGGL(kern, dim3(unsigned(blocks)), dim3(64 * WI * WJ), lds, s, q);
   return hipGetLastError();
 }
 
