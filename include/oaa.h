@@ -425,7 +425,9 @@ oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out
 typedef struct {
   int B, C, F;      /* images, channels of x, channels of h: B >= 0, C, F >= 1 (up to 2^20) */
   long long S;      /* positions per image, >= 0 (in planes below 2^21); at most 2^24 squares
-                       of 32 positions by 32 of max(C, 2 F) channels in all   */
+                       of 32 positions by 32 of max(C, 2 F) channels in all, where images
+                       count one by one unless positions follow each other evenly through
+                       them in all that a pass reads and writes               */
   int layout;       /* oaa_layout_t of x, h, dh and dx                        */
   int dtype;        /* oaa_dtype_t of every tensor but gate and up            */
   int activation;   /* oaa_activation_t                                       */

@@ -26,7 +26,7 @@ using oaa::Strided;
 constexpr long long kMostChannels = 1 << 20;   // C, F: offsets within a tile stay below 2^31
 constexpr long long kMostPlane = (1 << 21) - 1;  // S in planes: the same
 constexpr long long kMostPositions = 0x7fffffffll;
-constexpr long long kMostTiles = 1 << 24;      // a launch has fewer than 2^32 threads
+constexpr long long kMostTiles = 1 << 24;      // tiles are counted in an int, parts of sums besides
 constexpr long kTileOffset = 256;              // rows of a tile
 constexpr long kPartRows = 64;                 // rows summed at least by one workgroup, last
 constexpr long kMostParts = 1024;
@@ -91,7 +91,8 @@ oaa_status_t describe(const oaa_gated_t* d, Unit* u) {
 
 bool empty(const Unit& u) { return u.B == 0 || u.S == 0; }
 
-// The unit with its positions in one image where x, and `other` two tensors, allow.
+// The unit with its positions in one image where the strides of all tensors that the pass
+// reads or writes allow.
 Unit collapsed(Unit u, bool backward) {
   if (!u.last || u.B <= 1) return u;
   auto even = [&](long image, long row) { return u.S == 1 || image == u.S * row; };
@@ -320,21 +321,21 @@ ProductParams unit_product(const Layout& l, const void* gate_bias, const void* u
   return p;
 }
 
-// Whether every product has few enough tiles of 32 x 32, less than any uses; images
-// count as such (positions of several images may not follow each other evenly).
-oaa_status_t fits(const Unit& u) {
+// Whether every product has few enough tiles of 32 x 32, less than any uses, as the pass
+// runs: images that stay apart count one by one.
+oaa_status_t fits(const Unit& u, bool backward) {
   auto tiles = [](long long a, long long b) { return ((a + 31) / 32) * ((b + 31) / 32); };
-  const long long wide = std::max(2 * u.F, u.C);
-  if (u.B * tiles(u.S, wide) > kMostTiles && (!u.last || tiles((long long)u.B * u.S, wide) > kMostTiles || u.S > 1))
+  const Unit run = collapsed(u, backward);
+  if (run.B * tiles(run.S, std::max(2 * u.F, u.C)) > kMostTiles)
     return fail(OAA_ERR_UNSUPPORTED, "too large (B=%d C=%d F=%d S=%ld)", u.B, u.C, u.F, u.S);
   if (tiles(2 * u.F, u.C) > kMostTiles)
     return fail(OAA_ERR_UNSUPPORTED, "too many weights (C=%d F=%d)", u.C, u.F);
   return OAA_OK;
 }
 
-oaa_status_t check_size(const oaa_gated_t* d, Unit* u) {
+oaa_status_t check_size(const oaa_gated_t* d, bool backward, Unit* u) {
   if (oaa_status_t st = describe(d, u)) return st;
-  return empty(*u) ? OAA_OK : fits(*u);
+  return empty(*u) ? OAA_OK : fits(*u, backward);
 }
 
 // Memory of one tensor.
@@ -404,7 +405,7 @@ extern "C" {
 
 size_t oaa_gated_workspace_bytes(const oaa_gated_t* d, int backward, int any_address) {
   Unit u;
-  if (check_size(d, &u) || empty(u)) return 0;
+  if (check_size(d, backward != 0, &u) || empty(u)) return 0;
   // addresses as far from what a product reads in place as the type allows
   char* const none = nullptr;
   const void* at = any_address && u.size == 2 ? none + 2 : none;
@@ -415,14 +416,14 @@ size_t oaa_gated_workspace_bytes(const oaa_gated_t* d, int backward, int any_add
 
 int oaa_gated_keeps(const oaa_gated_t* d) {
   Unit u;
-  return !check_size(d, &u) && !oaa::product_remakes(int(u.size), u.C);
+  return !check_size(d, false, &u) && !oaa::product_remakes(int(u.size), u.C);
 }
 
 oaa_status_t oaa_gated_forward(const oaa_gated_t* d, const void* x, const void* gate_weight, const void* up_weight,
                                const void* gate_bias, const void* up_bias, void* h, float* gate, float* up,
                                void* ws, size_t ws_bytes, void* stream) {
   Unit whole_unit;
-  if (oaa_status_t st = check_size(d, &whole_unit)) return st;
+  if (oaa_status_t st = check_size(d, false, &whole_unit)) return st;
   if (empty(whole_unit)) return OAA_OK;
   const Unit& w = whole_unit;
   const Pointer pointers[] = {{x, true, w.dtype, "x"}, {gate_weight, true, w.dtype, "gate_weight"},
@@ -466,7 +467,7 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
                                 const float* up, void* dx, void* dgate_weight, void* dup_weight, void* dgate_bias,
                                 void* dup_bias, void* ws, size_t ws_bytes, void* stream) {
   Unit whole_unit;
-  if (oaa_status_t st = check_size(d, &whole_unit)) return st;
+  if (oaa_status_t st = check_size(d, true, &whole_unit)) return st;
   const Unit& w = whole_unit;
   if (!dx && !dgate_weight && !dup_weight && !dgate_bias && !dup_bias)
     return fail(OAA_ERR_INVALID_ARG, "all five gradients are NULL");

@@ -610,6 +610,26 @@ def test_graph_replays(gpu_lib, shape, F, dtype):
 
 
 @pytest.mark.gpu
+def test_many_small_images(gpu_lib):
+    """More images than the limit of squares would allow one by one: the bits of their
+    positions as tokens."""
+    gen = torch.Generator(device=DEV).manual_seed(39)
+    x, dh = (torch.randn((1 << 18, 2, n), generator=gen, device=DEV, dtype=torch.bfloat16).movedim(-1, 1)
+             for n in (64, 2048))
+    params = make((1, 64), 2048, dtype=torch.bfloat16, seed=39)[2:]
+
+    def rows(t):
+        return t.movedim(1, -1).reshape(-1, t.shape[1])
+
+    h, *kept = binding.gated_forward(x, *params)
+    got = (h, *binding.gated_backward(dh, x, *params[:2], *kept))
+    ref, *kept = binding.gated_forward(rows(x), *params)
+    refs = (ref, *binding.gated_backward(rows(dh), rows(x), *params[:2], *kept))
+    for g, r in zip(got, refs):
+        assert torch.equal(rows(g) if g.dim() == 3 else g, r)
+
+
+@pytest.mark.gpu
 def test_offsets_past_32_bits(gpu_lib):
     """h of 2^31 values and more, its last rows against the oracle."""
     T, C, F = (1 << 20) + 3, 16, 2056
@@ -726,6 +746,33 @@ def test_refused_workspaces(lib):
     with pytest.raises(binding.OaaError) as e:
         forward(desc(dtype=2), x=M + 2, ws=None, size=0)
     assert e.value.status == 3
+
+
+def test_size_of_images_that_follow_each_other(lib):
+    """Positions are counted as they run: evenly spaced, those of all images are one's."""
+    sizes = dict(layout=1, dtype=1, C=64, F=2048)
+    many, one = desc(B=1 << 18, S=2, **sizes), desc(B=1, S=1 << 19, **sizes)
+    need = binding.oaa_gated_workspace_bytes(many, True, False)
+    assert need == binding.oaa_gated_workspace_bytes(one, True, False) > 4 * 2048 << 19
+    assert binding.oaa_gated_keeps(many) == binding.oaa_gated_keeps(one)
+    with pytest.raises(binding.OaaError) as e:
+        backward(many, dh=1 << 40, x=1 << 44, dx=1 << 45, gate=None, up=None, ws=None, size=0)
+    assert e.value.status == 3, e.value
+    # 16-bit rows of odd length are copied
+    assert binding.oaa_gated_workspace_bytes(desc(B=1 << 18, S=2, layout=1, dtype=1, C=63, F=2048), False, False) > 64 << 19
+    # gaps between the images of a tensor that the pass reads or writes: each is one
+    gaps = (2 * 2048 + 8, 2048)
+    for change, back, fits in ((dict(x=(136, 64)), False, False), (dict(h=gaps), False, False), (dict(h=gaps), True, True),
+                               (dict(dh=gaps), True, False), (dict(dx=(136, 64)), True, False), (dict(dh=gaps), False, True)):
+        d = desc(B=1 << 18, S=2, **sizes, **change)
+        if back:
+            assert (binding.oaa_gated_workspace_bytes(d, True, False) > 0) == fits
+        with pytest.raises(binding.OaaError) as e:
+            if back:
+                backward(d, dh=1 << 40, x=1 << 44, dx=1 << 45, gate=None, up=None, ws=None, size=0)
+            else:
+                forward(d, x=1 << 40, gw=None, h=1 << 45, gate=None, up=None)
+        assert e.value.status == ((3 if back else 1) if fits else 2), e.value
 
 
 def test_slices_beside_each_other(lib):
