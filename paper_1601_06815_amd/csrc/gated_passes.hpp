@@ -45,7 +45,8 @@ __device__ __forceinline__ void write(T* p, long n, const float (&in)[V]) {
   }
 }
 
-// dg = dh u act'(g) and du = dh act(g) of four neighbours; columns from `n` on are
+// dg = dh (u act'(g)) and du = dh act(g) of four neighbours (dh u may be beyond float32, or
+// infinite times a slope of 0, where dg is not); columns from `n` on are
 // written as 0 up to `room`.
 template <typename T, int ACT>
 __device__ __forceinline__ void slope_of(const SlopeParams& p, const T* dh, long at, long to, long n, long room,
@@ -56,7 +57,7 @@ __device__ __forceinline__ void slope_of(const SlopeParams& p, const T* dh, long
   read<float, 4>(p.up + at, n, u);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    dg[i] = i < n ? d[i] * u[i] * act_slope<ACT>(g[i]) : 0.0f;
+    dg[i] = i < n ? d[i] * (u[i] * act_slope<ACT>(g[i])) : 0.0f;
     du[i] = i < n ? d[i] * act<ACT>(g[i]) : 0.0f;
     sg[i] += dg[i];
     su[i] += du[i];

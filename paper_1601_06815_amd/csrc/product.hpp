@@ -467,7 +467,8 @@ struct UnitEnd {
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const float d = float(w.dh[e]);
-            const float y = d * u[e] * act_slope<ACT>(g[e]), z = d * act<ACT>(g[e]);
+            // (d u may be beyond float32, or infinite times a slope of 0, where y is not)
+            const float y = d * (u[e] * act_slope<ACT>(g[e])), z = d * act<ACT>(g[e]);
             dg[e] = T(y);
             du[e] = T(z);
             if constexpr (PAIR == 1) {
@@ -650,7 +651,7 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float d = element<T, V>(needs.dh[y * kPieces + q], e);
-          const float s = d * u[e] * act_slope<ACT>(g[e]), t = d * act<ACT>(g[e]);
+          const float s = d * (u[e] * act_slope<ACT>(g[e])), t = d * act<ACT>(g[e]);
           set_element<T, V>(dg, e, s);
           set_element<T, V>(du, e, t);
           if constexpr (PAIR == 1) {

@@ -14,6 +14,7 @@ import ctypes
 import numpy as np
 import pytest
 import torch
+from scipy import special
 from torch.autograd import forward_ad
 
 from oracle import block as oracle
@@ -261,6 +262,64 @@ def test_range_of_float32(gpu_lib, shape, F, k):
     for got, want, scale in zip(binding.gated_backward(dh, x * s, gw / s, uw / s, *far[1:]), grads,
                                 (1 / s, s, s, 1.0, 1.0)):
         assert torch.equal(got, want * scale)
+
+
+def both_backwards(x, dh, gw, uw, gb, ub, act, need=(True,) * 5):
+    """The gradients (or None) with g and u stored, and made again: through the C entries."""
+    B, C, S = x.shape[0], x.shape[1], int(np.prod(x.shape[2:]))
+    F, dtype = gw.shape[0], x.dtype
+    last = binding._norm_layout(x, "x")[0]
+    d = desc(B=B, C=C, F=F, S=S, layout=last, dtype=binding._dtype_codes()[dtype], activation=binding.ACTIVATIONS[act])
+    stream = torch.cuda.current_stream().cuda_stream
+    ws = [torch.empty(max(1, binding.oaa_gated_workspace_bytes(d, back, 0)), dtype=torch.uint8, device=DEV)
+          for back in (0, 1)]
+    h, kept = torch.empty_like(dh), [torch.empty_like(dh, dtype=torch.float32) for _ in range(2)]
+    weights = [binding._pointer(t) for t in (gw, uw, gb, ub)]
+    binding.oaa_gated_forward(d, x.data_ptr(), *weights, h.data_ptr(), *(t.data_ptr() for t in kept), ws[0].data_ptr(),
+                              ws[0].numel(), stream)
+    for addresses in ([t.data_ptr() for t in kept], [None, None]):
+        shapes = (x, gw, uw, gw[:, 0], uw[:, 0])
+        grads = [torch.empty_like(t) if n else None for t, n in zip(shapes, need)]
+        binding.oaa_gated_backward(d, dh.data_ptr(), x.data_ptr(), *weights, *addresses, *map(binding._pointer, grads),
+                                   ws[1].data_ptr(), ws[1].numel(), stream)
+        yield grads
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape,F", [((3, 24, 5, 7), 40), ((2, 70, 31, 5), 150)])
+def test_large_gradients_of_small_slopes(gpu_lib, shape, F, layout, dtype, act):
+    """dh u is beyond float32 (1e40) where act'(g) is so small that dg is not, or 0.
+
+    The values are of one sign, so that a sum's bound is relative. g, down to -60, or to -8 for
+    GELU, is off by (C + 8) 2^-23 of itself, 6e-4 at most; act(g) and act'(g) then by as much
+    for SiLU and eight times as much of 8e-5 for GELU; their own errors (below 1e-4 there) and
+    a sum of 2 F + 8 terms add 2e-4: 1e-3 in all. Besides, half a step of dg or du and of the
+    result."""
+    rng = np.random.default_rng(45)
+    B, C = shape[:2]
+    far = 8.0 if act == "gelu" else 60.0
+    x = lay(torch.from_numpy(rng.uniform(0.5, 1.0, shape)).to(DEV, dtype), layout)
+    dh = lay(torch.from_numpy(rng.uniform(0.5, 1.0, (B, F, *shape[2:])) * 1e20).to(DEV, dtype), layout)
+    gw = torch.from_numpy(-far / C * rng.uniform(0.9, 1.0, (F, C))).to(DEV, dtype)
+    uw = torch.from_numpy(1e20 * rng.uniform(0.5, 1.0, (F, C))).to(DEV, dtype)
+    values = [wide(t) for t in (x, gw, uw)]
+    g, u = oracle.gated_preactivations(*values)
+    low = {"relu": 0.0 * g, "silu": np.exp(g) / (1.0 + np.exp(g)), "gelu": special.ndtr(g)}[act]
+    slope = {"relu": 0.0 * g, "silu": low * (1.0 + g * (1.0 - low)),
+             "gelu": low + g * np.exp(-0.5 * g * g) / np.sqrt(2.0 * np.pi)}[act]
+    D, V = oracle._flat(wide(dh)), oracle._flat(values[0])
+    dg, du = D * u * slope, D * g * low
+    dx = dg @ values[1] + du @ values[2]
+    size = np.abs(dg) @ np.abs(values[1]) + np.abs(du) @ np.abs(values[2])  # terms of either sign
+    ref = (oracle._back(dx, wide(x), C), dg.T @ V, du.T @ V, dg.sum(axis=0), du.sum(axis=0))
+    for grads in both_backwards(x, dh, gw, uw, None, None, act):
+        for name, got, r in zip(NAMES, grads, ref):
+            scale = oracle._back(size, wide(x), C) if name == "dx" else np.abs(r)
+            assert np.isfinite(r).all() and np.isfinite(wide(got)).all(), name
+            assert np.all(np.abs(wide(got) - r) <= (1e-3 + 2 * STEP[dtype]) * scale), name
 
 
 @pytest.mark.gpu
