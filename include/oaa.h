@@ -416,7 +416,11 @@ oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out
  * gradients are rounded once. g and u are stored in 32 bits for the backward pass, or it
  * makes them again. dg and du are rounded to the type of x where they enter the products
  * dx and dW: the matrix cores take both operands in one type, and a rounding of each of
- * many terms weighs less than that of the result. float32 values are multiplied as sums of
+ * many terms weighs less than that of the result. In float16 they are rounded times a power
+ * of two, the same for all of a call, where the largest finite magnitude of them is beyond
+ * 65504 or below 2^-4: it becomes 2^14 or more, and dx and dW are divided by it in 32 bits. So
+ * what is small loses digits below 2^-28 of the largest (2^-10 where the largest is between).
+ * float32 values are multiplied as sums of
  * three bfloat16 values, which is exact to float32's rounding for magnitudes from 2^-110
  * (below, digits are lost) to 3.39e38 (above, as infinite). What is not finite at a position
  * of x, or in a weight, makes what the formulas sum over it infinite or NaN (NaN, in float32,

@@ -10,6 +10,7 @@
 
 #include "activation.hpp"
 #include "gated.hpp"
+#include "gated_range.hpp"
 #include "scalar_types.hpp"
 
 namespace oaa {
@@ -50,7 +51,7 @@ __device__ __forceinline__ void write(T* p, long n, const float (&in)[V]) {
 // written as 0 up to `room`.
 template <typename T, int ACT>
 __device__ __forceinline__ void slope_of(const SlopeParams& p, const T* dh, long at, long to, long n, long room,
-                                         float (&sg)[4], float (&su)[4]) {
+                                         float scale, float& most, float (&sg)[4], float (&su)[4]) {
   float d[4], g[4], u[4], dg[4], du[4];
   read<T, 4>(dh, n, d);
   read<float, 4>(p.gate + at, n, g);
@@ -61,6 +62,12 @@ __device__ __forceinline__ void slope_of(const SlopeParams& p, const T* dh, long
     du[i] = i < n ? d[i] * act<ACT>(g[i]) : 0.0f;
     sg[i] += dg[i];
     su[i] += du[i];
+    if constexpr (range::kUsed<T>) {
+      range::note(most, dg[i]);
+      range::note(most, du[i]);
+      dg[i] *= scale;
+      du[i] *= scale;
+    }
   }
   write<T, 4>(static_cast<T*>(p.dgate) + to, room, dg);
   write<T, 4>(static_cast<T*>(p.dup) + to, room, du);
@@ -75,6 +82,12 @@ __global__ void __launch_bounds__(kThreads) slope_last_kernel(SlopeParams p) {
   const long row_blocks = (p.rows + p.part_rows - 1) / p.part_rows;
   const int cl = threadIdx.x & 63, rl = threadIdx.x >> 6;
   __shared__ float part[2][4][256];
+  float scale = 1.0f, most = 0.0f;
+  if constexpr (range::kUsed<T>)
+    if (p.range.again) {
+      scale = range::find<kThreads>(p.range, part[0][0]);
+      if (scale == 1.0f) return;
+    }
   for (long block = blockIdx.x; block < column_blocks * row_blocks * p.images; block += gridDim.x) {
     const long c = block % column_blocks * 256 + 4 * cl, rest = block / column_blocks;
     const long r0 = rest % row_blocks * p.part_rows, image = rest / row_blocks;
@@ -85,7 +98,8 @@ __global__ void __launch_bounds__(kThreads) slope_last_kernel(SlopeParams p) {
 #pragma unroll 2
       for (long r = r0 + rl; r < r1; r += 4) {
         const long line = image * p.rows + r;
-        slope_of<T, ACT>(p, dh + r * p.dh_row, line * p.columns + c, line * p.ld + c, p.columns - c, p.ld - c, sg, su);
+        slope_of<T, ACT>(p, dh + r * p.dh_row, line * p.columns + c, line * p.ld + c, p.columns - c, p.ld - c, scale, most,
+                         sg, su);
       }
     }
     if (!p.sums) continue;
@@ -103,6 +117,8 @@ __global__ void __launch_bounds__(kThreads) slope_last_kernel(SlopeParams p) {
                                                  (part[h][2][threadIdx.x] + part[h][3][threadIdx.x]);
     __syncthreads();
   }
+  if constexpr (range::kUsed<T>)
+    if (p.range.most && !p.range.again) range::leave<kThreads>(p.range, most, part[0][0]);
 }
 
 // Hidden channels as rows: LANES lanes a row of an image. Bound by memory: float32, 32 x 512
@@ -112,6 +128,12 @@ __global__ void __launch_bounds__(kThreads) slope_planes_kernel(SlopeParams p) {
   constexpr int ROWS = kThreads / LANES;
   const int cl = threadIdx.x % LANES, rl = threadIdx.x / LANES;
   __shared__ float part[2][kThreads / 64];
+  float scale = 1.0f, most = 0.0f;
+  if constexpr (range::kUsed<T>)
+    if (p.range.again) {
+      scale = range::find<kThreads>(p.range, part[0]);
+      if (scale == 1.0f) return;
+    }
   const long lines = p.images * p.rows;
   for (long block = blockIdx.x; block < (lines + ROWS - 1) / ROWS; block += gridDim.x) {
     const long line = block * ROWS + rl;
@@ -121,7 +143,8 @@ __global__ void __launch_bounds__(kThreads) slope_planes_kernel(SlopeParams p) {
       const T* dh = static_cast<const T*>(p.dh) + image * p.dh_image + f * p.columns;
 #pragma unroll 2
       for (long c = 4 * cl; c < p.ld; c += 4 * LANES)
-        slope_of<T, ACT>(p, dh + c, line * p.columns + c, line * p.ld + c, p.columns - c, p.ld - c, sg, su);
+        slope_of<T, ACT>(p, dh + c, line * p.columns + c, line * p.ld + c, p.columns - c, p.ld - c, scale, most,
+                         sg, su);
     }
     if (!p.sums) continue;
     float a = (sg[0] + sg[1]) + (sg[2] + sg[3]), b = (su[0] + su[1]) + (su[2] + su[3]);
@@ -146,6 +169,8 @@ __global__ void __launch_bounds__(kThreads) slope_planes_kernel(SlopeParams p) {
       p.sums[(image * 2 + 1) * p.rows + f] = b;
     }
   }
+  if constexpr (range::kUsed<T>)
+    if (p.range.most && !p.range.again) range::leave<kThreads>(p.range, most, part[0]);
 }
 
 // 16 hidden channels of gate's or up's by 64 shares of the parts a workgroup: the parts
@@ -200,6 +225,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(JoinParams p) {
         const long row = at / p.ni, image = row / p.nj;
         at = image * p.image + (row - image * p.nj) * p.ld + (at - row * p.ni);
       }
+      if constexpr (range::kUsed<T>)
+        if (p.undo) a *= *p.undo;
       static_cast<T*>(p.out[which])[at] = T(a);
     }
   }
@@ -239,6 +266,7 @@ hipError_t for_activation(int act, Fn&& f) {
 template <typename T>
 hipError_t launch_slope(const SlopeParams& p, hipStream_t s) {
   using namespace passes;
+  auto blocks_for = [&](long n) { return passes::blocks_for(p.range.most ? std::min(n, kRangeBlocks) : n); };
   return for_activation(p.act, [&](auto a) {
     constexpr int ACT = decltype(a)::value;
     if (p.last) {

@@ -174,6 +174,7 @@ struct Layout {
   void *dgate, *dup;
   long d_ld, d_image;
   float* sums;
+  oaa::Range range;
   long parts, part_rows;
   float* product_parts;
   int dx_splits, dw_splits;
@@ -279,6 +280,10 @@ Layout backward_layout(const Unit& whole_unit, const void* x, const void* gate_w
     else
       l.parts = u.last ? u.B * ((rows + l.part_rows - 1) / l.part_rows) : u.B;
     l.sums = static_cast<float*>(room.take(size_t(l.parts) * 2 * u.F * 4));
+  }
+  if (u.dtype == OAA_FLOAT16 && (need_x || need_w)) {
+    l.range.most = static_cast<float*>(room.take(oaa::kRangeBlocks * 4));
+    l.range.undo = static_cast<float*>(room.take(4));
   }
   const int unit_x = u.last ? kRows : kColumns, dw_x = u.last ? kColumns : kRows;
   if (need_x || remake) place_weights(&l, gate_w, up_w, (need_x ? kColumns : 0) | (remake ? kRows : 0), &room);
@@ -522,6 +527,10 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
   hipError_t e = make_copies(l, x, gate_weight, up_weight, s);
   if (e != hipSuccess) return hip_status(e, "gated unit, copies");
   const long dh_row = u.last ? u.dh_row : u.S;
+  auto twice = [&](auto&& launch) {
+    const hipError_t first = launch(false);
+    return first != hipSuccess || !l.range.most ? first : launch(true);
+  };
   if (remake) {
     ProductParams p = unit_product(l, gate_bias, up_bias);
     p.dh = dh;
@@ -532,8 +541,12 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
     p.d_image = l.d_image;
     p.d_ld = l.d_ld;
     p.sums = l.sums;
-    e = for_type(u.dtype, [&](auto t) {
-      return oaa::launch_product<decltype(t)>(p, u.last ? oaa::kUnitLastAgain : oaa::kUnitPlanesAgain, s);
+    p.range = l.range;
+    e = twice([&](bool again) {
+      p.range.again = again;
+      return for_type(u.dtype, [&](auto t) {
+        return oaa::launch_product<decltype(t)>(p, u.last ? oaa::kUnitLastAgain : oaa::kUnitPlanesAgain, s);
+      });
     });
   } else {
     oaa::SlopeParams slope{};
@@ -552,7 +565,11 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
     slope.last = u.last;
     slope.sums = l.sums;
     slope.part_rows = l.part_rows;
-    e = for_type(u.dtype, [&](auto t) { return oaa::launch_slope<decltype(t)>(slope, s); });
+    slope.range = l.range;
+    e = twice([&](bool again) {
+      slope.range.again = again;
+      return for_type(u.dtype, [&](auto t) { return oaa::launch_slope<decltype(t)>(slope, s); });
+    });
   }
   if (e != hipSuccess) return hip_status(e, "gated unit, slopes");
   if (need_b) {
@@ -565,6 +582,7 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
   const long d_half = bytes_between(l.dgate, l.dup);
   // a product, and the sum of its parts if it has any
   auto product = [&](ProductParams& p, ProductKind kind, void* first, void* second) {
+    p.undo = l.range.undo;
     p.out = p.splits > 1 ? l.product_parts : first;
     return for_type(u.dtype, [&](auto t) {
       using T = decltype(t);
@@ -583,6 +601,7 @@ oaa_status_t oaa_gated_backward(const oaa_gated_t* d, const void* dh, const void
         j.ld = p.out_ld;
         j.image = p.out_image;
       }
+      j.undo = p.undo;
       return oaa::launch_join<T>(j, s);
     });
   };

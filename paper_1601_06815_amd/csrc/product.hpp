@@ -38,6 +38,7 @@
 
 #include "activation.hpp"
 #include "gated.hpp"
+#include "gated_range.hpp"
 #include "product_choice.hpp"
 #include "scalar_types.hpp"
 #include "tile_common.hpp"
@@ -385,6 +386,7 @@ struct UnitEnd {
   float gate_bias[V], up_bias[V];  // PAIR 1
   float sum_g[V], sum_u[V];
   long part = 0;  // which part of the sums over the positions this wave's are
+  float scale = 1.0f, most = 0.0f;
 
   __device__ __forceinline__ UnitEnd(const ProductParams& p_, int image_, int first, int lane_)
       : p(p_), image(image_), lane(lane_), c(lane_ % kPieces), r0(lane_ / kPieces), i(first + c * V), n(p_.ni - i) {
@@ -469,8 +471,15 @@ struct UnitEnd {
             const float d = float(w.dh[e]);
             // (d u may be beyond float32, or infinite times a slope of 0, where y is not)
             const float y = d * (u[e] * act_slope<ACT>(g[e])), z = d * act<ACT>(g[e]);
-            dg[e] = T(y);
-            du[e] = T(z);
+            if constexpr (range::kUsed<T>) {
+              range::note(most, y);
+              range::note(most, z);
+              dg[e] = T(y * scale);
+              du[e] = T(z * scale);
+            } else {
+              dg[e] = T(y);
+              du[e] = T(z);
+            }
             if constexpr (PAIR == 1) {
               sum_g[e] += y;
               sum_u[e] += z;
@@ -614,7 +623,7 @@ struct UnitNeeds {
 template <typename T, int MI, int MJ, int PAIR, bool BACK, int ACT, int NI, int NJ>
 __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (&acc)[NI][NJ],
                                          const UnitNeeds<T, MI, MJ, PAIR, BACK>& needs, int image, long part, int i,
-                                         int j, int lane) {
+                                         int j, int lane, float scale, float& most) {
   using Needs = UnitNeeds<T, MI, MJ, PAIR, BACK>;
   constexpr int V = Needs::V, F = Needs::F, kPieces = Needs::kPieces;
   auto at = [](int q) { return Needs::at(q); };
@@ -652,8 +661,15 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
         for (int e = 0; e < V; ++e) {
           const float d = element<T, V>(needs.dh[y * kPieces + q], e);
           const float s = d * (u[e] * act_slope<ACT>(g[e])), t = d * act<ACT>(g[e]);
-          set_element<T, V>(dg, e, s);
-          set_element<T, V>(du, e, t);
+          if constexpr (range::kUsed<T>) {
+            range::note(most, s);
+            range::note(most, t);
+            set_element<T, V>(dg, e, s * scale);
+            set_element<T, V>(du, e, t * scale);
+          } else {
+            set_element<T, V>(dg, e, s);
+            set_element<T, V>(du, e, t);
+          }
           if constexpr (PAIR == 1) {
             sum_g[q * V + e] += s;
             sum_u[q * V + e] += t;
@@ -853,6 +869,13 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   // channels last 271 and 213, planes 297 and 268; but made again in the backward pass, in
   // planes, 455 and 540: pieces of d's rows that meet in a line are then written at other
   // times; float32 49 and 52).
+  float scale = 1.0f, most = 0.0f;
+  constexpr bool kRanged = BACK && range::kUsed<T>;
+  if constexpr (kRanged)
+    if (args.range.again) {
+      scale = range::find<64 * WAVES>(args.range, reinterpret_cast<float*>(lds_memory));
+      if (scale == 1.0f) return;
+    }
   unsigned number = blockIdx.x, stop = args.tiles;
   if constexpr (RUN) {
     number = unsigned(xcd_order(blockIdx.x, gridDim.x)) * args.run;
@@ -1068,7 +1091,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
         if (inside) {
           auto end_with = [&](auto which_act) {
             unit_end<T, MI, MJ, PAIR, BACK, decltype(which_act)::value>(p, acc, needs, image, part, iw + quad * kVec,
-                                                                        jw + row, lane);
+                                                                        jw + row, lane, scale, most);
           };
           switch (p.act) {
             case OAA_ACT_RELU: end_with(std::integral_constant<int, OAA_ACT_RELU>{}); break;
@@ -1081,6 +1104,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
           static_assert(kRows % 16 == 0 && 16 * MJ % kRows == 0, "");
           UnitEnd<T, RI, kRows, PAIR, BACK> finish(p, image, iw, lane);
           finish.part = part;
+          finish.scale = scale;
           typename UnitEnd<T, RI, kRows, PAIR, BACK>::Row ahead;
           constexpr int kPasses = 16 * MJ / kRows;
 #pragma unroll 1
@@ -1096,14 +1120,23 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
                   const int yy = q * kRows / 16 + y, four = row_in_fragment<T, true>(x, 4 * quad) / 4;
                   put<RI>(slab, 16 * y + row, four, acc[x][yy]);
                   const floatx4 u = acc[PAIR == 1 ? x + MI : x][PAIR == 2 ? yy + MJ : yy];
-                put<RI>(slab + kRows * RI * 4, 16 * y + row, four, u);
+                  put<RI>(slab + kRows * RI * 4, 16 * y + row, four, u);
                 }
             }
             finish.rows(ahead, slab, jw + pass * kRows);
-        }
-        finish.end();
+          }
+          finish.end();
+          if constexpr (kRanged) most = fmaxf(most, finish.most);
         }
       } else {
+        if constexpr (range::kUsed<T>)
+          if (p.undo && p.splits == 1) {
+            const float undo = *p.undo;
+#pragma unroll
+            for (int x = 0; x < NI; ++x)
+#pragma unroll
+              for (int y = 0; y < NJ; ++y) acc[x][y] *= undo;
+          }
         auto leave = [&](auto zero, auto* out, long ld) {
           using E = decltype(zero);
           constexpr int V = 16 / int(sizeof(E));
@@ -1150,6 +1183,13 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
     if (late) {
       __syncthreads();
       last = begin(w, true);
+    }
+  }
+  if constexpr (kRanged) {
+    const Range& r = again(args).range;
+    if (r.most && !r.again) {
+      __syncthreads();
+      range::leave<64 * WAVES>(r, most, reinterpret_cast<float*>(lds_memory));
     }
   }
 }

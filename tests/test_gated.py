@@ -323,6 +323,51 @@ def test_large_gradients_of_small_slopes(gpu_lib, shape, F, layout, dtype, act):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("shape,F", [((3, 40, 9, 8), 56), ((2, 70, 31, 5), 150), ((1, 260, 21, 1), 131), ((700, 40), 48),
+                                     ((9, 24, 29, 31), 700), ((12, 1200), 40)])
+@pytest.mark.parametrize("wanted", ["dx", "weights"])
+@pytest.mark.parametrize("k", [14, -20])
+def test_range_of_float16(gpu_lib, k, wanted, shape, F, act, layout):
+    """dg and du that float16 does not hold (beyond 65504, or of no more than four digits),
+    where dx or dW is in its range: x and the weights make up for it by powers of two.
+
+    As in Bounds, but the least step of dg and du is that of float16 scaled so that their largest is 2^14 or
+    more: half of it is 2^-39 of that."""
+    far = 2.0 ** {("dx", 14): 8, ("dx", -20): -10, ("weights", 14): -12, ("weights", -20): 10}[wanted, k]
+    x, dh, gw, uw, *_ = make(shape, F, layout, torch.float64, bias=False, seed=47)
+    more = 4.0 if k > 0 else 1.0  # (of g and u, so that many are beyond)
+    x, gw, uw = x * more * far, gw / far, uw / far
+    x, gw, uw, dh = (t.half() for t in (x, gw, uw, dh.clamp(-0.4, 0.4) * 10 * 2.0 ** (k - 1)))
+    assert bool(torch.isfinite(dh).all())
+    values = [wide(t) for t in (x, gw, uw)]
+    g, u = oracle.gated_preactivations(*values)
+    a, slope = _act(act, g)
+    D, V = np.abs(oracle._flat(wide(dh))), np.abs(oracle._flat(values[0]))
+    og, ou = ((shape[1] + 8) * E * (V @ np.abs(w).T) for w in values[1:])
+    dg, du = np.abs(D * u * slope), D * np.abs(a)
+    most = max(dg.max(), du.max())
+    assert most > 65504 if k > 0 else most < 2.0 ** -4
+    G, U, step = np.abs(g), np.abs(u), STEP[torch.float16]
+    rg = D * (0.8 * og * (U + ou) + 1.2 * ou + 3e-6 * U)
+    ru = D * (1.2 * og + 2e-6 * np.abs(a) + 2e-7 * G)
+    rg, ru = (o + step * (v + o) + 2.0 ** -39 * most for o, v in ((rg, dg), (ru, du)))
+    if wanted == "dx":
+        size = (dg + rg) @ np.abs(values[1]) + (du + ru) @ np.abs(values[2])
+        offs = [oracle._back(rg @ np.abs(values[1]) + ru @ np.abs(values[2]) + (2 * F + 8) * E * size, wide(x), shape[1])]
+    else:
+        offs = [r.T @ V + (len(V) + 8) * E * ((v + r).T @ V) for r, v in ((rg, dg), (ru, du))]
+    names = ("dx",) if wanted == "dx" else NAMES[1:3]
+    refs = dict(zip(NAMES, oracle.gated_backward(wide(dh), *values, activation=act)))
+    for grads in both_backwards(x, dh, gw, uw, None, None, act, [n in names for n in NAMES]):
+        for name, off in zip(names, offs):
+            ref, got = refs[name], grads[NAMES.index(name)]
+            assert np.abs(ref).max() < 65504 and np.abs(ref).max() > 2.0 ** -12
+            near(got, ref, off + step * (np.abs(ref) + off) + LEAST[torch.float16], torch.float16, name)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
 @pytest.mark.parametrize("view", ["channels", "channels last", "rows last", "images", "one image many times",
                                   "one position many times", "odd address", "odd address last"])
@@ -666,6 +711,41 @@ def test_graph_replays(gpu_lib, shape, F, dtype):
         torch.cuda.synchronize()
         for got, ref in zip(out, step()):
             assert torch.equal(got, ref)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_replays_of_another_range(gpu_lib, layout):
+    """Float16's dg and du in range, above and below it, from one replay to the next."""
+    x, dh, *params = make((3, 40, 9, 8), 56, layout, torch.float16, seed=49)
+    leaves = [t.requires_grad_() for t in (x, *params)]
+    base = dh.clone()
+
+    def step():
+        h = autograd.gated(*leaves)
+        return torch.autograd.grad(h, leaves, dh)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in (0, 17, 0, -12, 17, -12, 0):
+        dh.copy_(base * 2.0 ** k)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, ref in zip(out, step()):
+            assert bool(((got == ref) | (torch.isnan(got) & torch.isnan(ref))).all())
+        # of a power of two the digits are the same, but for what lies among the smallest numbers
+        if k == -12:
+            for got, ref in zip(out, plain):
+                ref = ref.float() * 2.0 ** k
+                assert float((got.float() - ref).abs().max()) <= 2.0 ** -24 + 2.0 ** -8 * float(ref.abs().max())
+        elif k == 0:
+            plain = [t.clone() for t in out]
 
 
 @pytest.mark.gpu
