@@ -125,7 +125,7 @@ __device__ __forceinline__ intx4 resource(const char* base, int bytes) {
 // of the load: wait_for_loads() does.
 __device__ __forceinline__ void load_16(unsigned lds, unsigned offset, intx4 rs) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(rs)
-               : "memory");
+               : "m0", "memory");
 }
 // Every load into LDS of this wave has landed and every read of LDS is done, in all
 // waves of the workgroup.
@@ -152,9 +152,11 @@ __device__ __forceinline__ int key_of(int r) {
     return (r >> 2 & 3) << 2;
 }
 
-// As wait_for_loads(), but not for the last N memory operations of this wave.
+// As wait_for_loads(), but not for the last N memory operations of this wave (which end in
+// their order; 63 is what the instruction can say, and none at all).
 template <int N>
 __device__ __forceinline__ void wait_but_for() {
+  static_assert(N <= 63, "");
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
@@ -617,6 +619,12 @@ struct UnitNeeds {
   }
 };
 
+// Stores that this wave makes at least, where it lies inside of j too: one of 16 bytes, an
+// instruction that nothing is wide enough to be merged with, for every piece of every column of
+// h, or of dg and du. The kernel's wait for the next tile's loads counts on them.
+template <typename T, int MI, int MJ, bool BACK>
+constexpr int kEndStores = MJ * (MI / (4 / int(sizeof(T)))) * (BACK ? 2 : 1);
+
 // The end of the unit from the registers, for such a wave: acc[x][y] are g, acc[x +
 // MI][y] or acc[x][y + MJ] u. Writes h (and g and u, if the call keeps them), or in the
 // backward pass dg and du with their sums over the positions.
@@ -626,6 +634,7 @@ __device__ __forceinline__ void unit_end(const ProductParams& p, const floatx4 (
                                          int j, int lane, float scale, float& most) {
   using Needs = UnitNeeds<T, MI, MJ, PAIR, BACK>;
   constexpr int V = Needs::V, F = Needs::F, kPieces = Needs::kPieces;
+  static_assert(V * sizeof(T) == 16 && MJ * kPieces * (BACK ? 2 : 1) == kEndStores<T, MI, MJ, BACK>, "");
   auto at = [](int q) { return Needs::at(q); };
   float sum_g[PAIR == 1 ? kPieces * V : 1], sum_u[PAIR == 1 ? kPieces * V : 1];
   if constexpr (PAIR == 1) {
@@ -774,7 +783,7 @@ constexpr bool kRuns = PAIR != 0 && !BACK && sizeof(T) == 2;
 // PAIR: 0 none, 1 on i, 2 on j. BACK: the unit in the backward pass. RUN: a workgroup takes
 // p.run tiles beside each other.
 template <typename T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, int PAIR, bool BACK, bool RUN>
-__global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 ? 1 : 2) kernel(ProductParams args) {
+__global__ void __launch_bounds__(64 * WI * WJ, 2) kernel(ProductParams args) {
   constexpr int WAVES = WI * WJ, GI = TI / WI, GJ = TJ / WJ;  // a wave's part of the tile
   constexpr int NI = GI / 16, NJ = GJ / 16;
   static_assert(GI % (PAIR == 1 ? 64 : 32) == 0 && GJ % (PAIR == 2 ? 32 : 16) == 0, "");
@@ -886,9 +895,10 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
   bool last = begin(w, true), another, late;
   constexpr int MI = PAIR == 1 ? NI / 2 : NI, MJ = PAIR == 2 ? NJ / 2 : NJ, RI = 16 * MI;
   constexpr int kVec = 16 / int(sizeof(T));
-  // Stores that a wave inside of i and j ends a tile with: they are younger than the loads
-  // of the next tile's first steps, which therefore need not wait for them.
-  constexpr int kStores = MI * MJ * 4 / kVec * (BACK ? 2 : 1);
+  // Stores that a wave inside of i and j ends a tile with, or more (the unit's if the call keeps
+  // g and u, a part's in 32 bits): they are younger than the loads of the next tile's first
+  // steps, which therefore need not wait for them.
+  constexpr int kStores = kEndStores<T, MI, MJ, BACK>;
   // The unit's needs are asked for while it multiplies. Large tiles have no registers for
   // them: a thread asks for one bias, and they meet in LDS behind the stages.
   constexpr bool kEarly = PAIR != 0 && TI * TJ <= 128 * 128, kShared = PAIR != 0 && !kEarly;
@@ -1145,6 +1155,7 @@ __global__ void __launch_bounds__(64 * WI * WJ, TI * TJ / (64 * WI * WJ) == 256 
             for (int y = 0; y < MJ; ++y) {
               if (jw + row + 16 * y >= p.nj) continue;
               E* to = out + iw + long(jw + row + 16 * y) * ld;
+              static_assert(MJ * (MI / (V / 4)) >= kStores && MI % (V / 4) == 0, "");
 #pragma unroll
               for (int x = 0; x < MI; x += V / 4) {
                 Vec<E, V> w;
