@@ -793,6 +793,47 @@ def test_offsets_past_32_bits(gpu_lib):
         assert np.abs(wide(got) - r).max() <= 2.0 ** -6 * np.abs(r).max()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout,B,C,S,F,dtype", [
+    ("last", 1, 16, (1 << 20) + 3, 2056, torch.bfloat16),   # h, dh, g, u, dg and du
+    ("last", 3, 2056, 349529, 16, torch.bfloat16),          # x and dx
+    ("planes", 3, 16, (1 << 19) + 5, 1400, torch.float16),  # h, dh, g, u, dg and du; x is copied
+    ("planes", 2, 1030, (1 << 20) + 4, 16, torch.bfloat16),  # x and dx
+], ids=str)
+def test_backward_past_32_bits(gpu_lib, layout, B, C, S, F, dtype):
+    """Tensors of more than 2^31 values in both passes, g and u stored and made again. dh is 0
+    but at the first, the last and some other positions, which are all that the gradients of the
+    weights and biases then come from."""
+    assert B * S * max(C, F) > 1 << 31
+    print(layout, B, C, S, F, dtype, flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(51)
+
+    def tensor(make, n):
+        return make((B, n, S)) if layout == "planes" else make((B, S, n)).movedim(-1, 1)
+
+    x = tensor(lambda size: torch.randn(size, generator=gen, device=DEV, dtype=dtype), C)
+    dh = tensor(lambda size: torch.zeros(size, device=DEV, dtype=dtype), F)
+    gw, uw, gb, ub = make((1, C), F, dtype=dtype, seed=51)[2:]
+    spots = [(b, s) for b in sorted({0, B - 1}) for s in (0, 1, S // 3, S - 65, S - 2, S - 1)]
+    for b, s in spots:
+        dh[b, :, s] = (torch.randn(F, generator=gen, device=DEV) * 0.1).to(dtype)
+
+    def rows(t):
+        return torch.stack([t[b, :, s] for b, s in spots])
+
+    bounds = Bounds(wide(rows(x)), *map(wide, (gw, uw, gb, ub)), "silu", dtype, wide(rows(dh)))
+    h = binding.gated_forward(x, gw, uw, gb, ub, keep=False)[0]
+    near(rows(h), bounds.h, bounds.h_off, dtype, "h", C)
+    del h
+    terms = (2 * F, *[len(spots)] * 4)
+    for dx, *rest in both_backwards(x, dh, gw, uw, gb, ub, "silu"):
+        for name, got, ref, off, n in zip(NAMES, (rows(dx), *rest), bounds.grads, bounds.offs, terms):
+            near(got, ref, off, dtype, name, n)
+        for b, s in spots:
+            dx[b, :, s] = 0.0
+        assert not bool(dx.any())
+
+
 # ---- refusals, without a GPU ----------------------------------------------------------
 
 @pytest.fixture(scope="module")
