@@ -415,17 +415,19 @@ oaa_status_t oaa_grad_clip(int count, const void* const* grads, void* const* out
  * Products and sums are held in 32 bits or more whatever the types, and h and the
  * gradients are rounded once. g and u are stored in 32 bits for the backward pass, or it
  * makes them again. dg and du are rounded to the type of x where they enter the products
- * dx and dW: the matrix cores take both operands in one type, and a rounding of each of
- * many terms weighs less than that of the result. In float16 they are rounded times a power
- * of two, the same for all of a call, where the largest finite magnitude of them is beyond
- * 65504 or below 2^-4: it becomes 2^14 or more, and dx and dW are divided by it in 32 bits. So
- * what is small loses digits below 2^-28 of the largest (2^-10 where the largest is between).
- * float32 values are multiplied as sums of
- * three bfloat16 values, which is exact to float32's rounding for magnitudes from 2^-110
- * (below, digits are lost) to 3.39e38 (above, as infinite). What is not finite at a position
- * of x, or in a weight, makes what the formulas sum over it infinite or NaN (NaN, in float32,
- * where they may say infinite), and nothing else: other positions' h and dx stay as they are.
- * Equal calls give equal bits. */
+ * dx and dW, because the matrix cores take both operands in one type: independent errors as
+ * large as that of the result's own rounding, so that 16-bit dx and dW are off by 1.4 times what one
+ * rounding gives (a second 16-bit piece of dg and du would take that away and double both
+ * products). In float16 they are rounded times a power of two, the same for all of a call,
+ * where the largest finite magnitude of them is beyond 65504 or below 2^-4: it becomes 2^14
+ * or more, and dx and dW are divided by the power in 32 bits. So what is small loses digits
+ * below 2^-28 of the largest (2^-10 where the largest is between). float32 values are
+ * multiplied as sums of three bfloat16 values, which is exact to float32's rounding for
+ * magnitudes from 2^-110 (below, digits are lost) to 3.39e38 (above, as infinite). What is not
+ * finite at a position of x, or in a weight, makes what the formulas sum over it infinite or
+ * NaN, and nothing else: other positions' h and dx stay as they are. (In float32 it is NaN where
+ * the formulas may say infinite, except in h of up to 32 positions in channels-last order,
+ * which float32 matrix instructions make.) Equal calls give equal bits. */
 typedef struct {
   int B, C, F;      /* images, channels of x, channels of h: B >= 0, C, F >= 1 (up to 2^20) */
   long long S;      /* positions per image, >= 0 (in planes below 2^21); at most 2^24 squares

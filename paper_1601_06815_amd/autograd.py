@@ -283,7 +283,9 @@ class Dropout(torch.nn.Module):
     captured graph draws another mask at each replay. A call that is made again for the
     backward pass, as by torch.utils.checkpoint, draws another one too: there, draw the
     seed once (``binding.dropout_next(state)``) and call ``dropout`` with it. Copies of a
-    layer have its key and draw the same masks."""
+    layer have its key and draw the same masks, and so do the ranks of a distributed job whose
+    torch generators were seeded alike, or whose wrapper sends rank 0's buffers to the others
+    (``broadcast_buffers=True``): give each rank another ``seed``, and keep its buffers."""
 
     def __init__(self, p=0.5, seed=None, device="cuda"):
         super().__init__()

@@ -23,9 +23,10 @@
 //   58 %; unit with g and u stored 1.75 ms, dx 1.26 (170 TFLOP/s), dW 1.15 (186).
 //   bfloat16, 128 planes of 54 x 54, 128 -> 512: two steps a tile, so what is around them: a
 //   tile of 256 that loads both operands waits for them (4200 cycles), multiplies (6600), asks
-//   for the next one's (3500) and turns sums into h (7400), of 23800; unit 0.28 ms (0.31 if
-//   every tile does), made again with dg and du 0.48 (2.6 TB/s), dx 0.23 and dW 0.24 (3.8 and
-//   3.6 TB/s).
+//   for the next one's (3500) and turns sums into h (7400), of 23800; unit 0.24 to 0.28 ms (0.28
+//   to 0.31 if every tile does), made again with dg and du 0.46 to 0.49 (2.9 TB/s; rows of dg and du
+//   begin at any 16 bytes, so that a lane's piece of 128 is part of two lines: 853 MB written for
+//   764), dx 0.23 and dW 0.24 (3.8 and 3.6 TB/s).
 // Transposing reads meet in pairs in the banks (40 to 50 % of LDS's cycles). Rows and keys
 // that avoid it, with the sums exchanged between lanes' registers at the end, brought no time
 // (dx 1.00 and 1.04 ms, dW 0.93 and 1.01): LDS is busy for half of the cycles only.
@@ -77,12 +78,14 @@ __device__ __forceinline__ floatx4 multiply(floatx4 a, floatx4 b, floatx4 c) {
   }
 }
 
-// float32 on the bf16 matrix cores, which are 16 times as fast as those of float32: every
-// value is the sum of three bf16 values (the nearest, the nearest to what is left, and to
-// what is left then: 24 bits), and of the nine products of two values' pieces the six
-// above 2^-24 of the whole are taken, the smallest first. That is exact to float32's own
-// rounding for magnitudes between 2^-110 (below, the third piece runs out of exponents) and
-// 3.38e38 (above, the first is infinite and the rest NaN, as for infinities).
+// float32 on the bf16 matrix cores, which are 16 times as fast as those of float32, as G. Henry,
+// P. T. P. Tang and A. Heinecke describe ("Leveraging the bfloat16 artificial intelligence
+// datatype for higher-precision computations", ARITH 2019): every value is the sum of three
+// bf16 values (the nearest, the nearest to what is left, and to what is left then: 24 bits), and
+// of the nine products of two values' pieces the six above 2^-24 of the whole are taken, the
+// smallest first. That is exact to float32's own rounding for magnitudes between 2^-110 (below,
+// the third piece runs out of exponents) and 3.39e38 (above, the first is infinite and the rest
+// NaN, as for infinities).
 struct Pieces {
   typedef bf16 vec __attribute__((ext_vector_type(8)));
   typedef bf16 two __attribute__((ext_vector_type(2)));
@@ -494,7 +497,8 @@ struct UnitEnd {
 #pragma unroll
             for (int e = 0; e < V; ++e)
               if (e >= n) dg[e] = du[e] = T(0.0f);
-          // whole pieces: the padding of d's rows is 0
+          // whole pieces, 0 beyond n. What d's rows have beyond the last piece (in 32 bits) is
+          // not written: the products clear it (cut()), or make of it what goes nowhere
           const long at = long(image) * p.d_image + long(j) * p.d_ld + i;
           store_values<T>(static_cast<T*>(p.dgate) + at, V, dg);
           store_values<T>(static_cast<T*>(p.dup) + at, V, du);
@@ -874,10 +878,12 @@ __global__ void __launch_bounds__(64 * WI * WJ, 2) kernel(ProductParams args) {
   // A workgroup takes one tile after the other. The first steps of the next are asked for
   // before the results of this one leave.
   // Where a sum is no longer than the two stages, these are tiles beside each other, and i's
-  // operand stays for those of the same rows (bfloat16, 128 images of 54 x 54, 128 -> 512, us:
-  // channels last 271 and 213, planes 297 and 268; but made again in the backward pass, in
-  // planes, 455 and 540: pieces of d's rows that meet in a line are then written at other
-  // times; float32 49 and 52).
+  // operand stays for those of the same rows. bfloat16, us without and with it: channels last
+  // 128 images of 54 x 54, 128 -> 512 269 and 215, 64 of 112 x 112, 64 -> 128 116 and 100; 65536
+  // tokens 128 -> 512 41 and 38. In planes it pays where they are many tiles long (54 x 54 281
+  // and 238) and costs where not (27 x 27 79 and 89; 28 x 28, 96 -> 384 64 and 70). Made again
+  // in the backward pass, in planes, 455 and 540: pieces of d's rows that meet in a line are
+  // then written at other times; float32 49 and 52.
   float scale = 1.0f, most = 0.0f;
   constexpr bool kRanged = BACK && range::kUsed<T>;
   if constexpr (kRanged)

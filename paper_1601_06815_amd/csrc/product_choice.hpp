@@ -35,15 +35,19 @@ struct ProductChoice {
 // (the wait for a tile's first operands, its results, and its steps), and the parts' way
 // through memory. Large tiles read least, but take longest alone, and their last round may
 // be nearly empty. Measured, us by side 64, 128, 256 (bfloat16 unit forward): 512 positions 512 ->
-// 2048 9.5, 10.5, 21.8; 2048 positions 1024 -> 4096 65, 37, 34; 16 images of 64 x 64 planes,
-// 256 -> 512 93, 58, 48. (A unit has to have its whole sums: it is not cut. In the backward pass
+// 2048 7.4, 9.2, 17.8; 2048 positions 1024 -> 4096 66, 39, 34; 16 images of 64 x 64 planes,
+// 256 -> 512 92, 57, 46. What passes through memory is not estimated, nor what a tile of few steps
+// waits for: there the estimate may be half of what is measured. (A unit has to have its whole sums: it is not cut. In the backward pass
 // it has no tile of 256: its registers do not hold what it needs besides the sums.)
 inline ProductChoice product_choice(int size, ProductKind kind, long ni, long nj, long images, long halves, long K,
                                     long segs) {
   // ns of a step: of a tile that has a compute unit to itself, and at the full rate
   static constexpr double alone[2][3] = {{400, 500, 1000}, {1100, 2100, 4400}};
   static constexpr double full[2][3] = {{200, 450, 1600}, {660, 1830, 5600}};
-  // around a tile's steps; small tiles' results in planes, many short pieces, take longer
+  // around a tile's steps; small tiles' results in planes, many short pieces, take longer (bfloat16,
+  // us without the 1500 ns and with: 128 planes of 54 x 54, 128 -> 512 252 and 238, 64 of 54 x 54,
+  // 32 -> 128 40 and 31, 4 of 112 x 112, 64 -> 128 10.9 and 9.6; but 2 of 218 x 218, 64 -> 192 24 and
+  // 30, in float32 43 and 49; ten other sizes the same)
   const double planes = kind == kUnitPlanes ? 1500 : 0, around[] = {3000 + planes, 3000 + planes, 6000};
   const bool again = kind == kUnitLastAgain || kind == kUnitPlanesAgain, pair = pair_on_i(kind) || pair_on_j(kind);
   const long step = 128 / size, steps = (K + step - 1) / step * segs;
@@ -81,10 +85,11 @@ constexpr long kFewPositions = 32;
 
 // Whether the backward pass makes g and u again from x rather than having them stored: the
 // product grows with C, what storing them moves (16 bytes a hidden value and position) does
-// not. us of both passes, stored and made again: float32, 8 planes of 56 x 56, 64 -> 256 102 and
-// 103, 16384 positions 256 -> 1024 394 and 441; bfloat16, 16384 positions, 512 -> 2048 495
-// and 405, 1024 -> 4096 1174 and 1218 (and 512 positions 86 and 75), 2048 -> 8192 3302 and
-// 4096. Of equals the one that needs no memory.
+// not. us of both passes, stored and made again: float32, 8 planes of 56 x 56, 64 -> 256 103 and
+// 102, 16384 positions 32 -> 128 59 and 49, 256 -> 1024 412 and 446; bfloat16, 16384 positions, 256
+// -> 1024 189 and 148, 512 -> 2048 486 and 412, 1024 -> 4096 1158 and 1233 (and 512 positions 87
+// and 80), 2048 -> 8192 3300 and 4160; float16, 512 -> 2048 495 and 441. Of equals the one that
+// needs no memory.
 inline bool product_remakes(int size, long C) { return size == 2 ? C <= 1024 : C <= 64; }
 
 }  // namespace oaa
