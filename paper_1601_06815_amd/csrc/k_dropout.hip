@@ -61,7 +61,10 @@ __global__ void __launch_bounds__(kThreads) dense_kernel(DropoutParams p, long n
   }
 }
 
-// Any strides: the four elements of one counter a thread, each found by its index.
+// Any strides: the four elements of one counter a thread, each found by its index. Bound by
+// instructions (a 64-bit division a thread, one element a load): 64 of 128 channels of 64 x 112 x
+// 112, 51 million values, float32 125 us in planes and 121 channels last (3.3 and 3.4 TB/s),
+// bfloat16 89 and 98; a dense tensor of them takes 57 and 34.
 template <typename TX, typename TY>
 __global__ void __launch_bounds__(kThreads) strided_kernel(DropoutParams p, long n) {
   const long group = long(blockIdx.x) * kThreads + threadIdx.x, at = 4 * group;

@@ -714,6 +714,63 @@ def test_graph_replays(gpu_lib, shape, F, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout,shape,F", [("last", (16500, 24), 1900), ("planes", (40, 24, 12, 30), 300),
+                                            ("last", (3, 40, 700, 9), 800), ("planes", (300, 16, 40, 26), 70)])
+@pytest.mark.parametrize("k", [14, -20])
+def test_range_of_float16_over_many_workgroups(gpu_lib, k, layout, shape, F):
+    """The same where each workgroup takes several rows or tiles, by what some positions
+    and some hidden channels need."""
+    gen = torch.Generator(device=DEV).manual_seed(53)
+
+    def normal(*size):
+        return torch.randn(size, generator=gen, device=DEV)
+
+    B, C = shape[:2]
+    step = STEP[torch.float16]
+    dh = lay((normal(B, F, *shape[2:]).clamp(-4.0, 4.0) * 2.0 ** (k - 1)).half(), layout)
+    x0, gw0, uw0 = normal(*shape) * (4.0 if k > 0 else 1.0), *(normal(F, C) / C ** 0.5 for _ in range(2))
+    T = x0.numel() // C
+    some = torch.tensor(sorted({0, 1, T // 3, T // 2, T - 66, T - 2, T - 1}), device=DEV)
+    few = torch.tensor([0, 1, 31, 63, F - 2, F - 1], device=DEV)
+
+    def rows(t):
+        return t.movedim(1, -1).reshape(T, -1)
+
+    for wanted in ("dx", "weights"):
+        far = 2.0 ** {("dx", 14): 8, ("dx", -20): -10, ("weights", 14): -14, ("weights", -20): 8}[wanted, k]
+        x, gw, uw = lay((x0 * far).half(), layout), (gw0 / far).half(), (uw0 / far).half()
+        d, W = (rows(dh)[some], (gw, uw)) if wanted == "dx" else (rows(dh)[:, few], (gw[few], uw[few]))
+        v, d = wide(rows(x)[some] if wanted == "dx" else rows(x)), wide(d)
+        W = [wide(w) for w in W]
+        g, u = (v @ w.T for w in W)
+        a, slope = _act("silu", g)
+        D, V = np.abs(d), np.abs(v)
+        og, ou = ((C + 8) * E * (V @ np.abs(w).T) for w in W)
+        rg = D * (0.8 * og * (np.abs(u) + ou) + 1.2 * ou + 3e-6 * np.abs(u))
+        ru = D * (1.2 * og + 2e-6 * np.abs(a) + 2e-7 * np.abs(g))
+        whole = [(rows(x).double() @ w.double().t()) for w in (gw, uw)]
+        s = torch.sigmoid(whole[0])
+        y = rows(dh).double().abs()
+        most = float(max((y * (whole[1] * s * (1 + whole[0] * (1 - s))).abs()).max(), (y * (whole[0] * s).abs()).max()))
+        del whole, s, y
+        assert most > 65504 if k > 0 else most < 2.0 ** -4
+        rg, ru = (o + step * (np.abs(t) + o) + 2.0 ** -39 * most for o, t in ((rg, d * u * slope), (ru, d * a)))
+        dg, du = d * u * slope, d * a
+        if wanted == "dx":
+            size = (np.abs(dg) + rg) @ np.abs(W[0]) + (np.abs(du) + ru) @ np.abs(W[1])
+            refs = [dg @ W[0] + du @ W[1]]
+            offs = [rg @ np.abs(W[0]) + ru @ np.abs(W[1]) + (2 * F + 8) * E * size]
+        else:
+            refs = [dg.T @ v, du.T @ v]
+            offs = [r.T @ V + (T + 8) * E * ((np.abs(t) + r).T @ V) for r, t in ((rg, dg), (ru, du))]
+        for grads in both_backwards(x, dh, gw, uw, None, None, "silu", [n in (("dx",) if wanted == "dx" else NAMES[1:3]) for n in NAMES]):
+            got = [rows(grads[0])[some]] if wanted == "dx" else [t[few] for t in grads[1:3]]
+            for t, ref, off in zip(got, refs, offs):
+                assert 2.0 ** -12 < np.abs(ref).max() < 65504
+                near(t, ref, off + step * (np.abs(ref) + off) + LEAST[torch.float16], torch.float16, wanted)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["planes", "last"])
 def test_replays_of_another_range(gpu_lib, layout):
     """Float16's dg and du in range, above and below it, from one replay to the next."""
