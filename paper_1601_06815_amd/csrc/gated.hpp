@@ -64,9 +64,9 @@ struct ProductParams {
   const void *gate_bias, *up_bias;
   float *gate, *up;
   int act;
-  // the unit in the backward pass: from dh (strides of elements) dg and du, of `d_ld`
-  // elements a row, 0 from the last one to the end of its 16 bytes, instead of h; and (or null) their sums over the
-  // positions in parts [product_sum_parts()][2][F]
+  // the unit in the backward pass: from dh (strides of elements) dg and du, of `d_ld` elements a
+  // row, 0 from the last one to the end of its 16 bytes, instead of h; and (or null) their sums
+  // over the positions in parts [product_sum_parts()][2][F]
   const void* dh;
   long dh_image, dh_ld;
   void *dgate, *dup;
